@@ -335,6 +335,154 @@ int32_t mp_plan_breadth_batch(const int64_t* begin, int64_t n_traces, const int3
                               int64_t n_tensors, int32_t policy, int64_t* offset_out,
                               int64_t* peak_out, int32_t* status_out, void* stream);
 
+/* ---- A key/value cache in 8 bits ------------------------------------------
+ *
+ * The memory of a decode loop that no static plan holds, because it grows by a
+ * token a step: the keys and values of attention, in blocks of tokens that a
+ * table gives to sequences.  The operators write it, read it back, attend to
+ * it and select blocks of it; their other arguments may be views at the
+ * offsets of a plan.
+ *
+ * mp_kv_cache (host struct of device pointers):
+ *   n_blocks blocks of `block` tokens (16, 32 or 64), `heads` heads of `dim`
+ *   values (64, 128 or 256); kind MP_KV_E4M3 (4 exponent and 3 fraction bits,
+ *   largest value 448) or MP_KV_INT8 (-127..127).
+ *   k_code [n_blocks][heads][block][dim]  bytes, 16-byte aligned
+ *   v_code [n_blocks][heads][dim][block]  bytes, 16-byte aligned
+ *   k_exp, v_exp [n_blocks][heads] int8: a value is code * 2^exp
+ *   mean_code [n_blocks][heads][dim] int8 (8-byte aligned), mean_exp
+ *              [n_blocks][heads] int8: the mean of the keys of a full block
+ *   Blocks that were never written may hold anything; so may the places of a
+ *   block past its sequence's length.
+ *   Scales are powers of two: the quotient by one is exact, so a code is the
+ *   one rounding of its value, and a block whose scale grows as tokens are
+ *   added keeps e4m3 codes exactly (down to their subnormal steps).
+ *
+ * mp_kv_seqs (host struct): n_seqs sequences.
+ *   table[s * table_stride + b] int32: the cache block of tokens
+ *              [b * block, (b + 1) * block) of sequence s; table_width entries
+ *              a row.  Entries past a sequence's last token are not read.
+ *   length[n_seqs] int32: tokens of each sequence, the call's own included.
+ *   begin[n_seqs + 1] int64: tokens [begin[s], begin[s + 1]) of the call's
+ *              n_tokens rows belong to sequence s and are its last ones;
+ *              begin[0] == 0, begin[n_seqs] == n_tokens.  NULL: one row for
+ *              each sequence (n_tokens == n_seqs).
+ *   most_new, longest: host bounds on the rows and the tokens of a sequence;
+ *              they set the launch.
+ *   Data errors (MP_EINVAL on the status word): bounds or lengths that
+ *   break these, table entries outside [0, n_blocks).  No such error causes
+ *   an access outside the arrays.
+ *
+ * mp_kv_rows (host struct): rows of a call, element (token, head, d) at
+ *   data[token * token_stride + head * head_stride + d]; dtype MP_BF16,
+ *   MP_F16 or MP_F32; strides in elements.  Rows of data and strides that are
+ *   multiples of 16 bytes are moved in wide loads, others in narrow ones. */
+#define MP_KV_E4M3 0
+#define MP_KV_INT8 1
+#define MP_BF16 0
+#define MP_F16 1
+#define MP_F32 2
+
+typedef struct {
+    uint8_t* k_code;
+    uint8_t* v_code;
+    int8_t* k_exp;
+    int8_t* v_exp;
+    int8_t* mean_code;
+    int8_t* mean_exp;
+    int64_t n_blocks;
+    int32_t heads;
+    int32_t dim;
+    int32_t block;
+    int32_t kind;
+} mp_kv_cache;
+
+typedef struct {
+    const int32_t* table;
+    int64_t table_stride;
+    int64_t table_width;
+    const int32_t* length;
+    const int64_t* begin;
+    int64_t n_seqs;
+    int64_t n_tokens;
+    int64_t most_new;
+    int64_t longest;
+} mp_kv_seqs;
+
+typedef struct {
+    void* data;
+    int64_t token_stride;
+    int64_t head_stride;
+    int32_t dtype;
+} mp_kv_rows;
+
+/* Store the call's keys and values (n_tokens rows of `heads` heads each, not
+ * written) in their sequences' blocks.  For each touched block and head, the
+ * exponent is the least e in [-100, 120] with largest |value| <= 448 * 2^e
+ * (127 * 2^e), over the call's values in the block; if earlier tokens are in
+ * the block, at least the block's own, and where it grows the held codes are
+ * rounded to the new one.  Rounding is to nearest even.  A block whose last
+ * place is written gets its mean: s = the sum of its codes over the tokens in
+ * each dim, e the exponent of s for int8 (-15 where s is zero), mean_code =
+ * round(s * 2^-e), mean_exp = k_exp + e - log2(block).
+ * A value that is not finite is a data error (MP_EINVAL on the status word);
+ * infinities are then held as the largest value and NaN as zero, so that the
+ * cache stays finite.  Sequences whose written blocks coincide race. */
+int32_t mp_kv_write(const mp_kv_cache* cache, const mp_kv_seqs* seqs, const mp_kv_rows* k,
+                    const mp_kv_rows* v, int32_t* status_out, void* stream);
+
+/* Read back the keys and values of the call's tokens, each rounded once to
+ * the rows' type. */
+int32_t mp_kv_read(const mp_kv_cache* cache, const mp_kv_seqs* seqs, const mp_kv_rows* k_out,
+                   const mp_kv_rows* v_out, int32_t* status_out, void* stream);
+
+/* Attention of the call's queries over the cache.  Row i of the n rows of a
+ * sequence of length L is at position p = L - n + i and sees positions 0..p:
+ *   out = sum_j exp(scale q.k_j) v_j / sum_j exp(scale q.k_j)
+ * q and out have q_heads heads, q_heads a multiple of cache->heads; query head
+ * g reads key head g / (q_heads / heads).  Types: MP_BF16 or MP_F16, the same
+ * for both.  A row that sees nothing (p < 0) is zero.
+ *   blocks [n_tokens][heads][keep] int32, or NULL for all: each row and key
+ *              head sees only positions in these of the sequence's blocks (indices
+ *              into its table row; -1: none; each at most once, a block past
+ *              the row's position or table is MP_EINVAL on the status word).
+ *   lse_out [n_tokens][q_heads] float, or NULL: log sum_j exp(scale q.k_j),
+ *              -infinity for a row that sees nothing.
+ *   workspace: mp_kv_workspace_size(MP_OP_KV_ATTEND, ...) bytes, 16-byte
+ *              aligned; contents need no initialisation.
+ * Products are in 32 bits of 16-bit factors that hold the codes exactly and
+ * queries exactly up to 2^-29 of their largest value; exp(...) is held to 11
+ * bits before the product with v, sums and maxima in 32 bits.  The order of every sum
+ * is fixed by the arguments, so a call repeats bit for bit. */
+int32_t mp_kv_attend(const mp_kv_cache* cache, const mp_kv_seqs* seqs, const mp_kv_rows* q,
+                     int32_t q_heads, float scale, const int32_t* blocks, int64_t keep,
+                     const mp_kv_rows* out, float* lse_out, void* workspace,
+                     size_t workspace_bytes, int32_t* status_out, void* stream);
+
+/* Select `keep` blocks for each row and key head by a score of the blocks'
+ * means.  A query head's code is c = round(q * 2^-e) in -127..127, e = x - 7 with
+ * largest |q| = m * 2^x, 1/2 <= m < 1; a block's score is the largest over the
+ * key head's query heads of (c . mean_code) * 2^(e + mean_exp): whole products,
+ * so scores are exact and ties real.  A row at position p has p / block + 1
+ * blocks; all are taken if they are at most `keep`, otherwise the first
+ * `first`, the last `recent` (at least 1) and the best-scored of the others,
+ * the lowest index among equals.
+ *   blocks_out [n_tokens][heads][keep] int32, ascending, -1 beyond the last.
+ *   workspace: mp_kv_workspace_size(MP_OP_KV_SELECT, ...) bytes, 16-byte
+ *              aligned; contents need no initialisation. */
+int32_t mp_kv_select(const mp_kv_cache* cache, const mp_kv_seqs* seqs, const mp_kv_rows* q,
+                     int32_t q_heads, int64_t keep, int64_t first, int64_t recent,
+                     int32_t* blocks_out, void* workspace, size_t workspace_bytes,
+                     int32_t* status_out, void* stream);
+
+/* Workspace bytes of mp_kv_attend (`keep` 0 without blocks) or mp_kv_select
+ * (host query; uses the shapes and counts of the structs, not their
+ * pointers).  0 for an unknown op or shapes that the call refuses. */
+#define MP_OP_KV_ATTEND 1
+#define MP_OP_KV_SELECT 2
+size_t mp_kv_workspace_size(int32_t op, const mp_kv_cache* cache, const mp_kv_seqs* seqs,
+                            int32_t q_heads, int64_t keep);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,296 @@
+// The 8-bit key/value cache: arguments of its kernels and their common device code.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "memoplan.h"
+#include "mp_device.hpp"
+
+namespace mp {
+
+// Rows of a call, with what the host found out about their alignment.
+struct KvRows {
+    char* data;
+    int64_t token_stride, head_stride;  // elements
+    int32_t dtype;
+    int32_t wide;  // data and strides are multiples of 16 bytes
+};
+
+struct KvArgs {
+    mp_kv_cache c;
+    mp_kv_seqs s;
+    int32_t log_block;
+    int32_t* status;
+};
+
+hipError_t launch_kv_write(const KvArgs& a, const KvRows& k, const KvRows& v, hipStream_t st);
+hipError_t launch_kv_read(const KvArgs& a, const KvRows& k, const KvRows& v, hipStream_t st);
+
+// What a call of mp_kv_attend launches (kv_attend.hip).
+struct KvAttendShape {
+    bool ok;
+    int32_t rows;      // rows (query, head) of a workgroup
+    int64_t units;     // row groups over all sequences, an upper bound
+    int64_t chunk;     // tokens (of the sequence, or of its listed blocks) of a workgroup
+    int64_t n_chunks;
+    size_t workspace;
+};
+
+struct KvAttend {
+    KvArgs a;
+    KvRows q, out;
+    float scale;
+    int32_t group;          // query heads of a key head
+    const int32_t* blocks;  // or null
+    int32_t keep;
+    float* lse;
+    void* ws;
+    KvAttendShape shape;
+};
+
+KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t q_heads,
+                              int64_t keep);
+hipError_t launch_kv_attend(const KvAttend& a, hipStream_t st);
+
+struct KvSelect {
+    KvArgs a;
+    KvRows q;
+    int32_t group;
+    int32_t keep, first, recent;
+    int32_t* out;
+    float* scores;  // [token][head][score_stride]
+    int64_t score_stride;
+};
+
+size_t kv_select_workspace(const mp_kv_cache& c, const mp_kv_seqs& s, int64_t* score_stride);
+hipError_t launch_kv_select(const KvSelect& a, hipStream_t st);
+
+// ---- device code
+
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef float float2_t __attribute__((ext_vector_type(2)));
+typedef float float4_t __attribute__((ext_vector_type(4)));
+typedef float float16_t __attribute__((ext_vector_type(16)));
+
+constexpr int kLeastExp = -100, kMostExp = 120;  // of a block's scale
+
+// 2^e for e in [-126, 127].
+__device__ __forceinline__ float pow2f(int e) { return __int_as_float((e + 127) << 23); }
+
+// x with top = m * 2^x, 1/2 <= m < 1, for a normal top; the fraction bits of m in *frac.
+__device__ __forceinline__ int exponent_of(float top, uint32_t* frac) {
+    const uint32_t b = __float_as_uint(top);
+    *frac = b & 0x7fffffu;
+    return (int)(b >> 23) - 126;
+}
+
+// The least e in [kLeastExp, kMostExp] with top <= 448 * 2^e (448 = 7/8 * 2^9) or, int8,
+// top <= 127 * 2^e (127 = 127/128 * 2^7); top finite, not negative.  A top below the normal
+// range falls to kLeastExp like zero.
+template <bool INT8>
+__device__ __forceinline__ int scale_exponent(float top) {
+    uint32_t frac;
+    const int x = exponent_of(top, &frac);
+    const int e = INT8 ? x - 7 + (frac > 0x7e0000u) : x - 9 + (frac > 0x600000u);
+    return min(kMostExp, max(kLeastExp, e));
+}
+
+// x (already scaled) to its code, nearest even.  |x| is at most the largest code.
+template <bool INT8>
+__device__ __forceinline__ uint32_t encode(float x) {
+    if (INT8) return (uint32_t)(int)__builtin_rintf(x) & 0xffu;
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false) & 0xffu;
+}
+template <bool INT8>
+__device__ __forceinline__ float decode(uint32_t code) {
+    if (INT8) return (float)(int)(int8_t)code;
+    return __builtin_amdgcn_cvt_f32_fp8((int)code, 0);
+}
+
+// Eight codes (two words) as eight 16-bit floats, exactly.
+template <bool INT8>
+__device__ __forceinline__ half8_t codes_to_half(uint32_t a, uint32_t b) {
+    union {
+        half2_t h[4];
+        half8_t v;
+    } o;
+    if (INT8) {
+        // byte + 128 put below the exponent of 1024, whose steps are 1: 1152 + code
+        const half2_t bias = {(_Float16)1152.0f, (_Float16)1152.0f};
+        const uint32_t x = a ^ 0x80808080u, y = b ^ 0x80808080u;
+        const uint32_t w[4] = {__builtin_amdgcn_perm(0x64646464u, x, 0x04010400u),
+                               __builtin_amdgcn_perm(0x64646464u, x, 0x04030402u),
+                               __builtin_amdgcn_perm(0x64646464u, y, 0x04010400u),
+                               __builtin_amdgcn_perm(0x64646464u, y, 0x04030402u)};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o.h[i] = __builtin_bit_cast(half2_t, w[i]) - bias;
+    } else {
+        o.h[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false);
+        o.h[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true);
+        o.h[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, false);
+        o.h[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, true);
+    }
+    return o.v;
+}
+
+__device__ __forceinline__ float half_to_float(uint32_t bits) {
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
+}
+__device__ __forceinline__ uint32_t float_to_half(float x) {
+    return __builtin_bit_cast(uint16_t, (_Float16)x);
+}
+__device__ __forceinline__ uint32_t float_to_bf16(float x) {
+    return __builtin_bit_cast(uint16_t, (__bf16)x);
+}
+
+// Eight consecutive elements of a row, at a multiple of eight.
+__device__ __forceinline__ void load8(const KvRows& r, int64_t token, int64_t head, int d,
+                                      float* x) {
+    const int64_t at = token * r.token_stride + head * r.head_stride + d;
+    if (r.dtype == MP_F32) {
+        const float* p = reinterpret_cast<const float*>(r.data) + at;
+        if (r.wide) {
+            *reinterpret_cast<float4_t*>(x) = *reinterpret_cast<const float4_t*>(p);
+            *reinterpret_cast<float4_t*>(x + 4) = *reinterpret_cast<const float4_t*>(p + 4);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = p[i];
+        }
+        return;
+    }
+    const uint16_t* p = reinterpret_cast<const uint16_t*>(r.data) + at;
+    uint32_t w[4];
+    if (r.wide) {
+        const uint4 u = *reinterpret_cast<const uint4*>(p);
+        w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (uint32_t)p[2 * i] | (uint32_t)p[2 * i + 1] << 16;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (r.dtype == MP_BF16) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        } else {
+            x[2 * i] = half_to_float(w[i] & 0xffffu);
+            x[2 * i + 1] = half_to_float(w[i] >> 16);
+        }
+    }
+}
+
+// The same place written, each value rounded once.
+__device__ __forceinline__ void store8(const KvRows& r, int64_t token, int64_t head, int d,
+                                       const float* x) {
+    const int64_t at = token * r.token_stride + head * r.head_stride + d;
+    if (r.dtype == MP_F32) {
+        float* p = reinterpret_cast<float*>(r.data) + at;
+        if (r.wide) {
+            *reinterpret_cast<float4_t*>(p) = *reinterpret_cast<const float4_t*>(x);
+            *reinterpret_cast<float4_t*>(p + 4) = *reinterpret_cast<const float4_t*>(x + 4);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p[i] = x[i];
+        }
+        return;
+    }
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        w[i] = r.dtype == MP_BF16
+                   ? float_to_bf16(x[2 * i]) | float_to_bf16(x[2 * i + 1]) << 16
+                   : float_to_half(x[2 * i]) | float_to_half(x[2 * i + 1]) << 16;
+    uint16_t* p = reinterpret_cast<uint16_t*>(r.data) + at;
+    if (r.wide) {
+        *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            p[2 * i] = (uint16_t)w[i];
+            p[2 * i + 1] = (uint16_t)(w[i] >> 16);
+        }
+    }
+}
+
+// One or four (at a multiple of four) elements written the same way.
+__device__ __forceinline__ void store1(const KvRows& r, int64_t token, int64_t head, int d,
+                                       float x) {
+    const int64_t at = token * r.token_stride + head * r.head_stride + d;
+    if (r.dtype == MP_F32)
+        reinterpret_cast<float*>(r.data)[at] = x;
+    else
+        reinterpret_cast<uint16_t*>(r.data)[at] =
+            (uint16_t)(r.dtype == MP_BF16 ? float_to_bf16(x) : float_to_half(x));
+}
+__device__ __forceinline__ void store4(const KvRows& r, int64_t token, int64_t head, int d,
+                                       const float* x) {
+    if (r.wide && r.dtype != MP_F32) {
+        const int64_t at = token * r.token_stride + head * r.head_stride + d;
+        uint32_t w[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            w[i] = r.dtype == MP_BF16
+                       ? float_to_bf16(x[2 * i]) | float_to_bf16(x[2 * i + 1]) << 16
+                       : float_to_half(x[2 * i]) | float_to_half(x[2 * i + 1]) << 16;
+        *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(r.data) + at) = make_uint2(w[0], w[1]);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) store1(r, token, head, d + i, x[i]);
+}
+
+// A sequence of a call: its rows [begin, begin + n) and its tokens.
+struct KvSeq {
+    int32_t s, length, n;
+    int64_t begin;
+    bool ok;
+};
+
+// The whole of begin[] checked, by the first workgroup of a launch.
+__device__ __forceinline__ void kv_check_begin(const KvArgs& a) {
+    if (!a.s.begin) return;
+    bool bad = a.s.begin[0] != 0 || a.s.begin[a.s.n_seqs] != a.s.n_tokens;
+    for (int64_t i = threadIdx.x; i < a.s.n_seqs; i += blockDim.x)
+        bad |= a.s.begin[i + 1] < a.s.begin[i];
+    if (bad) raise_status(a.status, MP_EINVAL);
+}
+
+__device__ __forceinline__ KvSeq kv_seq(const KvArgs& a, int64_t s) {
+    KvSeq q;
+    q.s = (int32_t)s;
+    q.length = a.s.length[s];
+    if (a.s.begin) {
+        const int64_t b = a.s.begin[s], e = a.s.begin[s + 1];
+        q.begin = b;
+        q.n = (int32_t)(e - b);
+        q.ok = b >= 0 && e >= b && e <= a.s.n_tokens && e - b <= a.s.most_new;
+    } else {
+        q.begin = s;
+        q.n = 1;
+        q.ok = true;
+    }
+    q.ok = q.ok && q.length >= 0 && q.length <= a.s.longest;
+    if (!q.ok) raise_status(a.status, MP_EINVAL);
+    return q;
+}
+
+// The last sequence whose key is at most u, where key(s) never falls with s; the
+// whole wave searches, 64 keys a turn.  Any keys give a sequence in range.
+template <typename Key>
+__device__ __forceinline__ int64_t kv_find(int64_t n_seqs, int64_t u, Key key) {
+    const int lane = threadIdx.x & (kWave - 1);
+    int64_t lo = 0, hi = n_seqs;
+    while (hi - lo > 1) {
+        const int64_t step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
+        const uint64_t below = __ballot(at < hi && key(at) <= u);
+        const int count = below == ~0ull ? kWave : __ffsll((unsigned long long)~below) - 1;
+        lo += (int64_t)max(0, count - 1) * step;
+        hi = min(hi, lo + step);
+    }
+    return lo;
+}
+
+}  // namespace mp

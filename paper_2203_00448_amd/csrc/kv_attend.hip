@@ -1,0 +1,511 @@
+// Attention over the 8-bit key/value cache.
+//
+// For a row (a query and one of its heads) with scores s_j = scale * q.k_j,
+//   out = sum_j 2^(c s_j - m) v_j / sum_j 2^(c s_j - m),   c = log2 e, m >= max_j c s_j,
+// in one pass over the cache with a running m: when it grows, what was summed so far is
+// multiplied by 2^(m_old - m_new).
+//
+// The codes are exact in 16-bit floats (4 or 8 significant bits, no code beyond 448), so
+// both products are matrix instructions on 16-bit floats with 32-bit sums, whatever the
+// rows' type: queries are brought to [2^14, 2^15) by a power of two per row, which holds
+// all bits of a bfloat16 or a 16-bit float down to 2^-29 of the row's largest.  The scale
+// of a block's keys multiplies its scores.  That of its values joins the exponent of the
+// weights, which enter the second product as w = 2^(c s_j - m + ve_j - vr + 15), vr the
+// largest ve so far: at most 2^15, normal down to 2^-29, where its contribution no longer
+// shows beside the largest.  The sum of weights takes 2^(c s_j - m) back from w in 32
+// bits.
+//
+// Both products are taken transposed, S^T = K Q^T and O^T = V^T W^T: the weights then
+// come out of the first product in the lanes that the second one wants them in, as long
+// as the token that a lane's key row holds is chosen for it, and the maximum and the sum
+// of a row are over one lane's registers and the few lanes of its column.
+#include "kv.hpp"
+#include "internal.hpp"
+
+namespace mp {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kWeightShift = 15;   // weights reach 2^15
+constexpr int kLeastShift = -80;   // of a block's value exponent below the largest
+constexpr int kNoExp = -127;       // the largest value exponent of nothing
+constexpr int kStep = 64;          // tokens a wave takes at a time
+
+// The partial result of a row over a chunk of tokens: o (normalised) and the base-2
+// logarithm of its sum of weights.
+struct Partials {
+    float* o;    // [row][chunk][dim]
+    float* lse;  // [row][chunk]
+};
+
+__device__ __forceinline__ Partials partials(const KvAttend& k) {
+    const int64_t rows = k.a.s.n_tokens * (int64_t)k.group * k.a.c.heads * k.shape.n_chunks;
+    Partials p;
+    p.o = static_cast<float*>(k.ws);
+    p.lse = p.o + rows * k.a.c.dim;
+    return p;
+}
+
+// The rows [row0, ...) of a workgroup: rows of a sequence and key head are (token, query
+// head) pairs in token order.
+struct RowGroup {
+    KvSeq q;
+    int64_t row0;
+    int32_t n_rows;  // of the sequence
+};
+
+// Row group `u` of the launch.  With a block list every token is a sequence of its own.
+__device__ __forceinline__ bool row_group(const KvAttend& k, int64_t u, RowGroup* g) {
+    const KvArgs& a = k.a;
+    if (k.blocks) {
+        const int64_t per = (k.group + k.shape.rows - 1) / k.shape.rows;
+        const int64_t token = u / per;
+        int64_t s = token;
+        if (a.s.begin)
+            s = kv_find(a.s.n_seqs, token, [&](int64_t i) { return a.s.begin[i]; });
+        g->q = kv_seq(a, s);
+        const int64_t i = token - g->q.begin;
+        if (!g->q.ok || i < 0 || i >= g->q.n) return false;
+        // the sequence as it is for this token: its last one
+        g->q.length -= (int32_t)(g->q.n - 1 - i);
+        g->q.begin = token;
+        g->q.n = 1;
+        g->row0 = u % per * k.shape.rows;
+    } else {
+        int64_t s, first;
+        if (a.s.begin) {
+            // n tokens are at most n * group / rows + 1 row groups
+            auto key = [&](int64_t i) { return a.s.begin[i] * k.group / k.shape.rows + i; };
+            s = kv_find(a.s.n_seqs, u, key);
+            first = u - key(s);
+        } else {
+            const int64_t per = (k.group + k.shape.rows - 1) / k.shape.rows;
+            s = u / per;
+            first = u % per;
+        }
+        g->q = kv_seq(a, s);
+        if (!g->q.ok || first < 0) return false;
+        g->row0 = first * k.shape.rows;
+    }
+    const int64_t n = (int64_t)g->q.n * k.group;
+    if (g->row0 >= n) return false;
+    g->n_rows = (int32_t)n;
+    return true;
+}
+
+// The place of a row: its token, its query head, the last position it sees (-1: none).
+struct Row {
+    int64_t token;
+    int32_t head;
+    int32_t last;
+    bool live;
+};
+__device__ __forceinline__ Row row_of(const KvAttend& k, const RowGroup& g, int key_head,
+                                      int64_t row) {
+    Row r;
+    r.live = row < g.n_rows;
+    const int32_t i = r.live ? (int32_t)row : g.n_rows - 1;
+    const int32_t t = i / k.group;
+    r.token = g.q.begin + t;
+    r.head = key_head * k.group + i % k.group;
+    r.last = r.live ? max(-1, g.q.length - g.q.n + t) : -1;
+    return r;
+}
+
+// Sixteen tokens of a step: their block and the position of the first.
+struct Place {
+    int64_t at;    // block * heads + head, for the codes and exponents
+    int32_t pos;   // INT32_MAX where there is none
+    int32_t slot;  // of the first token in its block
+};
+
+// Tokens [x, x + 16) of the sequence (or of the blocks listed for it).
+__device__ __forceinline__ Place place_of(const KvAttend& k, const int32_t* table,
+                                          const int32_t* list, int head, int64_t x,
+                                          int32_t most) {
+    Place p;
+    const int lb = k.a.log_block;
+    int64_t b = x >> lb;
+    p.slot = (int32_t)(x & ((1 << lb) - 1));
+    bool there = true;
+    if (list) {
+        const int32_t named = b < k.keep ? list[b] : -1;
+        there = named >= 0 && named <= (most >> lb);
+        if (!there && named != -1) raise_status(k.a.status, MP_EINVAL);
+        b = there ? named : 0;
+    } else {
+        there = x <= most;
+    }
+    p.pos = (int32_t)((b << lb) + p.slot);
+    there = there && p.pos <= most;
+    int32_t page = there ? table[b] : 0;
+    if (page < 0 || page >= k.a.c.n_blocks) {
+        raise_status(k.a.status, MP_EINVAL);
+        there = false;
+        page = 0;
+    }
+    if (!there) p.pos = INT32_MAX;
+    p.at = (int64_t)page * k.a.c.heads + head;
+    return p;
+}
+
+// A row's query as the factor of the first product; `scale` becomes what its scores are
+// multiplied by.  Lane (column n, quarter g) holds dims [64 c + 16 g, + 16).
+template <int D>
+__device__ __forceinline__ void load_query(const KvAttend& k, const Row& r, int g,
+                                           half8_t (&q)[D / 64][2], float* scale) {
+    float x[D / 64][16], top = 0.0f;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) {
+        load8(k.q, r.token, r.head, c * 64 + g * 16, x[c]);
+        load8(k.q, r.token, r.head, c * 64 + g * 16 + 8, x[c] + 8);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[c][i]));
+    }
+    top = fmaxf(top, __shfl_xor(top, 16, kWave));
+    top = fmaxf(top, __shfl_xor(top, 32, kWave));
+    uint32_t frac;
+    const int e = min(127, max(-90, exponent_of(top, &frac)));
+    const float f = pow2f(15 - e);
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) q[c][i / 8][i % 8] = (_Float16)(x[c][i] * f);
+    *scale = k.scale * kLog2e * pow2f(max(-126, e - 15));
+}
+
+// Values at places of which only the first n of 16 exist: the others' codes to zero.
+__device__ __forceinline__ uint4 first_codes(uint4 w, int n) {
+    uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int b = min(4, max(0, n - 4 * i));
+        x[i] = b == 0 ? 0 : b == 4 ? x[i] : x[i] & ((1u << (8 * b)) - 1);
+    }
+    return make_uint4(x[0], x[1], x[2], x[3]);
+}
+
+// Few rows: 16 columns of rows times NT, one key head, one chunk of tokens.  Each of four
+// waves takes every fourth step of 64 tokens, with its own running maxima, and the four
+// are joined at the end.  A wave reads the codes straight into registers, the next step's
+// while it computes this one; nothing is shared, so there is no barrier in the loop.
+//
+// Tokens: key row m of tile t holds token 16 (m / 4) + 4 t + m % 4 of the step.  Lane
+// quarter g then has the scores of tokens [16 g, 16 g + 16), four from each tile, which
+// are the columns of 16 bytes of each row of values.
+template <int D, bool INT8, int NT>
+__global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend k) {
+    constexpr int DT = D / 16, DC = D / 64;
+    __shared__ __align__(16) float so[4][16][D + 4];
+    __shared__ float sm[4][16], sl[4][16];
+    __shared__ int svr[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+    const KvArgs& a = k.a;
+    if (blockIdx.x == 0) kv_check_begin(a);
+    const int64_t u = blockIdx.x / ((int64_t)a.c.heads * k.shape.n_chunks);
+    const int rest = (int)(blockIdx.x % ((int64_t)a.c.heads * k.shape.n_chunks));
+    const int head = rest % a.c.heads;
+    const int64_t chunk = rest / a.c.heads;
+    RowGroup rg;
+    if (!row_group(k, u, &rg)) return;
+    const int64_t last_row = min((int64_t)rg.n_rows, rg.row0 + 16 * NT) - 1;
+    const int32_t most = row_of(k, rg, head, last_row).last;  // the last position any row sees
+    const int32_t least = row_of(k, rg, head, rg.row0).last;  // all rows see up to here
+    const int32_t* const table = a.s.table + rg.q.s * a.s.table_stride;
+    const int32_t* const list =
+        k.blocks ? k.blocks + (rg.q.begin * a.c.heads + head) * k.keep : nullptr;
+    const int64_t end_all = list ? (int64_t)k.keep << a.log_block : (int64_t)most + 1;
+    const int64_t x0 = chunk * k.shape.chunk, x1 = min(end_all, x0 + k.shape.chunk);
+    if (chunk > 0 && x0 >= end_all) return;
+
+    Row row[NT];
+    half8_t q[NT][DC][2];
+    float scale[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        row[j] = row_of(k, rg, head, rg.row0 + 16 * j + n);
+        load_query<D>(k, row[j], g, q[j], &scale[j]);
+    }
+    float4_t acc[NT][DT];
+    float m[NT], l[NT];
+    int vr = kNoExp;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        m[j] = -INFINITY;
+        l[j] = 0.0f;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) acc[j][t] = float4_t{0, 0, 0, 0};
+    }
+
+    const int lb = a.log_block;
+    const int64_t stride = 4 * kStep;
+    uint4 kw[4][DC], vw[DT];
+    int ke, ve;
+    Place kp, vp;  // of the loaded step
+    auto find = [&](int64_t x) {
+        kp = place_of(k, table, list, head, x + (n >> 2) * 16, most);
+        vp = place_of(k, table, list, head, x + g * 16, most);
+    };
+    auto load = [&]() {
+        const uint8_t* kc = a.c.k_code + ((kp.at << lb) + kp.slot + (n & 3)) * D + g * 16;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int c = 0; c < DC; ++c)
+                kw[t][c] = *reinterpret_cast<const uint4*>(kc + t * 4 * D + c * 64);
+        const uint8_t* vc = a.c.v_code + ((vp.at * D + n) << lb) + vp.slot;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+            vw[t] = *reinterpret_cast<const uint4*>(vc + ((int64_t)t * 16 << lb));
+        ke = a.c.k_exp[vp.at];
+        ve = a.c.v_exp[vp.at];
+    };
+    int64_t x = x0 + wave * kStep;
+    if (x < x1) {
+        find(x);
+        load();
+    }
+    for (; x < x1; x += stride) {
+        half8_t kh[4][DC][2], vh[DT][2];
+        const int32_t pos = vp.pos;
+        const int my_ke = ke, my_ve = ve;
+        // whether some row does not see some token of the step
+        const bool part = __any(pos == INT32_MAX || pos + 15 > least);
+        if (part) {
+            const int there = pos == INT32_MAX ? 0 : min(16, most - pos + 1);
+#pragma unroll
+            for (int t = 0; t < DT; ++t) vw[t] = first_codes(vw[t], there);
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int c = 0; c < DC; ++c) {
+                kh[t][c][0] = codes_to_half<INT8>(kw[t][c].x, kw[t][c].y);
+                kh[t][c][1] = codes_to_half<INT8>(kw[t][c].z, kw[t][c].w);
+            }
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+            vh[t][0] = codes_to_half<INT8>(vw[t].x, vw[t].y);
+            vh[t][1] = codes_to_half<INT8>(vw[t].z, vw[t].w);
+        }
+        if (x + stride < x1) {
+            find(x + stride);
+            load();
+        }
+        // the largest value exponent so far; places that are not there have none
+        int top_ve = pos == INT32_MAX ? kNoExp : my_ve;
+        top_ve = max(top_ve, __shfl_xor(top_ve, 16, kWave));
+        top_ve = max(top_ve, __shfl_xor(top_ve, 32, kWave));
+        const int new_vr = max(vr, top_ve);
+        const int shift = max(kLeastShift, min(0, my_ve - new_vr)) + kWeightShift;
+        const float v_fall = pow2f(max(-126, vr - new_vr)), unshift = pow2f(-shift);
+        vr = new_vr;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            float s[16];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                float4_t z = {0, 0, 0, 0};
+#pragma unroll
+                for (int c = 0; c < DC; ++c) {
+                    z = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh[t][c][0], q[j][c][0], z, 0, 0, 0);
+                    z = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh[t][c][1], q[j][c][1], z, 0, 0, 0);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[t * 4 + r] = z[r];
+            }
+            const float f = scale[j] * pow2f(my_ke);
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s[i] *= f;
+                if (part && (pos == INT32_MAX || pos + i > row[j].last)) s[i] = -INFINITY;
+                top = fmaxf(top, s[i]);
+            }
+            top = fmaxf(top, __shfl_xor(top, 16, kWave));
+            top = fmaxf(top, __shfl_xor(top, 32, kWave));
+            const float new_m = fmaxf(m[j], top);
+            const float base = new_m == -INFINITY ? 0.0f : new_m;
+            const float fall = __builtin_amdgcn_exp2f(m[j] - base);
+            m[j] = new_m;
+            const float add = (float)shift - base;
+            float sum = 0.0f;
+            half8_t w[2];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float e = __builtin_amdgcn_exp2f(s[i] + add);
+                sum += e;
+                w[i / 8][i % 8] = (_Float16)e;
+            }
+            l[j] = l[j] * fall + sum * unshift;
+            const float both = fall * v_fall;
+#pragma unroll
+            for (int t = 0; t < DT; ++t) {
+                acc[j][t] *= both;
+                acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh[t][0], w[0], acc[j][t], 0, 0, 0);
+                acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh[t][1], w[1], acc[j][t], 0, 0, 0);
+            }
+        }
+    }
+
+    // the four waves' results of a row joined
+    const Partials part_out = partials(k);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        float sum = l[j];
+        sum += __shfl_xor(sum, 16, kWave);
+        sum += __shfl_xor(sum, 32, kWave);
+        if (j) __syncthreads();
+        if (g == 0) {
+            sm[wave][n] = m[j];
+            sl[wave][n] = sum;
+        }
+        if (lane == 0) svr[wave] = vr;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+            *reinterpret_cast<float4_t*>(&so[wave][n][t * 16 + g * 4]) = acc[j][t];
+        __syncthreads();
+        const int col = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * (D / 16);
+        float top = fmaxf(fmaxf(sm[0][col], sm[1][col]), fmaxf(sm[2][col], sm[3][col]));
+        const float base = top == -INFINITY ? 0.0f : top;
+        const int most_vr = max(max(svr[0], svr[1]), max(svr[2], svr[3]));
+        float total = 0.0f, o[D / 16];
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) o[i] = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = __builtin_amdgcn_exp2f(sm[w][col] - base);
+            const float fv = f * pow2f(max(-126, svr[w] - most_vr));
+            total += sl[w][col] * f;
+#pragma unroll
+            for (int i = 0; i < D / 16; i += 4) {
+                const float4_t y = *reinterpret_cast<const float4_t*>(&so[w][col][d0 + i]);
+#pragma unroll
+                for (int z = 0; z < 4; ++z) o[i + z] += y[z] * fv;
+            }
+        }
+        const Row r = row_of(k, rg, head, rg.row0 + 16 * j + col);
+        if (!r.live) continue;
+        // a row that sees nothing: weights and sums are zero
+        const float norm = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
+        const float back = pow2f(max(-126, most_vr - kWeightShift));
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) o[i] = o[i] * norm * back;
+        const float lse = total > 0.0f ? base + log2f(total) : total == 0.0f ? -INFINITY : total;
+        const int64_t index = r.token * (int64_t)k.group * a.c.heads + r.head;
+        if (k.shape.n_chunks > 1) {
+            float* to = part_out.o + (index * k.shape.n_chunks + chunk) * D + d0;
+#pragma unroll
+            for (int i = 0; i < D / 16; i += 4)
+                *reinterpret_cast<float4_t*>(to + i) = float4_t{o[i], o[i + 1], o[i + 2], o[i + 3]};
+            if (d0 == 0) part_out.lse[index * k.shape.n_chunks + chunk] = lse;
+        } else {
+            if constexpr (D / 16 >= 8) {
+#pragma unroll
+                for (int i = 0; i < D / 16; i += 8) store8(k.out, r.token, r.head, d0 + i, o + i);
+            } else {
+                store4(k.out, r.token, r.head, d0, o);
+            }
+            if (k.lse && d0 == 0) k.lse[index] = lse * kLn2;
+        }
+    }
+}
+
+// The chunks of a row joined: a wave for each row.
+template <int D>
+__global__ __launch_bounds__(256) void kv_join_kernel(KvAttend k) {
+    const KvArgs& a = k.a;
+    const int lane = threadIdx.x & 63;
+    const int heads = k.group * a.c.heads;
+    const int64_t index = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (index >= a.s.n_tokens * (int64_t)heads) return;
+    const int64_t token = index / heads;
+    int64_t s = token;
+    if (a.s.begin) s = kv_find(a.s.n_seqs, token, [&](int64_t i) { return a.s.begin[i]; });
+    const KvSeq q = kv_seq(a, s);
+    if (!q.ok || token < q.begin || token >= q.begin + q.n) return;
+    // chunks that the row's last position reaches (one at least), or all of a block list
+    const int64_t seen = k.blocks ? (int64_t)k.keep << a.log_block
+                                  : (int64_t)q.length - (q.n - 1 - (token - q.begin));
+    const int64_t chunks = min(k.shape.n_chunks, max((int64_t)1, (seen + k.shape.chunk - 1) / k.shape.chunk));
+    const Partials p = partials(k);
+    const float* lse = p.lse + index * k.shape.n_chunks;
+    const float* o = p.o + index * k.shape.n_chunks * D;
+    float top = -INFINITY;
+    for (int64_t c = lane; c < chunks; c += kWave) top = fmaxf(top, lse[c]);
+    top = wave_reduce(top, OpMax<float>());
+    const float base = top == -INFINITY ? 0.0f : top;
+    float total = 0.0f;
+    for (int64_t c = lane; c < chunks; c += kWave) total += __builtin_amdgcn_exp2f(lse[c] - base);
+    total = wave_reduce(total, OpAdd<float>());
+    const float norm = total > 0.0f ? 1.0f / total : 0.0f;
+    constexpr int kPer = D / 64;  // a lane's dims, next to each other
+    float x[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) x[i] = 0.0f;
+    for (int64_t c = 0; c < chunks; ++c) {
+        const float f = __builtin_amdgcn_exp2f(lse[c] - base);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) x[i] += f * o[c * D + lane * kPer + i];
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) store1(k.out, token, (int)(index % heads), lane * kPer + i, x[i] * norm);
+    if (k.lse && lane == 0) k.lse[index] = total > 0.0f ? (base + log2f(total)) * kLn2 : -INFINITY;
+}
+
+template <int D, bool INT8>
+hipError_t launch_d(const KvAttend& k, hipStream_t st) {
+    const KvAttendShape& sh = k.shape;
+    const dim3 grid((uint32_t)(sh.units * k.a.c.heads * sh.n_chunks));
+    kv_rows_kernel<D, INT8, 1><<<grid, 256, 0, st>>>(k);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    if (sh.n_chunks > 1) {
+        const int64_t rows = k.a.s.n_tokens * (int64_t)k.group * k.a.c.heads;
+        kv_join_kernel<D><<<dim3((uint32_t)((rows + 3) / 4)), 256, 0, st>>>(k);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t q_heads,
+                              int64_t keep) {
+    KvAttendShape sh = {};
+    const int64_t group = q_heads / c.heads;
+    sh.rows = 16;
+    const int64_t per = (group + sh.rows - 1) / sh.rows;
+    if (keep > 0)
+        sh.units = s.n_tokens * per;
+    else if (s.begin)
+        sh.units = s.n_tokens * group / sh.rows + s.n_seqs;
+    else
+        sh.units = s.n_seqs * per;
+    const int64_t longest = keep > 0 ? keep * c.block : s.longest;
+    // enough workgroups for four a compute unit, of 512 tokens at least
+    const int64_t wide = sh.units * c.heads;
+    int64_t chunks = wide > 0 ? (4 * 256 + wide - 1) / wide : 1;
+    const int64_t most = (longest + 511) / 512;
+    chunks = chunks < most ? chunks : most;
+    if (chunks < 1) chunks = 1;
+    sh.chunk = ((longest + chunks - 1) / chunks + 255) / 256 * 256;
+    if (sh.chunk < 256) sh.chunk = 256;
+    sh.n_chunks = longest > 0 ? (longest + sh.chunk - 1) / sh.chunk : 1;
+    const int64_t rows = s.n_tokens * q_heads;
+    sh.ok = sh.units * c.heads * sh.n_chunks < INT32_MAX && rows < INT32_MAX;
+    sh.workspace = sh.n_chunks > 1 ? (size_t)rows * sh.n_chunks * (c.dim + 1) * 4 : 0;
+    return sh;
+}
+
+hipError_t launch_kv_attend(const KvAttend& k, hipStream_t st) {
+    if (k.a.s.n_tokens == 0) return hipSuccess;
+    const bool i8 = k.a.c.kind == MP_KV_INT8;
+    switch (k.a.c.dim) {
+        case 64: return i8 ? launch_d<64, true>(k, st) : launch_d<64, false>(k, st);
+        case 128: return i8 ? launch_d<128, true>(k, st) : launch_d<128, false>(k, st);
+        default: return i8 ? launch_d<256, true>(k, st) : launch_d<256, false>(k, st);
+    }
+}
+
+}  // namespace mp
