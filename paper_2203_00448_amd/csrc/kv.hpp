@@ -31,6 +31,7 @@ hipError_t launch_kv_read(const KvArgs& a, const KvRows& k, const KvRows& v, hip
 // What a call of mp_kv_attend launches (kv_attend.hip).
 struct KvAttendShape {
     bool ok;
+    bool tiles;        // the form for many rows
     int32_t rows;      // rows (query, head) of a workgroup
     int64_t units;     // row groups over all sequences, an upper bound
     int64_t chunk;     // tokens (of the sequence, or of its listed blocks) of a workgroup

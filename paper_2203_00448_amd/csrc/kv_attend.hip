@@ -413,6 +413,237 @@ __global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend k) {
     }
 }
 
+// Many rows: four waves of 32 rows, one key head, one chunk of tokens, in tiles of 64 tokens
+// whose codes the workgroup turns into 16-bit floats once, in LDS, for all 128 rows.  Two
+// tiles' room: while one is computed the next one's codes, already in registers, are
+// converted into the other and the loads of the one after are on their way, so a tile
+// costs one barrier.
+//
+// Keys lie by row of the instruction: row m of 32 is token m with bits 2 and 3 exchanged,
+// so that a lane's scores are those of eight consecutive tokens, as the second product
+// takes them.  Both arrays have their 16-byte pieces exchanged by the row's low bits, so that
+// the lanes of a read, which go down the rows, meet different banks.
+template <int D>
+struct TileLds {
+    uint4 k[64][D / 8];  // [32 * half + row][piece ^ row]
+    uint4 v[D][8];       // [dim][piece ^ dim]: eight tokens a piece
+};
+
+template <int D, bool INT8>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAttend k) {
+    constexpr int KS = D / 16, DT = D / 32, ROW = D / 16;  // ROW: loads of a token's keys
+    constexpr int KL = 64 * ROW / 256, VL = D * 4 / 256;   // loads of a thread for a tile
+    extern __shared__ __align__(16) char lds_raw[];
+    TileLds<D>* const lds = reinterpret_cast<TileLds<D>*>(lds_raw);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, h = lane >> 5;
+    const KvArgs& a = k.a;
+    if (blockIdx.x == 0) kv_check_begin(a);
+    // key heads fastest: workgroups of one head share an XCD's L2 where 8 and the number of
+    // heads divide; late row groups, which see the most, first
+    const int head = (int)(blockIdx.x % a.c.heads);
+    const int64_t rest = blockIdx.x / a.c.heads;
+    const int64_t u = k.shape.units - 1 - rest / k.shape.n_chunks, chunk = rest % k.shape.n_chunks;
+    RowGroup rg;
+    if (!row_group(k, u, &rg)) return;
+    const int32_t most = row_of(k, rg, head, min((int64_t)rg.n_rows, rg.row0 + 128) - 1).last;
+    const int64_t end_all = (int64_t)most + 1;
+    const int64_t x0 = chunk * k.shape.chunk, x1 = min(end_all, x0 + k.shape.chunk);
+    if (chunk > 0 && x0 >= end_all) return;
+    const int32_t* const table = a.s.table + rg.q.s * a.s.table_stride;
+
+    // this wave's rows: the last position that any sees, and the last that all see
+    const int64_t wave_row0 = rg.row0 + 32 * wave;
+    const bool awake = wave_row0 < rg.n_rows;
+    const int32_t wave_most = awake ? row_of(k, rg, head, min((int64_t)rg.n_rows, wave_row0 + 32) - 1).last : -1;
+    const int32_t wave_least = awake ? row_of(k, rg, head, wave_row0).last : -1;
+    const Row row = row_of(k, rg, head, wave_row0 + n);
+
+    half8_t q[KS];
+    float scale;
+    {
+        float top = 0.0f;
+        float x[KS][8];
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            load8(k.q, row.token, row.head, i * 16 + h * 8, x[i]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[i][j]));
+        }
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        uint32_t frac;
+        const int e = min(127, max(-90, exponent_of(top, &frac)));
+        const float f = k.scale < 0.0f ? -pow2f(15 - e) : pow2f(15 - e);
+#pragma unroll
+        for (int i = 0; i < KS; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q[i][j] = (_Float16)(x[i][j] * f);
+        scale = fabsf(k.scale) * kLog2e * pow2f(max(-126, e - 15));
+    }
+
+    float16_t acc[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t) acc[t] = float16_t{};
+    float m = -INFINITY, l = 0.0f;
+    int vr = kNoExp;
+
+    const int lb = a.log_block;
+    uint4 kw[KL], vw[VL];
+    int my_ke = 0, my_ve = 0;  // of tokens [16 (tid % 4), + 16) of the loaded tile
+    auto load = [&](int64_t x) {
+#pragma unroll
+        for (int i = 0; i < KL; ++i) {
+            const int item = tid + i * 256, t = item / ROW;
+            const Place p = place_of(k, table, nullptr, head, x + (t & 48), most);
+            kw[i] = *reinterpret_cast<const uint4*>(
+                a.c.k_code + ((p.at << lb) + p.slot + (t & 15)) * D + item % ROW * 16);
+        }
+        const Place p = place_of(k, table, nullptr, head, x + (tid & 3) * 16, most);
+        const int there = p.pos == INT32_MAX ? 0 : min(16, most - p.pos + 1);
+#pragma unroll
+        for (int i = 0; i < VL; ++i) {
+            const int d = (tid >> 2) + i * 64;
+            vw[i] = *reinterpret_cast<const uint4*>(a.c.v_code + ((p.at * D + d) << lb) + p.slot);
+            if (there < 16) vw[i] = first_codes(vw[i], there);
+        }
+        my_ke = a.c.k_exp[p.at];
+        my_ve = p.pos == INT32_MAX ? kNoExp : a.c.v_exp[p.at];
+    };
+    auto put = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < KL; ++i) {
+            const int item = tid + i * 256, t = item / ROW, piece = item % ROW * 2;
+            const int r = (t & 0x33) | (t & 4) << 1 | (t & 8) >> 1;
+            uint4* const to = lds[buf].k[r];
+            const half8_t x = codes_to_half<INT8>(kw[i].x, kw[i].y);
+            const half8_t y = codes_to_half<INT8>(kw[i].z, kw[i].w);
+            to[piece ^ (r & (D / 8 - 1) & 15)] = __builtin_bit_cast(uint4, x);
+            to[(piece + 1) ^ (r & (D / 8 - 1) & 15)] = __builtin_bit_cast(uint4, y);
+        }
+#pragma unroll
+        for (int i = 0; i < VL; ++i) {
+            const int d = (tid >> 2) + i * 64, piece = (tid & 3) * 2;
+            uint4* const to = lds[buf].v[d];
+            const half8_t x = codes_to_half<INT8>(vw[i].x, vw[i].y);
+            const half8_t y = codes_to_half<INT8>(vw[i].z, vw[i].w);
+            to[piece ^ (d & 7)] = __builtin_bit_cast(uint4, x);
+            to[(piece + 1) ^ (d & 7)] = __builtin_bit_cast(uint4, y);
+        }
+    };
+
+    int buf = 0;
+    int ke[4], ve[4];  // of the tile in `buf`
+    auto keep_exps = [&]() {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            ke[i] = __builtin_amdgcn_readlane(my_ke, i);
+            ve[i] = __builtin_amdgcn_readlane(my_ve, i);
+        }
+    };
+    if (x0 < x1) {
+        load(x0);
+        put(0);
+    }
+    for (int64_t x = x0; x < x1; x += 64, buf ^= 1) {
+        keep_exps();
+        if (x + 64 < x1) load(x + 64);
+        __syncthreads();  // the tile is whole; the other one is read no more
+        if (x <= wave_most) {
+            float16_t s[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                s[t] = float16_t{};
+#pragma unroll
+                for (int i = 0; i < KS; ++i) {
+                    const int r = t * 32 + n;
+                    const half8_t f = __builtin_bit_cast(
+                        half8_t, lds[buf].k[r][(i * 2 + h) ^ (r & (D / 8 - 1) & 15)]);
+                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, q[i], s[t], 0, 0, 0);
+                }
+            }
+            // register r of product t is token 32 t + 16 (r / 8) + 8 h + r % 8
+            if (x + 63 > wave_least) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (x + t * 32 + (r >> 3) * 16 + h * 8 + (r & 7) > row.last) s[t][r] = -INFINITY;
+            }
+            float c[4], top = -INFINITY;
+            int new_vr = vr;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                c[i] = scale * pow2f(ke[i]);
+                float part = -INFINITY;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) part = fmaxf(part, s[i / 2][i % 2 * 8 + r]);
+                top = fmaxf(top, part * c[i]);
+                new_vr = max(new_vr, ve[i]);
+            }
+            top = fmaxf(top, __shfl_xor(top, 32, kWave));
+            const float new_m = fmaxf(m, top);
+            const float base = new_m == -INFINITY ? 0.0f : new_m;
+            const float fall = __builtin_amdgcn_exp2f(m - base);
+            if (__any(new_m > m) || new_vr > vr) {
+                const float both = fall * pow2f(max(-126, vr - new_vr));
+#pragma unroll
+                for (int t = 0; t < DT; ++t) acc[t] *= both;
+                l *= fall;
+            }
+            m = new_m;
+            vr = new_vr;
+            half8_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int shift = max(kLeastShift, min(0, ve[i] - vr)) + kWeightShift;
+                const float add = (float)shift - base;
+                float sum = 0.0f;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 2][i % 2 * 8 + r], c[i], add));
+                    sum += e;
+                    w[i][r] = (_Float16)e;
+                }
+                l += sum * pow2f(-shift);
+            }
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int d = t * 32 + n;
+                    const half8_t f = __builtin_bit_cast(half8_t, lds[buf].v[d][(i * 2 + h) ^ (d & 7)]);
+                    acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, w[i], acc[t], 0, 0, 0);
+                }
+        }
+        if (x + 64 < x1) put(buf ^ 1);
+    }
+    if (!row.live) return;
+    const float total = l + __shfl_xor(l, 32, kWave);
+    const float norm = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
+    const float f = norm * pow2f(max(-126, vr - kWeightShift));
+    const float lse = total > 0.0f ? m + log2f(total) : total == 0.0f ? -INFINITY : total;
+    const int64_t index = row.token * (int64_t)k.group * a.c.heads + row.head;
+    const Partials part_out = partials(k);
+    const bool whole = k.shape.n_chunks == 1;
+    float* const to = part_out.o + (index * k.shape.n_chunks + chunk) * D;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int d = t * 32 + r * 2 + 4 * h;
+            float o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = acc[t][r + i] * f;
+            if (whole)
+                store4(k.out, row.token, row.head, d, o);
+            else
+                *reinterpret_cast<float4_t*>(to + d) = float4_t{o[0], o[1], o[2], o[3]};
+        }
+    if (h == 0) {
+        if (!whole) part_out.lse[index * k.shape.n_chunks + chunk] = lse;
+        else if (k.lse) k.lse[index] = lse * kLn2;
+    }
+}
+
 // The chunks of a row joined: a wave for each row.
 template <int D>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend k) {
@@ -459,7 +690,16 @@ template <int D, bool INT8>
 hipError_t launch_d(const KvAttend& k, hipStream_t st) {
     const KvAttendShape& sh = k.shape;
     const dim3 grid((uint32_t)(sh.units * k.a.c.heads * sh.n_chunks));
-    kv_rows_kernel<D, INT8, 1><<<grid, 256, 0, st>>>(k);
+    if (sh.tiles) {
+        constexpr int kLds = 2 * sizeof(TileLds<D>);
+        if (kLds > 65536)
+            if (hipError_t e = hipFuncSetAttribute((const void*)kv_tiles_kernel<D, INT8>,
+                                                   hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+                e != hipSuccess)
+                return e;
+        kv_tiles_kernel<D, INT8><<<grid, 256, kLds, st>>>(k);
+    } else
+        kv_rows_kernel<D, INT8, 1><<<grid, 256, 0, st>>>(k);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (sh.n_chunks > 1) {
         const int64_t rows = k.a.s.n_tokens * (int64_t)k.group * k.a.c.heads;
@@ -474,7 +714,8 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
                               int64_t keep) {
     KvAttendShape sh = {};
     const int64_t group = q_heads / c.heads;
-    sh.rows = 16;
+    sh.tiles = keep == 0 && s.begin && s.most_new * group > 16;
+    sh.rows = sh.tiles ? 128 : 16;
     const int64_t per = (group + sh.rows - 1) / sh.rows;
     if (keep > 0)
         sh.units = s.n_tokens * per;
