@@ -429,27 +429,44 @@ struct TileLds {
     uint4 v[D][8];       // [dim][piece ^ dim]: eight tokens a piece
 };
 
+// The pages of a sequence as its blocks are walked: entries of its table row, kept within the
+// row's last used block and the pool.
+struct Pages {
+    const int32_t* table;
+    uint32_t last_block, n_blocks;
+    bool bad;
+    __device__ __forceinline__ uint32_t entry(uint32_t block) const {
+        return (uint32_t)table[min(block, last_block)];
+    }
+    __device__ __forceinline__ uint32_t page(uint32_t e) {
+        bad |= e >= n_blocks;
+        return min(e, n_blocks - 1);
+    }
+};
+
 template <int D, bool INT8>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAttend k) {
     constexpr int KS = D / 16, DT = D / 32, ROW = D / 16;  // ROW: loads of a token's keys
     constexpr int KL = 64 * ROW / 256, VL = D * 4 / 256;   // loads of a thread for a tile
+    constexpr int KEY = (D / 8 - 1) & 15;
     extern __shared__ __align__(16) char lds_raw[];
     TileLds<D>* const lds = reinterpret_cast<TileLds<D>*>(lds_raw);
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 31, h = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const KvArgs& a = k.a;
     if (blockIdx.x == 0) kv_check_begin(a);
     // key heads fastest: workgroups of one head share an XCD's L2 where 8 and the number of
     // heads divide; late row groups, which see the most, first
-    const int head = (int)(blockIdx.x % a.c.heads);
-    const int64_t rest = blockIdx.x / a.c.heads;
-    const int64_t u = k.shape.units - 1 - rest / k.shape.n_chunks, chunk = rest % k.shape.n_chunks;
+    const uint32_t heads = a.c.heads, n_chunks = (uint32_t)k.shape.n_chunks;
+    const int head = (int)(blockIdx.x % heads);
+    const uint32_t rest = blockIdx.x / heads, chunk = rest % n_chunks;
     RowGroup rg;
-    if (!row_group(k, u, &rg)) return;
+    if (!row_group(k, k.shape.units - 1 - rest / n_chunks, &rg)) return;
     const int32_t most = row_of(k, rg, head, min((int64_t)rg.n_rows, rg.row0 + 128) - 1).last;
-    const int64_t end_all = (int64_t)most + 1;
-    const int64_t x0 = chunk * k.shape.chunk, x1 = min(end_all, x0 + k.shape.chunk);
-    if (chunk > 0 && x0 >= end_all) return;
-    const int32_t* const table = a.s.table + rg.q.s * a.s.table_stride;
+    const int64_t start = chunk * k.shape.chunk;
+    if (chunk > 0 && start > most) return;
+    const int32_t x0 = (int32_t)start;
+    const int32_t x1 = (int32_t)min((int64_t)most + 1, start + k.shape.chunk);
 
     // this wave's rows: the last position that any sees, and the last that all see
     const int64_t wave_row0 = rg.row0 + 32 * wave;
@@ -486,115 +503,125 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
     float m = -INFINITY, l = 0.0f;
     int vr = kNoExp;
 
-    const int lb = a.log_block;
+    // a thread's loads of a tile: 16 dims of KL tokens' keys, 16 tokens of VL dims' values; the
+    // table entries are read a tile ahead of them
+    const int lb = a.log_block, block = 1 << lb;
+    const uint32_t page_size = heads * (uint32_t)D << lb;
+    Pages pages = {a.s.table + rg.q.s * a.s.table_stride, (uint32_t)max(most, 0) >> lb,
+                   (uint32_t)a.c.n_blocks, false};
+    const uint8_t* const k_base = a.c.k_code + ((int64_t)head * D << lb) + (tid % ROW) * 16;
+    const uint8_t* const v_base = a.c.v_code + ((int64_t)head * D << lb) + (((tid >> 2) << lb) | ((tid & 3) * 16 & (block - 1)));
     uint4 kw[KL], vw[VL];
+    uint32_t k_entry[KL], v_entry;
     int my_ke = 0, my_ve = 0;  // of tokens [16 (tid % 4), + 16) of the loaded tile
-    auto load = [&](int64_t x) {
+    auto find = [&](int32_t x) {
 #pragma unroll
-        for (int i = 0; i < KL; ++i) {
-            const int item = tid + i * 256, t = item / ROW;
-            const Place p = place_of(k, table, nullptr, head, x + (t & 48), most);
-            kw[i] = *reinterpret_cast<const uint4*>(
-                a.c.k_code + ((p.at << lb) + p.slot + (t & 15)) * D + item % ROW * 16);
-        }
-        const Place p = place_of(k, table, nullptr, head, x + (tid & 3) * 16, most);
-        const int there = p.pos == INT32_MAX ? 0 : min(16, most - p.pos + 1);
-#pragma unroll
-        for (int i = 0; i < VL; ++i) {
-            const int d = (tid >> 2) + i * 64;
-            vw[i] = *reinterpret_cast<const uint4*>(a.c.v_code + ((p.at * D + d) << lb) + p.slot);
-            if (there < 16) vw[i] = first_codes(vw[i], there);
-        }
-        my_ke = a.c.k_exp[p.at];
-        my_ve = p.pos == INT32_MAX ? kNoExp : a.c.v_exp[p.at];
+        for (int i = 0; i < KL; ++i)
+            k_entry[i] = pages.entry((uint32_t)(x + (tid / ROW + i * (256 / ROW))) >> lb);
+        v_entry = pages.entry((uint32_t)(x + (tid & 3) * 16) >> lb);
     };
-    auto put = [&](int buf) {
+    auto load = [&]() {
 #pragma unroll
         for (int i = 0; i < KL; ++i) {
-            const int item = tid + i * 256, t = item / ROW, piece = item % ROW * 2;
+            const int slot = (tid / ROW + i * (256 / ROW)) & (block - 1);
+            kw[i] = *reinterpret_cast<const uint4*>(
+                k_base + (uint64_t)pages.page(k_entry[i]) * page_size + slot * D);
+        }
+        const uint32_t page = pages.page(v_entry);
+        const uint8_t* const v = v_base + (uint64_t)page * page_size;
+#pragma unroll
+        for (int i = 0; i < VL; ++i) vw[i] = *reinterpret_cast<const uint4*>(v + (i * 64 << lb));
+        my_ke = a.c.k_exp[(uint64_t)page * heads + head];
+        my_ve = a.c.v_exp[(uint64_t)page * heads + head];
+    };
+    // the loaded codes (of the tile at x) as 16-bit floats in LDS; places past the end, which may
+    // hold anything, as zeros among the values
+    auto put = [&](int buf, int32_t x) {
+        const bool tail = x + 63 > most;
+#pragma unroll
+        for (int i = 0; i < KL; ++i) {
+            const int t = tid / ROW + i * (256 / ROW), piece = tid % ROW * 2;
             const int r = (t & 0x33) | (t & 4) << 1 | (t & 8) >> 1;
             uint4* const to = lds[buf].k[r];
-            const half8_t x = codes_to_half<INT8>(kw[i].x, kw[i].y);
-            const half8_t y = codes_to_half<INT8>(kw[i].z, kw[i].w);
-            to[piece ^ (r & (D / 8 - 1) & 15)] = __builtin_bit_cast(uint4, x);
-            to[(piece + 1) ^ (r & (D / 8 - 1) & 15)] = __builtin_bit_cast(uint4, y);
+            to[piece ^ (r & KEY)] = __builtin_bit_cast(uint4, codes_to_half<INT8>(kw[i].x, kw[i].y));
+            to[(piece ^ (r & KEY)) ^ 1] = __builtin_bit_cast(uint4, codes_to_half<INT8>(kw[i].z, kw[i].w));
         }
 #pragma unroll
         for (int i = 0; i < VL; ++i) {
             const int d = (tid >> 2) + i * 64, piece = (tid & 3) * 2;
+            if (tail) vw[i] = first_codes(vw[i], most - (x + (tid & 3) * 16) + 1);
             uint4* const to = lds[buf].v[d];
-            const half8_t x = codes_to_half<INT8>(vw[i].x, vw[i].y);
-            const half8_t y = codes_to_half<INT8>(vw[i].z, vw[i].w);
-            to[piece ^ (d & 7)] = __builtin_bit_cast(uint4, x);
-            to[(piece + 1) ^ (d & 7)] = __builtin_bit_cast(uint4, y);
+            to[piece ^ (d & 7)] = __builtin_bit_cast(uint4, codes_to_half<INT8>(vw[i].x, vw[i].y));
+            to[(piece ^ (d & 7)) ^ 1] = __builtin_bit_cast(uint4, codes_to_half<INT8>(vw[i].z, vw[i].w));
         }
     };
 
     int buf = 0;
     int ke[4], ve[4];  // of the tile in `buf`
-    auto keep_exps = [&]() {
+    if (x0 < x1) {
+        find(x0);
+        load();
+        find(x0 + 64);
+        put(0, x0);
+    }
+    for (int32_t x = x0; x < x1; x += 64, buf ^= 1) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             ke[i] = __builtin_amdgcn_readlane(my_ke, i);
             ve[i] = __builtin_amdgcn_readlane(my_ve, i);
         }
-    };
-    if (x0 < x1) {
-        load(x0);
-        put(0);
-    }
-    for (int64_t x = x0; x < x1; x += 64, buf ^= 1) {
-        keep_exps();
-        if (x + 64 < x1) load(x + 64);
+        if (x + 64 < x1) {
+            load();
+            find(x + 128);
+        }
         __syncthreads();  // the tile is whole; the other one is read no more
         if (x <= wave_most) {
-            float16_t s[2];
+            float16_t s[2] = {float16_t{}, float16_t{}};
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                s[t] = float16_t{};
+            for (int i = 0; i < KS; ++i)
 #pragma unroll
-                for (int i = 0; i < KS; ++i) {
+                for (int t = 0; t < 2; ++t) {
                     const int r = t * 32 + n;
-                    const half8_t f = __builtin_bit_cast(
-                        half8_t, lds[buf].k[r][(i * 2 + h) ^ (r & (D / 8 - 1) & 15)]);
+                    const half8_t f = __builtin_bit_cast(half8_t, lds[buf].k[r][(i * 2 + h) ^ (r & KEY)]);
                     s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, q[i], s[t], 0, 0, 0);
                 }
-            }
             // register r of product t is token 32 t + 16 (r / 8) + 8 h + r % 8
             if (x + 63 > wave_least) {
+                const int seen = row.last - x - h * 8;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        if (x + t * 32 + (r >> 3) * 16 + h * 8 + (r & 7) > row.last) s[t][r] = -INFINITY;
+                        s[t][r] = t * 32 + (r >> 3) * 16 + (r & 7) > seen ? -INFINITY : s[t][r];
             }
             float c[4], top = -INFINITY;
             int new_vr = vr;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                c[i] = scale * pow2f(ke[i]);
+                c[i] = fmaxf(scale * pow2f(ke[i]), 1.17549435e-38f);  // -inf * 0 is no score
                 float part = -INFINITY;
 #pragma unroll
                 for (int r = 0; r < 8; ++r) part = fmaxf(part, s[i / 2][i % 2 * 8 + r]);
                 top = fmaxf(top, part * c[i]);
+                // places past the end have some block's exponent: no larger than one that was there
                 new_vr = max(new_vr, ve[i]);
             }
             top = fmaxf(top, __shfl_xor(top, 32, kWave));
             const float new_m = fmaxf(m, top);
             const float base = new_m == -INFINITY ? 0.0f : new_m;
-            const float fall = __builtin_amdgcn_exp2f(m - base);
             if (__any(new_m > m) || new_vr > vr) {
+                const float fall = __builtin_amdgcn_exp2f(m - base);
                 const float both = fall * pow2f(max(-126, vr - new_vr));
 #pragma unroll
                 for (int t = 0; t < DT; ++t) acc[t] *= both;
                 l *= fall;
+                m = new_m;
+                vr = new_vr;
             }
-            m = new_m;
-            vr = new_vr;
             half8_t w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int shift = max(kLeastShift, min(0, ve[i] - vr)) + kWeightShift;
+                const int shift = max(kLeastShift, ve[i] - vr) + kWeightShift;
                 const float add = (float)shift - base;
                 float sum = 0.0f;
 #pragma unroll
@@ -606,16 +633,17 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
                 l += sum * pow2f(-shift);
             }
 #pragma unroll
-            for (int t = 0; t < DT; ++t)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int t = 0; t < DT; ++t) {
                     const int d = t * 32 + n;
                     const half8_t f = __builtin_bit_cast(half8_t, lds[buf].v[d][(i * 2 + h) ^ (d & 7)]);
                     acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, w[i], acc[t], 0, 0, 0);
                 }
         }
-        if (x + 64 < x1) put(buf ^ 1);
+        if (x + 64 < x1) put(buf ^ 1, x + 64);
     }
+    if (pages.bad) raise_status(a.status, MP_EINVAL);
     if (!row.live) return;
     const float total = l + __shfl_xor(l, 32, kWave);
     const float norm = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
@@ -623,8 +651,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
     const float lse = total > 0.0f ? m + log2f(total) : total == 0.0f ? -INFINITY : total;
     const int64_t index = row.token * (int64_t)k.group * a.c.heads + row.head;
     const Partials part_out = partials(k);
-    const bool whole = k.shape.n_chunks == 1;
-    float* const to = part_out.o + (index * k.shape.n_chunks + chunk) * D;
+    const bool whole = n_chunks == 1;
+    float* const to = part_out.o + (index * n_chunks + chunk) * D;
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -639,7 +667,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
                 *reinterpret_cast<float4_t*>(to + d) = float4_t{o[0], o[1], o[2], o[3]};
         }
     if (h == 0) {
-        if (!whole) part_out.lse[index * k.shape.n_chunks + chunk] = lse;
+        if (!whole) part_out.lse[index * n_chunks + chunk] = lse;
         else if (k.lse) k.lse[index] = lse * kLn2;
     }
 }
