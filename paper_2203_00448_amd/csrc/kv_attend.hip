@@ -31,6 +31,9 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kWeightShift = 15;   // weights reach 2^15
 constexpr int kLeastShift = -80;   // of a block's value exponent below the largest
 constexpr int kNoExp = -127;       // the largest value exponent of nothing
+// The exponent of a weight is one multiply-add, c s - m, which is off the rounded m by half of its
+// last place; scores beyond this are rounded first, so that none is above its maximum.
+constexpr float kLargeScore = 0x1p20f;
 constexpr int kStep = 64;          // tokens a wave takes at a time
 
 // The partial result of a row over a chunk of tokens: o (normalised) and the base-2
@@ -114,45 +117,23 @@ __device__ __forceinline__ Row row_of(const KvAttend& k, const RowGroup& g, int 
     return r;
 }
 
-// Sixteen tokens of a step: their block and the position of the first.
-struct Place {
-    int64_t at;    // block * heads + head, for the codes and exponents
-    int32_t pos;   // INT32_MAX where there is none
-    int32_t slot;  // of the first token in its block
+// The pages of a sequence as its blocks are walked: entries of its table row, kept within the
+// row's last used block and the pool.
+struct Pages {
+    const int32_t* table;
+    uint32_t last_block, n_blocks;
+    bool bad;
+    __device__ __forceinline__ uint32_t entry(uint32_t block) const {
+        return (uint32_t)table[min(block, last_block)];
+    }
+    __device__ __forceinline__ uint32_t page(uint32_t e) {
+        bad |= e >= n_blocks;
+        return min(e, n_blocks - 1);
+    }
 };
 
-// Tokens [x, x + 16) of the sequence (or of the blocks listed for it).
-__device__ __forceinline__ Place place_of(const KvAttend& k, const int32_t* table,
-                                          const int32_t* list, int head, int64_t x,
-                                          int32_t most) {
-    Place p;
-    const int lb = k.a.log_block;
-    int64_t b = x >> lb;
-    p.slot = (int32_t)(x & ((1 << lb) - 1));
-    bool there = true;
-    if (list) {
-        const int32_t named = b < k.keep ? list[b] : -1;
-        there = named >= 0 && named <= (most >> lb);
-        if (!there && named != -1) raise_status(k.a.status, MP_EINVAL);
-        b = there ? named : 0;
-    } else {
-        there = x <= most;
-    }
-    p.pos = (int32_t)((b << lb) + p.slot);
-    there = there && p.pos <= most;
-    int32_t page = there ? table[b] : 0;
-    if (page < 0 || page >= k.a.c.n_blocks) {
-        raise_status(k.a.status, MP_EINVAL);
-        there = false;
-        page = 0;
-    }
-    if (!there) p.pos = INT32_MAX;
-    p.at = (int64_t)page * k.a.c.heads + head;
-    return p;
-}
-
 // A row's query as the factor of the first product; `scale` becomes what its scores are
-// multiplied by.  Lane (column n, quarter g) holds dims [64 c + 16 g, + 16).
+// multiplied by, not negative: the query takes the sign.  Lane (column n, quarter g) holds dims [64 c + 16 g, + 16).
 template <int D>
 __device__ __forceinline__ void load_query(const KvAttend& k, const Row& r, int g,
                                            half8_t (&q)[D / 64][2], float* scale) {
@@ -168,12 +149,12 @@ __device__ __forceinline__ void load_query(const KvAttend& k, const Row& r, int 
     top = fmaxf(top, __shfl_xor(top, 32, kWave));
     uint32_t frac;
     const int e = min(127, max(-90, exponent_of(top, &frac)));
-    const float f = pow2f(15 - e);
+    const float f = k.scale < 0.0f ? -pow2f(15 - e) : pow2f(15 - e);
 #pragma unroll
     for (int c = 0; c < D / 64; ++c)
 #pragma unroll
         for (int i = 0; i < 16; ++i) q[c][i / 8][i % 8] = (_Float16)(x[c][i] * f);
-    *scale = k.scale * kLog2e * pow2f(max(-126, e - 15));
+    *scale = fabsf(k.scale) * kLog2e * pow2f(max(-126, e - 15));
 }
 
 // Values at places of which only the first n of 16 exist: the others' codes to zero.
@@ -187,229 +168,245 @@ __device__ __forceinline__ uint4 first_codes(uint4 w, int n) {
     return make_uint4(x[0], x[1], x[2], x[3]);
 }
 
-// Few rows: 16 columns of rows times NT, one key head, one chunk of tokens.  Each of four
-// waves takes every fourth step of 64 tokens, with its own running maxima, and the four
-// are joined at the end.  A wave reads the codes straight into registers, the next step's
-// while it computes this one; nothing is shared, so there is no barrier in the loop.
+// Few rows: 16 columns of rows, one key head, one chunk of tokens.  Each of four waves takes
+// every fourth step of 64 tokens, with its own running maxima, and the four are joined at
+// the end.  A wave reads the codes straight into registers, the next step's keys as soon as
+// this one's are used, the values likewise; nothing is shared, so there is no barrier in
+// the loop and what hides the latency is the other waves of the SIMD.
 //
 // Tokens: key row m of tile t holds token 16 (m / 4) + 4 t + m % 4 of the step.  Lane
 // quarter g then has the scores of tokens [16 g, 16 g + 16), four from each tile, which
 // are the columns of 16 bytes of each row of values.
-template <int D, bool INT8, int NT>
-__global__ __launch_bounds__(256) void kv_rows_kernel(KvAttend k) {
+//
+// LIST: the tokens are those of the blocks listed for the row's token.
+template <int D, bool INT8, bool LIST>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend k) {
     constexpr int DT = D / 16, DC = D / 64;
     __shared__ __align__(16) float so[4][16][D + 4];
     __shared__ float sm[4][16], sl[4][16];
     __shared__ int svr[4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const KvArgs& a = k.a;
     if (blockIdx.x == 0) kv_check_begin(a);
-    const int64_t u = blockIdx.x / ((int64_t)a.c.heads * k.shape.n_chunks);
-    const int rest = (int)(blockIdx.x % ((int64_t)a.c.heads * k.shape.n_chunks));
-    const int head = rest % a.c.heads;
-    const int64_t chunk = rest / a.c.heads;
+    const uint32_t heads = a.c.heads, n_chunks = (uint32_t)k.shape.n_chunks;
+    const int head = (int)(blockIdx.x % heads);
+    const uint32_t rest = blockIdx.x / heads, chunk = rest % n_chunks;
     RowGroup rg;
-    if (!row_group(k, u, &rg)) return;
-    const int64_t last_row = min((int64_t)rg.n_rows, rg.row0 + 16 * NT) - 1;
+    if (!row_group(k, rest / n_chunks, &rg)) return;
+    const int64_t last_row = min((int64_t)rg.n_rows, rg.row0 + 16) - 1;
     const int32_t most = row_of(k, rg, head, last_row).last;  // the last position any row sees
     const int32_t least = row_of(k, rg, head, rg.row0).last;  // all rows see up to here
-    const int32_t* const table = a.s.table + rg.q.s * a.s.table_stride;
-    const int32_t* const list =
-        k.blocks ? k.blocks + (rg.q.begin * a.c.heads + head) * k.keep : nullptr;
-    const int64_t end_all = list ? (int64_t)k.keep << a.log_block : (int64_t)most + 1;
-    const int64_t x0 = chunk * k.shape.chunk, x1 = min(end_all, x0 + k.shape.chunk);
-    if (chunk > 0 && x0 >= end_all) return;
+    const int lb = a.log_block, block = 1 << lb;
+    const int64_t start = chunk * k.shape.chunk;
+    const int64_t end_all = LIST ? (int64_t)k.keep << lb : (int64_t)most + 1;
+    if (chunk > 0 && start >= end_all) return;
+    const int32_t x1 = (int32_t)min(end_all, start + k.shape.chunk);
 
-    Row row[NT];
-    half8_t q[NT][DC][2];
-    float scale[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        row[j] = row_of(k, rg, head, rg.row0 + 16 * j + n);
-        load_query<D>(k, row[j], g, q[j], &scale[j]);
-    }
-    float4_t acc[NT][DT];
-    float m[NT], l[NT];
-    int vr = kNoExp;
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        m[j] = -INFINITY;
-        l[j] = 0.0f;
-#pragma unroll
-        for (int t = 0; t < DT; ++t) acc[j][t] = float4_t{0, 0, 0, 0};
-    }
-
-    const int lb = a.log_block;
-    const int64_t stride = 4 * kStep;
+    Pages pages = {a.s.table + rg.q.s * a.s.table_stride, (uint32_t)max(most, 0) >> lb,
+                   (uint32_t)a.c.n_blocks, false};
+    const int32_t* const list = LIST ? k.blocks + (rg.q.begin * heads + head) * k.keep : nullptr;
+    const uint32_t page_size = heads * (uint32_t)D << lb;
+    const int k_slot = ((n >> 2) * 16) & (block - 1), v_slot = (g * 16) & (block - 1);
+    const uint8_t* const k_base =
+        a.c.k_code + ((int64_t)head * D << lb) + (k_slot + (n & 3)) * D + g * 16;
+    const uint8_t* const v_base = a.c.v_code + ((int64_t)head * D << lb) + ((n << lb) | v_slot);
     uint4 kw[4][DC], vw[DT];
-    int ke, ve;
-    Place kp, vp;  // of the loaded step
-    auto find = [&](int64_t x) {
-        kp = place_of(k, table, list, head, x + (n >> 2) * 16, most);
-        vp = place_of(k, table, list, head, x + g * 16, most);
+    // of the loaded step: the exponents of tokens [16 g, + 16), the position of the first;
+    // of the one after: the table entries of the keys' and the values' tokens
+    int ke = 0, ve = 0;
+    int32_t pos = 0, next_pos = 0;
+    uint32_t k_entry = 0, v_entry = 0;
+    const int32_t kNowhere = INT32_MAX - 64;  // the position of a place that names no block
+    auto named = [&](int32_t x) -> int32_t {
+        const int32_t b = x >> lb;
+        const int32_t id = b < k.keep ? list[b] : -1;
+        if (id != -1 && (uint32_t)id > (uint32_t)most >> lb) pages.bad = true;
+        return (uint32_t)id <= (uint32_t)most >> lb && most >= 0 ? id : -1;
     };
-    auto load = [&]() {
-        const uint8_t* kc = a.c.k_code + ((kp.at << lb) + kp.slot + (n & 3)) * D + g * 16;
+    auto find = [&](int32_t x) {
+        if (LIST) {
+            const int32_t kb = named(x + (n >> 2) * 16), vb = named(x + g * 16);
+            k_entry = kb < 0 ? 0 : pages.entry((uint32_t)kb);
+            v_entry = vb < 0 ? 0 : pages.entry((uint32_t)vb);
+            next_pos = vb < 0 ? kNowhere : (vb << lb) + v_slot;
+        } else {
+            k_entry = pages.entry((uint32_t)(x + (n >> 2) * 16) >> lb);
+            v_entry = pages.entry((uint32_t)(x + g * 16) >> lb);
+            next_pos = x + g * 16;
+        }
+    };
+    auto load_keys = [&]() {
+        const uint8_t* const p = k_base + (uint64_t)pages.page(k_entry) * page_size;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int c = 0; c < DC; ++c)
-                kw[t][c] = *reinterpret_cast<const uint4*>(kc + t * 4 * D + c * 64);
-        const uint8_t* vc = a.c.v_code + ((vp.at * D + n) << lb) + vp.slot;
-#pragma unroll
-        for (int t = 0; t < DT; ++t)
-            vw[t] = *reinterpret_cast<const uint4*>(vc + ((int64_t)t * 16 << lb));
-        ke = a.c.k_exp[vp.at];
-        ve = a.c.v_exp[vp.at];
+                kw[t][c] = *reinterpret_cast<const uint4*>(p + t * 4 * D + c * 64);
     };
-    int64_t x = x0 + wave * kStep;
+    auto load_values = [&]() {
+        const uint32_t page = pages.page(v_entry);
+        const uint8_t* const p = v_base + (uint64_t)page * page_size;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) vw[t] = *reinterpret_cast<const uint4*>(p + (t * 16 << lb));
+        ke = a.c.k_exp[(uint64_t)page * heads + head];
+        ve = a.c.v_exp[(uint64_t)page * heads + head];
+        pos = next_pos;
+    };
+    int32_t x = (int32_t)start + wave * kStep;
+    const int32_t stride = 4 * kStep;
     if (x < x1) {
         find(x);
-        load();
+        load_keys();
+        load_values();
+        if (x + stride < x1) find(x + stride);
     }
+    const Row row = row_of(k, rg, head, rg.row0 + n);
+    half8_t q[DC][2];
+    float scale;
+    load_query<D>(k, row, g, q, &scale);
+    float4_t acc[DT];
+    float m = -INFINITY, l = 0.0f;
+    int vr = kNoExp;
+#pragma unroll
+    for (int t = 0; t < DT; ++t) acc[t] = float4_t{0, 0, 0, 0};
+
     for (; x < x1; x += stride) {
-        half8_t kh[4][DC][2], vh[DT][2];
-        const int32_t pos = vp.pos;
-        const int my_ke = ke, my_ve = ve;
-        // whether some row does not see some token of the step
-        const bool part = __any(pos == INT32_MAX || pos + 15 > least);
-        if (part) {
-            const int there = pos == INT32_MAX ? 0 : min(16, most - pos + 1);
+        float s[16];
 #pragma unroll
-            for (int t = 0; t < DT; ++t) vw[t] = first_codes(vw[t], there);
-        }
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < 4; ++t) {
+            float4_t z = {0, 0, 0, 0};
 #pragma unroll
             for (int c = 0; c < DC; ++c) {
-                kh[t][c][0] = codes_to_half<INT8>(kw[t][c].x, kw[t][c].y);
-                kh[t][c][1] = codes_to_half<INT8>(kw[t][c].z, kw[t][c].w);
+                z = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                    codes_to_half<INT8>(kw[t][c].x, kw[t][c].y), q[c][0], z, 0, 0, 0);
+                z = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+                    codes_to_half<INT8>(kw[t][c].z, kw[t][c].w), q[c][1], z, 0, 0, 0);
             }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[t * 4 + r] = z[r];
+        }
+        const bool more = x + stride < x1;
+        if (more) load_keys();
+        // whether some row does not see some token of the step
+        if (LIST ? __any(pos + 15 > least) : x + kStep - 1 > least) {
+            const int seen = row.last - pos;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = i > seen ? -INFINITY : s[i];
+            // places past the end may hold anything
+#pragma unroll
+            for (int t = 0; t < DT; ++t) vw[t] = first_codes(vw[t], most - pos + 1);
+        }
+        float c = fmaxf(scale * pow2f(ke), 1.17549435e-38f);  // -inf * 0 is no score
+        float top = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+        top *= c;
+        top = fmaxf(top, __shfl_xor(top, 16, kWave));
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        // places that name no block have no exponent
+        int top_ve = LIST && pos == kNowhere ? kNoExp : ve;
+        if (lb < 6) {
+            top_ve = max(top_ve, __shfl_xor(top_ve, 16, kWave));
+            top_ve = max(top_ve, __shfl_xor(top_ve, 32, kWave));
+        }
+        const float new_m = fmaxf(m, top);
+        const int new_vr = max(vr, __builtin_amdgcn_readfirstlane(top_ve));
+        const float base = new_m == -INFINITY ? 0.0f : new_m;
+        if (__any(fabsf(base) > kLargeScore)) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] *= c;
+            c = 1.0f;
+        }
+        if (__any(new_m > m) || new_vr > vr) {
+            const float fall = __builtin_amdgcn_exp2f(m - base);
+            const float both = fall * pow2f(max(-126, vr - new_vr));
+#pragma unroll
+            for (int t = 0; t < DT; ++t) acc[t] *= both;
+            l *= fall;
+            m = new_m;
+            vr = new_vr;
+        }
+        const int shift = max(kLeastShift, min(0, ve - vr)) + kWeightShift;
+        const float add = (float)shift - base;
+        float sum = 0.0f;
+        half8_t w[2];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, add));
+            sum += e;
+            w[i / 8][i % 8] = (_Float16)e;
+        }
+        l += sum * pow2f(-shift);
 #pragma unroll
         for (int t = 0; t < DT; ++t) {
-            vh[t][0] = codes_to_half<INT8>(vw[t].x, vw[t].y);
-            vh[t][1] = codes_to_half<INT8>(vw[t].z, vw[t].w);
+            acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half<INT8>(vw[t].x, vw[t].y),
+                                                            w[0], acc[t], 0, 0, 0);
+            acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half<INT8>(vw[t].z, vw[t].w),
+                                                            w[1], acc[t], 0, 0, 0);
         }
-        if (x + stride < x1) {
-            find(x + stride);
-            load();
-        }
-        // the largest value exponent so far; places that are not there have none
-        int top_ve = pos == INT32_MAX ? kNoExp : my_ve;
-        top_ve = max(top_ve, __shfl_xor(top_ve, 16, kWave));
-        top_ve = max(top_ve, __shfl_xor(top_ve, 32, kWave));
-        const int new_vr = max(vr, top_ve);
-        const int shift = max(kLeastShift, min(0, my_ve - new_vr)) + kWeightShift;
-        const float v_fall = pow2f(max(-126, vr - new_vr)), unshift = pow2f(-shift);
-        vr = new_vr;
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            float s[16];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                float4_t z = {0, 0, 0, 0};
-#pragma unroll
-                for (int c = 0; c < DC; ++c) {
-                    z = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh[t][c][0], q[j][c][0], z, 0, 0, 0);
-                    z = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh[t][c][1], q[j][c][1], z, 0, 0, 0);
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s[t * 4 + r] = z[r];
-            }
-            const float f = scale[j] * pow2f(my_ke);
-            float top = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[i] *= f;
-                if (part && (pos == INT32_MAX || pos + i > row[j].last)) s[i] = -INFINITY;
-                top = fmaxf(top, s[i]);
-            }
-            top = fmaxf(top, __shfl_xor(top, 16, kWave));
-            top = fmaxf(top, __shfl_xor(top, 32, kWave));
-            const float new_m = fmaxf(m[j], top);
-            const float base = new_m == -INFINITY ? 0.0f : new_m;
-            const float fall = __builtin_amdgcn_exp2f(m[j] - base);
-            m[j] = new_m;
-            const float add = (float)shift - base;
-            float sum = 0.0f;
-            half8_t w[2];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float e = __builtin_amdgcn_exp2f(s[i] + add);
-                sum += e;
-                w[i / 8][i % 8] = (_Float16)e;
-            }
-            l[j] = l[j] * fall + sum * unshift;
-            const float both = fall * v_fall;
-#pragma unroll
-            for (int t = 0; t < DT; ++t) {
-                acc[j][t] *= both;
-                acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh[t][0], w[0], acc[j][t], 0, 0, 0);
-                acc[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh[t][1], w[1], acc[j][t], 0, 0, 0);
-            }
+        if (more) {
+            load_values();
+            if (x + 2 * stride < x1) find(x + 2 * stride);
         }
     }
+    if (pages.bad) raise_status(a.status, MP_EINVAL);
 
     // the four waves' results of a row joined
-    const Partials part_out = partials(k);
+    l += __shfl_xor(l, 16, kWave);
+    l += __shfl_xor(l, 32, kWave);
+    if (g == 0) {
+        sm[wave][n] = m;
+        sl[wave][n] = l;
+    }
+    if (lane == 0) svr[wave] = vr;
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        float sum = l[j];
-        sum += __shfl_xor(sum, 16, kWave);
-        sum += __shfl_xor(sum, 32, kWave);
-        if (j) __syncthreads();
-        if (g == 0) {
-            sm[wave][n] = m[j];
-            sl[wave][n] = sum;
+    for (int t = 0; t < DT; ++t)
+        *reinterpret_cast<float4_t*>(&so[wave][n][t * 16 + g * 4]) = acc[t];
+    __syncthreads();
+    const int col = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * (D / 16);
+    const float top = fmaxf(fmaxf(sm[0][col], sm[1][col]), fmaxf(sm[2][col], sm[3][col]));
+    const float base = top == -INFINITY ? 0.0f : top;
+    const int most_vr = max(max(svr[0], svr[1]), max(svr[2], svr[3]));
+    float total = 0.0f, o[D / 16];
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) o[i] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float f = __builtin_amdgcn_exp2f(sm[w][col] - base);
+        const float fv = f * pow2f(max(-126, svr[w] - most_vr));
+        total += sl[w][col] * f;
+#pragma unroll
+        for (int i = 0; i < D / 16; i += 4) {
+            const float4_t y = *reinterpret_cast<const float4_t*>(&so[w][col][d0 + i]);
+#pragma unroll
+            for (int z = 0; z < 4; ++z) o[i + z] += y[z] * fv;
         }
-        if (lane == 0) svr[wave] = vr;
+    }
+    const Row r = row_of(k, rg, head, rg.row0 + col);
+    if (!r.live) return;
+    // a row that sees nothing: weights and sums are zero
+    const float norm = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
+    const float back = norm * pow2f(max(-126, most_vr - kWeightShift));
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
-            *reinterpret_cast<float4_t*>(&so[wave][n][t * 16 + g * 4]) = acc[j][t];
-        __syncthreads();
-        const int col = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * (D / 16);
-        float top = fmaxf(fmaxf(sm[0][col], sm[1][col]), fmaxf(sm[2][col], sm[3][col]));
-        const float base = top == -INFINITY ? 0.0f : top;
-        const int most_vr = max(max(svr[0], svr[1]), max(svr[2], svr[3]));
-        float total = 0.0f, o[D / 16];
+    for (int i = 0; i < D / 16; ++i) o[i] *= back;
+    const float lse = total > 0.0f ? base + log2f(total) : total == 0.0f ? -INFINITY : total;
+    const int64_t index = r.token * (int64_t)k.group * heads + r.head;
+    if (n_chunks > 1) {
+        const Partials part_out = partials(k);
+        float* to = part_out.o + (index * n_chunks + chunk) * D + d0;
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) o[i] = 0.0f;
+        for (int i = 0; i < D / 16; i += 4)
+            *reinterpret_cast<float4_t*>(to + i) = float4_t{o[i], o[i + 1], o[i + 2], o[i + 3]};
+        if (d0 == 0) part_out.lse[index * n_chunks + chunk] = lse;
+    } else {
+        if constexpr (D / 16 >= 8) {
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float f = __builtin_amdgcn_exp2f(sm[w][col] - base);
-            const float fv = f * pow2f(max(-126, svr[w] - most_vr));
-            total += sl[w][col] * f;
-#pragma unroll
-            for (int i = 0; i < D / 16; i += 4) {
-                const float4_t y = *reinterpret_cast<const float4_t*>(&so[w][col][d0 + i]);
-#pragma unroll
-                for (int z = 0; z < 4; ++z) o[i + z] += y[z] * fv;
-            }
-        }
-        const Row r = row_of(k, rg, head, rg.row0 + 16 * j + col);
-        if (!r.live) continue;
-        // a row that sees nothing: weights and sums are zero
-        const float norm = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
-        const float back = pow2f(max(-126, most_vr - kWeightShift));
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) o[i] = o[i] * norm * back;
-        const float lse = total > 0.0f ? base + log2f(total) : total == 0.0f ? -INFINITY : total;
-        const int64_t index = r.token * (int64_t)k.group * a.c.heads + r.head;
-        if (k.shape.n_chunks > 1) {
-            float* to = part_out.o + (index * k.shape.n_chunks + chunk) * D + d0;
-#pragma unroll
-            for (int i = 0; i < D / 16; i += 4)
-                *reinterpret_cast<float4_t*>(to + i) = float4_t{o[i], o[i + 1], o[i + 2], o[i + 3]};
-            if (d0 == 0) part_out.lse[index * k.shape.n_chunks + chunk] = lse;
+            for (int i = 0; i < D / 16; i += 8) store8(k.out, r.token, r.head, d0 + i, o + i);
         } else {
-            if constexpr (D / 16 >= 8) {
-#pragma unroll
-                for (int i = 0; i < D / 16; i += 8) store8(k.out, r.token, r.head, d0 + i, o + i);
-            } else {
-                store4(k.out, r.token, r.head, d0, o);
-            }
-            if (k.lse && d0 == 0) k.lse[index] = lse * kLn2;
+            store4(k.out, r.token, r.head, d0, o);
         }
+        if (k.lse && d0 == 0) k.lse[index] = lse * kLn2;
     }
 }
 
@@ -427,21 +424,6 @@ template <int D>
 struct TileLds {
     uint4 k[64][D / 8];  // [32 * half + row][piece ^ row]
     uint4 v[D][8];       // [dim][piece ^ dim]: eight tokens a piece
-};
-
-// The pages of a sequence as its blocks are walked: entries of its table row, kept within the
-// row's last used block and the pool.
-struct Pages {
-    const int32_t* table;
-    uint32_t last_block, n_blocks;
-    bool bad;
-    __device__ __forceinline__ uint32_t entry(uint32_t block) const {
-        return (uint32_t)table[min(block, last_block)];
-    }
-    __device__ __forceinline__ uint32_t page(uint32_t e) {
-        bad |= e >= n_blocks;
-        return min(e, n_blocks - 1);
-    }
 };
 
 template <int D, bool INT8>
@@ -609,6 +591,14 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
             top = fmaxf(top, __shfl_xor(top, 32, kWave));
             const float new_m = fmaxf(m, top);
             const float base = new_m == -INFINITY ? 0.0f : new_m;
+            if (__any(fabsf(base) > kLargeScore)) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) s[i / 2][i % 2 * 8 + r] *= c[i];
+                    c[i] = 1.0f;
+                }
+            }
             if (__any(new_m > m) || new_vr > vr) {
                 const float fall = __builtin_amdgcn_exp2f(m - base);
                 const float both = fall * pow2f(max(-126, vr - new_vr));
@@ -726,8 +716,11 @@ hipError_t launch_d(const KvAttend& k, hipStream_t st) {
                 e != hipSuccess)
                 return e;
         kv_tiles_kernel<D, INT8><<<grid, 256, kLds, st>>>(k);
-    } else
-        kv_rows_kernel<D, INT8, 1><<<grid, 256, 0, st>>>(k);
+    } else if (k.blocks) {
+        kv_rows_kernel<D, INT8, true><<<grid, 256, 0, st>>>(k);
+    } else {
+        kv_rows_kernel<D, INT8, false><<<grid, 256, 0, st>>>(k);
+    }
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (sh.n_chunks > 1) {
         const int64_t rows = k.a.s.n_tokens * (int64_t)k.group * k.a.c.heads;

@@ -4,12 +4,15 @@ argument marshalling only, like binding.py.
 A program keeps a `Cache` (its memory), a `Seqs` for its batch (block table,
 lengths, the call's rows), a status word and workspaces, and calls `write`,
 `read`, `select` and `attend` on them; outputs may be views of a planned slab.
+Each takes `stream=` besides (the current one if not given); tensors that are
+in use on another stream are the caller's to wait for.
 The tensors that a handle was made of stay the caller's: changing their
 values, not their places, changes what the next call sees.
 """
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 
@@ -172,9 +175,21 @@ _MOVED = (torch.bfloat16, torch.float16, torch.float32)
 _QUERIES = (torch.bfloat16, torch.float16)
 
 
-def _stream(stream, device):
-    s = stream if stream is not None else torch.cuda.current_stream(device)
-    return s.cuda_stream
+def _on_stream(call):
+    """`call` with its `stream` made the current one, so that what it allocates belongs to that
+    stream and the wait of check=True is for it."""
+    @functools.wraps(call)
+    def on(*args, stream=None, **more):
+        if stream is None:
+            return call(*args, **more)
+        with torch.cuda.stream(stream):
+            return call(*args, **more)
+
+    return on
+
+
+def _stream(device):
+    return torch.cuda.current_stream(device).cuda_stream
 
 
 def workspace_size(op: int, cache: Cache, seqs: Seqs, *, q_heads: int, keep: int = 0) -> int:
@@ -188,21 +203,23 @@ def workspace(op: int, cache: Cache, seqs: Seqs, *, q_heads: int, keep: int = 0)
     return torch.empty(max(need, 16), dtype=torch.uint8, device=cache.device)
 
 
-def write(cache: Cache, seqs: Seqs, k, v, *, status=None, check: bool = True, stream=None):
+@_on_stream
+def write(cache: Cache, seqs: Seqs, k, v, *, status=None, check: bool = True):
     """Store the call's keys and values (mp_kv_write): k, v [tokens, heads, dim] in bfloat16,
     float16 or float32, any strides over a contiguous last dimension."""
     L = load_library()
     ka = _rows(k, "k", seqs.tokens, cache.heads, cache.dim, _MOVED)
     va = _rows(v, "v", seqs.tokens, cache.heads, cache.dim, _MOVED)
     if status is None:
-        status = new_status(cache.device, stream)
+        status = new_status(cache.device)
     rc = L.mp_kv_write(cache._ref, seqs._for(cache), ctypes.addressof(ka), ctypes.addressof(va),
-                       status.data_ptr(), _stream(stream, cache.device))
+                       status.data_ptr(), _stream(cache.device))
     _finish(rc, status, "kv.write", check)
 
 
+@_on_stream
 def read(cache: Cache, seqs: Seqs, *, dtype=torch.bfloat16, out=None, status=None,
-         check: bool = True, stream=None):
+         check: bool = True):
     """Read back the call's tokens (mp_kv_read): (k, v) [tokens, heads, dim]."""
     L = load_library()
     if out is None:
@@ -212,9 +229,9 @@ def read(cache: Cache, seqs: Seqs, *, dtype=torch.bfloat16, out=None, status=Non
     ka = _rows(k, "k", seqs.tokens, cache.heads, cache.dim, _MOVED)
     va = _rows(v, "v", seqs.tokens, cache.heads, cache.dim, _MOVED)
     if status is None:
-        status = new_status(cache.device, stream)
+        status = new_status(cache.device)
     rc = L.mp_kv_read(cache._ref, seqs._for(cache), ctypes.addressof(ka), ctypes.addressof(va),
-                      status.data_ptr(), _stream(stream, cache.device))
+                      status.data_ptr(), _stream(cache.device))
     _finish(rc, status, "kv.read", check)
     return k, v
 
@@ -225,8 +242,9 @@ def _space(op, cache, seqs, q_heads, keep, workspace):
     return workspace, workspace.numel() * workspace.element_size()
 
 
+@_on_stream
 def attend(cache: Cache, seqs: Seqs, q, *, scale: float | None = None, blocks=None, out=None,
-           lse=None, status=None, workspace=None, check: bool = True, stream=None):
+           lse=None, status=None, workspace=None, check: bool = True):
     """Attention of q [tokens, q_heads, dim] (bfloat16 or float16) over the cache
     (mp_kv_attend), causal: the rows of a sequence are its last tokens.  `scale` defaults to
     dim ** -0.5.  `blocks` int32 [tokens, heads, keep] limits each row to these of its
@@ -252,17 +270,18 @@ def attend(cache: Cache, seqs: Seqs, q, *, scale: float | None = None, blocks=No
             raise ValueError("lse must be contiguous")
     workspace, have = _space(OP_ATTEND, cache, seqs, heads, keep, workspace)
     if status is None:
-        status = new_status(cache.device, stream)
+        status = new_status(cache.device)
     rc = L.mp_kv_attend(cache._ref, seqs._for(cache), ctypes.addressof(qa), heads,
                         cache.dim ** -0.5 if scale is None else scale, named, keep,
                         ctypes.addressof(oa), lse.data_ptr() if lse is not None else None,
-                        workspace.data_ptr(), have, status.data_ptr(), _stream(stream, cache.device))
+                        workspace.data_ptr(), have, status.data_ptr(), _stream(cache.device))
     _finish(rc, status, "kv.attend", check)
     return out
 
 
+@_on_stream
 def select(cache: Cache, seqs: Seqs, q, *, keep: int, first: int = 1, recent: int = 1, out=None,
-           status=None, workspace=None, check: bool = True, stream=None):
+           status=None, workspace=None, check: bool = True):
     """The blocks of each row and key head that attend is to read (mp_kv_select): the first
     `first`, the last `recent` and the best-scored others, `keep` in all, int32 [tokens, heads,
     keep], ascending, -1 beyond the last."""
@@ -279,9 +298,9 @@ def select(cache: Cache, seqs: Seqs, q, *, keep: int, first: int = 1, recent: in
         raise ValueError("out must be contiguous")
     workspace, have = _space(OP_SELECT, cache, seqs, heads, keep, workspace)
     if status is None:
-        status = new_status(cache.device, stream)
+        status = new_status(cache.device)
     rc = L.mp_kv_select(cache._ref, seqs._for(cache), ctypes.addressof(qa), heads, keep, first, recent,
                         out.data_ptr() or None, workspace.data_ptr(), have, status.data_ptr(),
-                        _stream(stream, cache.device))
+                        _stream(cache.device))
     _finish(rc, status, "kv.select", check)
     return out
