@@ -34,6 +34,9 @@ constexpr int kNoExp = -127;       // the largest value exponent of nothing
 // The exponent of a weight is one multiply-add, c s - m, which is off the rounded m by half of its
 // last place; scores beyond this are rounded first, so that none is above its maximum.
 constexpr float kLargeScore = 0x1p20f;
+// How far (in powers of two) a score may be above the running maximum before that follows: a
+// weight then reaches 2^15.99, below the largest 16-bit float.
+constexpr float kSlack = 0.99f;
 constexpr int kStep = 64;          // tokens a wave takes at a time
 
 // The partial result of a row over a chunk of tokens: o (normalised) and the base-2
@@ -422,15 +425,21 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend
 // the lanes of a read, which go down the rows, meet different banks.
 template <int D>
 struct TileLds {
-    uint4 k[64][D / 8];  // [32 * half + row][piece ^ row]
-    uint4 v[D][8];       // [dim][piece ^ dim]: eight tokens a piece
+    uint4 k[64][D / 8];  // [32 * half + row][piece ^ k_key]
+    uint4 v[D][8];       // [dim][piece ^ v_key]: eight tokens a piece
 };
+// 16 lanes of a read share a turn at the 64 banks, 0-3 with 12-15, 20-23 and 24-27: rows of 256
+// bytes need 16 different keys among them, rows of 128 bytes 8 for each parity of the row.
+template <int D>
+__device__ __forceinline__ int k_key(int row) {
+    return D == 64 ? row >> 1 & 7 : row & 15;
+}
+__device__ __forceinline__ int v_key(int dim) { return dim >> 1 & 7; }
 
 template <int D, bool INT8>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAttend k) {
     constexpr int KS = D / 16, DT = D / 32, ROW = D / 16;  // ROW: loads of a token's keys
     constexpr int KL = 64 * ROW / 256, VL = D * 4 / 256;   // loads of a thread for a tile
-    constexpr int KEY = (D / 8 - 1) & 15;
     extern __shared__ __align__(16) char lds_raw[];
     TileLds<D>* const lds = reinterpret_cast<TileLds<D>*>(lds_raw);
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
@@ -491,26 +500,30 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
     const uint32_t page_size = heads * (uint32_t)D << lb;
     Pages pages = {a.s.table + rg.q.s * a.s.table_stride, (uint32_t)max(most, 0) >> lb,
                    (uint32_t)a.c.n_blocks, false};
-    const uint8_t* const k_base = a.c.k_code + ((int64_t)head * D << lb) + (tid % ROW) * 16;
-    const uint8_t* const v_base = a.c.v_code + ((int64_t)head * D << lb) + (((tid >> 2) << lb) | ((tid & 3) * 16 & (block - 1)));
+    // the 16 tokens that a wave's keys of one load lie in: their block is the same for the wave
+    auto group_of = [&](int i) { return (wave * (64 / ROW) + i * (256 / ROW)) >> 4; };
+    const uint32_t k_at = ((uint32_t)head * D << lb) + (tid % ROW) * 16;
+    const uint32_t v_at =
+        ((uint32_t)head * D << lb) + (((tid >> 2) << lb) | ((tid & 3) * 16 & (block - 1)));
     uint4 kw[KL], vw[VL];
     uint32_t k_entry[KL], v_entry;
     int my_ke = 0, my_ve = 0;  // of tokens [16 (tid % 4), + 16) of the loaded tile
     auto find = [&](int32_t x) {
 #pragma unroll
         for (int i = 0; i < KL; ++i)
-            k_entry[i] = pages.entry((uint32_t)(x + (tid / ROW + i * (256 / ROW))) >> lb);
+            k_entry[i] = pages.entry((uint32_t)(x + group_of(i) * 16) >> lb);
         v_entry = pages.entry((uint32_t)(x + (tid & 3) * 16) >> lb);
     };
     auto load = [&]() {
 #pragma unroll
         for (int i = 0; i < KL; ++i) {
-            const int slot = (tid / ROW + i * (256 / ROW)) & (block - 1);
-            kw[i] = *reinterpret_cast<const uint4*>(
-                k_base + (uint64_t)pages.page(k_entry[i]) * page_size + slot * D);
+            const uint32_t slot = (tid / ROW + i * (256 / ROW)) & (block - 1);
+            const uint32_t page = pages.page(__builtin_amdgcn_readfirstlane(k_entry[i]));
+            kw[i] = *reinterpret_cast<const uint4*>(a.c.k_code + (uint64_t)page * page_size +
+                                                    (k_at + slot * D));
         }
         const uint32_t page = pages.page(v_entry);
-        const uint8_t* const v = v_base + (uint64_t)page * page_size;
+        const uint8_t* const v = a.c.v_code + (uint64_t)page * page_size + v_at;
 #pragma unroll
         for (int i = 0; i < VL; ++i) vw[i] = *reinterpret_cast<const uint4*>(v + (i * 64 << lb));
         my_ke = a.c.k_exp[(uint64_t)page * heads + head];
@@ -525,16 +538,16 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
             const int t = tid / ROW + i * (256 / ROW), piece = tid % ROW * 2;
             const int r = (t & 0x33) | (t & 4) << 1 | (t & 8) >> 1;
             uint4* const to = lds[buf].k[r];
-            to[piece ^ (r & KEY)] = __builtin_bit_cast(uint4, codes_to_half<INT8>(kw[i].x, kw[i].y));
-            to[(piece ^ (r & KEY)) ^ 1] = __builtin_bit_cast(uint4, codes_to_half<INT8>(kw[i].z, kw[i].w));
+            to[piece ^ k_key<D>(r)] = __builtin_bit_cast(uint4, codes_to_half<INT8>(kw[i].x, kw[i].y));
+            to[(piece ^ k_key<D>(r)) ^ 1] = __builtin_bit_cast(uint4, codes_to_half<INT8>(kw[i].z, kw[i].w));
         }
 #pragma unroll
         for (int i = 0; i < VL; ++i) {
             const int d = (tid >> 2) + i * 64, piece = (tid & 3) * 2;
             if (tail) vw[i] = first_codes(vw[i], most - (x + (tid & 3) * 16) + 1);
             uint4* const to = lds[buf].v[d];
-            to[piece ^ (d & 7)] = __builtin_bit_cast(uint4, codes_to_half<INT8>(vw[i].x, vw[i].y));
-            to[(piece ^ (d & 7)) ^ 1] = __builtin_bit_cast(uint4, codes_to_half<INT8>(vw[i].z, vw[i].w));
+            to[piece ^ v_key(d)] = __builtin_bit_cast(uint4, codes_to_half<INT8>(vw[i].x, vw[i].y));
+            to[(piece ^ v_key(d)) ^ 1] = __builtin_bit_cast(uint4, codes_to_half<INT8>(vw[i].z, vw[i].w));
         }
     };
 
@@ -564,7 +577,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const int r = t * 32 + n;
-                    const half8_t f = __builtin_bit_cast(half8_t, lds[buf].k[r][(i * 2 + h) ^ (r & KEY)]);
+                    const half8_t f = __builtin_bit_cast(half8_t, lds[buf].k[r][(i * 2 + h) ^ k_key<D>(r)]);
                     s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, q[i], s[t], 0, 0, 0);
                 }
             // register r of product t is token 32 t + 16 (r / 8) + 8 h + r % 8
@@ -599,7 +612,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
                     c[i] = 1.0f;
                 }
             }
-            if (__any(new_m > m) || new_vr > vr) {
+            if (__any(new_m > m + kSlack) || new_vr > vr) {
                 const float fall = __builtin_amdgcn_exp2f(m - base);
                 const float both = fall * pow2f(max(-126, vr - new_vr));
 #pragma unroll
@@ -608,11 +621,12 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
                 m = new_m;
                 vr = new_vr;
             }
+            const float from = m == -INFINITY ? 0.0f : m;
             half8_t w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int shift = max(kLeastShift, ve[i] - vr) + kWeightShift;
-                const float add = (float)shift - base;
+                const float add = (float)shift - from;
                 float sum = 0.0f;
 #pragma unroll
                 for (int r = 0; r < 8; ++r) {
@@ -627,7 +641,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
 #pragma unroll
                 for (int t = 0; t < DT; ++t) {
                     const int d = t * 32 + n;
-                    const half8_t f = __builtin_bit_cast(half8_t, lds[buf].v[d][(i * 2 + h) ^ (d & 7)]);
+                    const half8_t f = __builtin_bit_cast(half8_t, lds[buf].v[d][(i * 2 + h) ^ v_key(d)]);
                     acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, w[i], acc[t], 0, 0, 0);
                 }
         }
