@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "memoplan.h"
 #include "mp_device.hpp"
 
@@ -61,8 +63,9 @@ struct KvSelect {
     int32_t group;
     int32_t keep, first, recent;
     int32_t* out;
-    float* scores;  // [token][head][score_stride]
+    float* scores;  // [token][head][score_stride], or in LDS
     int64_t score_stride;
+    int32_t tokens;  // of a workgroup
 };
 
 size_t kv_select_workspace(const mp_kv_cache& c, const mp_kv_seqs& s, int64_t* score_stride);

@@ -82,8 +82,7 @@ constexpr int32_t kMaxSelectGroup = 128;
 
 bool select_ok(const mp_kv_cache* c, const mp_kv_seqs* s, int32_t q_heads) {
     if (q_heads / c->heads > kMaxSelectGroup) return false;
-    const int64_t rows = s->n_tokens * c->heads;
-    return rows * ((s->longest / c->block + 260) / 256) < INT32_MAX;
+    return (s->n_tokens + s->n_seqs) * c->heads < INT32_MAX;
 }
 
 int32_t move_rows(const mp_kv_cache* cache, const mp_kv_seqs* seqs, const mp_kv_rows* k,

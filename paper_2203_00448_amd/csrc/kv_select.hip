@@ -2,102 +2,23 @@
 //
 // The score of a block is a product of 8-bit codes (the query's, made here, and the
 // block's mean, kept by the write), so it is a whole number below 2^23 times powers of
-// two: exact in 32 bits whatever the order of its sum, and the selection is one of exact
-// numbers, the lowest index among equals.
+// two: exact whatever the order of its sum, and the selection is one of exact numbers,
+// the lowest index among equals.
+//
+// One launch: a workgroup takes one key head and a few consecutive tokens of a sequence,
+// reads each block's mean once for all of them and keeps their scores in LDS; then each
+// wave selects for one token after the other.  Bytes read are a 1 / (2 block) part of the
+// cache's; what bounds a call of few tokens is the chain of dependent steps.
 #include "kv.hpp"
-#include "internal.hpp"
 
 namespace mp {
 
 namespace {
 
-constexpr int kThreads = 256;
+typedef int int4_t __attribute__((ext_vector_type(4)));
 
-// A row and key head of the launch: its sequence and its last position.
-struct SelectRow {
-    KvSeq q;
-    int32_t blocks;  // p / block + 1, or 0 for a row that sees nothing
-    bool ok;
-};
-
-__device__ __forceinline__ SelectRow select_row(const KvSelect& k, int64_t token) {
-    const KvArgs& a = k.a;
-    SelectRow r;
-    int64_t s = token;
-    if (a.s.begin) s = kv_find(a.s.n_seqs, token, [&](int64_t i) { return a.s.begin[i]; });
-    r.q = kv_seq(a, s);
-    const int64_t i = token - r.q.begin;
-    r.ok = r.q.ok && i >= 0 && i < r.q.n;
-    const int32_t last = r.q.length - r.q.n + (int32_t)i;
-    r.blocks = r.ok && last >= 0 ? (last >> a.log_block) + 1 : 0;
-    return r;
-}
-
-// Scores of 256 blocks for one row and key head, a block a thread: the block's mean is read
-// once and multiplied by the codes of every query head, which lie in LDS.
-__global__ __launch_bounds__(kThreads) void kv_score_kernel(KvSelect k, int32_t per_row) {
-    extern __shared__ __align__(16) uint32_t codes[];  // [group][dim / 4], then group scales
-    const KvArgs& a = k.a;
-    const int dim = a.c.dim, words = dim / 4, tid = threadIdx.x, lane = tid & 63;
-    float* const scales = reinterpret_cast<float*>(codes + k.group * words);
-    if (blockIdx.x == 0) kv_check_begin(a);
-    const int64_t row = blockIdx.x / per_row;
-    const int64_t token = row / a.c.heads;
-    const int head = (int)(row % a.c.heads);
-    const SelectRow r = select_row(k, token);
-    const int32_t b0 = (int32_t)(blockIdx.x % per_row) * kThreads;
-    const int32_t lo = k.first, hi = r.blocks - k.recent;  // the blocks that are scored
-    if (!r.ok || r.blocks <= k.keep || b0 >= hi || b0 + kThreads <= lo) return;
-    // query codes: a wave for each head, eight dims a lane
-    for (int g = tid >> 6; g < k.group; g += kThreads / kWave) {
-        float x[8], top = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-        if (lane * 8 < dim) load8(k.q, token, head * k.group + g, lane * 8, x);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float v = fabsf(x[i]);
-            if (v < INFINITY) top = fmaxf(top, v);
-        }
-        top = wave_reduce(top, OpMax<float>());
-        uint32_t frac;
-        const int e = max(-100, exponent_of(top, &frac));
-        const float f = pow2f(7 - e);
-        uint32_t w[2] = {0, 0};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float y = x[i] * f;
-            const float c = y != y ? 0.0f : fminf(127.0f, fmaxf(-127.0f, __builtin_rintf(y)));
-            w[i / 4] |= ((uint32_t)(int)c & 0xffu) << (8 * (i % 4));
-        }
-        if (lane * 8 < dim) {
-            codes[g * words + lane * 2] = w[0];
-            codes[g * words + lane * 2 + 1] = w[1];
-        }
-        if (lane == 0) scales[g] = pow2f(max(-126, e - 7));
-    }
-    __syncthreads();
-    const int32_t b = b0 + tid;
-    if (b < lo || b >= hi) return;
-    int32_t page = a.s.table[r.q.s * a.s.table_stride + b];
-    if (page < 0 || page >= a.c.n_blocks) {
-        raise_status(a.status, MP_EINVAL);
-        page = 0;
-    }
-    const int64_t at = (int64_t)page * a.c.heads + head;
-    const uint2* mean = reinterpret_cast<const uint2*>(a.c.mean_code + at * dim);
-    float best = -INFINITY;
-    for (int g = 0; g < k.group; ++g) {
-        int dot = 0;
-        for (int i = 0; i < words / 2; ++i) {
-            const uint2 w = mean[i];
-            dot = __builtin_amdgcn_sdot4((int)w.x, (int)codes[g * words + 2 * i], dot, false);
-            dot = __builtin_amdgcn_sdot4((int)w.y, (int)codes[g * words + 2 * i + 1], dot, false);
-        }
-        best = fmaxf(best, (float)dot * scales[g]);
-    }
-    k.scores[row * k.score_stride + b] = best * pow2f(max(-126, (int)a.c.mean_exp[at]));
-}
+constexpr int kMostTokens = 8;        // of a workgroup
+constexpr int kLdsScores = 16 * 1024;  // scores that a workgroup holds in LDS
 
 // Larger scores to larger keys.
 __device__ __forceinline__ uint32_t key_of(float score) {
@@ -105,87 +26,271 @@ __device__ __forceinline__ uint32_t key_of(float score) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// The selection of one row and key head: the key of the last one taken by four passes of
-// eight bits, then one pass that writes the taken blocks in order.
-__global__ __launch_bounds__(kThreads) void kv_pick_kernel(KvSelect k) {
-    __shared__ uint32_t hist[256];
-    __shared__ int32_t scratch[kThreads / kWave];
-    __shared__ uint32_t found_digit, found_left;
-    const KvArgs& a = k.a;
-    const int tid = threadIdx.x;
-    if (blockIdx.x == 0) kv_check_begin(a);
-    const int64_t row = blockIdx.x;
-    const SelectRow r = select_row(k, row / a.c.heads);
-    int32_t* const out = k.out + row * k.keep;
-    if (r.blocks <= k.keep) {
-        for (int i = tid; i < k.keep; i += kThreads) out[i] = i < r.blocks ? i : -1;
-        return;
-    }
-    const float* const score = k.scores + row * k.score_stride;
-    const int32_t lo = k.first, hi = r.blocks - k.recent;
-    uint32_t want = (uint32_t)(k.keep - k.first - k.recent), prefix = 0;
-    for (int shift = 24; want > 0 && shift >= 0; shift -= 8) {
-        hist[tid] = 0;
-        __syncthreads();
-        for (int32_t b = lo + tid; b < hi; b += kThreads) {
-            const uint32_t key = key_of(score[b]);
-            if (shift == 24 || key >> (shift + 8) == prefix >> (shift + 8))
+// The largest of a value over the 16 lanes of a row.
+__device__ __forceinline__ float row_max(float x) {
+    const auto turn = [](float v, auto dpp) {
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(dpp)::value,
+                                                          0xf, 0xf, true));
+    };
+    x = fmaxf(x, turn(x, std::integral_constant<int, 0x128>()));  // rotated by 8, 4, 2, 1
+    x = fmaxf(x, turn(x, std::integral_constant<int, 0x124>()));
+    x = fmaxf(x, turn(x, std::integral_constant<int, 0x122>()));
+    return fmaxf(x, turn(x, std::integral_constant<int, 0x121>()));
+}
+
+// One wave's selection for one token: `scores` of blocks [0, blocks), those of [lo, hi) valid.
+// The key of the last block taken by passes of eight bits over a histogram, then one pass
+// that writes the taken blocks in order.
+__device__ __forceinline__ void pick(const float* scores, int32_t blocks, int32_t lo, int32_t hi,
+                                     int32_t want, uint32_t* hist, int32_t* out) {
+    const int lane = threadIdx.x & 63;
+    const bool any = want > 0;
+    uint32_t prefix = 0;
+    uint32_t left = (uint32_t)want;
+    for (int shift = 24; any && shift >= 0; shift -= 8) {
+        *reinterpret_cast<uint4*>(hist + lane * 4) = make_uint4(0, 0, 0, 0);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        for (int32_t b = lo + lane; b < hi; b += kWave) {
+            const uint32_t key = key_of(scores[b]);
+            if (shift == 24 || (key ^ prefix) >> (shift + 8) == 0)
                 atomicAdd(&hist[key >> shift & 255u], 1u);
         }
-        __syncthreads();
-        // keys of larger digits come first: this thread's digit is 255 - tid
-        int32_t total;
-        const uint32_t mine = hist[255 - tid];
-        const uint32_t before = (uint32_t)block_exclusive_sum<kThreads>((int32_t)mine, &total, scratch);
-        if (before < want && want <= before + mine) {
-            found_digit = 255u - tid;
-            found_left = want - before;
-        }
-        __syncthreads();
-        prefix |= found_digit << shift;
-        want = found_left;
-        __syncthreads();
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        // keys of larger digits come first: this lane's digits are 255 - 4 lane and the next three
+        const uint4 c = *reinterpret_cast<const uint4*>(hist + 252 - lane * 4);
+        const uint32_t mine = c.x + c.y + c.z + c.w;
+        const uint32_t before = wave_inclusive_sum(mine) - mine;
+        const int at = __ffsll((unsigned long long)__ballot(before < left && left <= before + mine)) - 1;
+        const uint32_t four[4] = {(uint32_t)__builtin_amdgcn_readlane((int)c.w, at), (uint32_t)__builtin_amdgcn_readlane((int)c.z, at),
+                                  (uint32_t)__builtin_amdgcn_readlane((int)c.y, at), (uint32_t)__builtin_amdgcn_readlane((int)c.x, at)};
+        left -= (uint32_t)__builtin_amdgcn_readlane((int)before, at);
+        uint32_t digit = 255u - 4u * (uint32_t)at;
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (left > four[i] && digit == 255u - 4u * (uint32_t)at - i) {
+                left -= four[i];
+                --digit;
+            }
+        prefix |= digit << shift;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
-    // all keys above `prefix`, and the first `want` of those equal to it
-    const bool any = k.keep > k.first + k.recent;
-    int32_t at = 0, ties = 0;
-    for (int32_t b0 = 0; b0 < r.blocks; b0 += kThreads) {
-        const int32_t b = b0 + tid;
-        bool take = b < r.blocks && (b < lo || b >= hi), tie = false;
+    // all keys above `prefix`, and the first `left` of those equal to it
+    int32_t at = 0;
+    uint32_t ties = 0;
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    for (int32_t b0 = 0; b0 < blocks; b0 += kWave) {
+        const int32_t b = b0 + lane;
+        bool take = b < blocks && (b < lo || b >= hi), tie = false;
         if (any && b >= lo && b < hi) {
-            const uint32_t key = key_of(score[b]);
+            const uint32_t key = key_of(scores[b]);
             take = key > prefix;
             tie = key == prefix;
         }
-        int32_t n_ties, n_take;
-        const int32_t rank = ties + block_exclusive_sum<kThreads>((int32_t)tie, &n_ties, scratch);
-        take |= tie && rank < (int32_t)want;
-        const int32_t place = at + block_exclusive_sum<kThreads>((int32_t)take, &n_take, scratch);
-        if (take && place < k.keep) out[place] = b;
-        ties += n_ties;
-        at += n_take;
+        const uint64_t tied = __ballot(tie);
+        take |= tie && ties + (uint32_t)__popcll(tied & below) < left;
+        const uint64_t taken = __ballot(take);
+        if (take) out[at + __popcll(taken & below)] = b;
+        ties += (uint32_t)__popcll(tied);
+        at += __popcll(taken);
     }
+}
+
+// LDS: query codes [tokens][rows][dim] with rows padded by 16 bytes, their scales, the
+// histograms of the waves, and the scores unless they are in the workspace (GLOBAL).
+//
+// Scores by matrix instructions of 16 blocks x 16 query heads x 64 dims: a lane holds 16
+// dims of a block's mean and of a head's codes, and gets four blocks' products with one head;
+// the largest over the heads is over a row of lanes.
+template <int D, int THREADS, bool GLOBAL>
+__global__ __launch_bounds__(THREADS) void kv_select_kernel(KvSelect k) {
+    extern __shared__ __align__(16) char lds_raw[];
+    constexpr int DC = D / 64, PER_ROW = D / 8, ROW = D + 16;
+    const KvArgs& a = k.a;
+    const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    if (blockIdx.x == 0) kv_check_begin(a);
+    const uint32_t heads = a.c.heads;
+    const int head = (int)(blockIdx.x % heads);
+    const int64_t u = blockIdx.x / heads;
+    int64_t s = u, j = 0;
+    if (a.s.begin) {
+        // n tokens are at most n / tokens + 1 groups
+        auto key = [&](int64_t i) { return a.s.begin[i] / k.tokens + i; };
+        s = kv_find(a.s.n_seqs, u, key);
+        j = u - key(s);
+    }
+    const KvSeq q = kv_seq(a, s);
+    if (!q.ok || j < 0 || j * k.tokens >= q.n) return;
+    const int32_t i0 = (int32_t)j * k.tokens, count = min(k.tokens, q.n - i0);
+    // blocks of token t of this group: of its position / block + 1, or none
+    auto blocks_of = [&](int t) {
+        const int32_t last = q.length - q.n + i0 + t;
+        return last >= 0 ? (last >> a.log_block) + 1 : 0;
+    };
+    const int32_t most = blocks_of(count - 1);
+    int8_t* const codes = reinterpret_cast<int8_t*>(lds_raw);
+    float* const scales = reinterpret_cast<float*>(codes + (size_t)k.tokens * k.group * ROW);
+    uint32_t* const hist = reinterpret_cast<uint32_t*>(scales + (k.tokens * k.group + 3) / 4 * 4);
+    float* const scores = GLOBAL ? k.scores + ((q.begin + i0) * heads + head) * k.score_stride
+                                 : reinterpret_cast<float*>(hist + THREADS / kWave * 256);
+    const int64_t step = GLOBAL ? heads * k.score_stride : k.score_stride;  // to the next token's
+
+    if (most > k.keep) {
+        // query codes, eight dims a lane
+        const int rows = count * k.group, row_in = tid / PER_ROW, d = tid % PER_ROW * 8;
+        for (int r0 = 0; r0 < rows; r0 += THREADS / PER_ROW) {
+            const int r = min(r0 + row_in, rows - 1);
+            float x[8], top = 0.0f;
+            load8(k.q, q.begin + i0 + r / k.group, head * k.group + r % k.group, d, x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float v = fabsf(x[i]);
+                if (v < INFINITY) top = fmaxf(top, v);
+            }
+#pragma unroll
+            for (int o = PER_ROW / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+            uint32_t frac;
+            const int e = max(-100, exponent_of(top, &frac));
+            const float f = pow2f(7 - e);
+            uint32_t w[2] = {0, 0};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float y = x[i] * f;
+                const float c = y != y ? 0.0f : fminf(127.0f, fmaxf(-127.0f, __builtin_rintf(y)));
+                w[i / 4] |= ((uint32_t)(int)c & 0xffu) << (8 * (i % 4));
+            }
+            *reinterpret_cast<uint2*>(codes + r * ROW + d) = make_uint2(w[0], w[1]);
+            if (d == 0) scales[r] = pow2f(max(-126, e - 7));
+        }
+        __syncthreads();
+        const int32_t lo = k.first, hi = most - k.recent;  // the blocks that some token has scored
+        const int32_t* const table = a.s.table + q.s * a.s.table_stride;
+        const int columns = (k.group + 15) / 16;
+        // 64 blocks a turn: their table entries are read a turn ahead, all their means at once
+        constexpr int kStep = THREADS / kWave * 64;
+        int32_t entry[4];
+        auto find = [&](int32_t b0) {
+#pragma unroll
+            for (int z = 0; z < 4; ++z) entry[z] = table[min(b0 + z * 16 + n, most - 1)];
+        };
+        const int32_t from = (lo & ~15) + wave * 64;
+        if (from < hi) find(from);
+        for (int32_t b0 = from; b0 < hi; b0 += kStep) {
+            int4_t mean[4][DC];
+            int exps[4];
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+                int32_t page = entry[z];
+                if (page < 0 || page >= a.c.n_blocks) {
+                    raise_status(a.status, MP_EINVAL);
+                    page = 0;
+                }
+                const int64_t at = (int64_t)page * heads + head;
+#pragma unroll
+                for (int c = 0; c < DC; ++c)
+                    mean[z][c] = *reinterpret_cast<const int4_t*>(a.c.mean_code + at * D + c * 64 + g * 16);
+                exps[z] = a.c.mean_exp[at];
+            }
+            if (b0 + kStep < hi) find(b0 + kStep);
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+                const float unit = pow2f(max(-126, exps[z]));
+                // of the four blocks whose products this lane gets
+                float units[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) units[r] = __shfl(unit, g * 4 + r, kWave);
+                const int32_t b = b0 + z * 16;
+                if (b >= hi) break;
+                for (int t = 0; t < count; ++t) {
+                    float4_t best = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    for (int y = 0; y < columns; ++y) {
+                        // columns past the last head repeat it
+                        const int r = t * k.group + min(y * 16 + n, k.group - 1);
+                        int4_t dot = {0, 0, 0, 0};
+#pragma unroll
+                        for (int c = 0; c < DC; ++c)
+                            dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(
+                                mean[z][c],
+                                *reinterpret_cast<const int4_t*>(codes + r * ROW + c * 64 + g * 16), dot, 0, 0, 0);
+                        const float f = scales[r];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) best[i] = fmaxf(best[i], (float)dot[i] * f);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) best[i] = row_max(best[i]) * units[i];
+                    if (n == 0) *reinterpret_cast<float4_t*>(scores + t * step + b + g * 4) = best;
+                }
+            }
+        }
+        __syncthreads();  // (with GLOBAL: of this workgroup's own stores, read by it alone)
+    }
+    for (int t = wave; t < count; t += THREADS / kWave) {
+        const int32_t blocks = blocks_of(t);
+        int32_t* const out = k.out + ((q.begin + i0 + t) * heads + head) * k.keep;
+        if (blocks <= k.keep) {
+            for (int i = lane; i < k.keep; i += kWave) out[i] = i < blocks ? i : -1;
+        } else {
+            pick(scores + t * step, blocks, k.first, blocks - k.recent, k.keep - k.first - k.recent,
+                 hist + wave * 256, out);
+        }
+    }
+}
+
+// Tokens of a workgroup: as many as its scores leave room for, where sequences have several.
+int32_t tokens_of(const mp_kv_seqs& s, int64_t stride, bool global) {
+    if (!s.begin || global) return 1;
+    const int64_t room = kLdsScores / stride;
+    const int64_t some = room < kMostTokens ? room : kMostTokens;
+    const int64_t most = some < s.most_new ? some : s.most_new;
+    return (int32_t)(most < 1 ? 1 : most);
+}
+
+template <int D, int THREADS, bool GLOBAL>
+hipError_t launch_form(const KvSelect& k, hipStream_t st) {
+    const mp_kv_seqs& s = k.a.s;
+    const int64_t units = s.begin ? s.n_tokens / k.tokens + s.n_seqs : s.n_seqs;
+    size_t lds = (size_t)k.tokens * k.group * (D + 16) + ((size_t)k.tokens * k.group + 3) / 4 * 16 +
+                 THREADS / kWave * 1024;
+    if (!GLOBAL) lds += (size_t)k.tokens * k.score_stride * sizeof(float);
+    if (lds > 65536)
+        if (hipError_t e = hipFuncSetAttribute((const void*)kv_select_kernel<D, THREADS, GLOBAL>,
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            e != hipSuccess)
+            return e;
+    kv_select_kernel<D, THREADS, GLOBAL><<<dim3((uint32_t)(units * k.a.c.heads)), THREADS, lds, st>>>(k);
+    return hipGetLastError();
+}
+
+// Many threads where a workgroup has one token: it is alone with its blocks.
+template <int D>
+hipError_t launch_d(const KvSelect& k, bool global, hipStream_t st) {
+    if (global) return launch_form<D, 1024, true>(k, st);
+    if (k.tokens == 1) return launch_form<D, 1024, false>(k, st);
+    return launch_form<D, 256, false>(k, st);
 }
 
 }  // namespace
 
+// Scores of a token lie in LDS where a workgroup can hold them, else in the workspace.
 size_t kv_select_workspace(const mp_kv_cache& c, const mp_kv_seqs& s, int64_t* score_stride) {
     const int64_t most = (s.longest + c.block - 1) / c.block;
-    *score_stride = (most + 3) / 4 * 4;
-    return (size_t)s.n_tokens * c.heads * *score_stride * sizeof(float);
+    *score_stride = (most + 15) / 16 * 16;
+    if (*score_stride < 16) *score_stride = 16;
+    return *score_stride <= kLdsScores ? 0 : (size_t)s.n_tokens * c.heads * *score_stride * sizeof(float);
 }
 
-hipError_t launch_kv_select(const KvSelect& k, hipStream_t st) {
-    const int64_t rows = k.a.s.n_tokens * k.a.c.heads;
-    if (rows == 0) return hipSuccess;
-    const int64_t per_row = (k.score_stride + kThreads - 1) / kThreads;
-    if (k.score_stride > k.keep) {
-        const size_t lds = (size_t)k.group * (k.a.c.dim + 4);
-        kv_score_kernel<<<dim3((uint32_t)(rows * per_row)), kThreads, lds, st>>>(k, (int32_t)per_row);
-        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+hipError_t launch_kv_select(const KvSelect& a, hipStream_t st) {
+    if (a.a.s.n_tokens == 0) return hipSuccess;
+    KvSelect k = a;
+    const bool global = k.score_stride > kLdsScores;
+    k.tokens = tokens_of(k.a.s, k.score_stride, global);
+    // query codes of many heads take room too
+    while (k.tokens > 1 && (int64_t)k.tokens * k.group * (k.a.c.dim + 20) > 48 * 1024) --k.tokens;
+    switch (k.a.c.dim) {
+        case 64: return launch_d<64>(k, global, st);
+        case 128: return launch_d<128>(k, global, st);
+        default: return launch_d<256>(k, global, st);
     }
-    kv_pick_kernel<<<dim3((uint32_t)rows), kThreads, 0, st>>>(k);
-    return hipGetLastError();
 }
 
 }  // namespace mp

@@ -592,8 +592,6 @@ def test_argument_errors():
         kv.select(c, seqs, q, keep=3, first=2, recent=2)
     with pytest.raises(kv.PlanError):
         kv.select(c, seqs, q, keep=3, first=1, recent=0)
-    with pytest.raises(kv.PlanError):
-        kv.select(c, seqs, q, keep=3, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     with pytest.raises(ValueError):
         kv.Cache(c.k_code, c.v_code, c.k_exp, c.v_exp, c.mean_code[:, :, :32], c.mean_exp)
     with pytest.raises(ValueError):
@@ -603,3 +601,23 @@ def test_argument_errors():
                  k[..., :1].expand(1, 2, 96).contiguous())
     with pytest.raises(ValueError):
         kv.Seqs(s.d_table, seqs.length, tokens=3)
+
+
+def test_select_of_very_long_sequences():
+    """More blocks than scores fit on chip: the same selection from a workspace, which is asked for."""
+    blocks = 17_000
+    s = Setup([16 * 40], heads=2, dim=64, block=16)
+    s.fill()
+    # a table that names the same few blocks over and over
+    table = np.resize(s.table[:1, :40], (1, blocks)).astype(np.int64)
+    length = [blocks * 16 - 5]
+    s.table = table
+    seqs = s.kv.Seqs(torch.from_numpy(table.astype(np.int32)).cuda(),
+                     torch.tensor(length, dtype=torch.int32, device="cuda"),
+                     begin=torch.tensor([0, 3], dtype=torch.int64, device="cuda"), tokens=3)
+    q = s.rows(3, 6)
+    assert s.kv.workspace_size(s.kv.OP_SELECT, s.cache, seqs, q_heads=6, keep=50) > 0
+    got = s.kv.select(s.cache, seqs, q, keep=50, first=2, recent=3)
+    assert np.array_equal(host(got), s.ref.select(table, length, [0, 3], host(q.double()), 50, 2, 3))
+    with pytest.raises(s.kv.PlanError):
+        s.kv.select(s.cache, seqs, q, keep=50, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))

@@ -117,13 +117,18 @@ def test_attend_refusals(kv):
 
 def test_select_refusals(kv):
     for change in ({"keep": -1}, {"first": -1}, {"recent": 0}, {"first": 4}, {"recent": 5}, {"out": None},
-                   {"q_heads": 4 * 129}, {"ws": None}, {"first": 1 << 62}, {"recent": 1 << 62}):
+                   {"q_heads": 4 * 129}, {"first": 1 << 62}, {"recent": 1 << 62}):
         refused(kv, ("select",), **change)
+    # the scores of long sequences need a workspace
     c = Call(kv)
     c.keep = 4
+    c.seqs.table_stride = c.seqs.table_width = 1 << 16
+    c.seqs.longest = 1 << 22
     need = c.size(kv.OP_SELECT)
-    assert need >= 30 * 4 * 10 * 4
+    assert need >= 30 * 4 * (1 << 16) * 4
     c.room = need - 1
+    assert c.select() == -1
+    c.room, c.ws = need, None
     assert c.select() == -1
 
 
