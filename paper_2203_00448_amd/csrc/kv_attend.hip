@@ -194,9 +194,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend
     if (blockIdx.x == 0) kv_check_begin(a);
     const uint32_t heads = a.c.heads, n_chunks = (uint32_t)k.shape.n_chunks;
     const int head = (int)(blockIdx.x % heads);
-    const uint32_t rest = blockIdx.x / heads, chunk = rest % n_chunks;
+    // chunks slowest: workgroups go to the XCDs in turn, and first chunks, which every row group
+    // has, must not all meet one of them
+    const uint32_t rest = blockIdx.x / heads, units = (uint32_t)k.shape.units, chunk = rest / units;
     RowGroup rg;
-    if (!row_group(k, rest / n_chunks, &rg)) return;
+    if (!row_group(k, rest % units, &rg)) return;
     const int64_t last_row = min((int64_t)rg.n_rows, rg.row0 + 16) - 1;
     const int32_t most = row_of(k, rg, head, last_row).last;  // the last position any row sees
     const int32_t least = row_of(k, rg, head, rg.row0).last;  // all rows see up to here
@@ -676,46 +678,74 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
     }
 }
 
-// The chunks of a row joined: a wave for each row.
-template <int D>
+// The chunks of a row joined, by WAVES waves: one where there are few chunks, four of a
+// workgroup where one alone would take many turns.  The chunks' logarithms are read by the
+// lanes at once, their results four dims a lane and a few chunks at a time.
+template <int D, int WAVES>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend k) {
+    constexpr int LANES = D / 4, SIDE = kWave / LANES;  // lanes of a chunk, chunks side by side
+    __shared__ __align__(16) float so[4][D];
     const KvArgs& a = k.a;
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int heads = k.group * a.c.heads;
-    const int64_t index = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (index >= a.s.n_tokens * (int64_t)heads) return;
-    const int64_t token = index / heads;
+    const uint32_t index = WAVES == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
+    if (index >= (uint64_t)a.s.n_tokens * heads) return;
+    const uint32_t token = index / heads;
     int64_t s = token;
     if (a.s.begin) s = kv_find(a.s.n_seqs, token, [&](int64_t i) { return a.s.begin[i]; });
+    const Partials p = partials(k);
+    const int32_t n_chunks = (int32_t)k.shape.n_chunks;
+    const float* const lse = p.lse + (int64_t)index * n_chunks;
+    const float* const o = p.o + (int64_t)index * n_chunks * D;
+    // read beside the sequence's length: the first chunks' logarithms, written or not
+    const float first = lse[min(lane, n_chunks - 1)];
     const KvSeq q = kv_seq(a, s);
-    if (!q.ok || token < q.begin || token >= q.begin + q.n) return;
+    const bool ok = q.ok && token >= q.begin && token < q.begin + q.n;
+    if (!ok) return;  // the same for all waves of a row
     // chunks that the row's last position reaches (one at least), or all of a block list
     const int64_t seen = k.blocks ? (int64_t)k.keep << a.log_block
                                   : (int64_t)q.length - (q.n - 1 - (token - q.begin));
-    const int64_t chunks = min(k.shape.n_chunks, max((int64_t)1, (seen + k.shape.chunk - 1) / k.shape.chunk));
-    const Partials p = partials(k);
-    const float* lse = p.lse + index * k.shape.n_chunks;
-    const float* o = p.o + index * k.shape.n_chunks * D;
+    const int32_t chunks = (int32_t)min((int64_t)n_chunks, max((int64_t)1, (seen + k.shape.chunk - 1) / k.shape.chunk));
     float top = -INFINITY;
-    for (int64_t c = lane; c < chunks; c += kWave) top = fmaxf(top, lse[c]);
+    if (lane < chunks) top = first;
+    for (int32_t c = lane + kWave; c < chunks; c += kWave) top = fmaxf(top, lse[c]);
     top = wave_reduce(top, OpMax<float>());
     const float base = top == -INFINITY ? 0.0f : top;
+    const int side = lane / LANES, d = lane % LANES * 4;
+    float4_t x = {0, 0, 0, 0};
     float total = 0.0f;
-    for (int64_t c = lane; c < chunks; c += kWave) total += __builtin_amdgcn_exp2f(lse[c] - base);
-    total = wave_reduce(total, OpAdd<float>());
-    const float norm = total > 0.0f ? 1.0f / total : 0.0f;
-    constexpr int kPer = D / 64;  // a lane's dims, next to each other
-    float x[kPer];
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) x[i] = 0.0f;
-    for (int64_t c = 0; c < chunks; ++c) {
-        const float f = __builtin_amdgcn_exp2f(lse[c] - base);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) x[i] += f * o[c * D + lane * kPer + i];
+    for (int32_t c0 = 0; c0 < chunks; c0 += kWave) {
+        const int32_t mine = c0 + lane;
+        const float w = mine < chunks ? __builtin_amdgcn_exp2f((c0 == 0 ? first : lse[mine]) - base) : 0.0f;
+        total += w;
+        const int32_t here = min(kWave, chunks - c0);
+        for (int32_t c = (WAVES == 1 ? 0 : wave * SIDE); c < here; c += WAVES * SIDE) {
+            // a place past the last chunk has no weight, and reads the last one
+            const int32_t at = min(c + side, here - 1);
+            const float f = __shfl(w, min(c + side, kWave - 1), kWave);
+            x += (c + side < here ? f : 0.0f) * *reinterpret_cast<const float4_t*>(o + (int64_t)(c0 + at) * D + d);
+        }
     }
+    total = wave_reduce(total, OpAdd<float>());
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) store1(k.out, token, (int)(index % heads), lane * kPer + i, x[i] * norm);
-    if (k.lse && lane == 0) k.lse[index] = total > 0.0f ? (base + log2f(total)) * kLn2 : -INFINITY;
+    for (int i = LANES; i < kWave; i <<= 1)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] += __shfl_xor(x[j], i, kWave);
+    if (WAVES > 1) {
+        if (side == 0) *reinterpret_cast<float4_t*>(&so[wave][d]) = x;
+        __syncthreads();
+        if (wave > 0) return;
+        x = float4_t{0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) x += *reinterpret_cast<const float4_t*>(&so[w][d]);
+    }
+    const float norm = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
+    if (side == 0) {
+        const float y[4] = {x[0] * norm, x[1] * norm, x[2] * norm, x[3] * norm};
+        store4(k.out, token, (int)(index % heads), d, y);
+    }
+    if (k.lse && lane == 0)
+        k.lse[index] = total > 0.0f ? (base + log2f(total)) * kLn2 : total == 0.0f ? -INFINITY : total;
 }
 
 template <int D, bool INT8>
@@ -738,7 +768,10 @@ hipError_t launch_d(const KvAttend& k, hipStream_t st) {
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (sh.n_chunks > 1) {
         const int64_t rows = k.a.s.n_tokens * (int64_t)k.group * k.a.c.heads;
-        kv_join_kernel<D><<<dim3((uint32_t)((rows + 3) / 4)), 256, 0, st>>>(k);
+        if (sh.n_chunks > 16)
+            kv_join_kernel<D, 4><<<dim3((uint32_t)rows), 256, 0, st>>>(k);
+        else
+            kv_join_kernel<D, 1><<<dim3((uint32_t)((rows + 3) / 4)), 256, 0, st>>>(k);
     }
     return hipGetLastError();
 }
@@ -759,14 +792,25 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     else
         sh.units = s.n_seqs * per;
     const int64_t longest = keep > 0 ? keep * c.block : s.longest;
-    // enough workgroups for four a compute unit, of 512 tokens at least
+    // Tokens of a workgroup: a workgroup's start, end and part of the join cost as much as some
+    // hundred tokens, few long ones leave compute units idle.  2048, or less where that makes
+    // fewer workgroups than compute units, 512 at least and all in one up to 1024.  Measured with
+    // 512 / 1024 / 2048 / 4096: 64 sequences of 1-16384 tokens 155 / 146 / 149 / 157 us, of 8192
+    // each 196 / 186 / 182 / 179, one of 4000 13 / 16 / 21 / 28, 32 of 1-1000 17 / 13 / 13 / 13.
+    // Tiles are split only as far as four workgroups a compute unit need it: a piece of 333 rows
+    // after 20000 tokens 118 us (two: 149, eight: 114), prompts that fill the device without
+    // chunks 290 us (559 in chunks of 2048: the partial results are 32-bit).
     const int64_t wide = sh.units * c.heads;
-    int64_t chunks = wide > 0 ? (4 * 256 + wide - 1) / wide : 1;
-    const int64_t most = (longest + 511) / 512;
-    chunks = chunks < most ? chunks : most;
-    if (chunks < 1) chunks = 1;
-    sh.chunk = ((longest + chunks - 1) / chunks + 255) / 256 * 256;
-    if (sh.chunk < 256) sh.chunk = 256;
+    int64_t chunk = longest < ((int64_t)2048 * 256) / (wide > 0 ? wide : 1) ? longest * wide / 256 : 2048;
+    if (chunk < 512) chunk = 512;
+    if (longest <= 1024) chunk = 1024;
+    if (sh.tiles) {
+        const int64_t chunks = wide > 0 ? (4 * 256 + wide - 1) / wide : 1;
+        chunk = (longest + chunks - 1) / chunks;
+        if (chunk < 512) chunk = 512;
+    }
+    // a multiple of what the waves of a workgroup take together
+    sh.chunk = (chunk + 255) / 256 * 256;
     sh.n_chunks = longest > 0 ? (longest + sh.chunk - 1) / sh.chunk : 1;
     const int64_t rows = s.n_tokens * q_heads;
     sh.ok = sh.units * c.heads * sh.n_chunks < INT32_MAX && rows < INT32_MAX;
