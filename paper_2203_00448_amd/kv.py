@@ -4,15 +4,14 @@ argument marshalling only, like binding.py.
 A program keeps a `Cache` (its memory), a `Seqs` for its batch (block table,
 lengths, the call's rows), a status word and workspaces, and calls `write`,
 `read`, `select` and `attend` on them; outputs may be views of a planned slab.
-Each takes `stream=` besides (the current one if not given); tensors that are
-in use on another stream are the caller's to wait for.
+Each runs on `stream` (the current one if not given); tensors that are in use
+on another stream are the caller's to wait for.
 The tensors that a handle was made of stay the caller's: changing their
 values, not their places, changes what the next call sees.
 """
 from __future__ import annotations
 
 import ctypes
-import functools
 
 import torch
 
@@ -164,32 +163,31 @@ class Seqs:
         return self._ref
 
 
-def _rows(t, name, tokens, heads, dim, dtypes):
-    _need(t, dtypes, name, (tokens, heads, dim))
-    if t.stride(2) != 1:
-        raise ValueError(f"{name} must be contiguous in its last dimension")
-    return _RowsArg(t.data_ptr() or None, t.stride(0), t.stride(1), DTYPES[t.dtype])
-
-
 _MOVED = (torch.bfloat16, torch.float16, torch.float32)
 _QUERIES = (torch.bfloat16, torch.float16)
 
 
-def _on_stream(call):
-    """`call` with its `stream` made the current one, so that what it allocates belongs to that
-    stream and the wait of check=True is for it."""
-    @functools.wraps(call)
-    def on(*args, stream=None, **more):
-        if stream is None:
-            return call(*args, **more)
-        with torch.cuda.stream(stream):
-            return call(*args, **more)
-
-    return on
+def _rows(t, name, shape, dtypes):
+    """A tensor's rows as an argument.  These calls are short beside what a launch costs, so their
+    checks look at each property once."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtypes or t.shape != shape:
+        _need(t, dtypes, name, shape)
+    strides = t.stride()
+    if strides[2] != 1:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+    return _RowsArg(t.data_ptr(), strides[0], strides[1], DTYPES[t.dtype])
 
 
 def _stream(device):
-    return torch.cuda.current_stream(device).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+def _word(status, cache):
+    if status is None:
+        return new_status(cache.device)
+    if not status.is_cuda or status.dtype is not torch.int32:
+        _need(status, (torch.int32,), "status")
+    return status
 
 
 def workspace_size(op: int, cache: Cache, seqs: Seqs, *, q_heads: int, keep: int = 0) -> int:
@@ -203,33 +201,36 @@ def workspace(op: int, cache: Cache, seqs: Seqs, *, q_heads: int, keep: int = 0)
     return torch.empty(max(need, 16), dtype=torch.uint8, device=cache.device)
 
 
-@_on_stream
-def write(cache: Cache, seqs: Seqs, k, v, *, status=None, check: bool = True):
+def write(cache: Cache, seqs: Seqs, k, v, *, status=None, check: bool = True, stream=None):
     """Store the call's keys and values (mp_kv_write): k, v [tokens, heads, dim] in bfloat16,
     float16 or float32, any strides over a contiguous last dimension."""
+    if stream is not None:
+        # current for the call: what it allocates is that stream's, and so is the wait of check
+        with torch.cuda.stream(stream):
+            return write(cache, seqs, k, v, status=status, check=check)
     L = load_library()
-    ka = _rows(k, "k", seqs.tokens, cache.heads, cache.dim, _MOVED)
-    va = _rows(v, "v", seqs.tokens, cache.heads, cache.dim, _MOVED)
-    if status is None:
-        status = new_status(cache.device)
+    shape = (seqs.tokens, cache.heads, cache.dim)
+    ka, va = _rows(k, "k", shape, _MOVED), _rows(v, "v", shape, _MOVED)
+    status = _word(status, cache)
     rc = L.mp_kv_write(cache._ref, seqs._for(cache), ctypes.addressof(ka), ctypes.addressof(va),
                        status.data_ptr(), _stream(cache.device))
     _finish(rc, status, "kv.write", check)
 
 
-@_on_stream
 def read(cache: Cache, seqs: Seqs, *, dtype=torch.bfloat16, out=None, status=None,
-         check: bool = True):
+         check: bool = True, stream=None):
     """Read back the call's tokens (mp_kv_read): (k, v) [tokens, heads, dim]."""
+    if stream is not None:
+        # current for the call: what it allocates is that stream's, and so is the wait of check
+        with torch.cuda.stream(stream):
+            return read(cache, seqs, dtype=dtype, out=out, status=status, check=check)
     L = load_library()
+    shape = (seqs.tokens, cache.heads, cache.dim)
     if out is None:
-        shape = (seqs.tokens, cache.heads, cache.dim)
         out = tuple(torch.empty(shape, dtype=dtype, device=cache.device) for _ in range(2))
     k, v = out
-    ka = _rows(k, "k", seqs.tokens, cache.heads, cache.dim, _MOVED)
-    va = _rows(v, "v", seqs.tokens, cache.heads, cache.dim, _MOVED)
-    if status is None:
-        status = new_status(cache.device)
+    ka, va = _rows(k, "k", shape, _MOVED), _rows(v, "v", shape, _MOVED)
+    status = _word(status, cache)
     rc = L.mp_kv_read(cache._ref, seqs._for(cache), ctypes.addressof(ka), ctypes.addressof(va),
                       status.data_ptr(), _stream(cache.device))
     _finish(rc, status, "kv.read", check)
@@ -239,25 +240,32 @@ def read(cache: Cache, seqs: Seqs, *, dtype=torch.bfloat16, out=None, status=Non
 def _space(op, cache, seqs, q_heads, keep, workspace):
     if workspace is None:
         workspace = globals()["workspace"](op, cache, seqs, q_heads=q_heads, keep=keep)
-    return workspace, workspace.numel() * workspace.element_size()
+    elif not workspace.is_cuda:
+        raise TypeError("workspace must be a CUDA (HIP) tensor")
+    return workspace.data_ptr(), workspace.nbytes, workspace
 
 
-@_on_stream
 def attend(cache: Cache, seqs: Seqs, q, *, scale: float | None = None, blocks=None, out=None,
-           lse=None, status=None, workspace=None, check: bool = True):
+           lse=None, status=None, workspace=None, check: bool = True, stream=None):
     """Attention of q [tokens, q_heads, dim] (bfloat16 or float16) over the cache
     (mp_kv_attend), causal: the rows of a sequence are its last tokens.  `scale` defaults to
     dim ** -0.5.  `blocks` int32 [tokens, heads, keep] limits each row to these of its
     sequence's blocks.  `lse` float32 [tokens, q_heads], if given, gets the logarithms of the
     sums.  Returns out."""
+    if stream is not None:
+        # current for the call: what it allocates is that stream's, and so is the wait of check
+        with torch.cuda.stream(stream):
+            return attend(cache, seqs, q, scale=scale, blocks=blocks, out=out, lse=lse, status=status,
+                          workspace=workspace, check=check)
     L = load_library()
     if q.dim() != 3:
         raise ValueError("q must be [tokens, q_heads, dim]")
     heads = q.shape[1]
-    qa = _rows(q, "q", seqs.tokens, heads, cache.dim, _QUERIES)
+    rows = (seqs.tokens, heads, cache.dim)
+    qa = _rows(q, "q", rows, _QUERIES)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    oa = _rows(out, "out", seqs.tokens, heads, cache.dim, (q.dtype,))
+    oa = _rows(out, "out", rows, (q.dtype,))
     keep, named = 0, None
     if blocks is not None:
         _need(blocks, (torch.int32,), "blocks")
@@ -268,39 +276,42 @@ def attend(cache: Cache, seqs: Seqs, q, *, scale: float | None = None, blocks=No
         _need(lse, (torch.float32,), "lse", (seqs.tokens, heads))
         if not lse.is_contiguous():
             raise ValueError("lse must be contiguous")
-    workspace, have = _space(OP_ATTEND, cache, seqs, heads, keep, workspace)
-    if status is None:
-        status = new_status(cache.device)
+    space, have, _held = _space(OP_ATTEND, cache, seqs, heads, keep, workspace)
+    status = _word(status, cache)
     rc = L.mp_kv_attend(cache._ref, seqs._for(cache), ctypes.addressof(qa), heads,
                         cache.dim ** -0.5 if scale is None else scale, named, keep,
                         ctypes.addressof(oa), lse.data_ptr() if lse is not None else None,
-                        workspace.data_ptr(), have, status.data_ptr(), _stream(cache.device))
+                        space, have, status.data_ptr(), _stream(cache.device))
     _finish(rc, status, "kv.attend", check)
     return out
 
 
-@_on_stream
 def select(cache: Cache, seqs: Seqs, q, *, keep: int, first: int = 1, recent: int = 1, out=None,
-           status=None, workspace=None, check: bool = True):
+           status=None, workspace=None, check: bool = True, stream=None):
     """The blocks of each row and key head that attend is to read (mp_kv_select): the first
     `first`, the last `recent` and the best-scored others, `keep` in all, int32 [tokens, heads,
     keep], ascending, -1 beyond the last."""
+    if stream is not None:
+        # current for the call: what it allocates is that stream's, and so is the wait of check
+        with torch.cuda.stream(stream):
+            return select(cache, seqs, q, keep=keep, first=first, recent=recent, out=out, status=status,
+                          workspace=workspace, check=check)
     L = load_library()
     if q.dim() != 3:
         raise ValueError("q must be [tokens, q_heads, dim]")
     heads = q.shape[1]
-    qa = _rows(q, "q", seqs.tokens, heads, cache.dim, _QUERIES)
+    rows = (seqs.tokens, heads, cache.dim)
+    qa = _rows(q, "q", rows, _QUERIES)
     shape = (seqs.tokens, cache.heads, int(keep))
     if out is None:
         out = torch.empty(shape, dtype=torch.int32, device=q.device)
     _need(out, (torch.int32,), "out", shape)
     if not out.is_contiguous():
         raise ValueError("out must be contiguous")
-    workspace, have = _space(OP_SELECT, cache, seqs, heads, keep, workspace)
-    if status is None:
-        status = new_status(cache.device)
+    space, have, _held = _space(OP_SELECT, cache, seqs, heads, keep, workspace)
+    status = _word(status, cache)
     rc = L.mp_kv_select(cache._ref, seqs._for(cache), ctypes.addressof(qa), heads, keep, first, recent,
-                        out.data_ptr() or None, workspace.data_ptr(), have, status.data_ptr(),
+                        out.data_ptr() or None, space, have, status.data_ptr(),
                         _stream(cache.device))
     _finish(rc, status, "kv.select", check)
     return out
