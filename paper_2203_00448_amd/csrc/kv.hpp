@@ -262,39 +262,49 @@ __device__ __forceinline__ void kv_check_begin(const KvArgs& a) {
     if (bad) raise_status(a.status, MP_EINVAL);
 }
 
-__device__ __forceinline__ KvSeq kv_seq(const KvArgs& a, int64_t s) {
+// Rows [b, e) of sequence s, as begin[] gave them.
+__device__ __forceinline__ KvSeq kv_seq(const KvArgs& a, int64_t s, int64_t b, int64_t e) {
     KvSeq q;
     q.s = (int32_t)s;
     q.length = a.s.length[s];
-    if (a.s.begin) {
-        const int64_t b = a.s.begin[s], e = a.s.begin[s + 1];
-        q.begin = b;
-        q.n = (int32_t)(e - b);
-        q.ok = b >= 0 && e >= b && e <= a.s.n_tokens && e - b <= a.s.most_new;
-    } else {
-        q.begin = s;
-        q.n = 1;
-        q.ok = true;
-    }
-    q.ok = q.ok && q.length >= 0 && q.length <= a.s.longest;
+    q.begin = b;
+    q.n = (int32_t)(e - b);
+    q.ok = b >= 0 && e >= b && e <= a.s.n_tokens && (!a.s.begin || e - b <= a.s.most_new) &&
+           q.length >= 0 && q.length <= a.s.longest;
     if (!q.ok) raise_status(a.status, MP_EINVAL);
     return q;
 }
 
-// The last sequence whose key is at most u, where key(s) never falls with s; the
-// whole wave searches, 64 keys a turn.  Any keys give a sequence in range.
+// The last sequence whose key(begin[s], s) is at most u, where keys never fall with s (s itself
+// without begin), and u less its key; the whole wave searches, 64 keys a turn, and keeps what
+// it read of begin[].  Any values there give a sequence in range.
 template <typename Key>
-__device__ __forceinline__ int64_t kv_find(int64_t n_seqs, int64_t u, Key key) {
+__device__ __forceinline__ KvSeq kv_find(const KvArgs& a, int64_t u, Key key, int64_t* rest) {
+    if (!a.s.begin) {
+        *rest = 0;
+        return kv_seq(a, u, u, u + 1);
+    }
     const int lane = threadIdx.x & (kWave - 1);
-    int64_t lo = 0, hi = n_seqs;
+    int64_t lo = 0, hi = a.s.n_seqs, b = 0, e = 0;
+    int count = kWave;
     while (hi - lo > 1) {
         const int64_t step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
-        const uint64_t below = __ballot(at < hi && key(at) <= u);
-        const int count = below == ~0ull ? kWave : __ffsll((unsigned long long)~below) - 1;
+        b = at <= hi ? a.s.begin[at] : 0;
+        const uint64_t below = __ballot(at < hi && key(b, at) <= u);
+        count = below == ~0ull ? kWave : __ffsll((unsigned long long)~below) - 1;
+        if (step == 1 && count < kWave) {  // this turn read the sequence's rows and the next one's
+            const int i = max(0, count - 1);
+            e = __shfl(b, i + 1, kWave);
+            b = __shfl(b, i, kWave);
+            *rest = u - key(b, lo + i);
+            return kv_seq(a, lo + i, b, e);
+        }
         lo += (int64_t)max(0, count - 1) * step;
         hi = min(hi, lo + step);
     }
-    return lo;
+    b = a.s.begin[lo];
+    *rest = u - key(b, lo);
+    return kv_seq(a, lo, b, a.s.begin[lo + 1]);
 }
 
 }  // namespace mp

@@ -68,11 +68,8 @@ __device__ __forceinline__ bool row_group(const KvAttend& k, int64_t u, RowGroup
     if (k.blocks) {
         const int64_t per = (k.group + k.shape.rows - 1) / k.shape.rows;
         const int64_t token = u / per;
-        int64_t s = token;
-        if (a.s.begin)
-            s = kv_find(a.s.n_seqs, token, [&](int64_t i) { return a.s.begin[i]; });
-        g->q = kv_seq(a, s);
-        const int64_t i = token - g->q.begin;
+        int64_t i;
+        g->q = kv_find(a, token, [&](int64_t b, int64_t) { return b; }, &i);
         if (!g->q.ok || i < 0 || i >= g->q.n) return false;
         // the sequence as it is for this token: its last one
         g->q.length -= (int32_t)(g->q.n - 1 - i);
@@ -80,18 +77,16 @@ __device__ __forceinline__ bool row_group(const KvAttend& k, int64_t u, RowGroup
         g->q.n = 1;
         g->row0 = u % per * k.shape.rows;
     } else {
-        int64_t s, first;
+        int64_t first;
         if (a.s.begin) {
             // n tokens are at most n * group / rows + 1 row groups
-            auto key = [&](int64_t i) { return a.s.begin[i] * k.group / k.shape.rows + i; };
-            s = kv_find(a.s.n_seqs, u, key);
-            first = u - key(s);
+            auto key = [&](int64_t b, int64_t i) { return b * k.group / k.shape.rows + i; };
+            g->q = kv_find(a, u, key, &first);
         } else {
             const int64_t per = (k.group + k.shape.rows - 1) / k.shape.rows;
-            s = u / per;
+            g->q = kv_seq(a, u / per, u / per, u / per + 1);
             first = u % per;
         }
-        g->q = kv_seq(a, s);
         if (!g->q.ok || first < 0) return false;
         g->row0 = first * k.shape.rows;
     }
@@ -691,15 +686,14 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend k) {
     const uint32_t index = WAVES == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
     if (index >= (uint64_t)a.s.n_tokens * heads) return;
     const uint32_t token = index / heads;
-    int64_t s = token;
-    if (a.s.begin) s = kv_find(a.s.n_seqs, token, [&](int64_t i) { return a.s.begin[i]; });
     const Partials p = partials(k);
     const int32_t n_chunks = (int32_t)k.shape.n_chunks;
     const float* const lse = p.lse + (int64_t)index * n_chunks;
     const float* const o = p.o + (int64_t)index * n_chunks * D;
     // read beside the sequence's length: the first chunks' logarithms, written or not
     const float first = lse[min(lane, n_chunks - 1)];
-    const KvSeq q = kv_seq(a, s);
+    int64_t of;
+    const KvSeq q = kv_find(a, token, [&](int64_t b, int64_t) { return b; }, &of);
     const bool ok = q.ok && token >= q.begin && token < q.begin + q.n;
     if (!ok) return;  // the same for all waves of a row
     // chunks that the row's last position reaches (one at least), or all of a block list

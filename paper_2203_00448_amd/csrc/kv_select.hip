@@ -112,14 +112,9 @@ __global__ __launch_bounds__(THREADS) void kv_select_kernel(KvSelect k) {
     const uint32_t heads = a.c.heads;
     const int head = (int)(blockIdx.x % heads);
     const int64_t u = blockIdx.x / heads;
-    int64_t s = u, j = 0;
-    if (a.s.begin) {
-        // n tokens are at most n / tokens + 1 groups
-        auto key = [&](int64_t i) { return a.s.begin[i] / k.tokens + i; };
-        s = kv_find(a.s.n_seqs, u, key);
-        j = u - key(s);
-    }
-    const KvSeq q = kv_seq(a, s);
+    // n tokens are at most n / tokens + 1 groups
+    int64_t j;
+    const KvSeq q = kv_find(a, u, [&](int64_t b, int64_t i) { return b / k.tokens + i; }, &j);
     if (!q.ok || j < 0 || j * k.tokens >= q.n) return;
     const int32_t i0 = (int32_t)j * k.tokens, count = min(k.tokens, q.n - i0);
     // blocks of token t of this group: of its position / block + 1, or none

@@ -25,12 +25,8 @@ struct KvPiece {
 // tokens touch at most (n >> log_block) + 2 blocks, so no two sequences share one.
 __device__ __forceinline__ bool kv_piece(const KvArgs& a, int64_t u, KvPiece* p) {
     const int lb = a.log_block;
-    int64_t s = u, j = 0;
-    if (a.s.begin) {
-        s = kv_find(a.s.n_seqs, u, [&](int64_t i) { return (a.s.begin[i] >> lb) + 2 * i; });
-        j = u - ((a.s.begin[s] >> lb) + 2 * s);
-    }
-    const KvSeq q = kv_seq(a, s);
+    int64_t j;
+    const KvSeq q = kv_find(a, u, [&](int64_t b, int64_t i) { return (b >> lb) + 2 * i; }, &j);
     if (!q.ok || j < 0 || q.n == 0) return false;
     const int32_t start = q.length - q.n;
     if (start < 0) {  // more rows than tokens
@@ -40,7 +36,7 @@ __device__ __forceinline__ bool kv_piece(const KvArgs& a, int64_t u, KvPiece* p)
     const int64_t blk = (start >> lb) + j;
     const int64_t lo = max((int64_t)start, blk << lb), hi = min((int64_t)q.length, (blk + 1) << lb);
     if (lo >= hi) return false;
-    p->page = a.s.table[s * a.s.table_stride + blk];
+    p->page = a.s.table[q.s * a.s.table_stride + blk];
     if (p->page < 0 || p->page >= a.c.n_blocks) {
         raise_status(a.status, MP_EINVAL);
         return false;
