@@ -26,44 +26,64 @@ __device__ __forceinline__ uint32_t key_of(float score) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// The largest of a value over the 16 lanes of a row.
-__device__ __forceinline__ float row_max(float x) {
-    const auto turn = [](float v, auto dpp) {
+// The largest of a value over aligned groups of `span` lanes (1, 2, 4, 8 or 16), to all of them.
+__device__ __forceinline__ float span_max(float x, int span) {
+    const auto from = [](float v, auto dpp) {
         return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(dpp)::value,
                                                           0xf, 0xf, true));
     };
-    x = fmaxf(x, turn(x, std::integral_constant<int, 0x128>()));  // rotated by 8, 4, 2, 1
-    x = fmaxf(x, turn(x, std::integral_constant<int, 0x124>()));
-    x = fmaxf(x, turn(x, std::integral_constant<int, 0x122>()));
-    return fmaxf(x, turn(x, std::integral_constant<int, 0x121>()));
+    if (span > 1) x = fmaxf(x, from(x, std::integral_constant<int, 0xb1>()));   // pairs exchanged
+    if (span > 2) x = fmaxf(x, from(x, std::integral_constant<int, 0x4e>()));   // quads' halves
+    if (span > 4) x = fmaxf(x, from(x, std::integral_constant<int, 0x141>()));  // eight mirrored
+    if (span > 8) x = fmaxf(x, from(x, std::integral_constant<int, 0x140>()));  // sixteen mirrored
+    return x;
 }
 
-// One wave's selection for one token: `scores` of blocks [0, blocks), those of [lo, hi) valid.
-// The key of the last block taken by passes of eight bits over a histogram, then one pass
-// that writes the taken blocks in order.
+// LDS of a selection by WAVES waves: a histogram for each pass, and two turns' counts.
+template <int WAVES>
+struct PickLds {
+    uint32_t hist[4][256];
+    uint32_t sure[2][WAVES], tied[2][WAVES];
+};
+
+// The selection for one token by WAVES waves: `scores` of blocks [0, blocks), those of [lo, hi)
+// valid.  The key of the last block taken by passes of eight bits over a histogram, then one
+// pass that writes the taken blocks in order.
+template <int WAVES>
 __device__ __forceinline__ void pick(const float* scores, int32_t blocks, int32_t lo, int32_t hi,
-                                     int32_t want, uint32_t* hist, int32_t* out) {
-    const int lane = threadIdx.x & 63;
+                                     int32_t want, PickLds<WAVES>* lds, int32_t* out) {
+    const auto meet = []() {
+        if (WAVES > 1)
+            __syncthreads();
+        else
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    };
+    const int lane = threadIdx.x & 63, wave = WAVES > 1 ? threadIdx.x >> 6 : 0;
+    const int me = wave * kWave + lane;
     const bool any = want > 0;
     uint32_t prefix = 0;
     uint32_t left = (uint32_t)want;
+    if (any) {
+        for (int i = me; i < 256; i += WAVES * kWave)
+            *reinterpret_cast<uint4*>(&lds->hist[0][0] + i * 4) = make_uint4(0, 0, 0, 0);
+        meet();
+    }
     for (int shift = 24; any && shift >= 0; shift -= 8) {
-        *reinterpret_cast<uint4*>(hist + lane * 4) = make_uint4(0, 0, 0, 0);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        for (int32_t b = lo + lane; b < hi; b += kWave) {
+        uint32_t* const hist = lds->hist[shift >> 3];
+        for (int32_t b = lo + me; b < hi; b += WAVES * kWave) {
             const uint32_t key = key_of(scores[b]);
             if (shift == 24 || (key ^ prefix) >> (shift + 8) == 0)
                 atomicAdd(&hist[key >> shift & 255u], 1u);
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        meet();
         // keys of larger digits come first: this lane's digits are 255 - 4 lane and the next three
         const uint4 c = *reinterpret_cast<const uint4*>(hist + 252 - lane * 4);
         const uint32_t mine = c.x + c.y + c.z + c.w;
         const uint32_t before = wave_inclusive_sum(mine) - mine;
         const int at = __ffsll((unsigned long long)__ballot(before < left && left <= before + mine)) - 1;
-        const uint32_t four[4] = {(uint32_t)__builtin_amdgcn_readlane((int)c.w, at), (uint32_t)__builtin_amdgcn_readlane((int)c.z, at),
-                                  (uint32_t)__builtin_amdgcn_readlane((int)c.y, at), (uint32_t)__builtin_amdgcn_readlane((int)c.x, at)};
-        left -= (uint32_t)__builtin_amdgcn_readlane((int)before, at);
+        const auto of = [&](uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, at); };
+        const uint32_t four[3] = {of(c.w), of(c.z), of(c.y)};
+        left -= of(before);
         uint32_t digit = 255u - 4u * (uint32_t)at;
 #pragma unroll
         for (int i = 0; i < 3; ++i)
@@ -72,39 +92,56 @@ __device__ __forceinline__ void pick(const float* scores, int32_t blocks, int32_
                 --digit;
             }
         prefix |= digit << shift;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
     // all keys above `prefix`, and the first `left` of those equal to it
-    int32_t at = 0;
-    uint32_t ties = 0;
+    uint32_t at = 0, ties = 0;
     const uint64_t below = ((uint64_t)1 << lane) - 1;
-    for (int32_t b0 = 0; b0 < blocks; b0 += kWave) {
-        const int32_t b = b0 + lane;
-        bool take = b < blocks && (b < lo || b >= hi), tie = false;
+    int turn = 0;
+    for (int32_t b0 = 0; b0 < blocks; b0 += WAVES * kWave, turn ^= 1) {
+        const int32_t b = b0 + me;
+        bool sure = b < blocks && (b < lo || b >= hi), tie = false;
         if (any && b >= lo && b < hi) {
             const uint32_t key = key_of(scores[b]);
-            take = key > prefix;
+            sure = key > prefix;
             tie = key == prefix;
         }
-        const uint64_t tied = __ballot(tie);
-        take |= tie && ties + (uint32_t)__popcll(tied & below) < left;
-        const uint64_t taken = __ballot(take);
-        if (take) out[at + __popcll(taken & below)] = b;
-        ties += (uint32_t)__popcll(tied);
-        at += __popcll(taken);
+        const uint64_t tied = __ballot(tie), sures = __ballot(sure);
+        uint32_t my_at = at, my_ties = ties, all = __popcll(sures), all_ties = __popcll(tied);
+        if (WAVES > 1) {
+            // what the waves before this one take of this turn, and all of them
+            if (lane == 0) lds->sure[turn][wave] = all, lds->tied[turn][wave] = all_ties;
+            __syncthreads();
+            const uint32_t s = lane < WAVES ? lds->sure[turn][lane] : 0;
+            const uint32_t t = lane < WAVES ? lds->tied[turn][lane] : 0;
+            const uint32_t t_before = wave_inclusive_sum(t) - t;
+            const uint32_t room = left > ties + t_before ? left - ties - t_before : 0;
+            const uint32_t taken = s + min(t, room), to = wave_inclusive_sum(taken);
+            my_at += (uint32_t)__builtin_amdgcn_readlane((int)(to - taken), wave);
+            my_ties += (uint32_t)__builtin_amdgcn_readlane((int)t_before, wave);
+            all = (uint32_t)__builtin_amdgcn_readlane((int)to, WAVES - 1);
+            all_ties = (uint32_t)__builtin_amdgcn_readlane((int)(t_before + t), WAVES - 1);
+        }
+        const bool take = sure || (tie && my_ties + (uint32_t)__popcll(tied & below) < left);
+        const uint64_t takes = __ballot(take);
+        if (take) out[my_at + __popcll(takes & below)] = b;
+        at += WAVES > 1 ? all : (uint32_t)__popcll(takes);
+        ties += all_ties;
     }
 }
 
 // LDS: query codes [tokens][rows][dim] with rows padded by 16 bytes, their scales, the
 // histograms of the waves, and the scores unless they are in the workspace (GLOBAL).
 //
-// Scores by matrix instructions of 16 blocks x 16 query heads x 64 dims: a lane holds 16
-// dims of a block's mean and of a head's codes, and gets four blocks' products with one head;
-// the largest over the heads is over a row of lanes.
+// Scores by matrix instructions of 16 blocks x 16 query heads x 64 dims, the heads of as many
+// tokens as fit (`span` columns each, heads repeated to a power of two): a lane holds 16 dims of
+// a block's mean and of a head's codes, and gets four blocks' products with one head; the
+// largest over a token's heads is over a span of lanes.
 template <int D, int THREADS, bool GLOBAL>
 __global__ __launch_bounds__(THREADS) void kv_select_kernel(KvSelect k) {
     extern __shared__ __align__(16) char lds_raw[];
     constexpr int DC = D / 64, PER_ROW = D / 8, ROW = D + 16;
+    // waves that select for a token: all where there is one token
+    constexpr int kTeam = THREADS == 1024 ? THREADS / kWave : 1;
     const KvArgs& a = k.a;
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -125,9 +162,9 @@ __global__ __launch_bounds__(THREADS) void kv_select_kernel(KvSelect k) {
     const int32_t most = blocks_of(count - 1);
     int8_t* const codes = reinterpret_cast<int8_t*>(lds_raw);
     float* const scales = reinterpret_cast<float*>(codes + (size_t)k.tokens * k.group * ROW);
-    uint32_t* const hist = reinterpret_cast<uint32_t*>(scales + (k.tokens * k.group + 3) / 4 * 4);
+    PickLds<kTeam>* const picks = reinterpret_cast<PickLds<kTeam>*>(scales + (k.tokens * k.group + 3) / 4 * 4);
     float* const scores = GLOBAL ? k.scores + ((q.begin + i0) * heads + head) * k.score_stride
-                                 : reinterpret_cast<float*>(hist + THREADS / kWave * 256);
+                                 : reinterpret_cast<float*>(picks + THREADS / kWave / kTeam);
     const int64_t step = GLOBAL ? heads * k.score_stride : k.score_stride;  // to the next token's
 
     if (most > k.keep) {
@@ -161,6 +198,8 @@ __global__ __launch_bounds__(THREADS) void kv_select_kernel(KvSelect k) {
         const int32_t lo = k.first, hi = most - k.recent;  // the blocks that some token has scored
         const int32_t* const table = a.s.table + q.s * a.s.table_stride;
         const int columns = (k.group + 15) / 16;
+        int span = 1;
+        while (span < 16 && span < k.group) span *= 2;
         // 64 blocks a turn: their table entries are read a turn ahead, all their means at once
         constexpr int kStep = THREADS / kWave * 64;
         int32_t entry[4];
@@ -196,11 +235,12 @@ __global__ __launch_bounds__(THREADS) void kv_select_kernel(KvSelect k) {
                 for (int r = 0; r < 4; ++r) units[r] = __shfl(unit, g * 4 + r, kWave);
                 const int32_t b = b0 + z * 16;
                 if (b >= hi) break;
-                for (int t = 0; t < count; ++t) {
+                for (int t0 = 0; t0 < count; t0 += 16 / span) {
+                    const int t = t0 + n / span;
                     float4_t best = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                     for (int y = 0; y < columns; ++y) {
-                        // columns past the last head repeat it
-                        const int r = t * k.group + min(y * 16 + n, k.group - 1);
+                        // columns past a token's last head repeat it
+                        const int r = min(t, count - 1) * k.group + min(y * 16 + n % span, k.group - 1);
                         int4_t dot = {0, 0, 0, 0};
 #pragma unroll
                         for (int c = 0; c < DC; ++c)
@@ -212,21 +252,22 @@ __global__ __launch_bounds__(THREADS) void kv_select_kernel(KvSelect k) {
                         for (int i = 0; i < 4; ++i) best[i] = fmaxf(best[i], (float)dot[i] * f);
                     }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) best[i] = row_max(best[i]) * units[i];
-                    if (n == 0) *reinterpret_cast<float4_t*>(scores + t * step + b + g * 4) = best;
+                    for (int i = 0; i < 4; ++i) best[i] = span_max(best[i], span) * units[i];
+                    if (n % span == 0 && t < count)
+                        *reinterpret_cast<float4_t*>(scores + t * step + b + g * 4) = best;
                 }
             }
         }
         __syncthreads();  // (with GLOBAL: of this workgroup's own stores, read by it alone)
     }
-    for (int t = wave; t < count; t += THREADS / kWave) {
+    for (int t = wave / kTeam; t < count; t += THREADS / kWave / kTeam) {
         const int32_t blocks = blocks_of(t);
         int32_t* const out = k.out + ((q.begin + i0 + t) * heads + head) * k.keep;
         if (blocks <= k.keep) {
-            for (int i = lane; i < k.keep; i += kWave) out[i] = i < blocks ? i : -1;
+            for (int i = kTeam > 1 ? tid : lane; i < k.keep; i += kTeam * kWave) out[i] = i < blocks ? i : -1;
         } else {
-            pick(scores + t * step, blocks, k.first, blocks - k.recent, k.keep - k.first - k.recent,
-                 hist + wave * 256, out);
+            pick<kTeam>(scores + t * step, blocks, k.first, blocks - k.recent, k.keep - k.first - k.recent,
+                        picks + wave / kTeam, out);
         }
     }
 }
@@ -244,8 +285,8 @@ template <int D, int THREADS, bool GLOBAL>
 hipError_t launch_form(const KvSelect& k, hipStream_t st) {
     const mp_kv_seqs& s = k.a.s;
     const int64_t units = s.begin ? s.n_tokens / k.tokens + s.n_seqs : s.n_seqs;
-    size_t lds = (size_t)k.tokens * k.group * (D + 16) + ((size_t)k.tokens * k.group + 3) / 4 * 16 +
-                 THREADS / kWave * 1024;
+    constexpr size_t kPicks = THREADS == 1024 ? sizeof(PickLds<THREADS / kWave>) : THREADS / kWave * sizeof(PickLds<1>);
+    size_t lds = (size_t)k.tokens * k.group * (D + 16) + ((size_t)k.tokens * k.group + 3) / 4 * 16 + kPicks;
     if (!GLOBAL) lds += (size_t)k.tokens * k.score_stride * sizeof(float);
     if (lds > 65536)
         if (hipError_t e = hipFuncSetAttribute((const void*)kv_select_kernel<D, THREADS, GLOBAL>,
