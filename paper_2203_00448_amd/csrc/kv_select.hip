@@ -272,13 +272,13 @@ __global__ __launch_bounds__(THREADS) void kv_select_kernel(KvSelect k) {
     }
 }
 
-// Tokens of a workgroup: as many as its scores leave room for, where sequences have several.
-int32_t tokens_of(const mp_kv_seqs& s, int64_t stride, bool global) {
-    if (!s.begin || global) return 1;
-    const int64_t room = kLdsScores / stride;
-    const int64_t some = room < kMostTokens ? room : kMostTokens;
-    const int64_t most = some < s.most_new ? some : s.most_new;
-    return (int32_t)(most < 1 ? 1 : most);
+// Tokens of a workgroup, where sequences have several: as many as its scores leave room for and
+// leave 768 workgroups, three a compute unit (353 rows of 4 heads: two 19 us, four 22, eight 38).
+int32_t tokens_of(const mp_kv_cache& c, const mp_kv_seqs& s, int64_t stride, bool global) {
+    if (!s.begin || global || s.most_new < 2) return 1;
+    const int64_t room = kLdsScores / stride, some = s.n_tokens * c.heads / 768;
+    const int64_t most = some < 2 ? 2 : some > kMostTokens ? kMostTokens : some;
+    return (int32_t)(room < 1 ? 1 : room < most ? room : most);
 }
 
 template <int D, int THREADS, bool GLOBAL>
@@ -319,7 +319,7 @@ hipError_t launch_kv_select(const KvSelect& a, hipStream_t st) {
     if (a.a.s.n_tokens == 0) return hipSuccess;
     KvSelect k = a;
     const bool global = k.score_stride > kLdsScores;
-    k.tokens = tokens_of(k.a.s, k.score_stride, global);
+    k.tokens = tokens_of(k.a.c, k.a.s, k.score_stride, global);
     // query codes of many heads take room too
     while (k.tokens > 1 && (int64_t)k.tokens * k.group * (k.a.c.dim + 20) > 48 * 1024) --k.tokens;
     switch (k.a.c.dim) {
