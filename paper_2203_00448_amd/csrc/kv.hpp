@@ -31,9 +31,10 @@ hipError_t launch_kv_write(const KvArgs& a, const KvRows& k, const KvRows& v, hi
 hipError_t launch_kv_read(const KvArgs& a, const KvRows& k, const KvRows& v, hipStream_t st);
 
 // What a call of mp_kv_attend launches (kv_attend.hip).
+enum class KvForm { rows, tiles, pair };
 struct KvAttendShape {
     bool ok;
-    bool tiles;        // the form for many rows
+    KvForm form;
     int32_t rows;      // rows (query, head) of a workgroup
     int64_t units;     // row groups over all sequences, an upper bound
     int64_t chunk;     // tokens (of the sequence, or of its listed blocks) of a workgroup
@@ -75,6 +76,7 @@ hipError_t launch_kv_select(const KvSelect& a, hipStream_t st);
 
 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
 typedef float float2_t __attribute__((ext_vector_type(2)));
 typedef float float4_t __attribute__((ext_vector_type(4)));
 typedef float float16_t __attribute__((ext_vector_type(16)));
@@ -275,6 +277,21 @@ __device__ __forceinline__ KvSeq kv_seq(const KvArgs& a, int64_t s, int64_t b, i
     return q;
 }
 
+// What all lanes of the wave have alike, said so: scalar registers hold it.
+__device__ __forceinline__ int32_t wave_one(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t wave_one(int64_t x) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)x);
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | lo);
+}
+__device__ __forceinline__ KvSeq wave_one(KvSeq q) {
+    q.s = wave_one(q.s);
+    q.length = wave_one(q.length);
+    q.n = wave_one(q.n);
+    q.begin = wave_one(q.begin);
+    q.ok = wave_one((int32_t)q.ok) != 0;
+    return q;
+}
+
 // The last sequence whose key(begin[s], s) is at most u, where keys never fall with s (s itself
 // without begin), and u less its key; the whole wave searches, 64 keys a turn, and keeps what
 // it read of begin[].  Any values there give a sequence in range.
@@ -282,7 +299,7 @@ template <typename Key>
 __device__ __forceinline__ KvSeq kv_find(const KvArgs& a, int64_t u, Key key, int64_t* rest) {
     if (!a.s.begin) {
         *rest = 0;
-        return kv_seq(a, u, u, u + 1);
+        return wave_one(kv_seq(a, u, u, u + 1));
     }
     const int lane = threadIdx.x & (kWave - 1);
     int64_t lo = 0, hi = a.s.n_seqs, b = 0, e = 0;
@@ -296,15 +313,15 @@ __device__ __forceinline__ KvSeq kv_find(const KvArgs& a, int64_t u, Key key, in
             const int i = max(0, count - 1);
             e = __shfl(b, i + 1, kWave);
             b = __shfl(b, i, kWave);
-            *rest = u - key(b, lo + i);
-            return kv_seq(a, lo + i, b, e);
+            *rest = wave_one(u - key(b, lo + i));
+            return wave_one(kv_seq(a, lo + i, b, e));
         }
         lo += (int64_t)max(0, count - 1) * step;
         hi = min(hi, lo + step);
     }
     b = a.s.begin[lo];
-    *rest = u - key(b, lo);
-    return kv_seq(a, lo, b, a.s.begin[lo + 1]);
+    *rest = wave_one(u - key(b, lo));
+    return wave_one(kv_seq(a, lo, b, a.s.begin[lo + 1]));
 }
 
 }  // namespace mp

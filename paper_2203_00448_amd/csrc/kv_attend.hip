@@ -20,7 +20,6 @@
 // as the token that a lane's key row holds is chosen for it, and the maximum and the sum
 // of a row are over one lane's registers and the few lanes of its column.
 #include "kv.hpp"
-#include "internal.hpp"
 
 namespace mp {
 
@@ -84,7 +83,7 @@ __device__ __forceinline__ bool row_group(const KvAttend& k, int64_t u, RowGroup
             g->q = kv_find(a, u, key, &first);
         } else {
             const int64_t per = (k.group + k.shape.rows - 1) / k.shape.rows;
-            g->q = kv_seq(a, u / per, u / per, u / per + 1);
+            g->q = wave_one(kv_seq(a, u / per, u / per, u / per + 1));
             first = u % per;
         }
         if (!g->q.ok || first < 0) return false;
@@ -120,14 +119,15 @@ __device__ __forceinline__ Row row_of(const KvAttend& k, const RowGroup& g, int 
 struct Pages {
     const int32_t* table;
     uint32_t last_block, n_blocks;
-    bool bad;
+    uint32_t worst;  // the largest entry met
     __device__ __forceinline__ uint32_t entry(uint32_t block) const {
         return (uint32_t)table[min(block, last_block)];
     }
     __device__ __forceinline__ uint32_t page(uint32_t e) {
-        bad |= e >= n_blocks;
+        worst = max(worst, e);
         return min(e, n_blocks - 1);
     }
+    __device__ __forceinline__ bool bad() const { return worst >= n_blocks; }
 };
 
 // A row's query as the factor of the first product; `scale` becomes what its scores are
@@ -204,7 +204,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend
     const int32_t x1 = (int32_t)min(end_all, start + k.shape.chunk);
 
     Pages pages = {a.s.table + rg.q.s * a.s.table_stride, (uint32_t)max(most, 0) >> lb,
-                   (uint32_t)a.c.n_blocks, false};
+                   (uint32_t)a.c.n_blocks, 0};
     const int32_t* const list = LIST ? k.blocks + (rg.q.begin * heads + head) * k.keep : nullptr;
     const uint32_t page_size = heads * (uint32_t)D << lb;
     const int k_slot = ((n >> 2) * 16) & (block - 1), v_slot = (g * 16) & (block - 1);
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend
     auto named = [&](int32_t x) -> int32_t {
         const int32_t b = x >> lb;
         const int32_t id = b < k.keep ? list[b] : -1;
-        if (id != -1 && (uint32_t)id > (uint32_t)most >> lb) pages.bad = true;
+        if (id != -1 && (uint32_t)id > (uint32_t)most >> lb) pages.worst = ~0u;
         return (uint32_t)id <= (uint32_t)most >> lb && most >= 0 ? id : -1;
     };
     auto find = [&](int32_t x) {
@@ -350,7 +350,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend
             if (x + 2 * stride < x1) find(x + 2 * stride);
         }
     }
-    if (pages.bad) raise_status(a.status, MP_EINVAL);
+    if (pages.bad()) raise_status(a.status, MP_EINVAL);
 
     // the four waves' results of a row joined
     l += __shfl_xor(l, 16, kWave);
@@ -410,6 +410,121 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend
     }
 }
 
+// A row's query for the form of 32 rows a wave: half h of the wave has dims 16 i + 8 h + [0, 8).
+// `scale` as load_query.
+template <int D>
+__device__ __forceinline__ void load_rows(const KvAttend& k, const Row& row, int h,
+                                          half8_t (&q)[D / 16], float* scale) {
+    float x[D / 16][8], top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+        load8(k.q, row.token, row.head, i * 16 + h * 8, x[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[i][j]));
+    }
+    top = fmaxf(top, __shfl_xor(top, 32, kWave));
+    uint32_t frac;
+    const int e = min(127, max(-90, exponent_of(top, &frac)));
+    const float f = k.scale < 0.0f ? -pow2f(15 - e) : pow2f(15 - e);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[i][j] = (_Float16)(x[i][j] * f);
+    *scale = fabsf(k.scale) * kLog2e * pow2f(max(-126, e - 15));
+}
+
+// The result of a wave of 32 rows, a column each: lane half h has dims 4 h + [0, 4) of every eight.
+template <int D>
+__device__ __forceinline__ void store_rows(const KvAttend& k, const Row& row, uint32_t chunk,
+                                           const float16_t (&acc)[D / 32], float m, float l,
+                                           int vr, int h) {
+    const float total = l + __shfl_xor(l, 32, kWave);
+    if (!row.live) return;
+    const uint32_t n_chunks = (uint32_t)k.shape.n_chunks;
+    // a row that sees nothing: weights and sums are zero
+    const float norm = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
+    const float f = norm * pow2f(max(-126, vr - kWeightShift));
+    const float lse = total > 0.0f ? m + log2f(total) : total == 0.0f ? -INFINITY : total;
+    const int64_t index = row.token * (int64_t)k.group * k.a.c.heads + row.head;
+    const Partials part_out = partials(k);
+    const bool whole = n_chunks == 1;
+    float* const to = part_out.o + (index * n_chunks + chunk) * D;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int d = t * 32 + r * 2 + 4 * h;
+            float o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = acc[t][r + i] * f;
+            if (whole)
+                store4(k.out, row.token, row.head, d, o);
+            else
+                *reinterpret_cast<float4_t*>(to + d) = float4_t{o[0], o[1], o[2], o[3]};
+        }
+    if (h == 0) {
+        if (!whole) part_out.lse[index * n_chunks + chunk] = lse;
+        else if (k.lse) k.lse[index] = lse * kLn2;
+    }
+}
+
+// The sum of x over the wave.
+__device__ __forceinline__ int wave_sum(int x) {
+    const auto from = [](int v, auto dpp, auto rows) {
+        return __builtin_amdgcn_update_dpp(0, v, decltype(dpp)::value, decltype(rows)::value, 0xf, false);
+    };
+    using All = std::integral_constant<int, 0xf>;
+    x += from(x, std::integral_constant<int, 0x111>(), All());  // up by 1, 2, 4, 8 in rows of 16
+    x += from(x, std::integral_constant<int, 0x112>(), All());
+    x += from(x, std::integral_constant<int, 0x114>(), All());
+    x += from(x, std::integral_constant<int, 0x118>(), All());
+    x += from(x, std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());  // row 0 to 1, 2 to 3
+    x += from(x, std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());  // half to half
+    return __builtin_amdgcn_readlane(x, 63);
+}
+
+// Row group `u` of a launch of tiles: those that see the most first, so that the last ones to
+// start are short.  A lane has a sequence; group j of a sequence is at level (earlier tokens in
+// groups) + j, and u counts down the levels, sequences in order within one.  With more than 64
+// sequences, or chunks, the last sequences' last groups first.  Prompts of 228-4096 tokens: 273 us, 286
+// without the order; in chunks it gained nothing.
+template <int ROWS>
+__device__ __forceinline__ bool tile_group(const KvAttend& k, uint32_t u, RowGroup* g) {
+    const KvArgs& a = k.a;
+    if (!a.s.begin || a.s.n_seqs > kWave || k.shape.n_chunks > 1)
+        return row_group(k, k.shape.units - 1 - u, g);
+    const int lane = threadIdx.x & 63;
+    KvSeq q = {};
+    if (lane < a.s.n_seqs) q = kv_seq(a, lane, a.s.begin[lane], a.s.begin[lane + 1]);
+    const bool some = lane < a.s.n_seqs && q.ok && q.n > 0;
+    const int count = some ? (int)(((uint64_t)q.n * (uint32_t)k.group + ROWS - 1) / ROWS) : 0;
+    const int low = some ? (int)((uint64_t)max(0, q.length - q.n) * (uint32_t)k.group / ROWS) : 0;
+    if (u >= (uint32_t)wave_sum(count)) return false;
+    // the least level that at most u groups are above
+    const auto above = [&](int level) { return (uint32_t)wave_sum(min(count, max(0, low + count - 1 - level))); };
+    int from = 0, to = wave_reduce(low + count, OpMax<int>());
+    while (from < to) {
+        const int level = (from + to) >> 1;
+        if (above(level) <= u)
+            to = level;
+        else
+            from = level + 1;
+    }
+    const int nth = (int)(u - above(from));
+    const bool member = some && from >= low && from < low + count;
+    const uint64_t members = __ballot(member);
+    const int rank = __popcll(members & (((uint64_t)1 << lane) - 1));
+    const int of = __ffsll((unsigned long long)__ballot(member && rank == nth)) - 1;
+    g->q.s = of;
+    g->q.length = __builtin_amdgcn_readlane(q.length, of);
+    g->q.n = __builtin_amdgcn_readlane(q.n, of);
+    g->q.begin = wave_one(__shfl(q.begin, of, kWave));
+    g->q.ok = true;
+    g->row0 = (int64_t)(from - __builtin_amdgcn_readlane(low, of)) * ROWS;
+    g->n_rows = g->q.n * k.group;
+    return true;
+}
+
 // Many rows: four waves of 32 rows, one key head, one chunk of tokens, in tiles of 64 tokens
 // whose codes the workgroup turns into 16-bit floats once, in LDS, for all 128 rows.  Two
 // tiles' room: while one is computed the next one's codes, already in registers, are
@@ -444,12 +559,12 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
     const KvArgs& a = k.a;
     if (blockIdx.x == 0) kv_check_begin(a);
     // key heads fastest: workgroups of one head share an XCD's L2 where 8 and the number of
-    // heads divide; late row groups, which see the most, first
+    // heads divide
     const uint32_t heads = a.c.heads, n_chunks = (uint32_t)k.shape.n_chunks;
     const int head = (int)(blockIdx.x % heads);
     const uint32_t rest = blockIdx.x / heads, chunk = rest % n_chunks;
     RowGroup rg;
-    if (!row_group(k, k.shape.units - 1 - rest / n_chunks, &rg)) return;
+    if (!tile_group<128>(k, rest / n_chunks, &rg)) return;
     const int32_t most = row_of(k, rg, head, min((int64_t)rg.n_rows, rg.row0 + 128) - 1).last;
     const int64_t start = chunk * k.shape.chunk;
     if (chunk > 0 && start > most) return;
@@ -465,25 +580,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
 
     half8_t q[KS];
     float scale;
-    {
-        float top = 0.0f;
-        float x[KS][8];
-#pragma unroll
-        for (int i = 0; i < KS; ++i) {
-            load8(k.q, row.token, row.head, i * 16 + h * 8, x[i]);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[i][j]));
-        }
-        top = fmaxf(top, __shfl_xor(top, 32, kWave));
-        uint32_t frac;
-        const int e = min(127, max(-90, exponent_of(top, &frac)));
-        const float f = k.scale < 0.0f ? -pow2f(15 - e) : pow2f(15 - e);
-#pragma unroll
-        for (int i = 0; i < KS; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) q[i][j] = (_Float16)(x[i][j] * f);
-        scale = fabsf(k.scale) * kLog2e * pow2f(max(-126, e - 15));
-    }
+    load_rows<D>(k, row, h, q, &scale);
 
     float16_t acc[DT];
 #pragma unroll
@@ -496,7 +593,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
     const int lb = a.log_block, block = 1 << lb;
     const uint32_t page_size = heads * (uint32_t)D << lb;
     Pages pages = {a.s.table + rg.q.s * a.s.table_stride, (uint32_t)max(most, 0) >> lb,
-                   (uint32_t)a.c.n_blocks, false};
+                   (uint32_t)a.c.n_blocks, 0};
     // the 16 tokens that a wave's keys of one load lie in: their block is the same for the wave
     auto group_of = [&](int i) { return (wave * (64 / ROW) + i * (256 / ROW)) >> 4; };
     const uint32_t k_at = ((uint32_t)head * D << lb) + (tid % ROW) * 16;
@@ -644,33 +741,306 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
         }
         if (x + 64 < x1) put(buf ^ 1, x + 64);
     }
-    if (pages.bad) raise_status(a.status, MP_EINVAL);
-    if (!row.live) return;
-    const float total = l + __shfl_xor(l, 32, kWave);
-    const float norm = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
-    const float f = norm * pow2f(max(-126, vr - kWeightShift));
-    const float lse = total > 0.0f ? m + log2f(total) : total == 0.0f ? -INFINITY : total;
-    const int64_t index = row.token * (int64_t)k.group * a.c.heads + row.head;
-    const Partials part_out = partials(k);
-    const bool whole = n_chunks == 1;
-    float* const to = part_out.o + (index * n_chunks + chunk) * D;
+    if (pages.bad()) raise_status(a.status, MP_EINVAL);
+    store_rows<D>(k, row, chunk, acc, m, l, vr, h);
+}
+
+// Many rows, heads of 128: two teams of four waves, 32 rows each wave, over one key head
+// and one chunk of tokens in tiles of 64.  Of a SIMD's two waves one is of each team, and
+// the teams take turns: while one is at its matrix products (the last tile's second one,
+// this tile's first) the other is at its softmax; a barrier ends a turn.  Matrix and vector
+// instructions of two waves run beside each other on a SIMD, but left alone the waves fall
+// into step, as they meet at every tile's barrier, and wait for the same unit.
+//
+// A team's half of the conversion and of the loads for the next tiles goes between its matrix
+// instructions, whose 32 cycles leave room for seven others: in the turn of the first product
+// of tile i the keys of tile i + 1 and the values of tile i are put into LDS, loaded in the turn
+// before, and keys i + 2 and values i + 1 are loaded.  With team 0 at tile i in turn 2 i
+// and team 1 in turn 2 i + 1, keys i are read in these two turns and values i in the next two:
+// each is whole the turn before, and two tiles' room is enough for both.
+//
+// EXPS: exponents of a tile, 1 where a block is a tile.
+template <bool INT8, int EXPS>
+__global__ __launch_bounds__(512, 2) void kv_pair_kernel(KvAttend k) {
+    constexpr int D = 128, KS = D / 16, DT = D / 32, ROW = D / 16;  // ROW: loads of a token's keys
+    constexpr int LOADS = 2;  // of a thread for its team's half of a tile: of keys, of values
+    extern __shared__ __align__(16) char lds_raw[];
+    TileLds<D>* const lds = reinterpret_cast<TileLds<D>*>(lds_raw);
+    const int tid = threadIdx.x & 255, lane = tid & 63, n = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = wave >> 2;
+    const KvArgs& a = k.a;
+    if (blockIdx.x == 0) kv_check_begin(a);
+    // key heads fastest: workgroups of one head share an XCD's L2 where 8 and the number of
+    // heads divide
+    const uint32_t heads = a.c.heads, n_chunks = (uint32_t)k.shape.n_chunks;
+    const int head = (int)(blockIdx.x % heads);
+    const uint32_t rest = blockIdx.x / heads, chunk = rest % n_chunks;
+    RowGroup rg;
+    if (!tile_group<256>(k, rest / n_chunks, &rg)) return;
+    const int32_t most = row_of(k, rg, head, min((int64_t)rg.n_rows, rg.row0 + 256) - 1).last;
+    const int64_t start = chunk * k.shape.chunk;
+    if (chunk > 0 && start > most) return;
+    const int32_t x0 = (int32_t)start;
+    const int32_t x1 = (int32_t)min((int64_t)most + 1, start + k.shape.chunk);
+    const int32_t tiles = (x1 - x0 + 63) >> 6;  // 0 where no row sees anything
+
+    // this wave's rows, and the last position that all of them see
+    const int64_t wave_row0 = rg.row0 + 32 * wave;
+    const bool awake = wave_row0 < rg.n_rows;  // has rows
+    const int32_t wave_least = row_of(k, rg, head, wave_row0).last;
+    const Row row = row_of(k, rg, head, wave_row0 + n);
+
+    const int lb = a.log_block, block = 1 << lb;
+    const uint32_t page_size = heads * (uint32_t)D << lb;
+    Pages pages = {a.s.table + rg.q.s * a.s.table_stride, (uint32_t)max(most, 0) >> lb,
+                   (uint32_t)a.c.n_blocks, 0};
+    // load r: whether of values, the first token of its 16 in the tile, its place in a block's
+    // codes, in LDS; table entries are read a tile ahead of the loads
+    bool is_v[LOADS];
+    int first[LOADS];
+    const uint8_t* from[LOADS];
+    uint4* to[LOADS];
+    int piece[LOADS];
+    uint4 codes[LOADS];
+    uint32_t entry[LOADS];
 #pragma unroll
-    for (int t = 0; t < DT; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const int d = t * 32 + r * 2 + 4 * h;
-            float o[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = acc[t][r + i] * f;
-            if (whole)
-                store4(k.out, row.token, row.head, d, o);
-            else
-                *reinterpret_cast<float4_t*>(to + d) = float4_t{o[0], o[1], o[2], o[3]};
-        }
-    if (h == 0) {
-        if (!whole) part_out.lse[index * n_chunks + chunk] = lse;
-        else if (k.lse) k.lse[index] = lse * kLn2;
+    for (int r = 0; r < LOADS; ++r) {
+        is_v[r] = r == 1;
+        const int i = tid;
+        const int token = team * 32 + i / ROW, dim = team * (D / 2) + i / 4;
+        const int key_row = (token & 0x33) | (token & 4) << 1 | (token & 8) >> 1;
+        first[r] = is_v[r] ? (i & 3) * 16 : token & 48;
+        const uint32_t at = is_v[r] ? ((uint32_t)dim << lb) | (first[r] & (block - 1))
+                                    : (uint32_t)(token & (block - 1)) * D + i % ROW * 16;
+        from[r] = (is_v[r] ? a.c.v_code : a.c.k_code) + ((uint32_t)head * D << lb) + at;
+        to[r] = is_v[r] ? lds[0].v[dim] : lds[0].k[key_row];
+        piece[r] = is_v[r] ? ((i & 3) * 2) ^ v_key(dim) : (i % ROW * 2) ^ k_key<D>(key_row);
+        codes[r] = make_uint4(0, 0, 0, 0);
+        entry[r] = 0;
     }
+    // the tile of load r, with that of keys a tile ahead of that of values
+    auto tile_of = [&](int r, int v_tile) { return v_tile + (is_v[r] ? 0 : 1); };
+    auto find = [&](int r, int v_tile) {
+        entry[r] = pages.entry((uint32_t)(x0 + tile_of(r, v_tile) * 64 + first[r]) >> lb);
+    };
+    auto load = [&](int r) {
+        codes[r] = *reinterpret_cast<const uint4*>(from[r] + (uint64_t)pages.page(entry[r]) * page_size);
+    };
+    auto put = [&](int r, int v_tile, int half) {
+        uint4* const at = to[r] + (tile_of(r, v_tile) & 1) * (int)(sizeof(TileLds<D>) / 16);
+        const uint32_t lo = half ? codes[r].z : codes[r].x, hi = half ? codes[r].w : codes[r].y;
+        at[piece[r] ^ half] = __builtin_bit_cast(uint4, codes_to_half<INT8>(lo, hi));
+    };
+    // places past the end, which may hold anything, are zeros among the values
+    auto end_values = [&](int v_tile) {
+        if (x0 + v_tile * 64 + 63 <= most) return;
+#pragma unroll
+        for (int r = 0; r < LOADS; ++r)
+            if (is_v[r]) codes[r] = first_codes(codes[r], most - (x0 + v_tile * 64 + first[r]) + 1);
+    };
+    // the exponents of tokens [16 (tid % 4), + 16) of a tile
+    uint32_t exp_entry = 0;
+    int exp_k = 0, exp_v = 0;
+    auto find_exps = [&](int tile) {
+        exp_entry = pages.entry((uint32_t)(x0 + tile * 64 + (tid & 3) * 16) >> lb);
+    };
+    auto load_exps = [&]() {
+        const uint64_t at = (uint64_t)pages.page(exp_entry) * heads + head;
+        exp_k = a.c.k_exp[at];
+        exp_v = a.c.v_exp[at];
+    };
+    int ke[EXPS] = {}, ve[EXPS] = {};
+    auto read_exps = [&]() {
+#pragma unroll
+        for (int i = 0; i < EXPS; ++i) {
+            ke[i] = __builtin_amdgcn_readlane(exp_k, i);
+            ve[i] = __builtin_amdgcn_readlane(exp_v, i);
+        }
+    };
+    if (tiles > 0) {
+        find_exps(0);
+#pragma unroll
+        for (int r = 0; r < LOADS; ++r) find(r, -1);  // keys 0
+        load_exps();
+#pragma unroll
+        for (int r = 0; r < LOADS; ++r) load(r);
+        find_exps(1);
+#pragma unroll
+        for (int r = 0; r < LOADS; ++r) find(r, 0);  // keys 1, values 0
+    }
+
+    half8_t q[KS];
+    float scale;
+    load_rows<D>(k, row, h, q, &scale);
+    float16_t acc[DT], s[2];
+#pragma unroll
+    for (int t = 0; t < DT; ++t) acc[t] = float16_t{};
+    s[0] = s[1] = float16_t{};
+    half8_t w[4] = {};
+    float m = -INFINITY, l = 0.0f;
+    int vr = kNoExp;
+
+    auto turn = [&]() {
+        __builtin_amdgcn_sched_barrier(0);
+        __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // Piece `p` of a team's moving of data in the turn of tile i's first product: 2 LOADS pieces
+    // put keys i + 1 and values i, the others load the ones after.
+    constexpr int kPieces = 4 * LOADS + 1;
+    auto move = [&](int p, int i) {
+        if (p < 2 * LOADS) {
+            put(p / 2, i, p % 2);
+        } else if (p < 3 * LOADS) {
+            load(p - 2 * LOADS);
+        } else if (p < 4 * LOADS) {
+            find(p - 3 * LOADS, i + 2);
+        } else {
+            load_exps();
+            find_exps(i + 2);
+        }
+    };
+    // Factors from LDS: keys of instruction step i, product t; values of step i, dims t.  A lane's
+    // place in a row is its own but for the step's bits.
+    const int k_from = n * (D / 8), k_mine = h ^ k_key<D>(n), v_from = n * 8, v_mine = h ^ v_key(n);
+    auto k_factor = [&](int tile, int i, int t) {
+        const uint4* const at = &lds[tile & 1].k[0][0] + t * 32 * (D / 8) + k_from;
+        return __builtin_bit_cast(half8_t, at[k_mine ^ (i * 2)]);
+    };
+    auto v_factor = [&](int tile, int i, int t) {
+        const uint4* const at = &lds[tile & 1].v[0][0] + t * 32 * 8 + v_from;
+        return __builtin_bit_cast(half8_t, at[v_mine ^ (i * 2)]);
+    };
+    // The second product of tile i - 1 (SECOND) and the first of tile i (FIRST), factors read kAhead
+    // instructions ahead of their use: left to itself the compiler reads each just before.
+    auto products = [&](auto second, auto first_too, int i) {
+        constexpr int kSecond = second() ? 4 * DT : 0, kAll = kSecond + (first_too() ? 2 * KS : 0);
+        constexpr int kAhead = 6;
+        __builtin_amdgcn_s_setprio(1);  // the other wave's vector instructions fill what these leave
+        half8_t f[kAhead];
+        auto factor = [&](int j) {
+            return j < kSecond ? v_factor(i - 1, j / DT, j % DT)
+                               : k_factor(i, (j - kSecond) / 2, (j - kSecond) % 2);
+        };
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) f[j] = factor(j);
+        __builtin_amdgcn_sched_barrier(0);
+        if (first_too()) s[0] = s[1] = float16_t{};
+#pragma unroll
+        for (int j = 0; j < kAll; ++j) {
+            const half8_t use = f[j % kAhead];
+            if (j < kSecond) {
+                acc[j % DT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(use, w[j / DT], acc[j % DT], 0, 0, 0);
+            } else {
+                const int z = j - kSecond;
+                s[z % 2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(use, q[z / 2], s[z % 2], 0, 0, 0);
+            }
+            if (j + kAhead < kAll) f[j % kAhead] = factor(j + kAhead);
+            if (first_too() && j % 2 == 1 && j / 2 < kPieces) move(j / 2, i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+        if (first_too())
+#pragma unroll
+            for (int p = kAll / 2; p < kPieces; ++p) move(p, i);
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+
+    // keys 0 put before the first turn; then keys 1 and values 0 on their way
+    if (tiles > 0) {
+#pragma unroll
+        for (int r = 0; r < LOADS; ++r)
+            if (!is_v[r]) put(r, -1, 0), put(r, -1, 1);
+        read_exps();
+#pragma unroll
+        for (int r = 0; r < LOADS; ++r) load(r), find(r, 1);
+        end_values(0);
+    }
+    turn();
+    if (team) turn();
+    if (!awake) {  // only moves data
+        for (int tile = 0; tile < tiles; ++tile) {
+            for (int p = 0; p < kPieces; ++p) move(p, tile);
+            turn();
+            end_values(tile + 1);
+            turn();
+        }
+        if (!team) turn();
+        if (pages.bad()) raise_status(a.status, MP_EINVAL);
+        return;
+    }
+    if (tiles > 0) products(No{}, Yes{}, 0);
+    for (int tile = 0; tile < tiles; ++tile) {
+        const int32_t x = x0 + tile * 64;
+        turn();
+        end_values(tile + 1);
+        // register r of product t is token 32 t + 16 (r / 8) + 8 h + r % 8
+        if (x + 63 > wave_least) {
+            const int seen = row.last - x - h * 8;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    s[t][r] = t * 32 + (r >> 3) * 16 + (r & 7) > seen ? -INFINITY : s[t][r];
+        }
+        constexpr int kOf = 32 / EXPS;  // a lane's scores of one exponent
+        float c[EXPS], top = -INFINITY;
+        int new_vr = vr;
+#pragma unroll
+        for (int i = 0; i < EXPS; ++i) {
+            c[i] = fmaxf(scale * pow2f(ke[i]), 1.17549435e-38f);  // -inf * 0 is no score
+            float part = -INFINITY;
+#pragma unroll
+            for (int r = i * kOf; r < (i + 1) * kOf; ++r) part = fmaxf(part, s[r / 16][r % 16]);
+            top = fmaxf(top, part * c[i]);
+            // places past the end have some block's exponent: no larger than one that was there
+            new_vr = max(new_vr, ve[i]);
+        }
+        {
+            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+        }
+        const float new_m = fmaxf(m, top);
+        if (__any(new_m > m + kSlack || fabsf(new_m) > kLargeScore) || new_vr > vr) {
+            const float base = new_m == -INFINITY ? 0.0f : new_m;
+            if (__any(fabsf(base) > kLargeScore)) {
+#pragma unroll
+                for (int i = 0; i < EXPS; ++i) {
+#pragma unroll
+                    for (int r = i * kOf; r < (i + 1) * kOf; ++r) s[r / 16][r % 16] *= c[i];
+                    c[i] = 1.0f;
+                }
+            }
+            const float fall = __builtin_amdgcn_exp2f(m - base);
+            const float both = fall * pow2f(max(-126, vr - new_vr));
+#pragma unroll
+            for (int t = 0; t < DT; ++t) acc[t] *= both;
+            l *= fall;
+            m = new_m;
+            vr = new_vr;
+        }
+        const float origin = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int i = 0; i < EXPS; ++i) {
+            const int shift = max(kLeastShift, ve[i] - vr) + kWeightShift;
+            const float add = (float)shift - origin;
+            float sum = 0.0f;
+#pragma unroll
+            for (int r = i * kOf; r < (i + 1) * kOf; ++r) {
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r / 16][r % 16], c[i], add));
+                sum += e;
+                w[r / 8][r % 8] = (_Float16)e;
+            }
+            l += sum * pow2f(-shift);
+        }
+        read_exps();  // of the next tile, loaded a tile ago
+        turn();
+        products(Yes{}, Yes{}, tile + 1);  // the last one's scores are of no tile
+    }
+    if (!team) turn();
+    if (pages.bad()) raise_status(a.status, MP_EINVAL);
+    store_rows<D>(k, row, chunk, acc, m, l, vr, h);
 }
 
 // The chunks of a row joined, by WAVES waves: one where there are few chunks, four of a
@@ -746,14 +1116,19 @@ template <int D, bool INT8>
 hipError_t launch_d(const KvAttend& k, hipStream_t st) {
     const KvAttendShape& sh = k.shape;
     const dim3 grid((uint32_t)(sh.units * k.a.c.heads * sh.n_chunks));
-    if (sh.tiles) {
-        constexpr int kLds = 2 * sizeof(TileLds<D>);
+    constexpr int kLds = 2 * sizeof(TileLds<D>), kPairLds = 2 * sizeof(TileLds<128>);
+    if (sh.form == KvForm::tiles) {
         if (kLds > 65536)
             if (hipError_t e = hipFuncSetAttribute((const void*)kv_tiles_kernel<D, INT8>,
                                                    hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
                 e != hipSuccess)
                 return e;
         kv_tiles_kernel<D, INT8><<<grid, 256, kLds, st>>>(k);
+    } else if (sh.form == KvForm::pair) {  // heads of 128
+        if (k.a.c.block == 64)
+            kv_pair_kernel<INT8, 1><<<grid, 512, kPairLds, st>>>(k);
+        else
+            kv_pair_kernel<INT8, 4><<<grid, 512, kPairLds, st>>>(k);
     } else if (k.blocks) {
         kv_rows_kernel<D, INT8, true><<<grid, 256, 0, st>>>(k);
     } else {
@@ -776,8 +1151,17 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
                               int64_t keep) {
     KvAttendShape sh = {};
     const int64_t group = q_heads / c.heads;
-    sh.tiles = keep == 0 && s.begin && s.most_new * group > 16;
-    sh.rows = sh.tiles ? 128 : 16;
+    // The form by the rows of the longest piece.  Measured, us (rows / tiles / pair), query heads
+    // 4 a key head, dim 128: 64 sequences of 1-5000 tokens, 5 new 57 / 134 / 150, 8 new - / 139 /
+    // 165, 100 new - / 189 / 330; 4 of them, 16 new 29 / 30 / 25, 32 new 38 / 31 / 28; 16 of 2048, all
+    // new - / 795 / 763; one of 16384, all new - / 2482 / 2150.  A short piece of a short sequence
+    // (64 of 16 tokens, all new: 19 / 12 / 21) has little to share between row groups.
+    const int64_t piece = s.most_new * group;
+    if (keep > 0 || !s.begin || piece <= 16 || (piece <= 64 && s.longest > 512))
+        sh.form = KvForm::rows;
+    else
+        sh.form = c.dim == 128 && piece >= 4096 ? KvForm::pair : KvForm::tiles;
+    sh.rows = sh.form == KvForm::rows ? 16 : sh.form == KvForm::tiles ? 128 : 256;
     const int64_t per = (group + sh.rows - 1) / sh.rows;
     if (keep > 0)
         sh.units = s.n_tokens * per;
@@ -798,7 +1182,7 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     int64_t chunk = longest < ((int64_t)2048 * 256) / (wide > 0 ? wide : 1) ? longest * wide / 256 : 2048;
     if (chunk < 512) chunk = 512;
     if (longest <= 1024) chunk = 1024;
-    if (sh.tiles) {
+    if (sh.form != KvForm::rows) {
         const int64_t chunks = wide > 0 ? (4 * 256 + wide - 1) / wide : 1;
         chunk = (longest + chunks - 1) / chunks;
         if (chunk < 512) chunk = 512;

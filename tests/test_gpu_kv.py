@@ -621,3 +621,32 @@ def test_select_of_very_long_sequences():
     assert np.array_equal(host(got), s.ref.select(table, length, [0, 3], host(q.double()), 50, 2, 3))
     with pytest.raises(s.kv.PlanError):
         s.kv.select(s.cache, seqs, q, keep=50, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("block", [16, 64])
+def test_attend_long_prompt(kind, block):
+    """Prompts of over a thousand tokens beside short and empty ones and one that sees nothing
+    of its first rows: the form for the longest pieces."""
+    length, new = [1100, 300, 5, 0, 640], [1100, 20, 9, 3, 640]
+    s = Setup(length, heads=1, block=block, kind=kind)
+    s.fill()
+    seqs, begin = s.seqs(length, new)
+    q = s.rows(int(begin[-1]), 4)
+    lse = torch.empty(len(q), 4, device="cuda")
+    out = s.kv.attend(s.cache, seqs, q, lse=lse)
+    near(out, lse, s.ref.attend(s.table, length, begin, host(q.double()), 128 ** -0.5), torch.bfloat16)
+    out = s.kv.attend(s.cache, seqs, q * 20, scale=-0.3)
+    near(out, None, s.ref.attend(s.table, length, begin, host((q * 20).double()), -0.3), torch.bfloat16)
+
+
+@pytest.mark.parametrize("scale", [0.0, 1e-30])
+@pytest.mark.parametrize("new", [None, [6], [200], [1030]])
+def test_attend_scale_of_nothing(scale, new):
+    """Equal weights: the mean of what is seen, in every form."""
+    s = Setup([1030], heads=1, dim=128)
+    s.fill()
+    seqs, begin = s.seqs([1030], new)
+    q = s.rows(int(begin[-1]), 4)
+    out = s.kv.attend(s.cache, seqs, q, scale=scale)
+    near(out, None, s.ref.attend(s.table, [1030], begin, host(q.double()), scale), torch.bfloat16)
