@@ -208,9 +208,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend
     const int32_t* const list = LIST ? k.blocks + (rg.q.begin * heads + head) * k.keep : nullptr;
     const uint32_t page_size = heads * (uint32_t)D << lb;
     const int k_slot = ((n >> 2) * 16) & (block - 1), v_slot = (g * 16) & (block - 1);
-    const uint8_t* const k_base =
-        a.c.k_code + ((int64_t)head * D << lb) + (k_slot + (n & 3)) * D + g * 16;
-    const uint8_t* const v_base = a.c.v_code + ((int64_t)head * D << lb) + ((n << lb) | v_slot);
+    const uint32_t k_at = ((uint32_t)head * D << lb) + (k_slot + (n & 3)) * D + g * 16;
+    const uint32_t v_at = ((uint32_t)head * D << lb) + ((n << lb) | v_slot);
     uint4 kw[4][DC], vw[DT];
     // of the loaded step: the exponents of tokens [16 g, + 16), the position of the first;
     // of the one after: the table entries of the keys' and the values' tokens
@@ -237,7 +236,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend
         }
     };
     auto load_keys = [&]() {
-        const uint8_t* const p = k_base + (uint64_t)pages.page(k_entry) * page_size;
+        const uint8_t* const p = a.c.k_code + ((uint64_t)pages.page(k_entry) * page_size + k_at);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -246,7 +245,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend
     };
     auto load_values = [&]() {
         const uint32_t page = pages.page(v_entry);
-        const uint8_t* const p = v_base + (uint64_t)page * page_size;
+        const uint8_t* const p = a.c.v_code + ((uint64_t)page * page_size + v_at);
 #pragma unroll
         for (int t = 0; t < DT; ++t) vw[t] = *reinterpret_cast<const uint4*>(p + (t * 16 << lb));
         ke = a.c.k_exp[(uint64_t)page * heads + head];
@@ -258,13 +257,17 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend
     if (x < x1) {
         find(x);
         load_keys();
-        load_values();
-        if (x + stride < x1) find(x + stride);
     }
     const Row row = row_of(k, rg, head, rg.row0 + n);
     half8_t q[DC][2];
     float scale;
     load_query<D>(k, row, g, q, &scale);
+    // the values after the query, whose conversion wants registers: 64 sequences of 1-16384 tokens
+    // 152 us, 159 with these loads before it
+    if (x < x1) {
+        load_values();
+        if (x + stride < x1) find(x + stride);
+    }
     float4_t acc[DT];
     float m = -INFINITY, l = 0.0f;
     int vr = kNoExp;
