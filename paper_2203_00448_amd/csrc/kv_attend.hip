@@ -11,7 +11,7 @@
 // all bits of a bfloat16 or a 16-bit float down to 2^-29 of the row's largest.  The scale
 // of a block's keys multiplies its scores.  That of its values joins the exponent of the
 // weights, which enter the second product as w = 2^(c s_j - m + ve_j - vr + 15), vr the
-// largest ve so far: at most 2^15, normal down to 2^-29, where its contribution no longer
+// largest ve of the blocks that the row has seen so far: at most 2^15, normal down to 2^-29, where its contribution no longer
 // shows beside the largest.  The sum of weights takes 2^(c s_j - m) back from w in 32
 // bits.
 //
@@ -176,13 +176,18 @@ __device__ __forceinline__ uint4 first_codes(uint4 w, int n) {
 // quarter g then has the scores of tokens [16 g, 16 g + 16), four from each tile, which
 // are the columns of 16 bytes of each row of values.
 //
-// LIST: the tokens are those of the blocks listed for the row's token.
-template <int D, bool INT8, bool LIST>
+// Of: what the rows of a workgroup belong to, and the tokens they see.  With one token all rows
+// see the same ones, so the value exponent vr is one of the wave; with several it is a row's own (of a
+// block that some rows do not see yet, however large its values, those rows' weights must not lose
+// bits).  One token with a row's own: 64 sequences of 1-16384 tokens 160 us, 153 as it is.
+enum class Of { one, several, list };  // list: one token, and the blocks listed for it
+template <int D, bool INT8, Of OF>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend k) {
     constexpr int DT = D / 16, DC = D / 64;
+    constexpr bool LIST = OF == Of::list, OWN = OF == Of::several;
     __shared__ __align__(16) float so[4][16][D + 4];
     __shared__ float sm[4][16], sl[4][16];
-    __shared__ int svr[4];
+    __shared__ int svr[4][16];
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const KvArgs& a = k.a;
@@ -292,7 +297,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend
         const bool more = x + stride < x1;
         if (more) load_keys();
         // whether some row does not see some token of the step
-        if (LIST ? __any(pos + 15 > least) : x + kStep - 1 > least) {
+        const bool masked = LIST ? __any(pos + 15 > least) : x + kStep - 1 > least;
+        if (masked) {
             const int seen = row.last - pos;
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = i > seen ? -INFINITY : s[i];
@@ -307,21 +313,22 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend
         top *= c;
         top = fmaxf(top, __shfl_xor(top, 16, kWave));
         top = fmaxf(top, __shfl_xor(top, 32, kWave));
-        // places that name no block have no exponent
-        int top_ve = LIST && pos == kNowhere ? kNoExp : ve;
-        if (lb < 6) {
+        // of the blocks that the row sees; places that name no block have no exponent
+        int top_ve = ve;
+        if (OWN ? pos > row.last : LIST && pos == kNowhere) top_ve = kNoExp;
+        if (lb < 6 || (OWN && masked)) {
             top_ve = max(top_ve, __shfl_xor(top_ve, 16, kWave));
             top_ve = max(top_ve, __shfl_xor(top_ve, 32, kWave));
         }
         const float new_m = fmaxf(m, top);
-        const int new_vr = max(vr, __builtin_amdgcn_readfirstlane(top_ve));
+        const int new_vr = max(vr, OWN ? top_ve : __builtin_amdgcn_readfirstlane(top_ve));
         const float base = new_m == -INFINITY ? 0.0f : new_m;
         if (__any(fabsf(base) > kLargeScore)) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] *= c;
             c = 1.0f;
         }
-        if (__any(new_m > m) || new_vr > vr) {
+        if (OWN ? __any(new_m > m || new_vr > vr) : __any(new_m > m) || new_vr > vr) {
             const float fall = __builtin_amdgcn_exp2f(m - base);
             const float both = fall * pow2f(max(-126, vr - new_vr));
 #pragma unroll
@@ -361,8 +368,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend
     if (g == 0) {
         sm[wave][n] = m;
         sl[wave][n] = l;
+        svr[wave][n] = vr;
     }
-    if (lane == 0) svr[wave] = vr;
 #pragma unroll
     for (int t = 0; t < DT; ++t)
         *reinterpret_cast<float4_t*>(&so[wave][n][t * 16 + g * 4]) = acc[t];
@@ -370,14 +377,14 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend
     const int col = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * (D / 16);
     const float top = fmaxf(fmaxf(sm[0][col], sm[1][col]), fmaxf(sm[2][col], sm[3][col]));
     const float base = top == -INFINITY ? 0.0f : top;
-    const int most_vr = max(max(svr[0], svr[1]), max(svr[2], svr[3]));
+    const int most_vr = max(max(svr[0][col], svr[1][col]), max(svr[2][col], svr[3][col]));
     float total = 0.0f, o[D / 16];
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) o[i] = 0.0f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
         const float f = __builtin_amdgcn_exp2f(sm[w][col] - base);
-        const float fv = f * pow2f(max(-126, svr[w] - most_vr));
+        const float fv = f * pow2f(max(-126, svr[w][col] - most_vr));
         total += sl[w][col] * f;
 #pragma unroll
         for (int i = 0; i < D / 16; i += 4) {
@@ -526,6 +533,38 @@ __device__ __forceinline__ bool tile_group(const KvAttend& k, uint32_t u, RowGro
     g->row0 = (int64_t)(from - __builtin_amdgcn_readlane(low, of)) * ROWS;
     g->n_rows = g->q.n * k.group;
     return true;
+}
+
+// The largest value exponent that a row of a tile has met, with this tile's `ve` of N equal parts.
+// A masked tile ends `left` tokens after its first for the row, and what comes later must not cost
+// the row's weights bits.  Tiles before it are whole for all rows of the wave, so until then vr is the
+// same in all lanes, and its arithmetic is left to scalar registers.
+template <int N>
+__device__ __forceinline__ int seen_exp(bool masked, int vr, const int (&ve)[N], int left) {
+    if (!masked) {
+        int top = ve[0];
+#pragma unroll
+        for (int i = 1; i < N; ++i) top = max(top, ve[i]);
+        return max(vr, top);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) vr = max(vr, left >= i * (64 / N) ? ve[i] : kNoExp);
+    return vr;
+}
+
+// For each part of a tile, what is added to a weight's exponent, and the factor that takes the
+// shift back out of its sum.  Parts that a row does not see may be above its vr.
+template <int N>
+__device__ __forceinline__ void weight_shifts(bool masked, int vr, const int (&ve)[N], float from,
+                                              float (&add)[N], float (&back)[N]) {
+    const int whole = __builtin_amdgcn_readfirstlane(vr);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        int shift = max(kLeastShift, ve[i] - whole) + kWeightShift;
+        if (masked) shift = min(0, max(kLeastShift, ve[i] - vr)) + kWeightShift;
+        add[i] = (float)shift - from;
+        back[i] = pow2f(-shift);
+    }
 }
 
 // Many rows: four waves of 32 rows, one key head, one chunk of tokens, in tiles of 64 tokens
@@ -678,7 +717,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
                     s[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f, q[i], s[t], 0, 0, 0);
                 }
             // register r of product t is token 32 t + 16 (r / 8) + 8 h + r % 8
-            if (x + 63 > wave_least) {
+            const bool masked = x + 63 > wave_least;
+            if (masked) {
                 const int seen = row.last - x - h * 8;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
@@ -687,7 +727,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
                         s[t][r] = t * 32 + (r >> 3) * 16 + (r & 7) > seen ? -INFINITY : s[t][r];
             }
             float c[4], top = -INFINITY;
-            int new_vr = vr;
+            const int new_vr = seen_exp(masked, vr, ve, row.last - x);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 c[i] = fmaxf(scale * pow2f(ke[i]), 1.17549435e-38f);  // -inf * 0 is no score
@@ -695,8 +735,6 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
 #pragma unroll
                 for (int r = 0; r < 8; ++r) part = fmaxf(part, s[i / 2][i % 2 * 8 + r]);
                 top = fmaxf(top, part * c[i]);
-                // places past the end have some block's exponent: no larger than one that was there
-                new_vr = max(new_vr, ve[i]);
             }
             top = fmaxf(top, __shfl_xor(top, 32, kWave));
             const float new_m = fmaxf(m, top);
@@ -709,7 +747,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
                     c[i] = 1.0f;
                 }
             }
-            if (__any(new_m > m + kSlack) || new_vr > vr) {
+            if (__any(new_m > m + kSlack || new_vr > vr)) {
                 const float fall = __builtin_amdgcn_exp2f(m - base);
                 const float both = fall * pow2f(max(-126, vr - new_vr));
 #pragma unroll
@@ -720,18 +758,18 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
             }
             const float from = m == -INFINITY ? 0.0f : m;
             half8_t w[4];
+            float add[4], back[4];
+            weight_shifts(masked, vr, ve, from, add, back);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int shift = max(kLeastShift, ve[i] - vr) + kWeightShift;
-                const float add = (float)shift - from;
                 float sum = 0.0f;
 #pragma unroll
                 for (int r = 0; r < 8; ++r) {
-                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 2][i % 2 * 8 + r], c[i], add));
+                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 2][i % 2 * 8 + r], c[i], add[i]));
                     sum += e;
                     w[i][r] = (_Float16)e;
                 }
-                l += sum * pow2f(-shift);
+                l += sum * back[i];
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -979,7 +1017,8 @@ __global__ __launch_bounds__(512, 2) void kv_pair_kernel(KvAttend k) {
         turn();
         end_values(tile + 1);
         // register r of product t is token 32 t + 16 (r / 8) + 8 h + r % 8
-        if (x + 63 > wave_least) {
+        const bool masked = x + 63 > wave_least;
+        if (masked) {
             const int seen = row.last - x - h * 8;
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -989,7 +1028,7 @@ __global__ __launch_bounds__(512, 2) void kv_pair_kernel(KvAttend k) {
         }
         constexpr int kOf = 32 / EXPS;  // a lane's scores of one exponent
         float c[EXPS], top = -INFINITY;
-        int new_vr = vr;
+        const int new_vr = seen_exp(masked, vr, ve, row.last - x);
 #pragma unroll
         for (int i = 0; i < EXPS; ++i) {
             c[i] = fmaxf(scale * pow2f(ke[i]), 1.17549435e-38f);  // -inf * 0 is no score
@@ -997,15 +1036,13 @@ __global__ __launch_bounds__(512, 2) void kv_pair_kernel(KvAttend k) {
 #pragma unroll
             for (int r = i * kOf; r < (i + 1) * kOf; ++r) part = fmaxf(part, s[r / 16][r % 16]);
             top = fmaxf(top, part * c[i]);
-            // places past the end have some block's exponent: no larger than one that was there
-            new_vr = max(new_vr, ve[i]);
         }
         {
             const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
             top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
         }
         const float new_m = fmaxf(m, top);
-        if (__any(new_m > m + kSlack || fabsf(new_m) > kLargeScore) || new_vr > vr) {
+        if (__any(new_m > m + kSlack || fabsf(new_m) > kLargeScore || new_vr > vr)) {
             const float base = new_m == -INFINITY ? 0.0f : new_m;
             if (__any(fabsf(base) > kLargeScore)) {
 #pragma unroll
@@ -1024,18 +1061,18 @@ __global__ __launch_bounds__(512, 2) void kv_pair_kernel(KvAttend k) {
             vr = new_vr;
         }
         const float origin = m == -INFINITY ? 0.0f : m;
+        float add[EXPS], back[EXPS];
+        weight_shifts(masked, vr, ve, origin, add, back);
 #pragma unroll
         for (int i = 0; i < EXPS; ++i) {
-            const int shift = max(kLeastShift, ve[i] - vr) + kWeightShift;
-            const float add = (float)shift - origin;
             float sum = 0.0f;
 #pragma unroll
             for (int r = i * kOf; r < (i + 1) * kOf; ++r) {
-                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r / 16][r % 16], c[i], add));
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r / 16][r % 16], c[i], add[i]));
                 sum += e;
                 w[r / 8][r % 8] = (_Float16)e;
             }
-            l += sum * pow2f(-shift);
+            l += sum * back[i];
         }
         read_exps();  // of the next tile, loaded a tile ago
         turn();
@@ -1133,9 +1170,11 @@ hipError_t launch_d(const KvAttend& k, hipStream_t st) {
         else
             kv_pair_kernel<INT8, 4><<<grid, 512, kPairLds, st>>>(k);
     } else if (k.blocks) {
-        kv_rows_kernel<D, INT8, true><<<grid, 256, 0, st>>>(k);
+        kv_rows_kernel<D, INT8, Of::list><<<grid, 256, 0, st>>>(k);
+    } else if (k.a.s.begin && k.a.s.most_new > 1) {
+        kv_rows_kernel<D, INT8, Of::several><<<grid, 256, 0, st>>>(k);
     } else {
-        kv_rows_kernel<D, INT8, false><<<grid, 256, 0, st>>>(k);
+        kv_rows_kernel<D, INT8, Of::one><<<grid, 256, 0, st>>>(k);
     }
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (sh.n_chunks > 1) {

@@ -650,3 +650,28 @@ def test_attend_scale_of_nothing(scale, new):
     q = s.rows(int(begin[-1]), 4)
     out = s.kv.attend(s.cache, seqs, q, scale=scale)
     near(out, None, s.ref.attend(s.table, [1030], begin, host(q.double()), scale), torch.bfloat16)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dim,new", [(64, 16), (128, 70), (64, 300), (128, 1100)])
+def test_attend_ignores_sizes_of_later_blocks(kind, dim, new):
+    """Values that grow by 2^13 a block: what a row does not see yet, however large, costs it no
+    bits.  The bound is that of the blocks it sees."""
+    block, group, blocks = 16, 4, 70
+    s = Setup([block * blocks], heads=1, dim=dim, block=block, kind=kind)
+    for b in range(blocks):
+        n = b * block
+        seqs, begin = s.seqs([n + block], [block])
+        k, v = s.rows(block), s.rows(block, size=2.0 ** (13 * (b % 8) - 50))
+        s.kv.write(s.cache, seqs, k, v)
+        s.ref.write(s.table, [n + block], begin, host(k.double()), host(v.double()))
+    for length in (block * 8 - 3, block * blocks):
+        seqs, begin = s.seqs([length], [min(new, length)])
+        q = s.rows(int(begin[-1]), group)
+        out = s.kv.attend(s.cache, seqs, q)
+        ref, ref_lse, mass, delta, floor = s.ref.attend(s.table, [length], begin, host(q.double()), dim ** -0.5)
+        top = np.maximum.accumulate(s.ref.v_exp[s.table[0, :blocks], 0].astype(float))
+        last = length - len(q) + np.arange(len(q))
+        largest = (448.0 if kind == E4M3 else 127.0) * 2.0 ** top[last // block]
+        floor = np.broadcast_to(((last + 1) * largest)[:, None], floor.shape)
+        near(out, None, (ref, ref_lse, mass, delta, floor), torch.bfloat16)
