@@ -376,7 +376,9 @@ int32_t mp_plan_breadth_batch(const int64_t* begin, int64_t n_traces, const int3
  * mp_kv_rows (host struct): rows of a call, element (token, head, d) at
  *   data[token * token_stride + head * head_stride + d]; dtype MP_BF16,
  *   MP_F16 or MP_F32; strides in elements.  Rows of data and strides that are
- *   multiples of 16 bytes are moved in wide loads, others in narrow ones. */
+ *   multiples of 16 bytes are moved in wide loads, others in narrow ones.
+ *   Rows that a call reads may share places (strides of 0); of rows that it
+ *   writes, one axis lies within a step of the other, or it is refused. */
 #define MP_KV_E4M3 0
 #define MP_KV_INT8 1
 #define MP_BF16 0

@@ -63,6 +63,18 @@ bool rows_ok(const mp_kv_rows* r, int64_t tokens, int64_t heads, bool f32, KvRow
     return true;
 }
 
+// Whether no two elements of rows that a call writes share a place: one axis lies within a step
+// of the other.
+bool rows_apart(const mp_kv_rows* r, int64_t tokens, int64_t heads, int64_t dim) {
+    const bool tokens_outside = r->token_stride >= r->head_stride;
+    const int64_t inner = tokens_outside ? r->head_stride : r->token_stride;
+    const int64_t outer = tokens_outside ? r->token_stride : r->head_stride;
+    const int64_t n_inner = tokens_outside ? heads : tokens, n_outer = tokens_outside ? tokens : heads;
+    if (n_inner > 1 && inner < dim) return false;
+    const int64_t extent = n_inner > 1 ? (n_inner - 1) * inner + dim : dim;
+    return n_outer <= 1 || outer >= extent;
+}
+
 KvArgs args_of(const mp_kv_cache* c, const mp_kv_seqs* s, int32_t* status) {
     KvArgs a = {*c, *s, c->block == 16 ? 4 : c->block == 32 ? 5 : 6, status};
     return a;
@@ -92,6 +104,9 @@ int32_t move_rows(const mp_kv_cache* cache, const mp_kv_seqs* seqs, const mp_kv_
         !status_out || !pieces_ok(cache, seqs) ||
         !rows_ok(k, seqs->n_tokens, cache->heads, true, &kr) ||
         !rows_ok(v, seqs->n_tokens, cache->heads, true, &vr))
+        return MP_EINVAL;
+    if (!write && (!rows_apart(k, seqs->n_tokens, cache->heads, cache->dim) ||
+                   !rows_apart(v, seqs->n_tokens, cache->heads, cache->dim)))
         return MP_EINVAL;
     const KvArgs a = args_of(cache, seqs, status_out);
     const hipStream_t st = static_cast<hipStream_t>(stream);
@@ -124,7 +139,8 @@ extern "C" int32_t mp_kv_attend(const mp_kv_cache* cache, const mp_kv_seqs* seqs
     if (keep < 0 || keep > kMaxCount / 64) return MP_EINVAL;
     if ((blocks != nullptr) != (keep > 0) && seqs->n_tokens > 0) return MP_EINVAL;
     if (!rows_ok(q, seqs->n_tokens, q_heads, false, &k.q) ||
-        !rows_ok(out, seqs->n_tokens, q_heads, false, &k.out) || q->dtype != out->dtype)
+        !rows_ok(out, seqs->n_tokens, q_heads, false, &k.out) || q->dtype != out->dtype ||
+        !rows_apart(out, seqs->n_tokens, q_heads, cache->dim))
         return MP_EINVAL;
     k.shape = kv_attend_shape(*cache, *seqs, q_heads, keep);
     if (!k.shape.ok || workspace_bytes < k.shape.workspace || !aligned(workspace, 16) ||

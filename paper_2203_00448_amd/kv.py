@@ -5,7 +5,8 @@ A program keeps a `Cache` (its memory), a `Seqs` for its batch (block table,
 lengths, the call's rows), a status word and workspaces, and calls `write`,
 `read`, `select` and `attend` on them; outputs may be views of a planned slab.
 Each runs on `stream` (the current one if not given); tensors that are in use
-on another stream are the caller's to wait for.
+on another stream are the caller's to wait for.  They are for serving: none has
+a gradient, and an output shares no memory with an input.
 The tensors that a handle was made of stay the caller's: changing their
 values, not their places, changes what the next call sees.
 """
@@ -131,6 +132,8 @@ class Seqs:
             raise ValueError("table must be [n_seqs, width]")
         if table.shape[1] > 1 and table.stride(1) != 1:
             raise ValueError("a row of table must be contiguous")
+        if n > 1 and table.stride(0) < table.shape[1]:
+            raise ValueError("rows of table must not share places")
         if length.dim() != 1 or not length.is_contiguous():
             raise ValueError("length must be a contiguous vector")
         if table.device != length.device:
@@ -167,11 +170,13 @@ _MOVED = (torch.bfloat16, torch.float16, torch.float32)
 _QUERIES = (torch.bfloat16, torch.float16)
 
 
-def _rows(t, name, shape, dtypes):
+def _rows(t, name, shape, dtypes, device):
     """A tensor's rows as an argument.  These calls are short beside what a launch costs, so their
     checks look at each property once."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtypes or t.shape != shape:
         _need(t, dtypes, name, shape)
+    if t.get_device() != device.index:
+        raise ValueError(f"{name} must be on the device of the cache")
     strides = t.stride()
     if strides[2] != 1:
         raise ValueError(f"{name} must be contiguous in its last dimension")
@@ -187,6 +192,8 @@ def _word(status, cache):
         return new_status(cache.device)
     if not status.is_cuda or status.dtype is not torch.int32:
         _need(status, (torch.int32,), "status")
+    if status.numel() != 1 or status.get_device() != cache.device.index:
+        raise ValueError("status must be one word on the device of the cache")
     return status
 
 
@@ -210,7 +217,7 @@ def write(cache: Cache, seqs: Seqs, k, v, *, status=None, check: bool = True, st
             return write(cache, seqs, k, v, status=status, check=check)
     L = load_library()
     shape = (seqs.tokens, cache.heads, cache.dim)
-    ka, va = _rows(k, "k", shape, _MOVED), _rows(v, "v", shape, _MOVED)
+    ka, va = _rows(k, "k", shape, _MOVED, cache.device), _rows(v, "v", shape, _MOVED, cache.device)
     status = _word(status, cache)
     rc = L.mp_kv_write(cache._ref, seqs._for(cache), ctypes.addressof(ka), ctypes.addressof(va),
                        status.data_ptr(), _stream(cache.device))
@@ -229,7 +236,7 @@ def read(cache: Cache, seqs: Seqs, *, dtype=torch.bfloat16, out=None, status=Non
     if out is None:
         out = tuple(torch.empty(shape, dtype=dtype, device=cache.device) for _ in range(2))
     k, v = out
-    ka, va = _rows(k, "k", shape, _MOVED), _rows(v, "v", shape, _MOVED)
+    ka, va = _rows(k, "k", shape, _MOVED, cache.device), _rows(v, "v", shape, _MOVED, cache.device)
     status = _word(status, cache)
     rc = L.mp_kv_read(cache._ref, seqs._for(cache), ctypes.addressof(ka), ctypes.addressof(va),
                       status.data_ptr(), _stream(cache.device))
@@ -242,6 +249,8 @@ def _space(op, cache, seqs, q_heads, keep, workspace):
         workspace = globals()["workspace"](op, cache, seqs, q_heads=q_heads, keep=keep)
     elif not workspace.is_cuda:
         raise TypeError("workspace must be a CUDA (HIP) tensor")
+    elif not workspace.is_contiguous() or workspace.get_device() != cache.device.index:
+        raise ValueError("workspace must be contiguous and on the device of the cache")
     return workspace.data_ptr(), workspace.nbytes, workspace
 
 
@@ -262,20 +271,22 @@ def attend(cache: Cache, seqs: Seqs, q, *, scale: float | None = None, blocks=No
         raise ValueError("q must be [tokens, q_heads, dim]")
     heads = q.shape[1]
     rows = (seqs.tokens, heads, cache.dim)
-    qa = _rows(q, "q", rows, _QUERIES)
+    qa = _rows(q, "q", rows, _QUERIES, cache.device)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    oa = _rows(out, "out", rows, (q.dtype,))
+    oa = _rows(out, "out", rows, (q.dtype,), cache.device)
     keep, named = 0, None
     if blocks is not None:
         _need(blocks, (torch.int32,), "blocks")
         if blocks.dim() != 3 or blocks.shape[:2] != (seqs.tokens, cache.heads) or not blocks.is_contiguous():
             raise ValueError("blocks must be a contiguous [tokens, heads, keep]")
+        if blocks.shape[2] < 1 or blocks.get_device() != cache.device.index:
+            raise ValueError("blocks must name at least one place and be on the device of the cache")
         keep, named = blocks.shape[2], blocks.data_ptr()
     if lse is not None:
         _need(lse, (torch.float32,), "lse", (seqs.tokens, heads))
-        if not lse.is_contiguous():
-            raise ValueError("lse must be contiguous")
+        if not lse.is_contiguous() or lse.get_device() != cache.device.index:
+            raise ValueError("lse must be contiguous and on the device of the cache")
     space, have, _held = _space(OP_ATTEND, cache, seqs, heads, keep, workspace)
     status = _word(status, cache)
     rc = L.mp_kv_attend(cache._ref, seqs._for(cache), ctypes.addressof(qa), heads,
@@ -301,13 +312,13 @@ def select(cache: Cache, seqs: Seqs, q, *, keep: int, first: int = 1, recent: in
         raise ValueError("q must be [tokens, q_heads, dim]")
     heads = q.shape[1]
     rows = (seqs.tokens, heads, cache.dim)
-    qa = _rows(q, "q", rows, _QUERIES)
+    qa = _rows(q, "q", rows, _QUERIES, cache.device)
     shape = (seqs.tokens, cache.heads, int(keep))
     if out is None:
         out = torch.empty(shape, dtype=torch.int32, device=q.device)
     _need(out, (torch.int32,), "out", shape)
-    if not out.is_contiguous():
-        raise ValueError("out must be contiguous")
+    if not out.is_contiguous() or out.get_device() != cache.device.index:
+        raise ValueError("out must be contiguous and on the device of the cache")
     space, have, _held = _space(OP_SELECT, cache, seqs, heads, keep, workspace)
     status = _word(status, cache)
     rc = L.mp_kv_select(cache._ref, seqs._for(cache), ctypes.addressof(qa), heads, keep, first, recent,

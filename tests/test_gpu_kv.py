@@ -675,3 +675,39 @@ def test_attend_ignores_sizes_of_later_blocks(kind, dim, new):
         largest = (448.0 if kind == E4M3 else 127.0) * 2.0 ** top[last // block]
         floor = np.broadcast_to(((last + 1) * largest)[:, None], floor.shape)
         near(out, None, (ref, ref_lse, mass, delta, floor), torch.bfloat16)
+
+
+def test_inputs_that_share_places():
+    """One head's rows for all heads, one token's for all: read as they are."""
+    s = Setup([70], heads=3, dim=64, block=32, garbage=False)
+    seqs, begin = s.seqs([70], [70])
+    k, v = s.rows(70, 1).expand(70, 3, 64), s.rows(1, 3).expand(70, 3, 64)
+    s.kv.write(s.cache, seqs, k, v)
+    s.ref.write(s.table, [70], begin, host(k.double()), host(v.double()))
+    s.same()
+    s.same_codes([70])
+    q = s.rows(1, 1).expand(70, 6, 64)
+    near(s.kv.attend(s.cache, seqs, q), None, s.ref.attend(s.table, [70], begin, host(q.double()), 64 ** -0.5),
+         torch.bfloat16)
+
+
+def test_refusals_of_places():
+    """Outputs, tables, workspaces and lists whose memory is not what the call would take it for."""
+    s = Setup([100, 50], heads=2, dim=64, block=16)
+    seqs, _ = s.seqs([100, 50])
+    q, kv, c = s.rows(2, 4), s.kv, s.cache
+    for out in (torch.empty(1, 4, 64, dtype=q.dtype, device="cuda").expand(2, 4, 64),
+                torch.empty(2, 1, 64, dtype=q.dtype, device="cuda").expand(2, 4, 64)):
+        with pytest.raises(kv.PlanError):
+            kv.attend(c, seqs, q, out=out)
+        with pytest.raises(kv.PlanError):
+            kv.read(c, seqs, out=(out[:, :2], torch.empty(2, 2, 64, dtype=q.dtype, device="cuda")))
+    with pytest.raises(ValueError):
+        kv.Seqs(s.d_table[:1].expand(2, -1), seqs.length)
+    need = kv.workspace_size(kv.OP_ATTEND, c, seqs, q_heads=4, keep=4)
+    with pytest.raises(ValueError):
+        kv.attend(c, seqs, q, workspace=torch.empty(2 * (need + 64), dtype=torch.uint8, device="cuda")[::2])
+    with pytest.raises(ValueError):
+        kv.attend(c, seqs, q, blocks=torch.empty(2, 2, 0, dtype=torch.int32, device="cuda"))
+    with pytest.raises(ValueError):
+        kv.attend(c, seqs, q, status=torch.zeros(0, dtype=torch.int32, device="cuda"))

@@ -115,6 +115,13 @@ def test_attend_refusals(kv):
     assert c.attend() == -1
 
 
+@pytest.mark.parametrize("rows,call,heads", [("k", "read", 4), ("v", "read", 4), ("o", "attend", 8)])
+def test_outputs_whose_elements_share_places(kv, rows, call, heads):
+    wide, long = heads * 128, 30 * 128  # a token's heads, a head's tokens
+    for token, head in ((0, 128), (wide, 0), (wide - 1, 128), (wide, 127), (128, long - 1), (127, long)):
+        refused(kv, (call,), **{rows + "__token_stride": token, rows + "__head_stride": head})
+
+
 def test_select_refusals(kv):
     for change in ({"keep": -1}, {"first": -1}, {"recent": 0}, {"first": 4}, {"recent": 5}, {"out": None},
                    {"q_heads": 4 * 129}, {"first": 1 << 62}, {"recent": 1 << 62}):
