@@ -152,40 +152,68 @@ __device__ __forceinline__ uint32_t float_to_bf16(float x) {
     return __builtin_bit_cast(uint16_t, (__bf16)x);
 }
 
-// Eight consecutive elements of a row, at a multiple of eight.
-__device__ __forceinline__ void load8(const KvRows& r, int64_t token, int64_t head, int d,
-                                      float* x) {
+// Eight consecutive elements of a row, at a multiple of eight, as they lie in memory: loads only,
+// so that a caller has several on their way before the first is converted.
+struct Raw8 {
+    uint32_t w[8];  // 32-bit elements; wide 16-bit ones in pairs in the first four; narrow ones each
+};
+__device__ __forceinline__ Raw8 load_raw8(const KvRows& r, int64_t token, int64_t head, int d) {
     const int64_t at = token * r.token_stride + head * r.head_stride + d;
+    Raw8 x = {};
     if (r.dtype == MP_F32) {
-        const float* p = reinterpret_cast<const float*>(r.data) + at;
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(r.data) + at;
         if (r.wide) {
-            *reinterpret_cast<float4_t*>(x) = *reinterpret_cast<const float4_t*>(p);
-            *reinterpret_cast<float4_t*>(x + 4) = *reinterpret_cast<const float4_t*>(p + 4);
+            *reinterpret_cast<uint4_t*>(x.w) = *reinterpret_cast<const uint4_t*>(p);
+            *reinterpret_cast<uint4_t*>(x.w + 4) = *reinterpret_cast<const uint4_t*>(p + 4);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = p[i];
+            for (int i = 0; i < 8; ++i) x.w[i] = p[i];
         }
-        return;
+        return x;
     }
     const uint16_t* p = reinterpret_cast<const uint16_t*>(r.data) + at;
-    uint32_t w[4];
     if (r.wide) {
-        const uint4 u = *reinterpret_cast<const uint4*>(p);
-        w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+        *reinterpret_cast<uint4_t*>(x.w) = *reinterpret_cast<const uint4_t*>(p);
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = (uint32_t)p[2 * i] | (uint32_t)p[2 * i + 1] << 16;
+        for (int i = 0; i < 8; ++i) x.w[i] = p[i];
+    }
+    return x;
+}
+
+// Two 16-bit elements as floats.
+__device__ __forceinline__ void pair_to_float(bool bf16, uint32_t w, float* x) {
+    x[0] = bf16 ? __uint_as_float(w << 16) : half_to_float(w & 0xffffu);
+    x[1] = bf16 ? __uint_as_float(w & 0xffff0000u) : half_to_float(w >> 16);
+}
+__device__ __forceinline__ void raw8_to_float(const KvRows& r, const Raw8& raw, float* x) {
+    if (r.dtype == MP_F32) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(raw.w[i]);
+        return;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (r.dtype == MP_BF16) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        } else {
-            x[2 * i] = half_to_float(w[i] & 0xffffu);
-            x[2 * i + 1] = half_to_float(w[i] >> 16);
-        }
+        const uint32_t w = r.wide ? raw.w[i] : raw.w[2 * i] | raw.w[2 * i + 1] << 16;
+        pair_to_float(r.dtype == MP_BF16, w, x + 2 * i);
     }
+}
+
+// The same of rows of a 16-bit type, packed.
+__device__ __forceinline__ uint4 load8_16bit(const KvRows& r, int64_t token, int64_t head, int d) {
+    const uint16_t* p = reinterpret_cast<const uint16_t*>(r.data) + token * r.token_stride + head * r.head_stride + d;
+    if (r.wide) return *reinterpret_cast<const uint4*>(p);
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)p[2 * i] | (uint32_t)p[2 * i + 1] << 16;
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void to_float8(const KvRows& r, uint4 w, float* x) {
+    const bool bf16 = r.dtype == MP_BF16;
+    pair_to_float(bf16, w.x, x);
+    pair_to_float(bf16, w.y, x + 2);
+    pair_to_float(bf16, w.z, x + 4);
+    pair_to_float(bf16, w.w, x + 6);
 }
 
 // The same place written, each value rounded once.
@@ -221,31 +249,30 @@ __device__ __forceinline__ void store8(const KvRows& r, int64_t token, int64_t h
     }
 }
 
-// One or four (at a multiple of four) elements written the same way.
-__device__ __forceinline__ void store1(const KvRows& r, int64_t token, int64_t head, int d,
-                                       float x) {
-    const int64_t at = token * r.token_stride + head * r.head_stride + d;
-    if (r.dtype == MP_F32)
-        reinterpret_cast<float*>(r.data)[at] = x;
-    else
-        reinterpret_cast<uint16_t*>(r.data)[at] =
-            (uint16_t)(r.dtype == MP_BF16 ? float_to_bf16(x) : float_to_half(x));
-}
-__device__ __forceinline__ void store4(const KvRows& r, int64_t token, int64_t head, int d,
-                                       const float* x) {
-    if (r.wide && r.dtype != MP_F32) {
-        const int64_t at = token * r.token_stride + head * r.head_stride + d;
-        uint32_t w[2];
+// N (four or eight, at a multiple of it) elements of rows of a 16-bit type written the same way.
+template <int N>
+__device__ __forceinline__ void store_16bit(const KvRows& r, int64_t token, int64_t head, int d, const float* x) {
+    const bool bf16 = r.dtype == MP_BF16;
+    uint32_t w[N / 2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            w[i] = r.dtype == MP_BF16
-                       ? float_to_bf16(x[2 * i]) | float_to_bf16(x[2 * i + 1]) << 16
-                       : float_to_half(x[2 * i]) | float_to_half(x[2 * i + 1]) << 16;
-        *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(r.data) + at) = make_uint2(w[0], w[1]);
+    for (int i = 0; i < N / 2; ++i) {
+        const uint32_t b = float_to_bf16(x[2 * i]) | float_to_bf16(x[2 * i + 1]) << 16;
+        const uint32_t h = float_to_half(x[2 * i]) | float_to_half(x[2 * i + 1]) << 16;
+        w[i] = bf16 ? b : h;
+    }
+    uint16_t* p = reinterpret_cast<uint16_t*>(r.data) + token * r.token_stride + head * r.head_stride + d;
+    if (r.wide) {
+        if constexpr (N == 8)
+            *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        else
+            *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
         return;
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) store1(r, token, head, d + i, x[i]);
+    for (int i = 0; i < N / 2; ++i) {
+        p[2 * i] = (uint16_t)w[i];
+        p[2 * i + 1] = (uint16_t)(w[i] >> 16);
+    }
 }
 
 // A sequence of a call: its rows [begin, begin + n) and its tokens.

@@ -130,16 +130,31 @@ struct Pages {
     __device__ __forceinline__ bool bad() const { return worst >= n_blocks; }
 };
 
-// A row's query as the factor of the first product; `scale` becomes what its scores are
-// multiplied by, not negative: the query takes the sign.  Lane (column n, quarter g) holds dims [64 c + 16 g, + 16).
+// A row's query as it lies in memory: lane (column n, quarter g) holds dims [64 c + 16 g, + 16).
 template <int D>
-__device__ __forceinline__ void load_query(const KvAttend& k, const Row& r, int g,
-                                           half8_t (&q)[D / 64][2], float* scale) {
+struct Query {
+    uint4 w[D / 64][2];
+};
+template <int D>
+__device__ __forceinline__ Query<D> load_query(const KvAttend& k, const Row& r, int g) {
+    Query<D> x;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) x.w[c][i] = load8_16bit(k.q, r.token, r.head, c * 64 + g * 16 + i * 8);
+    return x;
+}
+
+// The same as the factor of the first product; `scale` becomes what its scores are multiplied
+// by, not negative: the query takes the sign.
+template <int D>
+__device__ __forceinline__ void query_factor(const KvAttend& k, const Query<D>& raw,
+                                             half8_t (&q)[D / 64][2], float* scale) {
     float x[D / 64][16], top = 0.0f;
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) {
-        load8(k.q, r.token, r.head, c * 64 + g * 16, x[c]);
-        load8(k.q, r.token, r.head, c * 64 + g * 16 + 8, x[c] + 8);
+        to_float8(k.q, raw.w[c][0], x[c]);
+        to_float8(k.q, raw.w[c][1], x[c] + 8);
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[c][i]));
     }
@@ -166,9 +181,9 @@ __device__ __forceinline__ uint4 first_codes(uint4 w, int n) {
     return make_uint4(x[0], x[1], x[2], x[3]);
 }
 
-// Few rows: 16 columns of rows, one key head, one chunk of tokens.  Each of four waves takes
-// every fourth step of 64 tokens, with its own running maxima, and the four are joined at
-// the end.  A wave reads the codes straight into registers, the next step's keys as soon as
+// Few rows: 16 columns of rows, one key head, one chunk of tokens.  Each of four or eight waves
+// takes every fourth or eighth step of 64 tokens, with its own running maxima, and they are joined
+// at the end.  A wave reads the codes straight into registers, the next step's keys as soon as
 // this one's are used, the values likewise; nothing is shared, so there is no barrier in
 // the loop and what hides the latency is the other waves of the SIMD.
 //
@@ -181,13 +196,13 @@ __device__ __forceinline__ uint4 first_codes(uint4 w, int n) {
 // block that some rows do not see yet, however large its values, those rows' weights must not lose
 // bits).  One token with a row's own: 64 sequences of 1-16384 tokens 160 us, 153 as it is.
 enum class Of { one, several, list };  // list: one token, and the blocks listed for it
-template <int D, bool INT8, Of OF>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend k) {
+template <int D, bool INT8, Of OF, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend k) {
     constexpr int DT = D / 16, DC = D / 64;
     constexpr bool LIST = OF == Of::list, OWN = OF == Of::several;
-    __shared__ __align__(16) float so[4][16][D + 4];
-    __shared__ float sm[4][16], sl[4][16];
-    __shared__ int svr[4][16];
+    __shared__ __align__(16) float so[WAVES][16][D + 4];
+    __shared__ float sm[WAVES][16], sl[WAVES][16];
+    __shared__ int svr[WAVES][16];
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const KvArgs& a = k.a;
@@ -257,16 +272,17 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend
         ve = a.c.v_exp[(uint64_t)page * heads + head];
         pos = next_pos;
     };
+    const Row row = row_of(k, rg, head, rg.row0 + n);
+    const Query<D> raw_q = load_query<D>(k, row, g);
     int32_t x = (int32_t)start + wave * kStep;
-    const int32_t stride = 4 * kStep;
+    const int32_t stride = WAVES * kStep;
     if (x < x1) {
         find(x);
         load_keys();
     }
-    const Row row = row_of(k, rg, head, rg.row0 + n);
     half8_t q[DC][2];
     float scale;
-    load_query<D>(k, row, g, q, &scale);
+    query_factor<D>(k, raw_q, q, &scale);
     // the values after the query, whose conversion wants registers: 64 sequences of 1-16384 tokens
     // 152 us, 159 with these loads before it
     if (x < x1) {
@@ -362,7 +378,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend
     }
     if (pages.bad()) raise_status(a.status, MP_EINVAL);
 
-    // the four waves' results of a row joined
+    // the waves' results of a row joined
     l += __shfl_xor(l, 16, kWave);
     l += __shfl_xor(l, 32, kWave);
     if (g == 0) {
@@ -374,15 +390,21 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend
     for (int t = 0; t < DT; ++t)
         *reinterpret_cast<float4_t*>(&so[wave][n][t * 16 + g * 4]) = acc[t];
     __syncthreads();
+    if (WAVES > 4 && threadIdx.x >= 256) return;
     const int col = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * (D / 16);
-    const float top = fmaxf(fmaxf(sm[0][col], sm[1][col]), fmaxf(sm[2][col], sm[3][col]));
+    float top = sm[0][col];
+    int most_vr = svr[0][col];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) {
+        top = fmaxf(top, sm[w][col]);
+        most_vr = max(most_vr, svr[w][col]);
+    }
     const float base = top == -INFINITY ? 0.0f : top;
-    const int most_vr = max(max(svr[0][col], svr[1][col]), max(svr[2][col], svr[3][col]));
     float total = 0.0f, o[D / 16];
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) o[i] = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
         const float f = __builtin_amdgcn_exp2f(sm[w][col] - base);
         const float fv = f * pow2f(max(-126, svr[w][col] - most_vr));
         total += sl[w][col] * f;
@@ -410,25 +432,25 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend
             *reinterpret_cast<float4_t*>(to + i) = float4_t{o[i], o[i + 1], o[i + 2], o[i + 3]};
         if (d0 == 0) part_out.lse[index * n_chunks + chunk] = lse;
     } else {
-        if constexpr (D / 16 >= 8) {
+        constexpr int kOnce = D / 16 >= 8 ? 8 : 4;
 #pragma unroll
-            for (int i = 0; i < D / 16; i += 8) store8(k.out, r.token, r.head, d0 + i, o + i);
-        } else {
-            store4(k.out, r.token, r.head, d0, o);
-        }
+        for (int i = 0; i < D / 16; i += kOnce) store_16bit<kOnce>(k.out, r.token, r.head, d0 + i, o + i);
         if (k.lse && d0 == 0) k.lse[index] = lse * kLn2;
     }
 }
 
 // A row's query for the form of 32 rows a wave: half h of the wave has dims 16 i + 8 h + [0, 8).
-// `scale` as load_query.
+// `scale` as query_factor.
 template <int D>
 __device__ __forceinline__ void load_rows(const KvAttend& k, const Row& row, int h,
                                           half8_t (&q)[D / 16], float* scale) {
+    uint4 raw[D / 16];
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) raw[i] = load8_16bit(k.q, row.token, row.head, i * 16 + h * 8);
     float x[D / 16][8], top = 0.0f;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
-        load8(k.q, row.token, row.head, i * 16 + h * 8, x[i]);
+        to_float8(k.q, raw[i], x[i]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[i][j]));
     }
@@ -468,7 +490,7 @@ __device__ __forceinline__ void store_rows(const KvAttend& k, const Row& row, ui
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[i] = acc[t][r + i] * f;
             if (whole)
-                store4(k.out, row.token, row.head, d, o);
+                store_16bit<4>(k.out, row.token, row.head, d, o);
             else
                 *reinterpret_cast<float4_t*>(to + d) = float4_t{o[0], o[1], o[2], o[3]};
         }
@@ -1146,10 +1168,22 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend k) {
     const float norm = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
     if (side == 0) {
         const float y[4] = {x[0] * norm, x[1] * norm, x[2] * norm, x[3] * norm};
-        store4(k.out, token, (int)(index % heads), d, y);
+        store_16bit<4>(k.out, token, (int)(index % heads), d, y);
     }
     if (k.lse && lane == 0)
         k.lse[index] = total > 0.0f ? (base + log2f(total)) * kLn2 : total == 0.0f ? -INFINITY : total;
+}
+
+// Eight waves where every workgroup has a compute unit of its own: half the steps of each.
+template <int D, bool INT8, Of OF>
+void launch_rows(const KvAttend& k, dim3 grid, hipStream_t st) {
+    if constexpr (D < 256) {
+        if (grid.x <= 256) {
+            kv_rows_kernel<D, INT8, OF, 8><<<grid, 512, 0, st>>>(k);
+            return;
+        }
+    }
+    kv_rows_kernel<D, INT8, OF, 4><<<grid, 256, 0, st>>>(k);
 }
 
 template <int D, bool INT8>
@@ -1170,11 +1204,11 @@ hipError_t launch_d(const KvAttend& k, hipStream_t st) {
         else
             kv_pair_kernel<INT8, 4><<<grid, 512, kPairLds, st>>>(k);
     } else if (k.blocks) {
-        kv_rows_kernel<D, INT8, Of::list><<<grid, 256, 0, st>>>(k);
+        launch_rows<D, INT8, Of::list>(k, grid, st);
     } else if (k.a.s.begin && k.a.s.most_new > 1) {
-        kv_rows_kernel<D, INT8, Of::several><<<grid, 256, 0, st>>>(k);
+        launch_rows<D, INT8, Of::several>(k, grid, st);
     } else {
-        kv_rows_kernel<D, INT8, Of::one><<<grid, 256, 0, st>>>(k);
+        launch_rows<D, INT8, Of::one>(k, grid, st);
     }
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (sh.n_chunks > 1) {

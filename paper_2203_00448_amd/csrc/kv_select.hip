@@ -173,7 +173,7 @@ __global__ __launch_bounds__(THREADS) void kv_select_kernel(KvSelect k) {
         for (int r0 = 0; r0 < rows; r0 += THREADS / PER_ROW) {
             const int r = min(r0 + row_in, rows - 1);
             float x[8], top = 0.0f;
-            load8(k.q, q.begin + i0 + r / k.group, head * k.group + r % k.group, d, x);
+            to_float8(k.q, load8_16bit(k.q, q.begin + i0 + r / k.group, head * k.group + r % k.group, d), x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float v = fabsf(x[i]);

@@ -122,20 +122,27 @@ __global__ __launch_bounds__(256) void kv_write_kernel(KvArgs a, KvRows k, KvRow
     };
     float kx[kItems][kRows][8], vx[kItems][kRows][8];
     float k_top = 0.0f, v_top = 0.0f;
+    // all loads before the first conversion; places that are not the call's as zeros
+    Raw8 k_raw[kItems][kRows], v_raw[kItems][kRows];
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
         const int item = tid + i * 256, d = item % vecs * 8;
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
+            k_raw[i][r] = v_raw[i][r] = Raw8{};
             if (is_new(item, r)) {
-                load8(k, p.token + place(item, r) - p.first, head, d, kx[i][r]);
-                load8(v, p.token + place(item, r) - p.first, head, d, vx[i][r]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) kx[i][r][j] = vx[i][r][j] = 0.0f;
+                k_raw[i][r] = load_raw8(k, p.token + place(item, r) - p.first, head, d);
+                v_raw[i][r] = load_raw8(v, p.token + place(item, r) - p.first, head, d);
             }
         }
     }
+#pragma unroll
+    for (int i = 0; i < kItems; ++i)
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            raw8_to_float(k, k_raw[i][r], kx[i][r]);
+            raw8_to_float(v, v_raw[i][r], vx[i][r]);
+        }
     bool finite = true;
 #pragma unroll
     for (int i = 0; i < kItems; ++i)
