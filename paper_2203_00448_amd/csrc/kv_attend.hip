@@ -170,16 +170,18 @@ __device__ __forceinline__ void query_factor(const KvAttend& k, const Query<D>& 
     *scale = fabsf(k.scale) * kLog2e * pow2f(max(-126, e - 15));
 }
 
-// Values at places of which only the first n of 16 exist: the others' codes to zero.
-__device__ __forceinline__ uint4 first_codes(uint4 w, int n) {
-    uint32_t x[4] = {w.x, w.y, w.z, w.w};
+// Of 16 places' codes those of the first n, which alone exist.  No branches: the step that needs it
+// is a sequence's last, and every other wave waits for it.
+struct FirstCodes {
+    uint32_t mask[4];
+    __device__ __forceinline__ explicit FirstCodes(int n) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int b = min(4, max(0, n - 4 * i));
-        x[i] = b == 0 ? 0 : b == 4 ? x[i] : x[i] & ((1u << (8 * b)) - 1);
+        for (int i = 0; i < 4; ++i) mask[i] = (uint32_t)(((uint64_t)1 << (8 * min(4, max(0, n - 4 * i)))) - 1);
     }
-    return make_uint4(x[0], x[1], x[2], x[3]);
-}
+    __device__ __forceinline__ uint4 operator()(uint4 w) const {
+        return make_uint4(w.x & mask[0], w.y & mask[1], w.z & mask[2], w.w & mask[3]);
+    }
+};
 
 // Few rows: 16 columns of rows, one key head, one chunk of tokens.  Each of four or eight waves
 // takes every fourth or eighth step of 64 tokens, with its own running maxima, and they are joined
@@ -200,6 +202,7 @@ template <int D, bool INT8, Of OF, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend k) {
     constexpr int DT = D / 16, DC = D / 64;
     constexpr bool LIST = OF == Of::list, OWN = OF == Of::several;
+    constexpr bool kEarly = WAVES == 8 && !LIST;  // values before the query
     __shared__ __align__(16) float so[WAVES][16][D + 4];
     __shared__ float sm[WAVES][16], sl[WAVES][16];
     __shared__ int svr[WAVES][16];
@@ -279,14 +282,15 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void
     if (x < x1) {
         find(x);
         load_keys();
+        if (kEarly) load_values();
     }
     half8_t q[DC][2];
     float scale;
     query_factor<D>(k, raw_q, q, &scale);
-    // the values after the query, whose conversion wants registers: 64 sequences of 1-16384 tokens
-    // 152 us, 159 with these loads before it
+    // the values after the query, whose conversion wants registers, where three waves share them: 64
+    // sequences of 1-16384 tokens 152 us, 159 with these loads before it
     if (x < x1) {
-        load_values();
+        if (!kEarly) load_values();
         if (x + stride < x1) find(x + stride);
     }
     float4_t acc[DT];
@@ -319,8 +323,9 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = i > seen ? -INFINITY : s[i];
             // places past the end may hold anything
+            const FirstCodes first(most - pos + 1);
 #pragma unroll
-            for (int t = 0; t < DT; ++t) vw[t] = first_codes(vw[t], most - pos + 1);
+            for (int t = 0; t < DT; ++t) vw[t] = first(vw[t]);
         }
         float c = fmaxf(scale * pow2f(ke), 1.17549435e-38f);  // -inf * 0 is no score
         float top = s[0];
@@ -691,6 +696,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
     // hold anything, as zeros among the values
     auto put = [&](int buf, int32_t x) {
         const bool tail = x + 63 > most;
+        const FirstCodes first(most - (x + (tid & 3) * 16) + 1);
 #pragma unroll
         for (int i = 0; i < KL; ++i) {
             const int t = tid / ROW + i * (256 / ROW), piece = tid % ROW * 2;
@@ -702,7 +708,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
 #pragma unroll
         for (int i = 0; i < VL; ++i) {
             const int d = (tid >> 2) + i * 64, piece = (tid & 3) * 2;
-            if (tail) vw[i] = first_codes(vw[i], most - (x + (tid & 3) * 16) + 1);
+            if (tail) vw[i] = first(vw[i]);
             uint4* const to = lds[buf].v[d];
             to[piece ^ v_key(d)] = __builtin_bit_cast(uint4, codes_to_half<INT8>(vw[i].x, vw[i].y));
             to[(piece ^ v_key(d)) ^ 1] = __builtin_bit_cast(uint4, codes_to_half<INT8>(vw[i].z, vw[i].w));
@@ -899,7 +905,7 @@ __global__ __launch_bounds__(512, 2) void kv_pair_kernel(KvAttend k) {
         if (x0 + v_tile * 64 + 63 <= most) return;
 #pragma unroll
         for (int r = 0; r < LOADS; ++r)
-            if (is_v[r]) codes[r] = first_codes(codes[r], most - (x0 + v_tile * 64 + first[r]) + 1);
+            if (is_v[r]) codes[r] = FirstCodes(most - (x0 + v_tile * 64 + first[r]) + 1)(codes[r]);
     };
     // the exponents of tokens [16 (tid % 4), + 16) of a tile
     uint32_t exp_entry = 0;
