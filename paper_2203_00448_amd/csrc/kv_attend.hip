@@ -193,6 +193,10 @@ struct FirstCodes {
 // quarter g then has the scores of tokens [16 g, 16 g + 16), four from each tile, which
 // are the columns of 16 bytes of each row of values.
 //
+// What bounds it is memory where there are many workgroups: 64 sequences of 1-16384 tokens 150 us,
+// 5.0 TB/s, two of 131072 101 us, 5.3 TB/s (a large copy: 5.1); one of 1000 tokens 10 us, a chain of
+// dependent loads (length, table, codes) and 16 steps.
+//
 // Of: what the rows of a workgroup belong to, and the tokens they see.  With one token all rows
 // see the same ones, so the value exponent vr is one of the wave; with several it is a row's own (of a
 // block that some rows do not see yet, however large its values, those rows' weights must not lose
@@ -600,6 +604,9 @@ __device__ __forceinline__ void weight_shifts(bool masked, int vr, const int (&v
 // converted into the other and the loads of the one after are on their way, so a tile
 // costs one barrier.
 //
+// Measured, 333 rows of heads of 64 after 20000 tokens: 117 us with the join, 460 TFLOP/s.  Of a
+// tile's work per wave the softmax's vector instructions take twice the cycles of its 16 products.
+//
 // Keys lie by row of the instruction: row m of 32 is token m with bits 2 and 3 exchanged,
 // so that a lane's scores are those of eight consecutive tokens, as the second product
 // takes them.  Both arrays have their 16-byte pieces exchanged by the row's low bits, so that
@@ -827,6 +834,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
 // before, and keys i + 2 and values i + 1 are loaded.  With team 0 at tile i in turn 2 i
 // and team 1 in turn 2 i + 1, keys i are read in these two turns and values i in the next two:
 // each is whole the turn before, and two tiles' room is enough for both.
+//
+// Measured, prompts of 228-4096 tokens, 32 query heads over 8: 279 us, 830 TFLOP/s.  A turn takes 1850
+// cycles: 1510 of products (1024 of matrix instructions; reading their factors takes the LDS as
+// long, as each serves one instruction) beside a softmax of 830, the rest barriers.
 //
 // EXPS: exponents of a tile, 1 where a block is a tile.
 template <bool INT8, int EXPS>
@@ -1113,7 +1124,8 @@ __global__ __launch_bounds__(512, 2) void kv_pair_kernel(KvAttend k) {
 
 // The chunks of a row joined, by WAVES waves: one where there are few chunks, four of a
 // workgroup where one alone would take many turns.  The chunks' logarithms are read by the
-// lanes at once, their results four dims a lane and a few chunks at a time.
+// lanes at once, their results four dims a lane and a few chunks at a time.  4-6 us for 2048 rows of
+// 8-64 chunks: the launch and three dependent loads.
 template <int D, int WAVES>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend k) {
     constexpr int LANES = D / 4, SIDE = kWave / LANES;  // lanes of a chunk, chunks side by side
@@ -1180,7 +1192,8 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend k) {
         k.lse[index] = total > 0.0f ? (base + log2f(total)) * kLn2 : total == 0.0f ? -INFINITY : total;
 }
 
-// Eight waves where every workgroup has a compute unit of its own: half the steps of each.
+// Eight waves where every workgroup has a compute unit of its own: half the steps of each.  16
+// sequences of 1-65536 tokens, 64 listed blocks of 64: 43 us with the selection, 49 by four waves.
 template <int D, bool INT8, Of OF>
 void launch_rows(const KvAttend& k, dim3 grid, hipStream_t st) {
     if constexpr (D < 256) {

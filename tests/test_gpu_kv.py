@@ -711,3 +711,21 @@ def test_refusals_of_places():
         kv.attend(c, seqs, q, blocks=torch.empty(2, 2, 0, dtype=torch.int32, device="cuda"))
     with pytest.raises(ValueError):
         kv.attend(c, seqs, q, status=torch.zeros(0, dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("new", [None, [3]])
+@pytest.mark.parametrize("blocks", [66, 258, 259, 515, 1026, 1027, 1028, 2500])
+def test_select_of_many_blocks(blocks, new):
+    """Around the numbers of blocks at which the selection changes its form, many ties among them."""
+    s = Setup([16 * 50], heads=2, dim=64, block=16)
+    s.fill()
+    table = np.resize(s.table[:1, :50], (1, blocks)).astype(np.int64)
+    length = [blocks * 16 - 5]
+    begin = np.array([0, 1 if new is None else new[0]])
+    seqs = s.kv.Seqs(torch.from_numpy(table.astype(np.int32)).cuda(),
+                     torch.tensor(length, dtype=torch.int32, device="cuda"),
+                     begin=None if new is None else torch.from_numpy(begin).cuda(), tokens=int(begin[-1]))
+    q = s.rows(int(begin[-1]), 6)
+    for keep, first, recent in ((1, 0, 1), (2, 1, 1), (17, 2, 3), (min(64, blocks - 1), 1, 2), (blocks - 1, 0, 1)):
+        got = s.kv.select(s.cache, seqs, q, keep=keep, first=first, recent=recent)
+        assert np.array_equal(host(got), s.ref.select(table, length, begin, host(q.double()), keep, first, recent))
