@@ -291,7 +291,7 @@ __global__ __launch_bounds__(256) void kv_write_kernel(KvArgs a, KvRows k, KvRow
 
 // A block's tokens back to rows, `per` key heads one after the other.  The values' bytes turn
 // in LDS; a row of it is four bytes longer than a block's so that the threads that read
-// along the dims meet different banks.  8 sequences of 1-16384 tokens, 8 heads of 128: 65 us, 4.6 TB/s.
+// along the dims meet different banks.  8 sequences of 1-16384 tokens, 8 heads of 128: 69 us, 4.4 TB/s.
 template <bool INT8>
 __global__ __launch_bounds__(256) void kv_read_kernel(KvArgs a, KvRows k, KvRows v, int32_t per) {
     extern __shared__ __align__(16) uint8_t sv[];
