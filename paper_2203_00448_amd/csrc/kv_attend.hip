@@ -32,9 +32,10 @@ constexpr int kLeastShift = -80;   // of a block's value exponent below the larg
 constexpr int kNoExp = -127;       // the largest value exponent of nothing
 // The exponent of a weight is one multiply-add, c s - m, which is off the rounded m by half of its
 // last place; scores beyond this are rounded first, so that none is above its maximum.
-constexpr float kLargeScore = 0x1p20f;
-// How far (in powers of two) a score may be above the running maximum before that follows: a
-// weight then reaches 2^15.99, below the largest 16-bit float.
+constexpr float kLargeScore = 0x1p16f;
+// How far (in powers of two) a score up to that size may be above the running maximum before that
+// follows.  The difference of the two is exact; with half a place of the score (2^-9) and of the
+// exponent's sum (2^-8) a weight reaches 2^15.996, where 16-bit floats end at 2^15.9995.
 constexpr float kSlack = 0.99f;
 constexpr int kStep = 64;          // tokens a wave takes at a time
 
@@ -774,7 +775,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
             top = fmaxf(top, __shfl_xor(top, 32, kWave));
             const float new_m = fmaxf(m, top);
             const float base = new_m == -INFINITY ? 0.0f : new_m;
-            if (__any(fabsf(base) > kLargeScore)) {
+            const bool large = __any(fabsf(base) > kLargeScore);
+            if (large) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
 #pragma unroll
@@ -782,7 +784,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
                     c[i] = 1.0f;
                 }
             }
-            if (__any(new_m > m + kSlack || new_vr > vr)) {
+            if (large || __any(new_m - m > kSlack || new_vr > vr)) {
                 const float fall = __builtin_amdgcn_exp2f(m - base);
                 const float both = fall * pow2f(max(-126, vr - new_vr));
 #pragma unroll
@@ -1081,7 +1083,7 @@ __global__ __launch_bounds__(512, 2) void kv_pair_kernel(KvAttend k) {
             top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
         }
         const float new_m = fmaxf(m, top);
-        if (__any(new_m > m + kSlack || fabsf(new_m) > kLargeScore || new_vr > vr)) {
+        if (__any(new_m - m > kSlack || fabsf(new_m) > kLargeScore || new_vr > vr)) {
             const float base = new_m == -INFINITY ? 0.0f : new_m;
             if (__any(fabsf(base) > kLargeScore)) {
 #pragma unroll
