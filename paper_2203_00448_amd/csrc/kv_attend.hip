@@ -31,26 +31,35 @@ constexpr int kWeightShift = 15;   // weights reach 2^15
 constexpr int kLeastShift = -80;   // of a block's value exponent below the largest
 constexpr int kNoExp = -127;       // the largest value exponent of nothing
 // The exponent of a weight is one multiply-add, c s - m, which is off the rounded m by half of its
-// last place; scores beyond this are rounded first, so that none is above its maximum.
+// last place.  Scores beyond this are rounded, as the maximum was, and taken from it first: none is
+// above it then, and what is added to the exponent does not vanish beside it.
 constexpr float kLargeScore = 0x1p16f;
 // How far (in powers of two) a score up to that size may be above the running maximum before that
 // follows.  The difference of the two is exact; with half a place of the score (2^-9) and of the
 // exponent's sum (2^-8) a weight reaches 2^15.996, where 16-bit floats end at 2^15.9995.
 constexpr float kSlack = 0.99f;
+
+// c s - m with the product rounded by itself: not positive where m is the largest such product.
+__device__ __forceinline__ float below_maximum(float s, float c, float m) {
+#pragma clang fp contract(off)
+    return s * c - m;
+}
+
 constexpr int kStep = 64;          // tokens a wave takes at a time
 
-// The partial result of a row over a chunk of tokens: o (normalised) and the base-2
-// logarithm of its sum of weights.
+// The partial result of a row over a chunk of tokens: o (normalised), the maximum of its weights'
+// exponents and the sum of its weights below that (one logarithm of both would lose the sum beside
+// a large maximum).
 struct Partials {
-    float* o;    // [row][chunk][dim]
-    float* lse;  // [row][chunk]
+    float* o;        // [row][chunk][dim]
+    float2_t* sums;  // [row][chunk]: maximum, sum
 };
 
 __device__ __forceinline__ Partials partials(const KvAttend& k) {
     const int64_t rows = k.a.s.n_tokens * (int64_t)k.group * k.a.c.heads * k.shape.n_chunks;
     Partials p;
     p.o = static_cast<float*>(k.ws);
-    p.lse = p.o + rows * k.a.c.dim;
+    p.sums = reinterpret_cast<float2_t*>(p.o + rows * k.a.c.dim);
     return p;
 }
 
@@ -349,10 +358,12 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void
         const float new_m = fmaxf(m, top);
         const int new_vr = max(vr, OWN ? top_ve : __builtin_amdgcn_readfirstlane(top_ve));
         const float base = new_m == -INFINITY ? 0.0f : new_m;
+        float from = base;  // taken from the scores with the multiply-add
         if (__any(fabsf(base) > kLargeScore)) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] *= c;
+            for (int i = 0; i < 16; ++i) s[i] = below_maximum(s[i], c, base);
             c = 1.0f;
+            from = 0.0f;
         }
         if (OWN ? __any(new_m > m || new_vr > vr) : __any(new_m > m) || new_vr > vr) {
             const float fall = __builtin_amdgcn_exp2f(m - base);
@@ -364,7 +375,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void
             vr = new_vr;
         }
         const int shift = max(kLeastShift, min(0, ve - vr)) + kWeightShift;
-        const float add = (float)shift - base;
+        const float add = (float)shift - from;
         float sum = 0.0f;
         half8_t w[2];
 #pragma unroll
@@ -440,7 +451,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void
 #pragma unroll
         for (int i = 0; i < D / 16; i += 4)
             *reinterpret_cast<float4_t*>(to + i) = float4_t{o[i], o[i + 1], o[i + 2], o[i + 3]};
-        if (d0 == 0) part_out.lse[index * n_chunks + chunk] = lse;
+        if (d0 == 0) part_out.sums[index * n_chunks + chunk] = float2_t{top, total};
     } else {
         constexpr int kOnce = D / 16 >= 8 ? 8 : 4;
 #pragma unroll
@@ -505,7 +516,7 @@ __device__ __forceinline__ void store_rows(const KvAttend& k, const Row& row, ui
                 *reinterpret_cast<float4_t*>(to + d) = float4_t{o[0], o[1], o[2], o[3]};
         }
     if (h == 0) {
-        if (!whole) part_out.lse[index * n_chunks + chunk] = lse;
+        if (!whole) part_out.sums[index * n_chunks + chunk] = float2_t{m, total};
         else if (k.lse) k.lse[index] = lse * kLn2;
     }
 }
@@ -780,7 +791,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
 #pragma unroll
-                    for (int r = 0; r < 8; ++r) s[i / 2][i % 2 * 8 + r] *= c[i];
+                    for (int r = 0; r < 8; ++r)
+                        s[i / 2][i % 2 * 8 + r] = below_maximum(s[i / 2][i % 2 * 8 + r], c[i], base);
                     c[i] = 1.0f;
                 }
             }
@@ -793,7 +805,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
                 m = new_m;
                 vr = new_vr;
             }
-            const float from = m == -INFINITY ? 0.0f : m;
+            const float from = large || m == -INFINITY ? 0.0f : m;  // taken from the scores yet
             half8_t w[4];
             float add[4], back[4];
             weight_shifts(masked, vr, ve, from, add, back);
@@ -1083,13 +1095,16 @@ __global__ __launch_bounds__(512, 2) void kv_pair_kernel(KvAttend k) {
             top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
         }
         const float new_m = fmaxf(m, top);
+        bool large = false;
         if (__any(new_m - m > kSlack || fabsf(new_m) > kLargeScore || new_vr > vr)) {
             const float base = new_m == -INFINITY ? 0.0f : new_m;
-            if (__any(fabsf(base) > kLargeScore)) {
+            large = __any(fabsf(base) > kLargeScore);
+            if (large) {
 #pragma unroll
                 for (int i = 0; i < EXPS; ++i) {
 #pragma unroll
-                    for (int r = i * kOf; r < (i + 1) * kOf; ++r) s[r / 16][r % 16] *= c[i];
+                    for (int r = i * kOf; r < (i + 1) * kOf; ++r)
+                        s[r / 16][r % 16] = below_maximum(s[r / 16][r % 16], c[i], base);
                     c[i] = 1.0f;
                 }
             }
@@ -1101,7 +1116,7 @@ __global__ __launch_bounds__(512, 2) void kv_pair_kernel(KvAttend k) {
             m = new_m;
             vr = new_vr;
         }
-        const float origin = m == -INFINITY ? 0.0f : m;
+        const float origin = large || m == -INFINITY ? 0.0f : m;  // taken from the scores yet
         float add[EXPS], back[EXPS];
         weight_shifts(masked, vr, ve, origin, add, back);
 #pragma unroll
@@ -1125,7 +1140,7 @@ __global__ __launch_bounds__(512, 2) void kv_pair_kernel(KvAttend k) {
 }
 
 // The chunks of a row joined, by WAVES waves: one where there are few chunks, four of a
-// workgroup where one alone would take many turns.  The chunks' logarithms are read by the
+// workgroup where one alone would take many turns.  The chunks' maxima and sums are read by the
 // lanes at once, their results four dims a lane and a few chunks at a time.  4-6 us for 2048 rows of
 // 8-64 chunks: the launch and three dependent loads.
 template <int D, int WAVES>
@@ -1140,10 +1155,10 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend k) {
     const uint32_t token = index / heads;
     const Partials p = partials(k);
     const int32_t n_chunks = (int32_t)k.shape.n_chunks;
-    const float* const lse = p.lse + (int64_t)index * n_chunks;
+    const float2_t* const sums = p.sums + (int64_t)index * n_chunks;
     const float* const o = p.o + (int64_t)index * n_chunks * D;
-    // read beside the sequence's length: the first chunks' logarithms, written or not
-    const float first = lse[min(lane, n_chunks - 1)];
+    // read beside the sequence's length: the first chunks' sums, written or not
+    const float2_t first = sums[min(lane, n_chunks - 1)];
     int64_t of;
     const KvSeq q = kv_find(a, token, [&](int64_t b, int64_t) { return b; }, &of);
     const bool ok = q.ok && token >= q.begin && token < q.begin + q.n;
@@ -1153,8 +1168,8 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend k) {
                                   : (int64_t)q.length - (q.n - 1 - (token - q.begin));
     const int32_t chunks = (int32_t)min((int64_t)n_chunks, max((int64_t)1, (seen + k.shape.chunk - 1) / k.shape.chunk));
     float top = -INFINITY;
-    if (lane < chunks) top = first;
-    for (int32_t c = lane + kWave; c < chunks; c += kWave) top = fmaxf(top, lse[c]);
+    if (lane < chunks) top = first[0];
+    for (int32_t c = lane + kWave; c < chunks; c += kWave) top = fmaxf(top, sums[c][0]);
     top = wave_reduce(top, OpMax<float>());
     const float base = top == -INFINITY ? 0.0f : top;
     const int side = lane / LANES, d = lane % LANES * 4;
@@ -1162,7 +1177,11 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend k) {
     float total = 0.0f;
     for (int32_t c0 = 0; c0 < chunks; c0 += kWave) {
         const int32_t mine = c0 + lane;
-        const float w = mine < chunks ? __builtin_amdgcn_exp2f((c0 == 0 ? first : lse[mine]) - base) : 0.0f;
+        float w = 0.0f;
+        if (mine < chunks) {
+            const float2_t both = c0 == 0 ? first : sums[mine];
+            w = both[1] * __builtin_amdgcn_exp2f(both[0] - base);
+        }
         total += w;
         const int32_t here = min(kWave, chunks - c0);
         for (int32_t c = (WAVES == 1 ? 0 : wave * SIDE); c < here; c += WAVES * SIDE) {
@@ -1289,7 +1308,7 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     sh.n_chunks = longest > 0 ? (longest + sh.chunk - 1) / sh.chunk : 1;
     const int64_t rows = s.n_tokens * q_heads;
     sh.ok = sh.units * c.heads * sh.n_chunks < INT32_MAX && rows < INT32_MAX;
-    sh.workspace = sh.n_chunks > 1 ? (size_t)rows * sh.n_chunks * (c.dim + 1) * 4 : 0;
+    sh.workspace = sh.n_chunks > 1 ? (size_t)rows * sh.n_chunks * (c.dim + 2) * 4 : 0;
     return sh;
 }
 

@@ -1,5 +1,6 @@
 """Attention over the 8-bit key/value cache where scores are large: successive tiles whose
-scores differ by one power of two of a weight.  Every form, against the definition in 64 bits."""
+scores differ by one power of two of a weight, and scores whose 32-bit steps are wider than
+the weights' whole range.  Every form, against the definition in 64 bits."""
 import math
 
 import numpy as np
@@ -86,3 +87,20 @@ def test_tiles_one_power_apart(kind, new, dim, block, power):
     for sign in (1, -1):
         out, want = attended(s, new, sign * 2.0 ** power / 64, 1.0, SCALE)
         check(out, want, 2.0 ** (2 * 2.0 ** (power - 24) + 2.0 ** -16) - 1)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("new,dim,block", FORMS)
+@pytest.mark.parametrize("lower", [False, True])
+def test_equal_huge_scores(kind, new, dim, block, lower):
+    """Equal scores, with values of other sizes from block to block: the plain mean of what is seen.
+    With `lower`, every third block's scores are half as far from zero: one sort alone counts.
+
+    Equal scores are rounded alike, so their weights are equal; the others are 2^20 powers apart."""
+    token = torch.arange(LENGTH)
+    first = torch.where((token // block % 3 == 1) & lower, 32.0, 64.0)
+    s = filled(kind, dim, block, first, 0.0, 2.0 ** (-3.0 * (token // block % 4)))
+    for power in (21, 24, 25, 26, 28, 40):
+        for part in (1.0, 1.2421875, -1.0, -1.2421875):
+            out, want = attended(s, new, part * 2.0 ** power / 64, 0.0, SCALE)
+            check(out, want, 0.0)
