@@ -453,8 +453,10 @@ int32_t mp_kv_read(const mp_kv_cache* cache, const mp_kv_seqs* seqs, const mp_kv
  *   workspace: mp_kv_workspace_size(MP_OP_KV_ATTEND, ...) bytes, 16-byte
  *              aligned; contents need no initialisation.
  * Products are in 32 bits of 16-bit factors that hold the codes exactly and
- * queries exactly up to 2^-29 of their largest value; exp(...) is held to 11
- * bits before the product with v, sums and maxima in 32 bits.  The order of every sum
+ * queries (rows whose largest is 2^-90 at least) exactly up to 2^-29 of their
+ * largest value.  exp(...) is held to 11 bits before the product with v, and in
+ * steps of 2^-28 where it, times the scale of v_j's block, is below 2^-18 of the row's
+ * largest such product; sums and maxima are in 32 bits.  The order of every sum
  * is fixed by the arguments, so a call repeats bit for bit. */
 int32_t mp_kv_attend(const mp_kv_cache* cache, const mp_kv_seqs* seqs, const mp_kv_rows* q,
                      int32_t q_heads, float scale, const int32_t* blocks, int64_t keep,

@@ -10,10 +10,12 @@
 // rows' type: queries are brought to [2^14, 2^15) by a power of two per row, which holds
 // all bits of a bfloat16 or a 16-bit float down to 2^-29 of the row's largest.  The scale
 // of a block's keys multiplies its scores.  That of its values joins the exponent of the
-// weights, which enter the second product as w = 2^(c s_j - m + ve_j - vr + 15), vr the
-// largest ve of the blocks that the row has seen so far: at most 2^15, normal down to 2^-29, where its contribution no longer
-// shows beside the largest.  The sum of weights takes 2^(c s_j - m) back from w in 32
-// bits.
+// weights, which enter the second product as w = 2^(c s_j - m + ve_j - vr + 15).  While the value
+// exponents that a wave has met differ by no more than 10, vr is the largest of them; from then on
+// m + vr follows the largest c s_j + ve_j of the row.  Either way no w is above 2^15, and the row's
+// largest contribution has one of 2^4 at least, normal down to 2^-14: a weight has its 11 bits down to
+// 2^-18 of that, and steps of 2^-28 of it below, whatever the sizes of other blocks.  The sum of weights
+// takes 2^(c s_j - m) back from w in 32 bits.
 //
 // Both products are taken transposed, S^T = K Q^T and O^T = V^T W^T: the weights then
 // come out of the first product in the lanes that the second one wants them in, as long
@@ -28,8 +30,8 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kWeightShift = 15;   // weights reach 2^15
-constexpr int kLeastShift = -80;   // of a block's value exponent below the largest
-constexpr int kNoExp = -127;       // the largest value exponent of nothing
+constexpr int kLeastShift = -80;   // of a block's value exponent below vr: its weights are zeros
+constexpr int kSpread = 10;        // of value exponents that share one vr
 // The exponent of a weight is one multiply-add, c s - m, which is off the rounded m by half of its
 // last place.  Scores beyond this are rounded, as the maximum was, and taken from it first: none is
 // above it then, and what is added to the exponent does not vanish beside it.
@@ -47,19 +49,44 @@ __device__ __forceinline__ float below_maximum(float s, float c, float m) {
 
 constexpr int kStep = 64;          // tokens a wave takes at a time
 
-// The partial result of a row over a chunk of tokens: o (normalised), the maximum of its weights'
-// exponents and the sum of its weights below that (one logarithm of both would lose the sum beside
-// a large maximum).
+// The value exponents that a wave has met.
+struct Met {
+    int lo = 127, hi = -128;
+    __device__ __forceinline__ void add(int ve) {
+        lo = min(lo, ve);
+        hi = max(hi, ve);
+    }
+    __device__ __forceinline__ bool apart() const { return hi - lo > kSpread; }
+};
+
+// vr for a new maximum: `top` the largest c s - new_m + ve of this step, what was summed so far at vr.
+__device__ __forceinline__ int joint_exp(float top, float m, int vr, float new_m) {
+    const float most = fmaxf(top, (m - new_m) + (float)vr);
+    return new_m == -INFINITY ? vr : (int)ceilf(most);
+}
+
+// What is summed so far, at m and vr, brought to new ones (base: new_m, or 0 for none).
+__device__ __forceinline__ float rescale(float m, int vr, float base, int new_vr) {
+    return __builtin_amdgcn_exp2f((m - base) + (float)(vr - new_vr));
+}
+
+// 2^-shift, where a weight's share of its row's sum is at most 2^-111 once that is out of range.
+__device__ __forceinline__ float back_from(int shift) { return pow2f(max(-126, -shift)); }
+
+// The partial result of a row over a chunk of tokens: its weighted values, 2^(maximum + power) of
+// them; the maximum of its weights' exponents, the sum of its weights below that, the power.  (One
+// logarithm of maximum and sum would lose the sum beside a large maximum; values at their own size
+// and weights at theirs could both leave the range of 32-bit floats where their product does not.)
 struct Partials {
     float* o;        // [row][chunk][dim]
-    float2_t* sums;  // [row][chunk]: maximum, sum
+    float4_t* sums;  // [row][chunk]: maximum, sum, power
 };
 
 __device__ __forceinline__ Partials partials(const KvAttend& k) {
     const int64_t rows = k.a.s.n_tokens * (int64_t)k.group * k.a.c.heads * k.shape.n_chunks;
     Partials p;
     p.o = static_cast<float*>(k.ws);
-    p.sums = reinterpret_cast<float2_t*>(p.o + rows * k.a.c.dim);
+    p.sums = reinterpret_cast<float4_t*>(p.o + rows * k.a.c.dim);
     return p;
 }
 
@@ -207,15 +234,10 @@ struct FirstCodes {
 // 5.0 TB/s, two of 131072 101 us, 5.3 TB/s (a large copy: 5.1); one of 1000 tokens 10 us, a chain of
 // dependent loads (length, table, codes) and 16 steps.
 //
-// Of: what the rows of a workgroup belong to, and the tokens they see.  With one token all rows
-// see the same ones, so the value exponent vr is one of the wave; with several it is a row's own (of a
-// block that some rows do not see yet, however large its values, those rows' weights must not lose
-// bits).  One token with a row's own: 64 sequences of 1-16384 tokens 160 us, 153 as it is.
-enum class Of { one, several, list };  // list: one token, and the blocks listed for it
-template <int D, bool INT8, Of OF, int WAVES>
+// LIST: one token, and the blocks listed for it.
+template <int D, bool INT8, bool LIST, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void kv_rows_kernel(KvAttend k) {
     constexpr int DT = D / 16, DC = D / 64;
-    constexpr bool LIST = OF == Of::list, OWN = OF == Of::several;
     constexpr bool kEarly = WAVES == 8 && !LIST;  // values before the query
     __shared__ __align__(16) float so[WAVES][16][D + 4];
     __shared__ float sm[WAVES][16], sl[WAVES][16];
@@ -309,7 +331,8 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void
     }
     float4_t acc[DT];
     float m = -INFINITY, l = 0.0f;
-    int vr = kNoExp;
+    int vr = 0;
+    Met met;
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[t] = float4_t{0, 0, 0, 0};
 
@@ -345,19 +368,26 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void
         float top = s[0];
 #pragma unroll
         for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+        const float mine = top;
         top *= c;
         top = fmaxf(top, __shfl_xor(top, 16, kWave));
         top = fmaxf(top, __shfl_xor(top, 32, kWave));
-        // of the blocks that the row sees; places that name no block have no exponent
-        int top_ve = ve;
-        if (OWN ? pos > row.last : LIST && pos == kNowhere) top_ve = kNoExp;
-        if (lb < 6 || (OWN && masked)) {
-            top_ve = max(top_ve, __shfl_xor(top_ve, 16, kWave));
-            top_ve = max(top_ve, __shfl_xor(top_ve, 32, kWave));
-        }
+        // places that name no block have no exponent
+        const int was = met.hi;
+        const auto meet = [&](int l) {
+            if (!LIST || __builtin_amdgcn_readlane(pos, l) != kNowhere) met.add(__builtin_amdgcn_readlane(ve, l));
+        };
+        meet(0);
+        if (lb < 6) meet(16), meet(32), meet(48);
         const float new_m = fmaxf(m, top);
-        const int new_vr = max(vr, OWN ? top_ve : __builtin_amdgcn_readfirstlane(top_ve));
         const float base = new_m == -INFINITY ? 0.0f : new_m;
+        int new_vr = met.hi;
+        if (met.apart()) {
+            float most = below_maximum(mine, c, base) + (float)ve;
+            most = fmaxf(most, __shfl_xor(most, 16, kWave));
+            most = fmaxf(most, __shfl_xor(most, 32, kWave));
+            new_vr = joint_exp(most, m, vr, new_m);
+        }
         float from = base;  // taken from the scores with the multiply-add
         if (__any(fabsf(base) > kLargeScore)) {
 #pragma unroll
@@ -365,16 +395,15 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void
             c = 1.0f;
             from = 0.0f;
         }
-        if (OWN ? __any(new_m > m || new_vr > vr) : __any(new_m > m) || new_vr > vr) {
-            const float fall = __builtin_amdgcn_exp2f(m - base);
-            const float both = fall * pow2f(max(-126, vr - new_vr));
+        if (met.apart() || met.hi > was || __any(new_m > m)) {
+            const float fall = __builtin_amdgcn_exp2f(m - base), both = rescale(m, vr, base, new_vr);
 #pragma unroll
             for (int t = 0; t < DT; ++t) acc[t] *= both;
             l *= fall;
             m = new_m;
             vr = new_vr;
         }
-        const int shift = max(kLeastShift, min(0, ve - vr)) + kWeightShift;
+        const int shift = max(kLeastShift, ve - vr) + kWeightShift;
         const float add = (float)shift - from;
         float sum = 0.0f;
         half8_t w[2];
@@ -384,7 +413,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void
             sum += e;
             w[i / 8][i % 8] = (_Float16)e;
         }
-        l += sum * pow2f(-shift);
+        l += sum * back_from(shift);
 #pragma unroll
         for (int t = 0; t < DT; ++t) {
             acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half<INT8>(vw[t].x, vw[t].y),
@@ -414,20 +443,24 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void
     if (WAVES > 4 && threadIdx.x >= 256) return;
     const int col = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * (D / 16);
     float top = sm[0][col];
-    int most_vr = svr[0][col];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) {
-        top = fmaxf(top, sm[w][col]);
-        most_vr = max(most_vr, svr[w][col]);
-    }
+    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, sm[w][col]);
     const float base = top == -INFINITY ? 0.0f : top;
+    // what a wave summed is 2^of[w] its numbers, counted from base
+    float of[WAVES], most_of = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        of[w] = (sm[w][col] - base) + (float)svr[w][col];
+        most_of = fmaxf(most_of, of[w]);
+    }
+    if (most_of == -INFINITY) most_of = 0.0f;
     float total = 0.0f, o[D / 16];
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) o[i] = 0.0f;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
         const float f = __builtin_amdgcn_exp2f(sm[w][col] - base);
-        const float fv = f * pow2f(max(-126, svr[w][col] - most_vr));
+        const float fv = __builtin_amdgcn_exp2f(of[w] - most_of);
         total += sl[w][col] * f;
 #pragma unroll
         for (int i = 0; i < D / 16; i += 4) {
@@ -438,12 +471,6 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void
     }
     const Row r = row_of(k, rg, head, rg.row0 + col);
     if (!r.live) return;
-    // a row that sees nothing: weights and sums are zero
-    const float norm = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
-    const float back = norm * pow2f(max(-126, most_vr - kWeightShift));
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) o[i] *= back;
-    const float lse = total > 0.0f ? base + log2f(total) : total == 0.0f ? -INFINITY : total;
     const int64_t index = r.token * (int64_t)k.group * heads + r.head;
     if (n_chunks > 1) {
         const Partials part_out = partials(k);
@@ -451,12 +478,19 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void
 #pragma unroll
         for (int i = 0; i < D / 16; i += 4)
             *reinterpret_cast<float4_t*>(to + i) = float4_t{o[i], o[i + 1], o[i + 2], o[i + 3]};
-        if (d0 == 0) part_out.sums[index * n_chunks + chunk] = float2_t{top, total};
+        if (d0 == 0)
+            part_out.sums[index * n_chunks + chunk] = float4_t{top, total, most_of - (float)kWeightShift, 0};
     } else {
+        // a row that sees nothing: weights and sums are zero
+        const float norm = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
+        const float back = norm * __builtin_amdgcn_exp2f(most_of - (float)kWeightShift);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) o[i] *= back;
         constexpr int kOnce = D / 16 >= 8 ? 8 : 4;
 #pragma unroll
         for (int i = 0; i < D / 16; i += kOnce) store_16bit<kOnce>(k.out, r.token, r.head, d0 + i, o + i);
-        if (k.lse && d0 == 0) k.lse[index] = lse * kLn2;
+        if (k.lse && d0 == 0)
+            k.lse[index] = total > 0.0f ? (base + log2f(total)) * kLn2 : total == 0.0f ? -INFINITY : total;
     }
 }
 
@@ -496,11 +530,10 @@ __device__ __forceinline__ void store_rows(const KvAttend& k, const Row& row, ui
     const uint32_t n_chunks = (uint32_t)k.shape.n_chunks;
     // a row that sees nothing: weights and sums are zero
     const float norm = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
-    const float f = norm * pow2f(max(-126, vr - kWeightShift));
-    const float lse = total > 0.0f ? m + log2f(total) : total == 0.0f ? -INFINITY : total;
     const int64_t index = row.token * (int64_t)k.group * k.a.c.heads + row.head;
     const Partials part_out = partials(k);
     const bool whole = n_chunks == 1;
+    const float f = whole ? norm * pow2f(max(-126, vr - kWeightShift)) : 1.0f;
     float* const to = part_out.o + (index * n_chunks + chunk) * D;
 #pragma unroll
     for (int t = 0; t < D / 32; ++t)
@@ -516,8 +549,10 @@ __device__ __forceinline__ void store_rows(const KvAttend& k, const Row& row, ui
                 *reinterpret_cast<float4_t*>(to + d) = float4_t{o[0], o[1], o[2], o[3]};
         }
     if (h == 0) {
-        if (!whole) part_out.sums[index * n_chunks + chunk] = float2_t{m, total};
-        else if (k.lse) k.lse[index] = lse * kLn2;
+        if (!whole)
+            part_out.sums[index * n_chunks + chunk] = float4_t{m, total, (float)(vr - kWeightShift), 0};
+        else if (k.lse)
+            k.lse[index] = total > 0.0f ? (m + log2f(total)) * kLn2 : total == 0.0f ? -INFINITY : total;
     }
 }
 
@@ -578,33 +613,41 @@ __device__ __forceinline__ bool tile_group(const KvAttend& k, uint32_t u, RowGro
     return true;
 }
 
-// The largest value exponent that a row of a tile has met, with this tile's `ve` of N equal parts.
-// A masked tile ends `left` tokens after its first for the row, and what comes later must not cost
-// the row's weights bits.  Tiles before it are whole for all rows of the wave, so until then vr is the
-// same in all lanes, and its arithmetic is left to scalar registers.
+// vr of a row for a tile whose blocks' value exponents are apart, before its scores are changed: N equal
+// parts of one exponent each.
 template <int N>
-__device__ __forceinline__ int seen_exp(bool masked, int vr, const int (&ve)[N], int left) {
-    if (!masked) {
-        int top = ve[0];
+__device__ __forceinline__ int tile_exp(const float16_t (&s)[2], const float (&c)[N], const int (&ve)[N], float m,
+                                        int vr, float new_m) {
+    float most = -INFINITY;
 #pragma unroll
-        for (int i = 1; i < N; ++i) top = max(top, ve[i]);
-        return max(vr, top);
+    for (int i = 0; i < N; ++i) {
+        float part = -INFINITY;
+#pragma unroll
+        for (int r = i * (32 / N); r < (i + 1) * (32 / N); ++r) part = fmaxf(part, s[r / 16][r % 16]);
+        most = fmaxf(most, below_maximum(part, c[i], new_m) + (float)ve[i]);
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i) vr = max(vr, left >= i * (64 / N) ? ve[i] : kNoExp);
-    return vr;
+    most = fmaxf(most, __shfl_xor(most, 32, kWave));
+    return joint_exp(most, m, vr, new_m);
 }
 
 // For each part of a tile, what is added to a weight's exponent, and the factor that takes the
-// shift back out of its sum.  Parts that a row does not see may be above its vr.
+// shift back out of its sum.  Where exponents are not apart vr is met.hi in all lanes, and the
+// arithmetic is left to scalar registers.
 template <int N>
-__device__ __forceinline__ void weight_shifts(bool masked, int vr, const int (&ve)[N], float from,
+__device__ __forceinline__ void weight_shifts(const Met& met, int vr, const int (&ve)[N], float from,
                                               float (&add)[N], float (&back)[N]) {
-    const int whole = __builtin_amdgcn_readfirstlane(vr);
+    if (met.apart()) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int shift = max(kLeastShift, ve[i] - vr) + kWeightShift;
+            add[i] = (float)shift - from;
+            back[i] = back_from(shift);
+        }
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        int shift = max(kLeastShift, ve[i] - whole) + kWeightShift;
-        if (masked) shift = min(0, max(kLeastShift, ve[i] - vr)) + kWeightShift;
+        const int shift = ve[i] - met.hi + kWeightShift;
         add[i] = (float)shift - from;
         back[i] = pow2f(-shift);
     }
@@ -674,7 +717,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[t] = float16_t{};
     float m = -INFINITY, l = 0.0f;
-    int vr = kNoExp;
+    int vr = 0;
+    Met met;
 
     // a thread's loads of a tile: 16 dims of KL tokens' keys, 16 tokens of VL dims' values; the
     // table entries are read a tile ahead of them
@@ -774,7 +818,6 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
                         s[t][r] = t * 32 + (r >> 3) * 16 + (r & 7) > seen ? -INFINITY : s[t][r];
             }
             float c[4], top = -INFINITY;
-            const int new_vr = seen_exp(masked, vr, ve, row.last - x);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 c[i] = fmaxf(scale * pow2f(ke[i]), 1.17549435e-38f);  // -inf * 0 is no score
@@ -786,6 +829,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
             top = fmaxf(top, __shfl_xor(top, 32, kWave));
             const float new_m = fmaxf(m, top);
             const float base = new_m == -INFINITY ? 0.0f : new_m;
+            const int was = met.hi;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) met.add(ve[i]);
+            int new_vr = met.hi;
+            if (met.apart()) new_vr = tile_exp<4>(s, c, ve, m, vr, new_m);
             const bool large = __any(fabsf(base) > kLargeScore);
             if (large) {
 #pragma unroll
@@ -796,9 +844,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
                     c[i] = 1.0f;
                 }
             }
-            if (large || __any(new_m - m > kSlack || new_vr > vr)) {
-                const float fall = __builtin_amdgcn_exp2f(m - base);
-                const float both = fall * pow2f(max(-126, vr - new_vr));
+            const bool moved = large || met.hi > was || met.apart();
+            if (__any(new_m - m > kSlack || moved)) {
+                const float fall = __builtin_amdgcn_exp2f(m - base), both = rescale(m, vr, base, new_vr);
 #pragma unroll
                 for (int t = 0; t < DT; ++t) acc[t] *= both;
                 l *= fall;
@@ -808,7 +856,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
             const float from = large || m == -INFINITY ? 0.0f : m;  // taken from the scores yet
             half8_t w[4];
             float add[4], back[4];
-            weight_shifts(masked, vr, ve, from, add, back);
+            weight_shifts(met, vr, ve, from, add, back);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float sum = 0.0f;
@@ -972,7 +1020,8 @@ __global__ __launch_bounds__(512, 2) void kv_pair_kernel(KvAttend k) {
     s[0] = s[1] = float16_t{};
     half8_t w[4] = {};
     float m = -INFINITY, l = 0.0f;
-    int vr = kNoExp;
+    int vr = 0;
+    Met met;
 
     auto turn = [&]() {
         __builtin_amdgcn_sched_barrier(0);
@@ -1081,7 +1130,6 @@ __global__ __launch_bounds__(512, 2) void kv_pair_kernel(KvAttend k) {
         }
         constexpr int kOf = 32 / EXPS;  // a lane's scores of one exponent
         float c[EXPS], top = -INFINITY;
-        const int new_vr = seen_exp(masked, vr, ve, row.last - x);
 #pragma unroll
         for (int i = 0; i < EXPS; ++i) {
             c[i] = fmaxf(scale * pow2f(ke[i]), 1.17549435e-38f);  // -inf * 0 is no score
@@ -1095,9 +1143,15 @@ __global__ __launch_bounds__(512, 2) void kv_pair_kernel(KvAttend k) {
             top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
         }
         const float new_m = fmaxf(m, top);
+        const int was = met.hi;
+#pragma unroll
+        for (int i = 0; i < EXPS; ++i) met.add(ve[i]);
         bool large = false;
-        if (__any(new_m - m > kSlack || fabsf(new_m) > kLargeScore || new_vr > vr)) {
+        const bool moved = met.hi > was || met.apart();
+        if (__any(new_m - m > kSlack || fabsf(new_m) > kLargeScore || moved)) {
             const float base = new_m == -INFINITY ? 0.0f : new_m;
+            int new_vr = met.hi;
+            if (met.apart()) new_vr = tile_exp<EXPS>(s, c, ve, m, vr, new_m);
             large = __any(fabsf(base) > kLargeScore);
             if (large) {
 #pragma unroll
@@ -1108,8 +1162,7 @@ __global__ __launch_bounds__(512, 2) void kv_pair_kernel(KvAttend k) {
                     c[i] = 1.0f;
                 }
             }
-            const float fall = __builtin_amdgcn_exp2f(m - base);
-            const float both = fall * pow2f(max(-126, vr - new_vr));
+            const float fall = __builtin_amdgcn_exp2f(m - base), both = rescale(m, vr, base, new_vr);
 #pragma unroll
             for (int t = 0; t < DT; ++t) acc[t] *= both;
             l *= fall;
@@ -1118,7 +1171,7 @@ __global__ __launch_bounds__(512, 2) void kv_pair_kernel(KvAttend k) {
         }
         const float origin = large || m == -INFINITY ? 0.0f : m;  // taken from the scores yet
         float add[EXPS], back[EXPS];
-        weight_shifts(masked, vr, ve, origin, add, back);
+        weight_shifts(met, vr, ve, origin, add, back);
 #pragma unroll
         for (int i = 0; i < EXPS; ++i) {
             float sum = 0.0f;
@@ -1155,10 +1208,10 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend k) {
     const uint32_t token = index / heads;
     const Partials p = partials(k);
     const int32_t n_chunks = (int32_t)k.shape.n_chunks;
-    const float2_t* const sums = p.sums + (int64_t)index * n_chunks;
+    const float4_t* const sums = p.sums + (int64_t)index * n_chunks;
     const float* const o = p.o + (int64_t)index * n_chunks * D;
     // read beside the sequence's length: the first chunks' sums, written or not
-    const float2_t first = sums[min(lane, n_chunks - 1)];
+    const float4_t first = sums[min(lane, n_chunks - 1)];
     int64_t of;
     const KvSeq q = kv_find(a, token, [&](int64_t b, int64_t) { return b; }, &of);
     const bool ok = q.ok && token >= q.begin && token < q.begin + q.n;
@@ -1172,6 +1225,12 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend k) {
     for (int32_t c = lane + kWave; c < chunks; c += kWave) top = fmaxf(top, sums[c][0]);
     top = wave_reduce(top, OpMax<float>());
     const float base = top == -INFINITY ? 0.0f : top;
+    // the chunks' values at one power
+    float power = -INFINITY;
+    if (lane < chunks) power = (first[0] - base) + first[2];
+    for (int32_t c = lane + kWave; c < chunks; c += kWave) power = fmaxf(power, (sums[c][0] - base) + sums[c][2]);
+    power = wave_reduce(power, OpMax<float>());
+    if (power == -INFINITY) power = 0.0f;
     const int side = lane / LANES, d = lane % LANES * 4;
     float4_t x = {0, 0, 0, 0};
     float total = 0.0f;
@@ -1179,10 +1238,10 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend k) {
         const int32_t mine = c0 + lane;
         float w = 0.0f;
         if (mine < chunks) {
-            const float2_t both = c0 == 0 ? first : sums[mine];
-            w = both[1] * __builtin_amdgcn_exp2f(both[0] - base);
+            const float4_t of = c0 == 0 ? first : sums[mine];
+            total += of[1] * __builtin_amdgcn_exp2f(of[0] - base);
+            w = __builtin_amdgcn_exp2f((of[0] - base) + of[2] - power);
         }
-        total += w;
         const int32_t here = min(kWave, chunks - c0);
         for (int32_t c = (WAVES == 1 ? 0 : wave * SIDE); c < here; c += WAVES * SIDE) {
             // a place past the last chunk has no weight, and reads the last one
@@ -1204,7 +1263,8 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend k) {
 #pragma unroll
         for (int w = 0; w < 4; ++w) x += *reinterpret_cast<const float4_t*>(&so[w][d]);
     }
-    const float norm = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
+    // a row that sees nothing: weights and sums are zero
+    const float norm = (total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total) * __builtin_amdgcn_exp2f(power);
     if (side == 0) {
         const float y[4] = {x[0] * norm, x[1] * norm, x[2] * norm, x[3] * norm};
         store_16bit<4>(k.out, token, (int)(index % heads), d, y);
@@ -1215,15 +1275,15 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttend k) {
 
 // Eight waves where every workgroup has a compute unit of its own: half the steps of each.  16
 // sequences of 1-65536 tokens, 64 listed blocks of 64: 43 us with the selection, 49 by four waves.
-template <int D, bool INT8, Of OF>
+template <int D, bool INT8, bool LIST>
 void launch_rows(const KvAttend& k, dim3 grid, hipStream_t st) {
     if constexpr (D < 256) {
         if (grid.x <= 256) {
-            kv_rows_kernel<D, INT8, OF, 8><<<grid, 512, 0, st>>>(k);
+            kv_rows_kernel<D, INT8, LIST, 8><<<grid, 512, 0, st>>>(k);
             return;
         }
     }
-    kv_rows_kernel<D, INT8, OF, 4><<<grid, 256, 0, st>>>(k);
+    kv_rows_kernel<D, INT8, LIST, 4><<<grid, 256, 0, st>>>(k);
 }
 
 template <int D, bool INT8>
@@ -1244,11 +1304,9 @@ hipError_t launch_d(const KvAttend& k, hipStream_t st) {
         else
             kv_pair_kernel<INT8, 4><<<grid, 512, kPairLds, st>>>(k);
     } else if (k.blocks) {
-        launch_rows<D, INT8, Of::list>(k, grid, st);
-    } else if (k.a.s.begin && k.a.s.most_new > 1) {
-        launch_rows<D, INT8, Of::several>(k, grid, st);
+        launch_rows<D, INT8, true>(k, grid, st);
     } else {
-        launch_rows<D, INT8, Of::one>(k, grid, st);
+        launch_rows<D, INT8, false>(k, grid, st);
     }
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (sh.n_chunks > 1) {
@@ -1308,7 +1366,7 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     sh.n_chunks = longest > 0 ? (longest + sh.chunk - 1) / sh.chunk : 1;
     const int64_t rows = s.n_tokens * q_heads;
     sh.ok = sh.units * c.heads * sh.n_chunks < INT32_MAX && rows < INT32_MAX;
-    sh.workspace = sh.n_chunks > 1 ? (size_t)rows * sh.n_chunks * (c.dim + 2) * 4 : 0;
+    sh.workspace = sh.n_chunks > 1 ? (size_t)rows * sh.n_chunks * (c.dim + 4) * 4 : 0;
     return sh;
 }
 
