@@ -3,9 +3,10 @@ intermediates are planned once, from the trace of one step, and then live at
 their offsets of one slab for every step.
 
 The trace has what a step makes and drops: the projected rows, the selected
-blocks, the attention's result, the operators' workspaces, the hidden states.  What
-outlives the step is not in it: the caches, which grow by a token a step, are
-held in blocks (kv.py).  The operators write into the planned views, so a step
+blocks, the attention's result, the operators' workspaces, the hidden states between
+layers.  What outlives the step is not in it: the caches, which grow by a token a step, are
+held in blocks (kv.py), and the last hidden state, which the caller may keep or pass to
+the next step, has memory of its own.  The operators write into the planned views, so a step
 allocates nothing and can be recorded in a graph.
 
     python -m paper_2203_00448_amd.decode_step [steps]
@@ -56,8 +57,9 @@ class DecodeStep:
                     ("select_space", i, torch.uint8, (max(16, spaces[0]),), select, select),
                     ("result", i, torch.bfloat16, (n, self.q_heads, self.dim), attend, merge),
                     ("attend_space", i, torch.uint8, (max(16, spaces[1]),), attend, attend),
-                    ("merged", i, torch.bfloat16, (n, self.hidden), merge, min(merge + 5, 5 * self.layers - 1)),
                     ("added", i, torch.bfloat16, (n, self.hidden), merge, merge)]
+            if i < self.layers - 1:
+                out.append(("merged", i, torch.bfloat16, (n, self.hidden), merge, merge + 5))
         return out
 
     def _lay_out(self, planned):
@@ -88,9 +90,11 @@ class DecodeStep:
             for x in shape:
                 count *= x
             self.at[name, layer] = view[:count * dtype.itemsize].view(dtype).view(shape)
+        self.at["merged", self.layers - 1] = torch.empty(self.n_seqs, self.hidden, dtype=torch.bfloat16, device="cuda")
 
     def run(self, x):
-        """One token of every sequence: x [n_seqs, hidden] in, the last layer's hidden state out."""
+        """One token of every sequence: x [n_seqs, hidden] in, the last layer's hidden state out.  That
+        is one tensor for all steps: the next step's x may be it, and its end writes it again."""
         self.length.add_(1)
         for i, cache in enumerate(self.caches):
             at = {name: self.at[name, i] for name in ("rows", "blocks", "select_space", "result", "attend_space",
