@@ -107,6 +107,9 @@ def new_status(device="cuda", stream=None) -> torch.Tensor:
 
 
 def reset_status(status: torch.Tensor, stream=None):
+    if stream is None and status.is_cuda and torch._C._cuda_getDevice() != status.device.index:
+        with torch.cuda.device(status.device):  # its own device's current stream
+            return reset_status(status)
     rc = load_library().mp_status_reset(_p(status), _stream(stream))
     if rc != MP_OK:
         raise PlanError(rc, "status_reset")

@@ -4,14 +4,16 @@ argument marshalling only, like binding.py.
 A program keeps a `Cache` (its memory), a `Seqs` for its batch (block table,
 lengths, the call's rows), a status word and workspaces, and calls `write`,
 `read`, `select` and `attend` on them; outputs may be views of a planned slab.
-Each runs on `stream` (the current one if not given); tensors that are in use
-on another stream are the caller's to wait for.  They are for serving: none has
+Each runs on `stream` (the current one of the cache's device if not given),
+whichever device is current; tensors that are in use on another stream are the
+caller's to wait for.  They are for serving: none has
 a gradient, and an output shares no memory with an input.
 The tensors that a handle was made of stay the caller's: changing their
 values, not their places, changes what the next call sees.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 
 import torch
@@ -187,6 +189,21 @@ def _stream(device):
     return torch._C._cuda_getCurrentRawStream(device.index)
 
 
+def _elsewhere(cache):
+    """Whether another device than the cache's is current: a launch would be that one's."""
+    return torch._C._cuda_getDevice() != cache.device.index
+
+
+@contextlib.contextmanager
+def _current(cache, stream):
+    """The cache's device and `stream`, if given, current for a call: what it allocates is theirs, and so
+    is the wait of check."""
+    if stream is not None and stream.device != cache.device:
+        raise ValueError("stream must be of the device of the cache")
+    with torch.cuda.device(cache.device), torch.cuda.stream(stream):
+        yield
+
+
 def _word(status, cache):
     if status is None:
         return new_status(cache.device)
@@ -211,9 +228,8 @@ def workspace(op: int, cache: Cache, seqs: Seqs, *, q_heads: int, keep: int = 0)
 def write(cache: Cache, seqs: Seqs, k, v, *, status=None, check: bool = True, stream=None):
     """Store the call's keys and values (mp_kv_write): k, v [tokens, heads, dim] in bfloat16,
     float16 or float32, any strides over a contiguous last dimension."""
-    if stream is not None:
-        # current for the call: what it allocates is that stream's, and so is the wait of check
-        with torch.cuda.stream(stream):
+    if stream is not None or _elsewhere(cache):
+        with _current(cache, stream):
             return write(cache, seqs, k, v, status=status, check=check)
     L = load_library()
     shape = (seqs.tokens, cache.heads, cache.dim)
@@ -227,9 +243,8 @@ def write(cache: Cache, seqs: Seqs, k, v, *, status=None, check: bool = True, st
 def read(cache: Cache, seqs: Seqs, *, dtype=torch.bfloat16, out=None, status=None,
          check: bool = True, stream=None):
     """Read back the call's tokens (mp_kv_read): (k, v) [tokens, heads, dim]."""
-    if stream is not None:
-        # current for the call: what it allocates is that stream's, and so is the wait of check
-        with torch.cuda.stream(stream):
+    if stream is not None or _elsewhere(cache):
+        with _current(cache, stream):
             return read(cache, seqs, dtype=dtype, out=out, status=status, check=check)
     L = load_library()
     shape = (seqs.tokens, cache.heads, cache.dim)
@@ -261,9 +276,8 @@ def attend(cache: Cache, seqs: Seqs, q, *, scale: float | None = None, blocks=No
     dim ** -0.5.  `blocks` int32 [tokens, heads, keep] limits each row to these of its
     sequence's blocks.  `lse` float32 [tokens, q_heads], if given, gets the logarithms of the
     sums.  Returns out."""
-    if stream is not None:
-        # current for the call: what it allocates is that stream's, and so is the wait of check
-        with torch.cuda.stream(stream):
+    if stream is not None or _elsewhere(cache):
+        with _current(cache, stream):
             return attend(cache, seqs, q, scale=scale, blocks=blocks, out=out, lse=lse, status=status,
                           workspace=workspace, check=check)
     L = load_library()
@@ -302,9 +316,8 @@ def select(cache: Cache, seqs: Seqs, q, *, keep: int, first: int = 1, recent: in
     """The blocks of each row and key head that attend is to read (mp_kv_select): the first
     `first`, the last `recent` and the best-scored others, `keep` in all, int32 [tokens, heads,
     keep], ascending, -1 beyond the last."""
-    if stream is not None:
-        # current for the call: what it allocates is that stream's, and so is the wait of check
-        with torch.cuda.stream(stream):
+    if stream is not None or _elsewhere(cache):
+        with _current(cache, stream):
             return select(cache, seqs, q, keep=keep, first=first, recent=recent, out=out, status=status,
                           workspace=workspace, check=check)
     L = load_library()
