@@ -155,17 +155,20 @@ class Seqs:
         self.most_new = int(most_new) if most_new is not None else self.tokens if begin is not None else 1
         self.longest, self.device = longest, length.device
         width = table.shape[1]
-        self._arg = _SeqsArg(table.data_ptr() or None, max(width, table.stride(0)), width, length.data_ptr() or None,
-                             begin.data_ptr() if begin is not None else None, n, self.tokens,
-                             self.most_new, 0)
-        self._ref = ctypes.addressof(self._arg)
+        self._fields = (table.data_ptr() or None, max(width, table.stride(0)), width, length.data_ptr() or None,
+                        begin.data_ptr() if begin is not None else None, n, self.tokens, self.most_new)
+        self._last = (None, None)
 
     def _for(self, cache: Cache):
-        """Its argument, with the bound on the lengths, for a cache's blocks."""
+        """Its argument, with the bound on the lengths, for a cache's blocks.  One that was handed out never
+        changes (another thread's call may be reading it): the caller holds it during its call."""
         if cache.device != self.device:
             raise ValueError("cache and sequences must be on one device")
-        self._arg.longest = self._arg.table_width * cache.block if self.longest is None else self.longest
-        return self._ref
+        longest = self._fields[2] * cache.block if self.longest is None else self.longest
+        last = self._last
+        if last[0] != longest:
+            last = self._last = (longest, _SeqsArg(*self._fields, longest))
+        return last[1]
 
 
 _MOVED = (torch.bfloat16, torch.float16, torch.float32)
@@ -216,7 +219,8 @@ def _word(status, cache):
 
 def workspace_size(op: int, cache: Cache, seqs: Seqs, *, q_heads: int, keep: int = 0) -> int:
     """mp_kv_workspace_size: bytes of workspace of attend (`keep` 0 without blocks) or select."""
-    return int(load_library().mp_kv_workspace_size(op, cache._ref, seqs._for(cache), q_heads, keep))
+    held = seqs._for(cache)
+    return int(load_library().mp_kv_workspace_size(op, cache._ref, ctypes.addressof(held), q_heads, keep))
 
 
 def workspace(op: int, cache: Cache, seqs: Seqs, *, q_heads: int, keep: int = 0):
@@ -235,7 +239,8 @@ def write(cache: Cache, seqs: Seqs, k, v, *, status=None, check: bool = True, st
     shape = (seqs.tokens, cache.heads, cache.dim)
     ka, va = _rows(k, "k", shape, _MOVED, cache.device), _rows(v, "v", shape, _MOVED, cache.device)
     status = _word(status, cache)
-    rc = L.mp_kv_write(cache._ref, seqs._for(cache), ctypes.addressof(ka), ctypes.addressof(va),
+    held = seqs._for(cache)
+    rc = L.mp_kv_write(cache._ref, ctypes.addressof(held), ctypes.addressof(ka), ctypes.addressof(va),
                        status.data_ptr(), _stream(cache.device))
     _finish(rc, status, "kv.write", check)
 
@@ -253,7 +258,8 @@ def read(cache: Cache, seqs: Seqs, *, dtype=torch.bfloat16, out=None, status=Non
     k, v = out
     ka, va = _rows(k, "k", shape, _MOVED, cache.device), _rows(v, "v", shape, _MOVED, cache.device)
     status = _word(status, cache)
-    rc = L.mp_kv_read(cache._ref, seqs._for(cache), ctypes.addressof(ka), ctypes.addressof(va),
+    held = seqs._for(cache)
+    rc = L.mp_kv_read(cache._ref, ctypes.addressof(held), ctypes.addressof(ka), ctypes.addressof(va),
                       status.data_ptr(), _stream(cache.device))
     _finish(rc, status, "kv.read", check)
     return k, v
@@ -303,7 +309,8 @@ def attend(cache: Cache, seqs: Seqs, q, *, scale: float | None = None, blocks=No
             raise ValueError("lse must be contiguous and on the device of the cache")
     space, have, _held = _space(OP_ATTEND, cache, seqs, heads, keep, workspace)
     status = _word(status, cache)
-    rc = L.mp_kv_attend(cache._ref, seqs._for(cache), ctypes.addressof(qa), heads,
+    held = seqs._for(cache)
+    rc = L.mp_kv_attend(cache._ref, ctypes.addressof(held), ctypes.addressof(qa), heads,
                         cache.dim ** -0.5 if scale is None else scale, named, keep,
                         ctypes.addressof(oa), lse.data_ptr() if lse is not None else None,
                         space, have, status.data_ptr(), _stream(cache.device))
@@ -334,7 +341,8 @@ def select(cache: Cache, seqs: Seqs, q, *, keep: int, first: int = 1, recent: in
         raise ValueError("out must be contiguous and on the device of the cache")
     space, have, _held = _space(OP_SELECT, cache, seqs, heads, keep, workspace)
     status = _word(status, cache)
-    rc = L.mp_kv_select(cache._ref, seqs._for(cache), ctypes.addressof(qa), heads, keep, first, recent,
+    held = seqs._for(cache)
+    rc = L.mp_kv_select(cache._ref, ctypes.addressof(held), ctypes.addressof(qa), heads, keep, first, recent,
                         out.data_ptr() or None, space, have, status.data_ptr(),
                         _stream(cache.device))
     _finish(rc, status, "kv.select", check)
