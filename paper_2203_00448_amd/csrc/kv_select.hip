@@ -18,6 +18,7 @@ namespace mp {
 namespace {
 
 typedef int int4_t __attribute__((ext_vector_type(4)));
+typedef int4_t mean4_t __attribute__((aligned(8)));  // as the means are: 8 bytes
 
 constexpr int kMostTokens = 8;        // of a workgroup
 constexpr int kLdsScores = 16 * 1024;  // scores that a workgroup holds in LDS
@@ -224,7 +225,7 @@ __global__ __launch_bounds__(THREADS) void kv_select_kernel(KvSelect k) {
                 const int64_t at = (int64_t)page * heads + head;
 #pragma unroll
                 for (int c = 0; c < DC; ++c)
-                    mean[z][c] = *reinterpret_cast<const int4_t*>(a.c.mean_code + at * D + c * 64 + g * 16);
+                    mean[z][c] = *reinterpret_cast<const mean4_t*>(a.c.mean_code + at * D + c * 64 + g * 16);
                 exps[z] = a.c.mean_exp[at];
             }
             if (b0 + kStep < hi) find(b0 + kStep);
