@@ -367,8 +367,8 @@ int32_t mp_plan_breadth_batch(const int64_t* begin, int64_t n_traces, const int3
  *              n_tokens rows belong to sequence s and are its last ones;
  *              begin[0] == 0, begin[n_seqs] == n_tokens.  NULL: one row for
  *              each sequence (n_tokens == n_seqs).
- *   most_new, longest: host bounds on the rows and the tokens of a sequence;
- *              they set the launch.
+ *   most_new, longest: host bounds on the rows and the tokens of a sequence
+ *              (longest at most 2^31 - 4097); they set the launch.
  *   Data errors (MP_EINVAL on the status word): bounds or lengths that
  *   break these, table entries outside [0, n_blocks).  No such error causes
  *   an access outside the arrays.

@@ -10,6 +10,8 @@ int32_t launched(hipError_t e) { return e == hipSuccess ? MP_OK : MP_EDEVICE; }
 
 constexpr int64_t kMaxCount = (int64_t)1 << 30;  // sequences, rows of a call, blocks
 constexpr int32_t kMaxHeads = 1 << 16;
+// Tokens of a sequence: the kernels step through it, and look some steps ahead, in 32 bits.
+constexpr int64_t kMostTokens = INT32_MAX - 4096;
 
 bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
@@ -29,7 +31,7 @@ bool counts_ok(const mp_kv_cache* c, const mp_kv_seqs* s) {
     if (s->table_width < 0 || s->table_width > kMaxCount || s->table_stride < s->table_width)
         return false;
     if (s->n_seqs > 0 && s->table_stride > INT64_MAX / 8 / s->n_seqs) return false;
-    if (s->most_new < 0 || s->longest < 0 || s->longest > INT32_MAX - 64) return false;
+    if (s->most_new < 0 || s->longest < 0 || s->longest > kMostTokens) return false;
     return s->longest <= s->table_width * c->block;
 }
 
