@@ -27,6 +27,12 @@ struct KvArgs {
     int32_t* status;
 };
 
+// Whether a launch of so many workgroups is possible: fewer than 2^32 threads.
+inline bool grid_ok(int64_t workgroups, int threads) { return workgroups <= (((int64_t)1 << 32) - 1) / threads; }
+
+// Workgroups (of 256 threads) of a write or a read.
+int64_t kv_write_groups(const KvArgs& a);
+int64_t kv_read_groups(const KvArgs& a);
 hipError_t launch_kv_write(const KvArgs& a, const KvRows& k, const KvRows& v, hipStream_t st);
 hipError_t launch_kv_read(const KvArgs& a, const KvRows& k, const KvRows& v, hipStream_t st);
 
@@ -67,9 +73,19 @@ struct KvSelect {
     float* scores;  // [token][head][score_stride], or in LDS
     int64_t score_stride;
     int32_t tokens;  // of a workgroup
+    int64_t units;   // groups of so many tokens over all sequences, an upper bound
 };
 
-size_t kv_select_workspace(const mp_kv_cache& c, const mp_kv_seqs& s, int64_t* score_stride);
+// What a call of mp_kv_select launches (kv_select.hip).
+struct KvSelectShape {
+    bool ok;
+    bool global;  // scores in the workspace
+    int32_t tokens;
+    int64_t units, score_stride;
+    size_t workspace;
+};
+
+KvSelectShape kv_select_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t q_heads);
 hipError_t launch_kv_select(const KvSelect& a, hipStream_t st);
 
 // ---- device code

@@ -82,11 +82,6 @@ KvArgs args_of(const mp_kv_cache* c, const mp_kv_seqs* s, int32_t* status) {
     return a;
 }
 
-// Whether a grid of a workgroup for each head of each touched block can be launched.
-bool pieces_ok(const mp_kv_cache* c, const mp_kv_seqs* s) {
-    return (s->n_tokens / c->block + 2 * s->n_seqs) * c->heads < INT32_MAX;
-}
-
 bool heads_ok(const mp_kv_cache* c, int32_t q_heads) {
     return q_heads >= c->heads && q_heads % c->heads == 0 && q_heads <= kMaxHeads;
 }
@@ -94,16 +89,11 @@ bool heads_ok(const mp_kv_cache* c, int32_t q_heads) {
 // Query heads of a key head whose codes fit the scores' LDS.
 constexpr int32_t kMaxSelectGroup = 128;
 
-bool select_ok(const mp_kv_cache* c, const mp_kv_seqs* s, int32_t q_heads) {
-    if (q_heads / c->heads > kMaxSelectGroup) return false;
-    return (s->n_tokens + s->n_seqs) * c->heads < INT32_MAX;
-}
-
 int32_t move_rows(const mp_kv_cache* cache, const mp_kv_seqs* seqs, const mp_kv_rows* k,
                   const mp_kv_rows* v, int32_t* status_out, void* stream, bool write) {
     KvRows kr, vr;
     if (!shape_ok(cache) || !counts_ok(cache, seqs) || !cache_ok(cache) || !seqs_ok(seqs) ||
-        !status_out || !pieces_ok(cache, seqs) ||
+        !status_out ||
         !rows_ok(k, seqs->n_tokens, cache->heads, true, &kr) ||
         !rows_ok(v, seqs->n_tokens, cache->heads, true, &vr))
         return MP_EINVAL;
@@ -111,6 +101,7 @@ int32_t move_rows(const mp_kv_cache* cache, const mp_kv_seqs* seqs, const mp_kv_
                    !rows_apart(v, seqs->n_tokens, cache->heads, cache->dim)))
         return MP_EINVAL;
     const KvArgs a = args_of(cache, seqs, status_out);
+    if (!grid_ok(write ? kv_write_groups(a) : kv_read_groups(a), 256)) return MP_EINVAL;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     return launched(write ? launch_kv_write(a, kr, vr, st) : launch_kv_read(a, kr, vr, st));
 }
@@ -164,14 +155,14 @@ extern "C" int32_t mp_kv_select(const mp_kv_cache* cache, const mp_kv_seqs* seqs
                                 size_t workspace_bytes, int32_t* status_out, void* stream) {
     KvSelect k = {};
     if (!shape_ok(cache) || !counts_ok(cache, seqs) || !cache_ok(cache) || !seqs_ok(seqs) ||
-        !status_out || !heads_ok(cache, q_heads) || !select_ok(cache, seqs, q_heads))
+        !status_out || !heads_ok(cache, q_heads) || q_heads / cache->heads > kMaxSelectGroup)
         return MP_EINVAL;
     if (keep < 1 || keep > kMaxCount / 64 || first < 0 || recent < 1 || first > keep ||
         recent > keep - first || (!blocks_out && seqs->n_tokens > 0))
         return MP_EINVAL;
     if (!rows_ok(q, seqs->n_tokens, q_heads, false, &k.q)) return MP_EINVAL;
-    const size_t need = kv_select_workspace(*cache, *seqs, &k.score_stride);
-    if (workspace_bytes < need || (need > 0 && !workspace) || !aligned(workspace, 16))
+    const KvSelectShape sh = kv_select_shape(*cache, *seqs, q_heads);
+    if (!sh.ok || workspace_bytes < sh.workspace || (sh.workspace > 0 && !workspace) || !aligned(workspace, 16))
         return MP_EINVAL;
     k.a = args_of(cache, seqs, status_out);
     k.group = q_heads / cache->heads;
@@ -180,6 +171,9 @@ extern "C" int32_t mp_kv_select(const mp_kv_cache* cache, const mp_kv_seqs* seqs
     k.recent = (int32_t)recent;
     k.out = blocks_out;
     k.scores = static_cast<float*>(workspace);
+    k.score_stride = sh.score_stride;
+    k.tokens = sh.tokens;
+    k.units = sh.units;
     return launched(launch_kv_select(k, static_cast<hipStream_t>(stream)));
 }
 
@@ -193,8 +187,8 @@ extern "C" size_t mp_kv_workspace_size(int32_t op, const mp_kv_cache* cache,
         return sh.ok ? sh.workspace : 0;
     }
     if (op == MP_OP_KV_SELECT) {
-        int64_t stride;
-        return select_ok(cache, seqs, q_heads) ? kv_select_workspace(*cache, *seqs, &stride) : 0;
+        if (q_heads / cache->heads > kMaxSelectGroup) return 0;
+        return kv_select_shape(*cache, *seqs, q_heads).workspace;
     }
     return 0;
 }

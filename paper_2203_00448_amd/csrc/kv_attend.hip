@@ -1330,7 +1330,7 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     // 165, 100 new - / 189 / 330; 4 of them, 16 new 29 / 30 / 25, 32 new 38 / 31 / 28; 16 of 2048, all
     // new - / 795 / 763; one of 16384, all new - / 2482 / 2150.  A short piece of a short sequence
     // (64 of 16 tokens, all new: 19 / 12 / 21) has little to share between row groups.
-    const int64_t piece = s.most_new * group;
+    const int64_t piece = (s.most_new < s.n_tokens ? s.most_new : s.n_tokens) * group;
     if (keep > 0 || !s.begin || piece <= 16 || (piece <= 64 && s.longest > 512))
         sh.form = KvForm::rows;
     else
@@ -1364,9 +1364,13 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     // a multiple of what the waves of a workgroup take together
     sh.chunk = (chunk + 255) / 256 * 256;
     sh.n_chunks = longest > 0 ? (longest + sh.chunk - 1) / sh.chunk : 1;
-    const int64_t rows = s.n_tokens * q_heads;
-    sh.ok = sh.units * c.heads * sh.n_chunks < INT32_MAX && rows < INT32_MAX;
-    sh.workspace = sh.n_chunks > 1 ? (size_t)rows * sh.n_chunks * (c.dim + 4) * 4 : 0;
+    const int64_t rows = s.n_tokens * q_heads, most = INT32_MAX;
+    // the product of workgroups and chunks may be past 64 bits
+    sh.ok = rows < most && wide < most && (wide == 0 || sh.n_chunks <= most / wide) &&
+            grid_ok(wide * sh.n_chunks, sh.form == KvForm::pair ? 512 : 256);
+    if (sh.ok && sh.n_chunks > 1)
+        sh.ok = sh.n_chunks > 16 ? grid_ok(rows, 256) : grid_ok((rows + 3) / 4, 256);
+    sh.workspace = sh.ok && sh.n_chunks > 1 ? (size_t)rows * sh.n_chunks * (c.dim + 4) * 4 : 0;
     return sh;
 }
 

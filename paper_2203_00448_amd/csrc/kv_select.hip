@@ -286,8 +286,6 @@ int32_t tokens_of(const mp_kv_cache& c, const mp_kv_seqs& s, int64_t stride, boo
 
 template <int D, int THREADS, bool GLOBAL>
 hipError_t launch_form(const KvSelect& k, hipStream_t st) {
-    const mp_kv_seqs& s = k.a.s;
-    const int64_t units = s.begin ? s.n_tokens / k.tokens + s.n_seqs : s.n_seqs;
     constexpr size_t kPicks = THREADS == 1024 ? sizeof(PickLds<THREADS / kWave>) : THREADS / kWave * sizeof(PickLds<1>);
     size_t lds = (size_t)k.tokens * k.group * (D + 16) + ((size_t)k.tokens * k.group + 3) / 4 * 16 + kPicks;
     if (!GLOBAL) lds += (size_t)k.tokens * k.score_stride * sizeof(float);
@@ -296,11 +294,10 @@ hipError_t launch_form(const KvSelect& k, hipStream_t st) {
                                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
             e != hipSuccess)
             return e;
-    kv_select_kernel<D, THREADS, GLOBAL><<<dim3((uint32_t)(units * k.a.c.heads)), THREADS, lds, st>>>(k);
+    kv_select_kernel<D, THREADS, GLOBAL><<<dim3((uint32_t)(k.units * k.a.c.heads)), THREADS, lds, st>>>(k);
     return hipGetLastError();
 }
 
-// Many threads where a workgroup has one token: it is alone with its blocks.
 template <int D>
 hipError_t launch_d(const KvSelect& k, bool global, hipStream_t st) {
     if (global) return launch_form<D, 1024, true>(k, st);
@@ -310,21 +307,25 @@ hipError_t launch_d(const KvSelect& k, bool global, hipStream_t st) {
 
 }  // namespace
 
-// Scores of a token lie in LDS where a workgroup can hold them, else in the workspace.
-size_t kv_select_workspace(const mp_kv_cache& c, const mp_kv_seqs& s, int64_t* score_stride) {
-    const int64_t most = (s.longest + c.block - 1) / c.block;
-    *score_stride = (most + 15) / 16 * 16;
-    if (*score_stride < 16) *score_stride = 16;
-    return *score_stride <= kLdsScores ? 0 : (size_t)s.n_tokens * c.heads * *score_stride * sizeof(float);
+KvSelectShape kv_select_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t q_heads) {
+    KvSelectShape sh = {};
+    const int64_t most = (s.longest + c.block - 1) / c.block, group = q_heads / c.heads;
+    sh.score_stride = most < 16 ? 16 : (most + 15) / 16 * 16;
+    // scores of a token lie in LDS where a workgroup can hold them, else in the workspace
+    sh.global = sh.score_stride > kLdsScores;
+    sh.tokens = tokens_of(c, s, sh.score_stride, sh.global);
+    // query codes of many heads take room too
+    while (sh.tokens > 1 && sh.tokens * group * (c.dim + 20) > 48 * 1024) --sh.tokens;
+    sh.units = s.begin ? s.n_tokens / sh.tokens + s.n_seqs : s.n_seqs;
+    // many threads where a workgroup has one token: it is alone with its blocks
+    sh.ok = grid_ok(sh.units * c.heads, sh.tokens == 1 ? 1024 : 256);
+    if (sh.ok && sh.global) sh.workspace = (size_t)s.n_tokens * c.heads * sh.score_stride * sizeof(float);
+    return sh;
 }
 
-hipError_t launch_kv_select(const KvSelect& a, hipStream_t st) {
-    if (a.a.s.n_tokens == 0) return hipSuccess;
-    KvSelect k = a;
+hipError_t launch_kv_select(const KvSelect& k, hipStream_t st) {
+    if (k.a.s.n_tokens == 0) return hipSuccess;
     const bool global = k.score_stride > kLdsScores;
-    k.tokens = tokens_of(k.a.c, k.a.s, k.score_stride, global);
-    // query codes of many heads take room too
-    while (k.tokens > 1 && (int64_t)k.tokens * k.group * (k.a.c.dim + 20) > 48 * 1024) --k.tokens;
     switch (k.a.c.dim) {
         case 64: return launch_d<64>(k, global, st);
         case 128: return launch_d<128>(k, global, st);

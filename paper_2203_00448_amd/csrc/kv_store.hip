@@ -346,10 +346,23 @@ int64_t pieces(const KvArgs& a) {
     return a.s.begin ? (a.s.n_tokens >> a.log_block) + 2 * a.s.n_seqs : a.s.n_seqs;
 }
 
+// Heads that a workgroup reads: as many as leave 2048 workgroups, which the device holds at once.
+int64_t heads_of(const KvArgs& a) {
+    const int64_t per = pieces(a) * a.c.heads / 2048;
+    return per < 1 ? 1 : per > a.c.heads ? a.c.heads : per > 8 ? 8 : per;
+}
+
 }  // namespace
 
+int64_t kv_write_groups(const KvArgs& a) { return pieces(a) * a.c.heads; }
+
+int64_t kv_read_groups(const KvArgs& a) {
+    const int64_t per = heads_of(a);
+    return pieces(a) * ((a.c.heads + per - 1) / per);
+}
+
 hipError_t launch_kv_write(const KvArgs& a, const KvRows& k, const KvRows& v, hipStream_t st) {
-    const dim3 grid((uint32_t)(pieces(a) * a.c.heads));
+    const dim3 grid((uint32_t)kv_write_groups(a));
     if (grid.x == 0) return hipSuccess;
     const size_t room = (size_t)a.c.dim * ((2 << a.log_block) + 4);
     const bool i8 = a.c.kind == MP_KV_INT8;
@@ -364,12 +377,9 @@ hipError_t launch_kv_write(const KvArgs& a, const KvRows& k, const KvRows& v, hi
 }
 
 hipError_t launch_kv_read(const KvArgs& a, const KvRows& k, const KvRows& v, hipStream_t st) {
-    const int64_t n = pieces(a);
-    if (n == 0) return hipSuccess;
-    // heads of a workgroup: as many as leave 2048 workgroups, which the device holds at once
-    int64_t per = n * a.c.heads / 2048;
-    per = per < 1 ? 1 : per > a.c.heads ? a.c.heads : per > 8 ? 8 : per;
-    const dim3 grid((uint32_t)(n * ((a.c.heads + per - 1) / per)));
+    const dim3 grid((uint32_t)kv_read_groups(a));
+    if (grid.x == 0) return hipSuccess;
+    const int64_t per = heads_of(a);
     const size_t room = (size_t)a.c.dim * ((1 << a.log_block) + 4);
     if (a.c.kind == MP_KV_INT8)
         kv_read_kernel<true><<<grid, 256, room, st>>>(a, k, v, (int32_t)per);
