@@ -45,6 +45,7 @@ struct KvAttendShape {
     int64_t units;     // row groups over all sequences, an upper bound
     int64_t chunk;     // tokens (of the sequence, or of its listed blocks) of a workgroup
     int64_t n_chunks;
+    bool ordered;      // row groups of tiles by what they see
     size_t workspace;
 };
 

@@ -579,8 +579,7 @@ __device__ __forceinline__ int wave_sum(int x) {
 template <int ROWS>
 __device__ __forceinline__ bool tile_group(const KvAttend& k, uint32_t u, RowGroup* g) {
     const KvArgs& a = k.a;
-    if (!a.s.begin || a.s.n_seqs > kWave || k.shape.n_chunks > 1)
-        return row_group(k, k.shape.units - 1 - u, g);
+    if (!k.shape.ordered) return row_group(k, k.shape.units - 1 - u, g);
     const int lane = threadIdx.x & 63;
     KvSeq q = {};
     if (lane < a.s.n_seqs) q = kv_seq(a, lane, a.s.begin[lane], a.s.begin[lane + 1]);
@@ -1371,6 +1370,9 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     if (sh.ok && sh.n_chunks > 1)
         sh.ok = sh.n_chunks > 16 ? grid_ok(rows, 256) : grid_ok((rows + 3) / 4, 256);
     sh.workspace = sh.ok && sh.n_chunks > 1 ? (size_t)rows * sh.n_chunks * (c.dim + 4) * 4 : 0;
+    // a level of a row group (the rows before it over the group's) has 30 bits
+    sh.ordered = sh.form != KvForm::rows && s.begin && s.n_seqs <= 64 && sh.n_chunks == 1 &&
+                 s.longest < ((int64_t)1 << 30) * sh.rows / group;
     return sh;
 }
 

@@ -1,11 +1,20 @@
 // Sanitizer driver for the sizes that the key/value cache's host side computes (test infrastructure):
 // built with its sources by tests/test_kv_limit_sanitizers.py with the host pass under
 // -fsanitize=address,undefined and run without a GPU.  Counts, lengths and bounds up to the ends of
-// what is accepted.
+// what is accepted; and the rule by which row groups are ordered, where a level would leave its bits.
 #include <stdint.h>
 #include <stdio.h>
 
-#include "memoplan.h"
+#include "kv.hpp"
+
+static int failures = 0;
+#define CHECK(c)                                                             \
+    do {                                                                     \
+        if (!(c)) {                                                          \
+            fprintf(stderr, "check failed at line %d: %s\n", __LINE__, #c);  \
+            ++failures;                                                      \
+        }                                                                    \
+    } while (0)
 
 int main() {
     int64_t begin = 0;
@@ -38,6 +47,23 @@ int main() {
                                     (void)mp_kv_workspace_size(MP_OP_KV_SELECT, &c, &s, q_heads, keep);
                                 }
                             }
+    // many long sequences of many query heads, in one chunk
+    mp_kv_cache c = {};
+    c.n_blocks = 16, c.heads = 1, c.dim = 64, c.block = 64;
+    mp_kv_seqs s = {};
+    s.begin = &begin, s.n_seqs = 8, s.n_tokens = 2048, s.most_new = 2048;
+    s.table_width = s.table_stride = 1 << 26;
+    for (int32_t group : {1, 16, 64, 256, 1024}) {
+        for (int64_t longest : {(int64_t)1 << 16, (int64_t)1 << 24, (int64_t)1 << 27, (int64_t)INT32_MAX - 4096}) {
+            s.longest = longest;
+            const mp::KvAttendShape sh = mp::kv_attend_shape(c, s, group, 0);
+            CHECK(sh.ok && sh.form == mp::KvForm::tiles);
+            // its level: the rows before a group, over the group's
+            if (sh.ordered) CHECK((unsigned __int128)longest * group / sh.rows < (1u << 30));
+            if (sh.n_chunks == 1 && longest <= (1 << 24) && group <= 256) CHECK(sh.ordered);
+        }
+    }
+    if (failures) return 1;
     printf("all checks passed\n");
     return 0;
 }
