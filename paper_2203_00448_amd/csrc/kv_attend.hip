@@ -279,8 +279,9 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void
     auto named = [&](int32_t x) -> int32_t {
         const int32_t b = x >> lb;
         const int32_t id = b < k.keep ? list[b] : -1;
-        if (id != -1 && (uint32_t)id > (uint32_t)most >> lb) pages.worst = ~0u;
-        return (uint32_t)id <= (uint32_t)most >> lb && most >= 0 ? id : -1;
+        const bool seen = id >= 0 && id <= most >> lb;  // none where most is -1
+        if (id != -1 && !seen) pages.worst = ~0u;
+        return seen ? id : -1;
     };
     auto find = [&](int32_t x) {
         if (LIST) {
@@ -573,9 +574,10 @@ __device__ __forceinline__ int wave_sum(int x) {
 
 // Row group `u` of a launch of tiles: those that see the most first, so that the last ones to
 // start are short.  A lane has a sequence; group j of a sequence is at level (earlier tokens in
-// groups) + j, and u counts down the levels, sequences in order within one.  With more than 64
-// sequences, or chunks, the last sequences' last groups first.  Prompts of 228-4096 tokens: 273 us, 286
-// without the order; in chunks it gained nothing.
+// groups) + j, and u counts down the levels, sequences in order within one.  Where they are
+// not ordered (more than 64 sequences, chunks, levels past 30 bits), the last sequences' last
+// groups come first.  Prompts of 228-4096 tokens: 273 us, 286 without the order; in chunks it gained
+// nothing.
 template <int ROWS>
 __device__ __forceinline__ bool tile_group(const KvAttend& k, uint32_t u, RowGroup* g) {
     const KvArgs& a = k.a;
