@@ -467,7 +467,8 @@ int32_t mp_kv_attend(const mp_kv_cache* cache, const mp_kv_seqs* seqs, const mp_
  * means.  A query head's code is c = round(q * 2^-e) in -127..127, e = x - 7 with
  * largest |q| = m * 2^x, 1/2 <= m < 1; a block's score is the largest over the
  * key head's query heads of (c . mean_code) * 2^(e + mean_exp): whole products,
- * so scores are exact and ties real.  A row at position p has p / block + 1
+ * so scores are exact and ties real (but for query heads so much smaller than the
+ * key head's largest, 2^e times, that mean_exp - e is below -129).  A row at position p has p / block + 1
  * blocks; all are taken if they are at most `keep`, otherwise the first
  * `first`, the last `recent` (at least 1) and the best-scored of the others,
  * the lowest index among equals.

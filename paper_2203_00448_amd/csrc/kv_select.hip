@@ -1,9 +1,11 @@
 // Blocks of the 8-bit key/value cache selected for each row and key head.
 //
 // The score of a block is a product of 8-bit codes (the query's, made here, and the
-// block's mean, kept by the write), so it is a whole number below 2^23 times powers of
+// block's mean, kept by the write), so it is a whole number below 2^22 times powers of
 // two: exact whatever the order of its sum, and the selection is one of exact numbers,
-// the lowest index among equals.
+// the lowest index among equals.  Only the order of a row's scores counts: they are held 2^(13 + x)
+// times too small, x the largest exponent of the key head's queries, which 32-bit floats hold
+// for keys of any size, the least of them as subnormal ones.
 //
 // One launch: a workgroup takes one key head and a few consecutive tokens of a sequence,
 // reads each block's mean once for all of them and keeps their scores in LDS; then each
@@ -22,6 +24,8 @@ typedef int4_t mean4_t __attribute__((aligned(8)));  // as the means are: 8 byte
 
 constexpr int kMostTokens = 8;        // of a workgroup
 constexpr int kLdsScores = 16 * 1024;  // scores that a workgroup holds in LDS
+constexpr int kNoQuery = -10000;      // the exponent of a query of zeros
+constexpr int kDown = -20;            // of scores below 2^(22 + 124)
 
 // Larger scores to larger keys.
 __device__ __forceinline__ uint32_t key_of(float score) {
@@ -132,7 +136,7 @@ __device__ __forceinline__ void pick(const float* scores, int32_t blocks, int32_
     }
 }
 
-// LDS: query codes [tokens][rows][dim] with rows padded by 16 bytes, their scales, the
+// LDS: query codes [tokens][rows][dim] with rows padded by 16 bytes, their exponents, the
 // histograms of the waves, and the scores unless they are in the workspace (GLOBAL).
 //
 // Scores by matrix instructions of 16 blocks x 16 query heads x 64 dims, the heads of as many
@@ -164,13 +168,16 @@ __global__ __launch_bounds__(THREADS) void kv_select_kernel(KvSelect k) {
     };
     const int32_t most = blocks_of(count - 1);
     int8_t* const codes = reinterpret_cast<int8_t*>(lds_raw);
-    float* const scales = reinterpret_cast<float*>(codes + (size_t)k.tokens * k.group * ROW);
-    PickLds<kTeam>* const picks = reinterpret_cast<PickLds<kTeam>*>(scales + (k.tokens * k.group + 3) / 4 * 4);
+    int* const q_exps = reinterpret_cast<int*>(codes + (size_t)k.tokens * k.group * ROW);
+    PickLds<kTeam>* const picks = reinterpret_cast<PickLds<kTeam>*>(q_exps + (k.tokens * k.group + 3) / 4 * 4);
+    __shared__ int tops[kMostTokens];  // the largest of a token's
     float* const scores = GLOBAL ? k.scores + ((q.begin + i0) * heads + head) * k.score_stride
                                  : reinterpret_cast<float*>(picks + THREADS / kWave / kTeam);
     const int64_t step = GLOBAL ? heads * k.score_stride : k.score_stride;  // to the next token's
 
     if (most > k.keep) {
+        if (tid < count) tops[tid] = kNoQuery;
+        __syncthreads();
         // query codes, eight dims a lane
         const int rows = count * k.group, row_in = tid / PER_ROW, d = tid % PER_ROW * 8;
         for (int r0 = 0; r0 < rows; r0 += THREADS / PER_ROW) {
@@ -184,18 +191,19 @@ __global__ __launch_bounds__(THREADS) void kv_select_kernel(KvSelect k) {
             }
 #pragma unroll
             for (int o = PER_ROW / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
-            uint32_t frac;
-            const int e = max(-100, exponent_of(top, &frac));
-            const float f = pow2f(7 - e);
+            const int e = top > 0.0f ? __builtin_amdgcn_frexp_expf(top) : kNoQuery;
             uint32_t w[2] = {0, 0};
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float y = x[i] * f;
+                const float y = __builtin_amdgcn_ldexpf(x[i], 7 - e);
                 const float c = y != y ? 0.0f : fminf(127.0f, fmaxf(-127.0f, __builtin_rintf(y)));
                 w[i / 4] |= ((uint32_t)(int)c & 0xffu) << (8 * (i % 4));
             }
             *reinterpret_cast<uint2*>(codes + r * ROW + d) = make_uint2(w[0], w[1]);
-            if (d == 0) scales[r] = pow2f(max(-126, e - 7));
+            if (d == 0) {
+                q_exps[r] = e;
+                atomicMax(&tops[r / k.group], e);
+            }
         }
         __syncthreads();
         const int32_t lo = k.first, hi = most - k.recent;  // the blocks that some token has scored
@@ -231,11 +239,10 @@ __global__ __launch_bounds__(THREADS) void kv_select_kernel(KvSelect k) {
             if (b0 + kStep < hi) find(b0 + kStep);
 #pragma unroll
             for (int z = 0; z < 4; ++z) {
-                const float unit = pow2f(max(-126, exps[z]));
                 // of the four blocks whose products this lane gets
-                float units[4];
+                int units[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) units[r] = __shfl(unit, g * 4 + r, kWave);
+                for (int r = 0; r < 4; ++r) units[r] = __shfl(exps[z], g * 4 + r, kWave) + kDown;
                 const int32_t b = b0 + z * 16;
                 if (b >= hi) break;
                 for (int t0 = 0; t0 < count; t0 += 16 / span) {
@@ -250,12 +257,12 @@ __global__ __launch_bounds__(THREADS) void kv_select_kernel(KvSelect k) {
                             dot = __builtin_amdgcn_mfma_i32_16x16x64_i8(
                                 mean[z][c],
                                 *reinterpret_cast<const int4_t*>(codes + r * ROW + c * 64 + g * 16), dot, 0, 0, 0);
-                        const float f = scales[r];
+                        const float f = pow2f(max(-126, q_exps[r] - tops[min(t, count - 1)]));
 #pragma unroll
                         for (int i = 0; i < 4; ++i) best[i] = fmaxf(best[i], (float)dot[i] * f);
                     }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) best[i] = span_max(best[i], span) * units[i];
+                    for (int i = 0; i < 4; ++i) best[i] = __builtin_amdgcn_ldexpf(span_max(best[i], span), units[i]);
                     if (n % span == 0 && t < count)
                         *reinterpret_cast<float4_t*>(scores + t * step + b + g * 4) = best;
                 }
