@@ -98,7 +98,7 @@ class Cache:
                 raise ValueError("a cache's tensors must be contiguous and on one device")
         self.k_code, self.v_code, self.k_exp, self.v_exp, self.mean_code, self.mean_exp = self.tensors
         self.n_blocks, self.heads, self.block, self.dim, self.kind = n, h, t, d, kind
-        self.device = k_code.device
+        self.device, self.index = k_code.device, k_code.get_device()
         self._arg = _CacheArg(*(x.data_ptr() for x in self.tensors), n, h, d, t, kind)
         self._ref = ctypes.addressof(self._arg)
 
@@ -175,12 +175,12 @@ _MOVED = (torch.bfloat16, torch.float16, torch.float32)
 _QUERIES = (torch.bfloat16, torch.float16)
 
 
-def _rows(t, name, shape, dtypes, device):
+def _rows(t, name, shape, dtypes, index):
     """A tensor's rows as an argument.  These calls are short beside what a launch costs, so their
     checks look at each property once."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtypes or t.shape != shape:
         _need(t, dtypes, name, shape)
-    if t.get_device() != device.index:
+    if t.get_device() != index:
         raise ValueError(f"{name} must be on the device of the cache")
     strides = t.stride()
     if strides[2] != 1:
@@ -188,13 +188,7 @@ def _rows(t, name, shape, dtypes, device):
     return _RowsArg(t.data_ptr(), strides[0], strides[1], DTYPES[t.dtype])
 
 
-def _stream(device):
-    return torch._C._cuda_getCurrentRawStream(device.index)
-
-
-def _elsewhere(cache):
-    """Whether another device than the cache's is current: a launch would be that one's."""
-    return torch._C._cuda_getDevice() != cache.device.index
+_stream, _device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
 @contextlib.contextmanager
@@ -212,7 +206,7 @@ def _word(status, cache):
         return new_status(cache.device)
     if not status.is_cuda or status.dtype is not torch.int32:
         _need(status, (torch.int32,), "status")
-    if status.numel() != 1 or status.get_device() != cache.device.index:
+    if status.numel() != 1 or status.get_device() != cache.index:
         raise ValueError("status must be one word on the device of the cache")
     return status
 
@@ -232,23 +226,23 @@ def workspace(op: int, cache: Cache, seqs: Seqs, *, q_heads: int, keep: int = 0)
 def write(cache: Cache, seqs: Seqs, k, v, *, status=None, check: bool = True, stream=None):
     """Store the call's keys and values (mp_kv_write): k, v [tokens, heads, dim] in bfloat16,
     float16 or float32, any strides over a contiguous last dimension."""
-    if stream is not None or _elsewhere(cache):
+    if stream is not None or _device() != cache.index:  # a launch would be the current device's
         with _current(cache, stream):
             return write(cache, seqs, k, v, status=status, check=check)
     L = load_library()
     shape = (seqs.tokens, cache.heads, cache.dim)
-    ka, va = _rows(k, "k", shape, _MOVED, cache.device), _rows(v, "v", shape, _MOVED, cache.device)
+    ka, va = _rows(k, "k", shape, _MOVED, cache.index), _rows(v, "v", shape, _MOVED, cache.index)
     status = _word(status, cache)
     held = seqs._for(cache)
     rc = L.mp_kv_write(cache._ref, ctypes.addressof(held), ctypes.addressof(ka), ctypes.addressof(va),
-                       status.data_ptr(), _stream(cache.device))
+                       status.data_ptr(), _stream(cache.index))
     _finish(rc, status, "kv.write", check)
 
 
 def read(cache: Cache, seqs: Seqs, *, dtype=torch.bfloat16, out=None, status=None,
          check: bool = True, stream=None):
     """Read back the call's tokens (mp_kv_read): (k, v) [tokens, heads, dim]."""
-    if stream is not None or _elsewhere(cache):
+    if stream is not None or _device() != cache.index:  # a launch would be the current device's
         with _current(cache, stream):
             return read(cache, seqs, dtype=dtype, out=out, status=status, check=check)
     L = load_library()
@@ -256,11 +250,11 @@ def read(cache: Cache, seqs: Seqs, *, dtype=torch.bfloat16, out=None, status=Non
     if out is None:
         out = tuple(torch.empty(shape, dtype=dtype, device=cache.device) for _ in range(2))
     k, v = out
-    ka, va = _rows(k, "k", shape, _MOVED, cache.device), _rows(v, "v", shape, _MOVED, cache.device)
+    ka, va = _rows(k, "k", shape, _MOVED, cache.index), _rows(v, "v", shape, _MOVED, cache.index)
     status = _word(status, cache)
     held = seqs._for(cache)
     rc = L.mp_kv_read(cache._ref, ctypes.addressof(held), ctypes.addressof(ka), ctypes.addressof(va),
-                      status.data_ptr(), _stream(cache.device))
+                      status.data_ptr(), _stream(cache.index))
     _finish(rc, status, "kv.read", check)
     return k, v
 
@@ -270,7 +264,7 @@ def _space(op, cache, seqs, q_heads, keep, workspace):
         workspace = globals()["workspace"](op, cache, seqs, q_heads=q_heads, keep=keep)
     elif not workspace.is_cuda:
         raise TypeError("workspace must be a CUDA (HIP) tensor")
-    elif not workspace.is_contiguous() or workspace.get_device() != cache.device.index:
+    elif not workspace.is_contiguous() or workspace.get_device() != cache.index:
         raise ValueError("workspace must be contiguous and on the device of the cache")
     return workspace.data_ptr(), workspace.nbytes, workspace
 
@@ -282,7 +276,7 @@ def attend(cache: Cache, seqs: Seqs, q, *, scale: float | None = None, blocks=No
     dim ** -0.5.  `blocks` int32 [tokens, heads, keep] limits each row to these of its
     sequence's blocks.  `lse` float32 [tokens, q_heads], if given, gets the logarithms of the
     sums.  Returns out."""
-    if stream is not None or _elsewhere(cache):
+    if stream is not None or _device() != cache.index:  # a launch would be the current device's
         with _current(cache, stream):
             return attend(cache, seqs, q, scale=scale, blocks=blocks, out=out, lse=lse, status=status,
                           workspace=workspace, check=check)
@@ -291,21 +285,21 @@ def attend(cache: Cache, seqs: Seqs, q, *, scale: float | None = None, blocks=No
         raise ValueError("q must be [tokens, q_heads, dim]")
     heads = q.shape[1]
     rows = (seqs.tokens, heads, cache.dim)
-    qa = _rows(q, "q", rows, _QUERIES, cache.device)
+    qa = _rows(q, "q", rows, _QUERIES, cache.index)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    oa = _rows(out, "out", rows, (q.dtype,), cache.device)
+    oa = _rows(out, "out", rows, (q.dtype,), cache.index)
     keep, named = 0, None
     if blocks is not None:
         _need(blocks, (torch.int32,), "blocks")
         if blocks.dim() != 3 or blocks.shape[:2] != (seqs.tokens, cache.heads) or not blocks.is_contiguous():
             raise ValueError("blocks must be a contiguous [tokens, heads, keep]")
-        if blocks.shape[2] < 1 or blocks.get_device() != cache.device.index:
+        if blocks.shape[2] < 1 or blocks.get_device() != cache.index:
             raise ValueError("blocks must name at least one place and be on the device of the cache")
         keep, named = blocks.shape[2], blocks.data_ptr()
     if lse is not None:
         _need(lse, (torch.float32,), "lse", (seqs.tokens, heads))
-        if not lse.is_contiguous() or lse.get_device() != cache.device.index:
+        if not lse.is_contiguous() or lse.get_device() != cache.index:
             raise ValueError("lse must be contiguous and on the device of the cache")
     space, have, _held = _space(OP_ATTEND, cache, seqs, heads, keep, workspace)
     status = _word(status, cache)
@@ -313,7 +307,7 @@ def attend(cache: Cache, seqs: Seqs, q, *, scale: float | None = None, blocks=No
     rc = L.mp_kv_attend(cache._ref, ctypes.addressof(held), ctypes.addressof(qa), heads,
                         cache.dim ** -0.5 if scale is None else scale, named, keep,
                         ctypes.addressof(oa), lse.data_ptr() if lse is not None else None,
-                        space, have, status.data_ptr(), _stream(cache.device))
+                        space, have, status.data_ptr(), _stream(cache.index))
     _finish(rc, status, "kv.attend", check)
     return out
 
@@ -323,7 +317,7 @@ def select(cache: Cache, seqs: Seqs, q, *, keep: int, first: int = 1, recent: in
     """The blocks of each row and key head that attend is to read (mp_kv_select): the first
     `first`, the last `recent` and the best-scored others, `keep` in all, int32 [tokens, heads,
     keep], ascending, -1 beyond the last."""
-    if stream is not None or _elsewhere(cache):
+    if stream is not None or _device() != cache.index:  # a launch would be the current device's
         with _current(cache, stream):
             return select(cache, seqs, q, keep=keep, first=first, recent=recent, out=out, status=status,
                           workspace=workspace, check=check)
@@ -332,18 +326,18 @@ def select(cache: Cache, seqs: Seqs, q, *, keep: int, first: int = 1, recent: in
         raise ValueError("q must be [tokens, q_heads, dim]")
     heads = q.shape[1]
     rows = (seqs.tokens, heads, cache.dim)
-    qa = _rows(q, "q", rows, _QUERIES, cache.device)
+    qa = _rows(q, "q", rows, _QUERIES, cache.index)
     shape = (seqs.tokens, cache.heads, int(keep))
     if out is None:
         out = torch.empty(shape, dtype=torch.int32, device=q.device)
     _need(out, (torch.int32,), "out", shape)
-    if not out.is_contiguous() or out.get_device() != cache.device.index:
+    if not out.is_contiguous() or out.get_device() != cache.index:
         raise ValueError("out must be contiguous and on the device of the cache")
     space, have, _held = _space(OP_SELECT, cache, seqs, heads, keep, workspace)
     status = _word(status, cache)
     held = seqs._for(cache)
     rc = L.mp_kv_select(cache._ref, ctypes.addressof(held), ctypes.addressof(qa), heads, keep, first, recent,
                         out.data_ptr() or None, space, have, status.data_ptr(),
-                        _stream(cache.device))
+                        _stream(cache.index))
     _finish(rc, status, "kv.select", check)
     return out

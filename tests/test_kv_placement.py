@@ -46,10 +46,11 @@ def placed(monkeypatch):
         yield
 
     state = types.SimpleNamespace(now=0)
-    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: state.now, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: state.now)
+    monkeypatch.setattr(kv, "_device", lambda: state.now)
     monkeypatch.setattr(torch.cuda, "device", device)
     monkeypatch.setattr(torch.cuda, "stream", stream)
-    cache = types.SimpleNamespace(device=torch.device("cuda", 1), heads=1, dim=64)
+    cache = types.SimpleNamespace(device=torch.device("cuda", 1), index=1, heads=1, dim=64)
     return kv, cache, made, state
 
 
