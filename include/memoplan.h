@@ -429,7 +429,8 @@ typedef struct {
  * round(s * 2^-e), mean_exp = k_exp + e - log2(block).
  * A value that is not finite is a data error (MP_EINVAL on the status word);
  * infinities are then held as the largest value and NaN as zero, so that the
- * cache stays finite.  Sequences whose written blocks coincide race. */
+ * cache stays finite.  (Values beyond the largest scale, from 2^127 on with int8, are
+ * held as the largest value too, and are no error.)  Sequences whose written blocks coincide race. */
 int32_t mp_kv_write(const mp_kv_cache* cache, const mp_kv_seqs* seqs, const mp_kv_rows* k,
                     const mp_kv_rows* v, int32_t* status_out, void* stream);
 

@@ -23,7 +23,7 @@ PHASE_LIB_PATH = os.path.join(PKG, "libmemoplan_phase.so")
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",
     "-Wall", "-Wno-unused-function",
-    # packed-FP32 instructions stay off (no floating point here anyway)
+    # packed-FP32 instructions stay off: the key/value cache's kernels, which compute in 32-bit floats, use none
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
 

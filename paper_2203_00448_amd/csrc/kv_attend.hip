@@ -230,9 +230,12 @@ struct FirstCodes {
 // quarter g then has the scores of tokens [16 g, 16 g + 16), four from each tile, which
 // are the columns of 16 bytes of each row of values.
 //
-// What bounds it is memory where there are many workgroups: 64 sequences of 1-16384 tokens 150 us,
-// 5.0 TB/s, two of 131072 101 us, 5.3 TB/s (a large copy: 5.1); one of 1000 tokens 10 us, a chain of
-// dependent loads (length, table, codes) and 16 steps.
+// What bounds it is memory where there are many workgroups: 64 sequences of 1-16384 tokens 151 us,
+// 5.0 TB/s, two of 131072 103 us, 5.2 TB/s (a large copy: 5.2); one of 1000 tokens 11 us, a chain of
+// dependent loads (length, table, codes) and 16 steps.  Heads of 256 likewise, with one wave a SIMD: 64
+// sequences of 8192 tokens 400 us, 5.4 TB/s (heads of 128: 195 us, 5.5); with 4 new tokens each of
+// 4096 305 us, 3.5 TB/s, where a step's 16 columns are all rows and its products show (138 us, 3.9).
+// Three waves a SIMD have 168 registers: heads of 128 spill up to three of them.
 //
 // LIST: one token, and the blocks listed for it.
 template <int D, bool INT8, bool LIST, int WAVES>
@@ -660,8 +663,11 @@ __device__ __forceinline__ void weight_shifts(const Met& met, int vr, const int 
 // converted into the other and the loads of the one after are on their way, so a tile
 // costs one barrier.
 //
-// Measured, 333 rows of heads of 64 after 20000 tokens: 117 us with the join, 460 TFLOP/s.  Of a
+// Measured, 333 rows of heads of 64 after 20000 tokens: 117 us with the join, 466 TFLOP/s.  Of a
 // tile's work per wave the softmax's vector instructions take twice the cycles of its 16 products.
+// Four prompts of 4096 tokens, 32 query heads over 8: heads of 64 369 us, 745 TFLOP/s; of 256 1817 us,
+// 605 TFLOP/s, by one wave a SIMD beside whose softmax nothing runs.  With value exponents apart
+// (2^15): 403 and 2103 us, the row's largest product of weight and scale being looked for.
 //
 // Keys lie by row of the instruction: row m of 32 is token m with bits 2 and 3 exchanged,
 // so that a lane's scores are those of eight consecutive tokens, as the second product
@@ -898,7 +904,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv_tiles_kernel(KvAtten
 // and team 1 in turn 2 i + 1, keys i are read in these two turns and values i in the next two:
 // each is whole the turn before, and two tiles' room is enough for both.
 //
-// Measured, prompts of 228-4096 tokens, 32 query heads over 8: 279 us, 830 TFLOP/s.  A turn takes 1850
+// Measured, prompts of 228-4096 tokens, 32 query heads over 8: 276 us, 838 TFLOP/s; four of 4096 tokens
+// 575 us, 956 TFLOP/s (620 with value exponents apart).  A turn takes 1850
 // cycles: 1510 of products (1024 of matrix instructions; reading their factors takes the LDS as
 // long, as each serves one instruction) beside a softmax of 830, the rest barriers.
 //
@@ -1326,11 +1333,21 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
                               int64_t keep) {
     KvAttendShape sh = {};
     const int64_t group = q_heads / c.heads;
-    // The form by the rows of the longest piece.  Measured, us (rows / tiles / pair), query heads
-    // 4 a key head, dim 128: 64 sequences of 1-5000 tokens, 5 new 57 / 134 / 150, 8 new - / 139 /
-    // 165, 100 new - / 189 / 330; 4 of them, 16 new 29 / 30 / 25, 32 new 38 / 31 / 28; 16 of 2048, all
-    // new - / 795 / 763; one of 16384, all new - / 2482 / 2150.  A short piece of a short sequence
-    // (64 of 16 tokens, all new: 19 / 12 / 21) has little to share between row groups.
+    // The form by the rows of the longest piece (new tokens times query heads a key head).  Rows against
+    // tiles, us, query heads 4 a key head, dim 128: 64 sequences of 1-5000 tokens, 5 new 57 / 134; 4
+    // of them, 16 new 29 / 30, 32 new 38 / 31.  A short piece of a short sequence (64 of 16 tokens,
+    // all new: 19 / 12) has little to share between row groups.
+    // Tiles against pairs, us, 8 key heads, new tokens of each sequence of 2048 (or 8192) tokens:
+    //             512 new      1024 new     2048 new     2048 of 8192
+    //   1 seq.    46 / 44      79 / 75      107 / 131    339 / 298
+    //   4         125 / 143    132 / 211    183 / 168    1063 / 870
+    //   16        302 / 269    522 / 458    745 / 672    4424 / 3539
+    //   64        1284 / 1112  2222 / 1933  3156 / 2824
+    // So a pair's workgroup, alone on its compute unit, wins by 10-20% where there are many of them and
+    // loses where about one or two a compute unit are left to end alone (256 and 512 workgroups: the two
+    // entries at which this rule, 4096 rows, picks the slower form).  Shorter pieces gain by pairs only with
+    // over 1000 workgroups of long sequences (16 of 8192 tokens, 100 new: 387 / 352), and lose otherwise
+    // (64 of 2048, 32 new: 98 / 167; of 512, all new: 310 / 361).
     const int64_t piece = (s.most_new < s.n_tokens ? s.most_new : s.n_tokens) * group;
     if (keep > 0 || !s.begin || piece <= 16 || (piece <= 64 && s.longest > 512))
         sh.form = KvForm::rows;

@@ -11,7 +11,7 @@
 // reads each block's mean once for all of them and keeps their scores in LDS; then each
 // wave selects for one token after the other.  Bytes read are a 1 / (2 block) part of the
 // cache's; what bounds a call of few tokens is the chain of dependent steps.  16 sequences of up to
-// 1024 blocks, one token each, 8 heads: 15 us, of it query codes 2, scores 7, selection 5; 353 tokens of
+// 1024 blocks, one token each, 8 heads: 16 us, of it query codes 2, scores 7, selection 5; 353 tokens of
 // up to 386 blocks, 4 heads: 18 us.
 #include "kv.hpp"
 
