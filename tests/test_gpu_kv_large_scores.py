@@ -36,12 +36,12 @@ def definition(s, q, scale):
     return w @ v, w @ np.abs(v), (place + 1) * largest
 
 
-def check(out, want, part):
+def check(out, want, part, step=2.0 ** -40):
     """`part`: how far a weight may be off by its score's roundings.  The others: its own to 11 bits
-    and in steps of 2^-40 of the largest, the sums', the result's."""
+    and in steps of `step` of the largest, the sums', the result's."""
     ref, mass, largest = want
     bound = HALF_STEP[torch.bfloat16] * np.abs(ref) + (2.0 ** -11 + 2.0 ** -20 + 2.1 * part) * mass * 1.01
-    bound += 2.0 ** -40 * largest[:, None] + LEAST_STEP[torch.bfloat16]
+    bound += step * largest[:, None] + LEAST_STEP[torch.bfloat16]
     off = np.abs(host(out.double()) - ref[:, None])
     assert np.all(off <= bound[:, None]), np.nanmax(off / bound[:, None])
 
@@ -104,3 +104,17 @@ def test_equal_huge_scores(kind, new, dim, block, lower):
         for part in (1.0, 1.2421875, -1.0, -1.2421875):
             out, want = attended(s, new, part * 2.0 ** power / 64, 0.0, SCALE)
             check(out, want, 0.0)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("new,dim,block", FORMS)
+def test_huge_scores_of_values_apart(kind, new, dim, block):
+    """The same with sizes too far apart to share one exponent: weights end in steps of 2^-29 of what the
+    largest contribution may be."""
+    token = torch.arange(LENGTH)
+    first = torch.where(token // block % 3 == 1, 32.0, 64.0)
+    s = filled(kind, dim, block, first, 0.0, 2.0 ** (-9.0 * (token // block % 4)))
+    for power in (12, 18, 24, 25, 28, 40):
+        for part in (1.2421875, -1.2421875):
+            out, want = attended(s, new, part * 2.0 ** power / 64, 0.0, SCALE)
+            check(out, want, 2.0 ** (2 * 2.0 ** (power - 24) + 2.0 ** -16) - 1 if power < 21 else 0.0, 2.0 ** -29)
