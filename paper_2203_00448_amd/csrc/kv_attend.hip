@@ -12,10 +12,10 @@
 // of a block's keys multiplies its scores.  That of its values joins the exponent of the
 // weights, which enter the second product as w = 2^(c s_j - m + ve_j - vr + 15).  While the value
 // exponents that a wave has met differ by no more than 10, vr is the largest of them; from then on
-// m + vr follows the largest c s_j + ve_j of the row.  Either way no w is above 2^15, and the row's
-// largest contribution has one of 2^4 at least, normal down to 2^-14: a weight has its 11 bits down to
-// 2^-18 of that, and steps of 2^-28 of it below, whatever the sizes of other blocks.  The sum of weights
-// takes 2^(c s_j - m) back from w in 32 bits.
+// m + vr follows the largest c s_j + ve_j of the row.  Either way no w reaches 2^16 (m may lag behind
+// by less than one), and the row's largest contribution has one of 2^4 at least, normal down to 2^-14:
+// a weight has its 11 bits down to 2^-18 of that, and steps of 2^-28 of it below, whatever the sizes
+// of other blocks.  The sum of weights takes 2^(c s_j - m) back from w in 32 bits.
 //
 // Both products are taken transposed, S^T = K Q^T and O^T = V^T W^T: the weights then
 // come out of the first product in the lanes that the second one wants them in, as long
@@ -378,8 +378,8 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void
         top = fmaxf(top, __shfl_xor(top, 32, kWave));
         // places that name no block have no exponent
         const int was = met.hi;
-        const auto meet = [&](int l) {
-            if (!LIST || __builtin_amdgcn_readlane(pos, l) != kNowhere) met.add(__builtin_amdgcn_readlane(ve, l));
+        const auto meet = [&](int of) {
+            if (!LIST || __builtin_amdgcn_readlane(pos, of) != kNowhere) met.add(__builtin_amdgcn_readlane(ve, of));
         };
         meet(0);
         if (lb < 6) meet(16), meet(32), meet(48);
