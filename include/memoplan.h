@@ -381,6 +381,17 @@ int32_t mp_plan_breadth_batch(const int64_t* begin, int64_t n_traces, const int3
  *   writes, one axis lies within a step of the other, or it is refused. */
 #define MP_KV_E4M3 0
 #define MP_KV_INT8 1
+/* Kind MP_KV_E2M1, 4 bits: a sign, two exponent bits and one fraction bit (0, 0.5,
+ * 1, 1.5, 2, 3, 4, 6).  Each 32 dims of a token and head share one scale, so that
+ * no token's codes depend on another's.
+ *   k_code, v_code [n_blocks][heads][block][dim / 2] bytes, 16-byte aligned;
+ *              dims 2 i and 2 i + 1 in the low and the high half of byte i
+ *   k_exp, v_exp [n_blocks][heads][dim / 32][block] bytes (unsigned), 16-byte
+ *              aligned: a value is code * 2^(exp - 127); those of tokens that a
+ *              sequence holds lie in 27..247
+ *   mean_code, mean_exp: NULL.  There are no means, so mp_kv_select and the
+ *              block lists of mp_kv_attend refuse this kind. */
+#define MP_KV_E2M1 4
 #define MP_BF16 0
 #define MP_F16 1
 #define MP_F32 2
@@ -430,7 +441,10 @@ typedef struct {
  * A value that is not finite is a data error (MP_EINVAL on the status word);
  * infinities are then held as the largest value and NaN as zero, so that the
  * cache stays finite.  (Values beyond the largest scale, from 2^127 on with int8, are
- * held as the largest value too, and are no error.)  Sequences whose written blocks coincide race. */
+ * held as the largest value too, and are no error.)  Sequences whose written blocks coincide race.
+ * Kind MP_KV_E2M1: for each token, head and 32 dims the exponent is the least e in [-100, 120]
+ * with largest |value| <= 7 * 2^e: 6, the largest code, and half of the step that ends there.
+ * Larger scaled values are held as 6; the rest as above. */
 int32_t mp_kv_write(const mp_kv_cache* cache, const mp_kv_seqs* seqs, const mp_kv_rows* k,
                     const mp_kv_rows* v, int32_t* status_out, void* stream);
 
@@ -488,6 +502,77 @@ int32_t mp_kv_select(const mp_kv_cache* cache, const mp_kv_seqs* seqs, const mp_
 #define MP_OP_KV_SELECT 2
 size_t mp_kv_workspace_size(int32_t op, const mp_kv_cache* cache, const mp_kv_seqs* seqs,
                             int32_t q_heads, int64_t keep);
+
+/* ---- Blocks for requests -----------------------------------------------------
+ *
+ * The tables, lengths, row bounds and positions of the cache's calls, kept on the
+ * device: nothing of a step waits for the host.
+ *
+ * A pool of blocks: ids[n_ids] int32, of which ids[0 .. *used) are taken (their
+ * order there means nothing) and the others free, given out in order.  `used_out`
+ * may be `used`, `length_out` may be `length`; other outputs share no memory with
+ * any argument.  `block` is 16, 32 or 64; table_stride, table_width and table as
+ * in mp_kv_seqs.
+ *   workspace: mp_kv_pages_workspace_size(n_seqs) bytes, 16-byte aligned; contents
+ *              need no initialisation.  One call at a time may use it.
+ *
+ * Data errors, on the status word: MP_EINVAL for negative counts, lengths that the
+ * table's rows cannot hold, a pool whose counter is out of range, negative ids;
+ * MP_ENOSPC for more tokens than n_tokens or more blocks than are free.  Where one
+ * is found before blocks are given (all but negative ids), the call changes no
+ * table and no pool, writes length_out = length and used_out = used, and zeros to
+ * begin_out. */
+
+/* Give blocks to sequences that hold length[s] tokens and get more[s] new ones:
+ *   table[s][b] for ceil(length / block) <= b < ceil((length + more) / block): the
+ *              next free ids, sequence by sequence; other entries are left
+ *   length_out[n_seqs] int32: length + more
+ *   begin_out[n_seqs + 1] int64: the sums of more[] before each sequence, the
+ *              `begin` of mp_kv_seqs
+ *   position_out[n_tokens] int32, slot_out[n_tokens] int64, or NULL: for each new
+ *              token, sequence by sequence, its position and its place in the cache,
+ *              table[s][position / block] * block + position % block.  n_tokens is
+ *              what they have room for; what is past the last new token is left. */
+int32_t mp_kv_extend(const int32_t* ids, int64_t n_ids, const int64_t* used, int32_t* table,
+                     int64_t table_stride, int64_t table_width, int32_t block,
+                     const int32_t* length, const int32_t* more, int64_t n_seqs, int64_t n_tokens,
+                     int32_t* length_out, int64_t* used_out, int64_t* begin_out,
+                     int32_t* position_out, int64_t* slot_out, void* workspace,
+                     size_t workspace_bytes, int32_t* status_out, void* stream);
+
+/* Take back all blocks of the sequences with done[s] != 0: their ids, sequence by
+ * sequence, go to ids[*used - freed .. *used); used_out = *used - freed; length_out
+ * is 0 for them and length[s] for the others.  Tables are left. */
+int32_t mp_kv_release(int32_t* ids, int64_t n_ids, const int64_t* used, const int32_t* table,
+                      int64_t table_stride, int64_t table_width, int32_t block,
+                      const int32_t* length, const uint8_t* done, int64_t n_seqs,
+                      int32_t* length_out, int64_t* used_out, void* workspace,
+                      size_t workspace_bytes, int32_t* status_out, void* stream);
+
+/* Workspace bytes of both; 0 for a count that they refuse. */
+size_t mp_kv_pages_workspace_size(int64_t n_seqs);
+
+/* ---- Rotary positions --------------------------------------------------------
+ *
+ * Turn pairs of elements of rows (queries and keys) by angles that grow with the
+ * token's position.  Pair i of the first `turned` (even) elements of a head is
+ * (a, b) = elements (i, i + turned / 2), or with MP_ROTARY_PAIRS elements
+ * (2 i, 2 i + 1); theta = position * freq[i], rounded to 64 bits:
+ *   a' = m (a cos theta - b sin theta),  b' = m (a sin theta + b cos theta)
+ * Sines and cosines are those of the 64-bit angle to about 2^-23, for positions of
+ * any size; products are in 32 bits and rounded once.  The other elements of a head
+ * are copied.  `inverse` turns by -theta: the gradient of the turn (m is kept).
+ *   position[n_tokens] int32; freq[turned / 2] double, device memory
+ *   q, k: rows of q_heads and k_heads heads of `dim` elements (k_heads 0: no k,
+ *              which may then be NULL); q_out, k_out of the same types.  An output
+ *              is its input (the same data and strides) or shares no memory with
+ *              an input or the other output. */
+#define MP_ROTARY_HALVES 0
+#define MP_ROTARY_PAIRS 1
+int32_t mp_rotate(const int32_t* position, int64_t n_tokens, const double* freq, int32_t turned,
+                  int32_t layout, float magnitude, int32_t inverse, int32_t dim,
+                  const mp_kv_rows* q, int32_t q_heads, const mp_kv_rows* q_out,
+                  const mp_kv_rows* k, int32_t k_heads, const mp_kv_rows* k_out, void* stream);
 
 #ifdef __cplusplus
 }

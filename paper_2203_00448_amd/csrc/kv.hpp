@@ -36,6 +36,11 @@ int64_t kv_read_groups(const KvArgs& a);
 hipError_t launch_kv_write(const KvArgs& a, const KvRows& k, const KvRows& v, hipStream_t st);
 hipError_t launch_kv_read(const KvArgs& a, const KvRows& k, const KvRows& v, hipStream_t st);
 
+// The same of a cache in 4 bits (kv4_store.hip).
+int64_t kv4_move_groups(const KvArgs& a);
+hipError_t launch_kv4_write(const KvArgs& a, const KvRows& k, const KvRows& v, hipStream_t st);
+hipError_t launch_kv4_read(const KvArgs& a, const KvRows& k, const KvRows& v, hipStream_t st);
+
 // What a call of mp_kv_attend launches (kv_attend.hip).
 enum class KvForm { rows, tiles, pair };
 struct KvAttendShape {

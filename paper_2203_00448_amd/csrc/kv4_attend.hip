@@ -1,0 +1,643 @@
+// Attention over the 4-bit key/value cache.
+//
+// For a row (a query and one of its heads) with scores s_j = scale * q.k_j,
+//   out = sum_j 2^(c s_j - M) v_j / sum_j 2^(c s_j - M),   c = log2 e, M = max_j c s_j + 24,
+// in one pass over the cache with a running M: when it grows, what was summed so far is multiplied
+// by 2^(M_old - M_new).
+//
+// A code times its group's scale has two significant bits: exact in bfloat16, whose exponents hold every
+// scale.  So both products are matrix instructions on bfloat16 with 32-bit sums, and no scale is
+// left to be followed: sizes that differ between tokens, groups or blocks cost nothing.  Queries are
+// brought to [2^-4, 2^-3) by a power of two per row, and weights lie 24 powers below one, so that no product
+// leaves the range of 32-bit floats.  A 16-bit float query is two bfloat16 pieces, which hold it
+// exactly.  Weights are two pieces (16 bits) where few rows share what is read, and where results are 16-bit
+// floats; one (8 bits, as the results have) in the tiles of bfloat16 rows, whose time is the products'.
+//
+// Both products are taken transposed, S^T = K Q^T and O^T = V^T W^T: the weights come out of the first
+// in the lanes that the second one wants them in.
+#include "kv_attend.hpp"
+
+namespace mp {
+
+namespace {
+
+typedef __bf16 bf2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf8_t __attribute__((ext_vector_type(8)));
+typedef short short4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kStep = 64;           // tokens a wave takes at a time
+constexpr float kBelow = 24.0f;     // of a row's largest weight below one, in powers of two
+constexpr int kQueryExp = -4;       // of a row's largest query value
+// How far the largest weight may grow above that before the running maximum follows: bfloat16 weights
+// lose no bits by it.
+constexpr float kSlack = 6.0f;
+
+union Words8 {
+    uint32_t w[4];
+    bf8_t v;
+};
+
+// Two codes (byte SEL of w) at their scale as bfloat16, the lower one low.
+template <int SEL>
+__device__ __forceinline__ uint32_t pair_of(uint32_t w, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, SEL));
+}
+// Eight codes the same way.
+__device__ __forceinline__ bf8_t codes_to_bf(uint32_t w, float scale) {
+    Words8 o;
+    o.w[0] = pair_of<0>(w, scale);
+    o.w[1] = pair_of<1>(w, scale);
+    o.w[2] = pair_of<2>(w, scale);
+    o.w[3] = pair_of<3>(w, scale);
+    return o.v;
+}
+// Byte `at` of w as the scale that it stands for.
+__device__ __forceinline__ float scale_of(uint32_t w, int at) {
+    return __uint_as_float((w >> (8 * at) & 0xffu) << 23);
+}
+
+// Eight values as bfloat16: their upper halves, and what these leave.
+__device__ __forceinline__ void split8(const float* x, bf8_t* hi, bf8_t* lo) {
+    Words8 h, l;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t a = __float_as_uint(x[2 * i]), b = __float_as_uint(x[2 * i + 1]);
+        h.w[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+        const float ra = x[2 * i] - __uint_as_float(a & 0xffff0000u);
+        const float rb = x[2 * i + 1] - __uint_as_float(b & 0xffff0000u);
+        const bf2_t r = {(__bf16)ra, (__bf16)rb};
+        l.w[i] = __builtin_bit_cast(uint32_t, r);
+    }
+    *hi = h.v;
+    *lo = l.v;
+}
+__device__ __forceinline__ bf8_t round8(const float* x) {
+    Words8 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bf2_t r = {(__bf16)x[2 * i], (__bf16)x[2 * i + 1]};
+        o.w[i] = __builtin_bit_cast(uint32_t, r);
+    }
+    return o.v;
+}
+
+// Values of a query, a row's largest `top`, as factors of the first product (PIECES of them); *scale what
+// their scores are multiplied by, not negative: the query takes the sign.
+template <int PIECES, int N>
+__device__ __forceinline__ void query_pieces(const KvAttend& k, const float (&x)[N][8], float top,
+                                             bf8_t (&q)[PIECES][N], float* scale) {
+    uint32_t frac;
+    const int e = min(127, max(-90, exponent_of(top, &frac) - 1));  // 2^e <= top < 2^(e + 1)
+    const int up = kQueryExp - e;  // in two steps: -131 is no exponent of a float
+    const float f = pow2f(up / 2), f2 = k.scale < 0.0f ? -pow2f(up - up / 2) : pow2f(up - up / 2);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float y[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = x[i][j] * f * f2;
+        if constexpr (PIECES == 1)
+            q[0][i] = round8(y);
+        else
+            split8(y, &q[0][i], &q[1][i]);
+    }
+    // not infinite, and not zero beside a masked score's infinity
+    const float c = fabsf(k.scale) * kLog2e * pow2f(-up / 2) * pow2f(up / 2 - up);
+    *scale = fminf(fmaxf(c, 1.17549435e-38f), 3.4e38f);
+}
+
+// Few rows: 16 columns of rows, one key head, one chunk of tokens.  Each of four or eight waves takes
+// every fourth or eighth step of 64 tokens, with its own running maxima, and they are joined at the
+// end.  A wave reads the codes straight into registers; nothing is shared, so there is no barrier in the loop
+// and what hides the latency is the other waves of the SIMD.
+//
+// Tokens: key row n of tile t holds token 4 n + t of the step, lane quarter g a quarter of its dims.  A lane
+// of quarter g then has the scores of tokens [16 g, + 16), four in a row from the four tiles.  Of the
+// values it reads those tokens' dims [D/16 n, + D/16): row n of the second product's tile t is dim D/16 n + t.
+template <int D, int PIECES, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void kv4_rows_kernel(KvAttend k) {
+    constexpr int KD = D / 4, KS = KD / 8;  // dims of a lane's keys; steps of the first product
+    constexpr int VD = D / 16;              // dims of a lane's values
+    constexpr int KE = D == 256 ? 2 : 1;    // scales of a lane's dims of a key
+    __shared__ __align__(16) float so[WAVES][16][D + 4];
+    __shared__ float sm[WAVES][16], sl[WAVES][16];
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const KvArgs& a = k.a;
+    if (blockIdx.x == 0) kv_check_begin(a);
+    const uint32_t heads = a.c.heads, n_chunks = (uint32_t)k.shape.n_chunks;
+    const int head = (int)(blockIdx.x % heads);
+    // chunks slowest: workgroups go to the XCDs in turn, and first chunks, which every row group
+    // has, must not all meet one of them
+    const uint32_t rest = blockIdx.x / heads, units = (uint32_t)k.shape.units, chunk = rest / units;
+    RowGroup rg;
+    if (!row_group(k, rest % units, &rg)) return;
+    const int64_t last_row = min((int64_t)rg.n_rows, rg.row0 + 16) - 1;
+    const int32_t most = row_of(k, rg, head, last_row).last;  // the last position any row sees
+    const int32_t least = row_of(k, rg, head, rg.row0).last;  // all rows see up to here
+    const int lb = a.log_block, block = 1 << lb;
+    const int64_t start = chunk * k.shape.chunk, end_all = (int64_t)most + 1;
+    if (chunk > 0 && start >= end_all) return;
+    const int32_t x1 = (int32_t)min(end_all, start + k.shape.chunk);
+
+    Pages pages = {a.s.table + rg.q.s * a.s.table_stride, (uint32_t)max(most, 0) >> lb,
+                   (uint32_t)a.c.n_blocks, 0};
+    const uint32_t page_size = heads * (uint32_t)(D / 2) << lb, exp_size = heads * (uint32_t)(D / 32) << lb;
+    const int k_slot = (((n >> 2) * 16) & (block - 1)) + (n & 3) * 4, v_slot = (g * 16) & (block - 1);
+    const uint32_t k_at = (((uint32_t)head << lb) + k_slot) * (D / 2) + g * (KD / 2);
+    const uint32_t v_at = (((uint32_t)head << lb) + v_slot) * (D / 2) + n * (VD / 2);
+    const uint32_t ke_at = (((uint32_t)head * (D / 32) + g * KD / 32) << lb) + k_slot;
+    const uint32_t ve_at = (((uint32_t)head * (D / 32) + n * VD / 32) << lb) + v_slot;
+    uint32_t kw[4][KS], vw[16][VD > 8 ? 2 : 1], ke[KE];
+    uint4 ve;
+    uint32_t k_entry = 0, v_entry = 0;
+    auto find = [&](int32_t x) {
+        k_entry = pages.entry((uint32_t)(x + (n >> 2) * 16) >> lb);
+        v_entry = pages.entry((uint32_t)(x + g * 16) >> lb);
+    };
+    auto load_keys = [&]() {
+        const uint64_t page = pages.page(k_entry);
+        const uint8_t* const p = a.c.k_code + (page * page_size + k_at);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            if constexpr (KS == 2) {
+                const uint2 w = *reinterpret_cast<const uint2*>(p + t * (D / 2));
+                kw[t][0] = w.x, kw[t][1] = w.y;
+            } else {
+#pragma unroll
+                for (int c = 0; c < KS / 4; ++c) {
+                    const uint4 w = *reinterpret_cast<const uint4*>(p + t * (D / 2) + c * 16);
+                    kw[t][4 * c] = w.x, kw[t][4 * c + 1] = w.y, kw[t][4 * c + 2] = w.z, kw[t][4 * c + 3] = w.w;
+                }
+            }
+        }
+        const int8_t* const e = a.c.k_exp + (page * exp_size + ke_at);
+#pragma unroll
+        for (int i = 0; i < KE; ++i) ke[i] = *reinterpret_cast<const uint32_t*>(e + (i << lb));
+    };
+    auto load_values = [&]() {
+        const uint64_t page = pages.page(v_entry);
+        const uint8_t* const p = a.c.v_code + (page * page_size + v_at);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            if constexpr (VD == 4) {
+                vw[j][0] = *reinterpret_cast<const uint16_t*>(p + j * (D / 2));
+            } else if constexpr (VD == 8) {
+                vw[j][0] = *reinterpret_cast<const uint32_t*>(p + j * (D / 2));
+            } else {
+                const uint2 w = *reinterpret_cast<const uint2*>(p + j * (D / 2));
+                vw[j][0] = w.x, vw[j][1] = w.y;
+            }
+        }
+        ve = *reinterpret_cast<const uint4*>(a.c.v_exp + (page * exp_size + ve_at));
+    };
+    const Row row = row_of(k, rg, head, rg.row0 + n);
+    int32_t x = (int32_t)start + wave * kStep;
+    const int32_t stride = WAVES * kStep;
+    uint4 raw[KS];
+#pragma unroll
+    for (int i = 0; i < KS; ++i) raw[i] = load8_16bit(k.q, row.token, row.head, g * KD + i * 8);
+    if (x < x1) {
+        find(x);
+        load_keys();
+        load_values();
+        if (x + stride < x1) find(x + stride);
+    }
+    bf8_t q[PIECES][KS];
+    float c;
+    {
+        float y[KS][8], top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            to_float8(k.q, raw[i], y[i]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(y[i][j]));
+        }
+        top = fmaxf(top, __shfl_xor(top, 16, kWave));
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        query_pieces<PIECES>(k, y, top, q, &c);
+    }
+    float4_t acc[VD];
+    float m = -INFINITY, l = 0.0f;
+#pragma unroll
+    for (int t = 0; t < VD; ++t) acc[t] = float4_t{0, 0, 0, 0};
+
+    for (; x < x1; x += stride) {
+        float s[16];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            float4_t z = {0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                const bf8_t f = codes_to_bf(kw[t][i], scale_of(ke[i * KE / KS], t));
+#pragma unroll
+                for (int p = 0; p < PIECES; ++p)
+                    z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, q[p][i], z, 0, 0, 0);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[4 * r + t] = z[r];
+        }
+        const bool more = x + stride < x1;
+        if (more) load_keys();
+        if (x + kStep - 1 > least) {  // some row does not see some token of the step
+            const int seen = row.last - x - g * 16;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = i > seen ? -INFINITY : s[i];
+            // places past the end may hold anything: a scale of one makes their values finite
+            const int held = most - x - g * 16;
+            uint32_t e[4] = {ve.x, ve.y, ve.z, ve.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t keep = (uint32_t)(((uint64_t)1 << (8 * min(4, max(0, held + 1 - 4 * i)))) - 1);
+                e[i] = (e[i] & keep) | (0x7f7f7f7fu & ~keep);
+            }
+            ve = make_uint4(e[0], e[1], e[2], e[3]);
+        }
+        float top = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+        top = fmaxf(top, __shfl_xor(top, 16, kWave));
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        const float new_m = fmaxf(m, top * c + kBelow);
+        if (__any(new_m - m > kSlack)) {
+            const float fall = __builtin_amdgcn_exp2f(m - (new_m == -INFINITY ? 0.0f : new_m));
+#pragma unroll
+            for (int t = 0; t < VD; ++t) acc[t] *= fall;
+            l *= fall;
+            m = new_m;
+        }
+        const float from = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -from));
+            l += s[i];
+        }
+        const uint32_t e[4] = {ve.x, ve.y, ve.z, ve.w};
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            bf8_t hi, lo;
+            split8(s + 8 * half, &hi, &lo);
+            // two tokens' dims d and d + 1 as they come, to two dims of two tokens
+            Words8 f[VD];
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                const int at = 8 * half + j;
+                const float sa = scale_of(e[at / 4], at % 4), sb = scale_of(e[at / 4], at % 4 + 1);
+                const auto turn = [&](auto sel, int word, int d) {
+                    const uint32_t ta = pair_of<decltype(sel)::value>(vw[at][word], sa);
+                    const uint32_t tb = pair_of<decltype(sel)::value>(vw[at + 1][word], sb);
+                    f[d].w[j / 2] = __builtin_amdgcn_perm(tb, ta, 0x05040100u);
+                    f[d + 1].w[j / 2] = __builtin_amdgcn_perm(tb, ta, 0x07060302u);
+                };
+#pragma unroll
+                for (int word = 0; word < (VD > 8 ? 2 : 1); ++word) {
+                    turn(std::integral_constant<int, 0>(), word, 8 * word);
+                    turn(std::integral_constant<int, 1>(), word, 8 * word + 2);
+                    if constexpr (VD >= 8) {
+                        turn(std::integral_constant<int, 2>(), word, 8 * word + 4);
+                        turn(std::integral_constant<int, 3>(), word, 8 * word + 6);
+                    }
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < VD; ++t) {
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[t].v, hi, acc[t], 0, 0, 0);
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[t].v, lo, acc[t], 0, 0, 0);
+            }
+        }
+        if (more) {
+            load_values();
+            if (x + 2 * (int64_t)stride < x1) find(x + 2 * stride);
+        }
+    }
+    if (pages.bad()) raise_status(a.status, MP_EINVAL);
+
+    // the waves' results of a row joined; a lane has dims [4 VD g, + 4 VD)
+    l += __shfl_xor(l, 16, kWave);
+    l += __shfl_xor(l, 32, kWave);
+    if (g == 0) {
+        sm[wave][n] = m;
+        sl[wave][n] = l;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int t = 0; t < VD; t += 4)
+            *reinterpret_cast<float4_t*>(&so[wave][n][(4 * g + r) * VD + t]) =
+                float4_t{acc[t][r], acc[t + 1][r], acc[t + 2][r], acc[t + 3][r]};
+    __syncthreads();
+    if (WAVES > 4 && threadIdx.x >= 256) return;
+    const int col = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * (D / 16);
+    float top = sm[0][col];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, sm[w][col]);
+    const float base = top == -INFINITY ? 0.0f : top;
+    float total = 0.0f, o[D / 16];
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) o[i] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        const float f = __builtin_amdgcn_exp2f(sm[w][col] - base);
+        total += sl[w][col] * f;
+#pragma unroll
+        for (int i = 0; i < D / 16; i += 4) {
+            const float4_t y = *reinterpret_cast<const float4_t*>(&so[w][col][d0 + i]);
+#pragma unroll
+            for (int z = 0; z < 4; ++z) o[i + z] += y[z] * f;
+        }
+    }
+    const Row r = row_of(k, rg, head, rg.row0 + col);
+    if (!r.live) return;
+    const int64_t index = r.token * (int64_t)k.group * heads + r.head;
+    if (n_chunks > 1) {
+        const Partials part_out = partials(k);
+        float* to = part_out.o + (index * n_chunks + chunk) * D + d0;
+#pragma unroll
+        for (int i = 0; i < D / 16; i += 4)
+            *reinterpret_cast<float4_t*>(to + i) = float4_t{o[i], o[i + 1], o[i + 2], o[i + 3]};
+        if (d0 == 0) part_out.sums[index * n_chunks + chunk] = float4_t{top, total, 0, 0};
+    } else {
+        // a row that sees nothing: weights and sums are zero
+        const float norm = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) o[i] *= norm;
+        constexpr int kOnce = D / 16 >= 8 ? 8 : 4;
+#pragma unroll
+        for (int i = 0; i < D / 16; i += kOnce) store_16bit<kOnce>(k.out, r.token, r.head, d0 + i, o + i);
+        if (k.lse && d0 == 0)
+            k.lse[index] = total > 0.0f ? (base + log2f(total)) * kLn2 : total == 0.0f ? -INFINITY : total;
+    }
+}
+
+// The result of a wave of 32 rows, a column each: lane half h has dims 4 h + [0, 4) of every eight.
+template <int D>
+__device__ __forceinline__ void store_rows(const KvAttend& k, const Row& row, uint32_t chunk,
+                                           const float16_t (&acc)[D / 32], float m, float l, int h) {
+    const float total = l + __shfl_xor(l, 32, kWave);
+    if (!row.live) return;
+    const uint32_t n_chunks = (uint32_t)k.shape.n_chunks;
+    // a row that sees nothing: weights and sums are zero
+    const float norm = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
+    const int64_t index = row.token * (int64_t)k.group * k.a.c.heads + row.head;
+    const Partials part_out = partials(k);
+    const bool whole = n_chunks == 1;
+    const float f = whole ? norm : 1.0f;
+    float* const to = part_out.o + (index * n_chunks + chunk) * D;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int d = t * 32 + r * 2 + 4 * h;
+            float o[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = acc[t][r + i] * f;
+            if (whole)
+                store_16bit<4>(k.out, row.token, row.head, d, o);
+            else
+                *reinterpret_cast<float4_t*>(to + d) = float4_t{o[0], o[1], o[2], o[3]};
+        }
+    if (h == 0) {
+        if (!whole)
+            part_out.sums[index * n_chunks + chunk] = float4_t{m, total, 0, 0};
+        else if (k.lse)
+            k.lse[index] = total > 0.0f ? (m + log2f(total)) * kLn2 : total == 0.0f ? -INFINITY : total;
+    }
+}
+
+// Many rows: four waves of 32 rows, one key head, one chunk of tokens, in tiles of 64 tokens whose
+// codes the workgroup turns into bfloat16 once, in LDS, for all 128 rows.  Two tiles' room: while one
+// is computed the next one's codes, already in registers, are converted into the other and the
+// loads of the one after are on their way, so a tile costs one barrier.
+//
+// Both arrays lie by token, in 16-byte pieces exchanged by the token's low bits, so that the lanes of a
+// read meet different banks.  Keys are read along their dims, row n of 32 being token n with bits 2 and 3
+// exchanged: a lane's scores are those of eight consecutive tokens, as the second product takes
+// them.  Values are read by the transposing loads, 16 lanes of which take four tokens' 16 dims and have
+// one dim of the four each.
+template <int D>
+struct Tile4 {
+    uint4 k[64][D / 8];
+    uint4 v[64][D / 8];
+};
+template <int D>
+__device__ __forceinline__ int k4_key(int token) {
+    return D == 64 ? token >> 1 & 7 : token & 15;
+}
+template <int D>
+__device__ __forceinline__ int v4_key(int token) {
+    return D == 64 ? (token >> 1 & 1) << 2 : (token & 3) << 2;
+}
+
+template <int D, int PIECES>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_tiles_kernel(KvAttend k) {
+    constexpr int KS = D / 16, DT = D / 32, GROUPS = D / 32;
+    constexpr int UNITS = 128 * GROUPS / 256;  // groups of 32 dims that a thread moves in a tile, keys first
+    extern __shared__ __align__(16) char lds_raw[];
+    Tile4<D>* const lds = reinterpret_cast<Tile4<D>*>(lds_raw);
+    const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const KvArgs& a = k.a;
+    if (blockIdx.x == 0) kv_check_begin(a);
+    // key heads fastest: workgroups of one head share an XCD's L2 where 8 and the number of
+    // heads divide
+    const uint32_t heads = a.c.heads, n_chunks = (uint32_t)k.shape.n_chunks;
+    const int head = (int)(blockIdx.x % heads);
+    const uint32_t rest = blockIdx.x / heads, chunk = rest % n_chunks;
+    RowGroup rg;
+    if (!tile_group<128>(k, rest / n_chunks, &rg)) return;
+    const int32_t most = row_of(k, rg, head, min((int64_t)rg.n_rows, rg.row0 + 128) - 1).last;
+    const int64_t start = chunk * k.shape.chunk;
+    if (chunk > 0 && start > most) return;
+    const int32_t x0 = (int32_t)start;
+    const int32_t x1 = (int32_t)min((int64_t)most + 1, start + k.shape.chunk);
+
+    // this wave's rows: the last position that any sees, and the last that all see
+    const int64_t wave_row0 = rg.row0 + 32 * wave;
+    const bool awake = wave_row0 < rg.n_rows;
+    const int32_t wave_most = awake ? row_of(k, rg, head, min((int64_t)rg.n_rows, wave_row0 + 32) - 1).last : -1;
+    const int32_t wave_least = awake ? row_of(k, rg, head, wave_row0).last : -1;
+    const Row row = row_of(k, rg, head, wave_row0 + n);
+
+    bf8_t q[PIECES][KS];
+    float c;
+    {
+        uint4 raw[KS];
+#pragma unroll
+        for (int i = 0; i < KS; ++i) raw[i] = load8_16bit(k.q, row.token, row.head, i * 16 + h * 8);
+        float y[KS][8], top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            to_float8(k.q, raw[i], y[i]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(y[i][j]));
+        }
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        query_pieces<PIECES>(k, y, top, q, &c);
+    }
+    float16_t acc[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t) acc[t] = float16_t{};
+    float m = -INFINITY, l = 0.0f;
+
+    // unit u of a thread: 32 dims of a token's keys or values; table entries are read a tile ahead
+    const int lb = a.log_block, block = 1 << lb;
+    const uint32_t page_size = heads * (uint32_t)(D / 2) << lb, exp_size = heads * (uint32_t)(D / 32) << lb;
+    Pages pages = {a.s.table + rg.q.s * a.s.table_stride, (uint32_t)max(most, 0) >> lb,
+                   (uint32_t)a.c.n_blocks, 0};
+    const auto is_v = [&](int u) { return u * 256 + tid >= 64 * GROUPS; };
+    const auto token_of = [&](int u) { return ((u * 256 + tid) / GROUPS) & 63; };
+    const int group = tid % GROUPS;
+    uint4 codes[UNITS];
+    uint32_t exps[UNITS], entry[UNITS];
+    auto find = [&](int32_t x) {
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) entry[u] = pages.entry((uint32_t)(x + token_of(u)) >> lb);
+    };
+    auto load = [&]() {
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            const uint64_t page = pages.page(entry[u]);
+            const uint32_t slot = token_of(u) & (block - 1);
+            const uint8_t* const from = is_v(u) ? a.c.v_code : a.c.k_code;
+            const int8_t* const exp = is_v(u) ? a.c.v_exp : a.c.k_exp;
+            codes[u] = *reinterpret_cast<const uint4*>(
+                from + (page * page_size + (((uint32_t)head << lb) + slot) * (D / 2) + group * 16));
+            exps[u] = (uint8_t)exp[page * exp_size + ((((uint32_t)head * GROUPS + group) << lb) + slot)];
+        }
+    };
+    // the loaded codes (of the tile at x) in LDS; places past the end may hold anything: a scale of one
+    // makes their values finite
+    auto put = [&](int buf, int32_t x) {
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            const int token = token_of(u);
+            const uint32_t e = x + token > most ? 127u : exps[u];
+            const float scale = __uint_as_float(e << 23);
+            uint4* const to = is_v(u) ? lds[buf].v[token] : lds[buf].k[token];
+            const int key = is_v(u) ? v4_key<D>(token) : k4_key<D>(token);
+            const uint32_t w[4] = {codes[u].x, codes[u].y, codes[u].z, codes[u].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                to[(group * 4 + i) ^ key] = __builtin_bit_cast(uint4, codes_to_bf(w[i], scale));
+        }
+    };
+    const int k_token = (n & 0x13) | (n & 4) << 1 | (n & 8) >> 1;
+    const int v_token = 8 * h + (lane >> 2 & 3), v_dim = (n & 16) + (lane & 3) * 4;
+
+    int buf = 0;
+    if (x0 < x1) {
+        find(x0);
+        load();
+        find(x0 + 64);
+        put(0, x0);
+    }
+    for (int32_t x = x0; x < x1; x += 64, buf ^= 1) {
+        if (x + 64 < x1) {
+            load();
+            find(x + 128);
+        }
+        __syncthreads();  // the tile is whole; the other one is read no more
+        if (x <= wave_most) {
+            float16_t s[2] = {float16_t{}, float16_t{}};
+#pragma unroll
+            for (int i = 0; i < KS; ++i)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const int token = t * 32 + k_token;
+                    const bf8_t f = __builtin_bit_cast(bf8_t, lds[buf].k[token][(i * 2 + h) ^ k4_key<D>(token)]);
+#pragma unroll
+                    for (int p = 0; p < PIECES; ++p)
+                        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[p][i], s[t], 0, 0, 0);
+                }
+            // register r of product t is token 32 t + 16 (r / 8) + 8 h + r % 8
+            if (x + 63 > wave_least) {
+                const int seen = row.last - x - h * 8;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        s[t][r] = t * 32 + (r >> 3) * 16 + (r & 7) > seen ? -INFINITY : s[t][r];
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int r = 0; r < 32; ++r) top = fmaxf(top, s[r / 16][r % 16]);
+            top = fmaxf(top, __shfl_xor(top, 32, kWave));
+            const float new_m = fmaxf(m, top * c + kBelow);
+            if (__any(new_m - m > kSlack)) {
+                const float fall = __builtin_amdgcn_exp2f(m - (new_m == -INFINITY ? 0.0f : new_m));
+#pragma unroll
+                for (int t = 0; t < DT; ++t) acc[t] *= fall;
+                l *= fall;
+                m = new_m;
+            }
+            const float from = m == -INFINITY ? 0.0f : m;
+            bf8_t w[PIECES][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float e[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 2][i % 2 * 8 + r], c, -from));
+                    l += e[r];
+                }
+                if constexpr (PIECES == 1)
+                    w[0][i] = round8(e);
+                else
+                    split8(e, &w[0][i], &w[1][i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int t = 0; t < DT; ++t) {
+                    union {
+                        short4_t s[2];
+                        bf8_t v;
+                    } f;
+#pragma unroll
+                    for (int z = 0; z < 2; ++z) {
+                        const int token = i * 16 + 4 * z + v_token, d = t * 32 + v_dim;
+                        auto* const from8 = reinterpret_cast<short4_t*>(&lds[buf].v[token][(d >> 3) ^ v4_key<D>(token)]) + (d >> 2 & 1);
+                        f.s[z] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)from8);
+                    }
+#pragma unroll
+                    for (int p = 0; p < PIECES; ++p)
+                        acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, w[p][i], acc[t], 0, 0, 0);
+                }
+        }
+        if (x + 64 < x1) put(buf ^ 1, x + 64);
+    }
+    if (pages.bad()) raise_status(a.status, MP_EINVAL);
+    store_rows<D>(k, row, chunk, acc, m, l, h);
+}
+
+template <int D, int PIECES>
+hipError_t launch_d(const KvAttend& k, hipStream_t st) {
+    const KvAttendShape& sh = k.shape;
+    const dim3 grid((uint32_t)(sh.units * k.a.c.heads * sh.n_chunks));
+    constexpr int kLds = 2 * sizeof(Tile4<D>);
+    if (sh.form == KvForm::tiles) {
+        if (kLds > 65536)
+            if (hipError_t e = hipFuncSetAttribute((const void*)kv4_tiles_kernel<D, PIECES>,
+                                                   hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+                e != hipSuccess)
+                return e;
+        kv4_tiles_kernel<D, PIECES><<<grid, 256, kLds, st>>>(k);
+    } else if (D < 256 && grid.x <= 256) {  // a compute unit for every workgroup
+        if constexpr (D < 256) kv4_rows_kernel<D, PIECES, 8><<<grid, 512, 0, st>>>(k);
+    } else {
+        kv4_rows_kernel<D, PIECES, 4><<<grid, 256, 0, st>>>(k);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv4_attend(const KvAttend& k, hipStream_t st) {
+    const bool two = k.q.dtype == MP_F16;
+    switch (k.a.c.dim) {
+        case 64: return two ? launch_d<64, 2>(k, st) : launch_d<64, 1>(k, st);
+        case 128: return two ? launch_d<128, 2>(k, st) : launch_d<128, 1>(k, st);
+        default: return two ? launch_d<256, 2>(k, st) : launch_d<256, 1>(k, st);
+    }
+}
+
+}  // namespace mp

@@ -21,7 +21,7 @@ bool shape_ok(const mp_kv_cache* c) {
         return false;
     if (c->dim != 64 && c->dim != 128 && c->dim != 256) return false;
     if (c->block != 16 && c->block != 32 && c->block != 64) return false;
-    return c->kind == MP_KV_E4M3 || c->kind == MP_KV_INT8;
+    return c->kind == MP_KV_E4M3 || c->kind == MP_KV_INT8 || c->kind == MP_KV_E2M1;
 }
 
 bool counts_ok(const mp_kv_cache* c, const mp_kv_seqs* s) {
@@ -36,8 +36,11 @@ bool counts_ok(const mp_kv_cache* c, const mp_kv_seqs* s) {
 }
 
 bool cache_ok(const mp_kv_cache* c) {
-    if (!c->k_code || !c->v_code || !c->k_exp || !c->v_exp || !c->mean_code || !c->mean_exp)
-        return false;
+    if (!c->k_code || !c->v_code || !c->k_exp || !c->v_exp) return false;
+    if (c->kind == MP_KV_E2M1)  // no means
+        return !c->mean_code && !c->mean_exp && aligned(c->k_code, 16) && aligned(c->v_code, 16) &&
+               aligned(c->k_exp, 16) && aligned(c->v_exp, 16);
+    if (!c->mean_code || !c->mean_exp) return false;
     return aligned(c->k_code, 16) && aligned(c->v_code, 16) && aligned(c->mean_code, 8);
 }
 
@@ -101,8 +104,12 @@ int32_t move_rows(const mp_kv_cache* cache, const mp_kv_seqs* seqs, const mp_kv_
                    !rows_apart(v, seqs->n_tokens, cache->heads, cache->dim)))
         return MP_EINVAL;
     const KvArgs a = args_of(cache, seqs, status_out);
-    if (!grid_ok(write ? kv_write_groups(a) : kv_read_groups(a), 256)) return MP_EINVAL;
     const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (cache->kind == MP_KV_E2M1) {
+        if (!grid_ok(kv4_move_groups(a), 256)) return MP_EINVAL;
+        return launched(write ? launch_kv4_write(a, kr, vr, st) : launch_kv4_read(a, kr, vr, st));
+    }
+    if (!grid_ok(write ? kv_write_groups(a) : kv_read_groups(a), 256)) return MP_EINVAL;
     return launched(write ? launch_kv_write(a, kr, vr, st) : launch_kv_read(a, kr, vr, st));
 }
 
@@ -131,6 +138,7 @@ extern "C" int32_t mp_kv_attend(const mp_kv_cache* cache, const mp_kv_seqs* seqs
         return MP_EINVAL;
     if (keep < 0 || keep > kMaxCount / 64) return MP_EINVAL;
     if ((blocks != nullptr) != (keep > 0) && seqs->n_tokens > 0) return MP_EINVAL;
+    if (cache->kind == MP_KV_E2M1 && keep > 0) return MP_EINVAL;  // blocks are selected by means
     if (!rows_ok(q, seqs->n_tokens, q_heads, false, &k.q) ||
         !rows_ok(out, seqs->n_tokens, q_heads, false, &k.out) || q->dtype != out->dtype ||
         !rows_apart(out, seqs->n_tokens, q_heads, cache->dim))
@@ -155,7 +163,8 @@ extern "C" int32_t mp_kv_select(const mp_kv_cache* cache, const mp_kv_seqs* seqs
                                 size_t workspace_bytes, int32_t* status_out, void* stream) {
     KvSelect k = {};
     if (!shape_ok(cache) || !counts_ok(cache, seqs) || !cache_ok(cache) || !seqs_ok(seqs) ||
-        !status_out || !heads_ok(cache, q_heads) || q_heads / cache->heads > kMaxSelectGroup)
+        !status_out || !heads_ok(cache, q_heads) || q_heads / cache->heads > kMaxSelectGroup ||
+        cache->kind == MP_KV_E2M1)
         return MP_EINVAL;
     if (keep < 1 || keep > kMaxCount / 64 || first < 0 || recent < 1 || first > keep ||
         recent > keep - first || (!blocks_out && seqs->n_tokens > 0))
@@ -180,7 +189,7 @@ extern "C" int32_t mp_kv_select(const mp_kv_cache* cache, const mp_kv_seqs* seqs
 extern "C" size_t mp_kv_workspace_size(int32_t op, const mp_kv_cache* cache,
                                        const mp_kv_seqs* seqs, int32_t q_heads, int64_t keep) {
     if (!shape_ok(cache) || !counts_ok(cache, seqs) || !heads_ok(cache, q_heads) || keep < 0 ||
-        keep > kMaxCount / 64)
+        keep > kMaxCount / 64 || (cache->kind == MP_KV_E2M1 && (op != MP_OP_KV_ATTEND || keep > 0)))
         return 0;
     if (op == MP_OP_KV_ATTEND) {
         const KvAttendShape sh = kv_attend_shape(*cache, *seqs, q_heads, keep);

@@ -21,14 +21,12 @@
 // come out of the first product in the lanes that the second one wants them in, as long
 // as the token that a lane's key row holds is chosen for it, and the maximum and the sum
 // of a row are over one lane's registers and the few lanes of its column.
-#include "kv.hpp"
+#include "kv_attend.hpp"
 
 namespace mp {
 
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kWeightShift = 15;   // weights reach 2^15
 constexpr int kLeastShift = -80;   // of a block's value exponent below vr: its weights are zeros
 constexpr int kSpread = 10;        // of value exponents that share one vr
@@ -72,100 +70,6 @@ __device__ __forceinline__ float rescale(float m, int vr, float base, int new_vr
 
 // 2^-shift, where a weight's share of its row's sum is at most 2^-111 once that is out of range.
 __device__ __forceinline__ float back_from(int shift) { return pow2f(max(-126, -shift)); }
-
-// The partial result of a row over a chunk of tokens: its weighted values, 2^(maximum + power) of
-// them; the maximum of its weights' exponents, the sum of its weights below that, the power.  (One
-// logarithm of maximum and sum would lose the sum beside a large maximum; values at their own size
-// and weights at theirs could both leave the range of 32-bit floats where their product does not.)
-struct Partials {
-    float* o;        // [row][chunk][dim]
-    float4_t* sums;  // [row][chunk]: maximum, sum, power
-};
-
-__device__ __forceinline__ Partials partials(const KvAttend& k) {
-    const int64_t rows = k.a.s.n_tokens * (int64_t)k.group * k.a.c.heads * k.shape.n_chunks;
-    Partials p;
-    p.o = static_cast<float*>(k.ws);
-    p.sums = reinterpret_cast<float4_t*>(p.o + rows * k.a.c.dim);
-    return p;
-}
-
-// The rows [row0, ...) of a workgroup: rows of a sequence and key head are (token, query
-// head) pairs in token order.
-struct RowGroup {
-    KvSeq q;
-    int64_t row0;
-    int32_t n_rows;  // of the sequence
-};
-
-// Row group `u` of the launch.  With a block list every token is a sequence of its own.
-__device__ __forceinline__ bool row_group(const KvAttend& k, int64_t u, RowGroup* g) {
-    const KvArgs& a = k.a;
-    if (k.blocks) {
-        const int64_t per = (k.group + k.shape.rows - 1) / k.shape.rows;
-        const int64_t token = u / per;
-        int64_t i;
-        g->q = kv_find(a, token, [&](int64_t b, int64_t) { return b; }, &i);
-        if (!g->q.ok || i < 0 || i >= g->q.n) return false;
-        // the sequence as it is for this token: its last one
-        g->q.length -= (int32_t)(g->q.n - 1 - i);
-        g->q.begin = token;
-        g->q.n = 1;
-        g->row0 = u % per * k.shape.rows;
-    } else {
-        int64_t first;
-        if (a.s.begin) {
-            // n tokens are at most n * group / rows + 1 row groups
-            auto key = [&](int64_t b, int64_t i) { return b * k.group / k.shape.rows + i; };
-            g->q = kv_find(a, u, key, &first);
-        } else {
-            const int64_t per = (k.group + k.shape.rows - 1) / k.shape.rows;
-            g->q = wave_one(kv_seq(a, u / per, u / per, u / per + 1));
-            first = u % per;
-        }
-        if (!g->q.ok || first < 0) return false;
-        g->row0 = first * k.shape.rows;
-    }
-    const int64_t n = (int64_t)g->q.n * k.group;
-    if (g->row0 >= n) return false;
-    g->n_rows = (int32_t)n;
-    return true;
-}
-
-// The place of a row: its token, its query head, the last position it sees (-1: none).
-struct Row {
-    int64_t token;
-    int32_t head;
-    int32_t last;
-    bool live;
-};
-__device__ __forceinline__ Row row_of(const KvAttend& k, const RowGroup& g, int key_head,
-                                      int64_t row) {
-    Row r;
-    r.live = row < g.n_rows;
-    const int32_t i = r.live ? (int32_t)row : g.n_rows - 1;
-    const int32_t t = i / k.group;
-    r.token = g.q.begin + t;
-    r.head = key_head * k.group + i % k.group;
-    r.last = r.live ? max(-1, g.q.length - g.q.n + t) : -1;
-    return r;
-}
-
-// The pages of a sequence as its blocks are walked: entries of its table row, kept within the
-// row's last used block and the pool.
-struct Pages {
-    const int32_t* table;
-    uint32_t last_block, n_blocks;
-    uint32_t worst;  // the largest entry met
-    __device__ __forceinline__ uint32_t entry(uint32_t block) const {
-        return (uint32_t)table[min(block, last_block)];
-    }
-    __device__ __forceinline__ uint32_t page(uint32_t e) {
-        worst = max(worst, e);
-        return min(e, n_blocks - 1);
-    }
-    __device__ __forceinline__ bool bad() const { return worst >= n_blocks; }
-};
 
 // A row's query as it lies in memory: lane (column n, quarter g) holds dims [64 c + 16 g, + 16).
 template <int D>
@@ -558,63 +462,6 @@ __device__ __forceinline__ void store_rows(const KvAttend& k, const Row& row, ui
         else if (k.lse)
             k.lse[index] = total > 0.0f ? (m + log2f(total)) * kLn2 : total == 0.0f ? -INFINITY : total;
     }
-}
-
-// The sum of x over the wave.
-__device__ __forceinline__ int wave_sum(int x) {
-    const auto from = [](int v, auto dpp, auto rows) {
-        return __builtin_amdgcn_update_dpp(0, v, decltype(dpp)::value, decltype(rows)::value, 0xf, false);
-    };
-    using All = std::integral_constant<int, 0xf>;
-    x += from(x, std::integral_constant<int, 0x111>(), All());  // up by 1, 2, 4, 8 in rows of 16
-    x += from(x, std::integral_constant<int, 0x112>(), All());
-    x += from(x, std::integral_constant<int, 0x114>(), All());
-    x += from(x, std::integral_constant<int, 0x118>(), All());
-    x += from(x, std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());  // row 0 to 1, 2 to 3
-    x += from(x, std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());  // half to half
-    return __builtin_amdgcn_readlane(x, 63);
-}
-
-// Row group `u` of a launch of tiles: those that see the most first, so that the last ones to
-// start are short.  A lane has a sequence; group j of a sequence is at level (earlier tokens in
-// groups) + j, and u counts down the levels, sequences in order within one.  Where they are
-// not ordered (more than 64 sequences, chunks, levels past 30 bits), the last sequences' last
-// groups come first.  Prompts of 228-4096 tokens: 273 us, 286 without the order; in chunks it gained
-// nothing.
-template <int ROWS>
-__device__ __forceinline__ bool tile_group(const KvAttend& k, uint32_t u, RowGroup* g) {
-    const KvArgs& a = k.a;
-    if (!k.shape.ordered) return row_group(k, k.shape.units - 1 - u, g);
-    const int lane = threadIdx.x & 63;
-    KvSeq q = {};
-    if (lane < a.s.n_seqs) q = kv_seq(a, lane, a.s.begin[lane], a.s.begin[lane + 1]);
-    const bool some = lane < a.s.n_seqs && q.ok && q.n > 0;
-    const int count = some ? (int)(((uint64_t)q.n * (uint32_t)k.group + ROWS - 1) / ROWS) : 0;
-    const int low = some ? (int)((uint64_t)max(0, q.length - q.n) * (uint32_t)k.group / ROWS) : 0;
-    if (u >= (uint32_t)wave_sum(count)) return false;
-    // the least level that at most u groups are above
-    const auto above = [&](int level) { return (uint32_t)wave_sum(min(count, max(0, low + count - 1 - level))); };
-    int from = 0, to = wave_reduce(low + count, OpMax<int>());
-    while (from < to) {
-        const int level = (from + to) >> 1;
-        if (above(level) <= u)
-            to = level;
-        else
-            from = level + 1;
-    }
-    const int nth = (int)(u - above(from));
-    const bool member = some && from >= low && from < low + count;
-    const uint64_t members = __ballot(member);
-    const int rank = __popcll(members & (((uint64_t)1 << lane) - 1));
-    const int of = __ffsll((unsigned long long)__ballot(member && rank == nth)) - 1;
-    g->q.s = of;
-    g->q.length = __builtin_amdgcn_readlane(q.length, of);
-    g->q.n = __builtin_amdgcn_readlane(q.n, of);
-    g->q.begin = wave_one(__shfl(q.begin, of, kWave));
-    g->q.ok = true;
-    g->row0 = (int64_t)(from - __builtin_amdgcn_readlane(low, of)) * ROWS;
-    g->n_rows = g->q.n * k.group;
-    return true;
 }
 
 // vr of a row for a tile whose blocks' value exponents are apart, before its scores are changed: N equal
@@ -1316,18 +1163,37 @@ hipError_t launch_d(const KvAttend& k, hipStream_t st) {
     } else {
         launch_rows<D, INT8, false>(k, grid, st);
     }
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    if (sh.n_chunks > 1) {
-        const int64_t rows = k.a.s.n_tokens * (int64_t)k.group * k.a.c.heads;
-        if (sh.n_chunks > 16)
-            kv_join_kernel<D, 4><<<dim3((uint32_t)rows), 256, 0, st>>>(k);
-        else
-            kv_join_kernel<D, 1><<<dim3((uint32_t)((rows + 3) / 4)), 256, 0, st>>>(k);
-    }
     return hipGetLastError();
 }
 
+template <int D>
+void launch_join(const KvAttend& k, hipStream_t st) {
+    const int64_t rows = k.a.s.n_tokens * (int64_t)k.group * k.a.c.heads;
+    if (k.shape.n_chunks > 16)
+        kv_join_kernel<D, 4><<<dim3((uint32_t)rows), 256, 0, st>>>(k);
+    else
+        kv_join_kernel<D, 1><<<dim3((uint32_t)((rows + 3) / 4)), 256, 0, st>>>(k);
+}
+
+hipError_t launch_8bit(const KvAttend& k, hipStream_t st) {
+    const bool i8 = k.a.c.kind == MP_KV_INT8;
+    switch (k.a.c.dim) {
+        case 64: return i8 ? launch_d<64, true>(k, st) : launch_d<64, false>(k, st);
+        case 128: return i8 ? launch_d<128, true>(k, st) : launch_d<128, false>(k, st);
+        default: return i8 ? launch_d<256, true>(k, st) : launch_d<256, false>(k, st);
+    }
+}
+
 }  // namespace
+
+hipError_t launch_kv_join(const KvAttend& k, hipStream_t st) {
+    switch (k.a.c.dim) {
+        case 64: launch_join<64>(k, st); break;
+        case 128: launch_join<128>(k, st); break;
+        default: launch_join<256>(k, st);
+    }
+    return hipGetLastError();
+}
 
 KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t q_heads,
                               int64_t keep) {
@@ -1352,7 +1218,7 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     if (keep > 0 || !s.begin || piece <= 16 || (piece <= 64 && s.longest > 512))
         sh.form = KvForm::rows;
     else
-        sh.form = c.dim == 128 && piece >= 4096 ? KvForm::pair : KvForm::tiles;
+        sh.form = c.dim == 128 && piece >= 4096 && c.kind != MP_KV_E2M1 ? KvForm::pair : KvForm::tiles;
     sh.rows = sh.form == KvForm::rows ? 16 : sh.form == KvForm::tiles ? 128 : 256;
     const int64_t per = (group + sh.rows - 1) / sh.rows;
     if (keep > 0)
@@ -1397,12 +1263,9 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
 
 hipError_t launch_kv_attend(const KvAttend& k, hipStream_t st) {
     if (k.a.s.n_tokens == 0) return hipSuccess;
-    const bool i8 = k.a.c.kind == MP_KV_INT8;
-    switch (k.a.c.dim) {
-        case 64: return i8 ? launch_d<64, true>(k, st) : launch_d<64, false>(k, st);
-        case 128: return i8 ? launch_d<128, true>(k, st) : launch_d<128, false>(k, st);
-        default: return i8 ? launch_d<256, true>(k, st) : launch_d<256, false>(k, st);
-    }
+    const hipError_t e = k.a.c.kind == MP_KV_E2M1 ? launch_kv4_attend(k, st) : launch_8bit(k, st);
+    if (e != hipSuccess || k.shape.n_chunks == 1) return e;
+    return launch_kv_join(k, st);
 }
 
 }  // namespace mp

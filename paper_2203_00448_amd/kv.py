@@ -1,4 +1,4 @@
-"""Python binding of the 8-bit key/value cache (mp_kv_* of libmemoplan.so):
+"""Python binding of the key/value cache in 8 or 4 bits (mp_kv_* of libmemoplan.so):
 argument marshalling only, like binding.py.
 
 A program keeps a `Cache` (its memory), a `Seqs` for its batch (block table,
@@ -21,7 +21,7 @@ import torch
 from . import binding
 from .binding import PlanError, _finish, _p, new_status  # noqa: F401
 
-E4M3, INT8 = 0, 1
+E4M3, INT8, E2M1 = 0, 1, 4
 OP_ATTEND, OP_SELECT = 1, 2
 DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
@@ -77,29 +77,44 @@ def _need(t, dtypes, name, shape=None):
 
 
 class Cache:
-    """Blocks of keys and values: k_code uint8 [n_blocks, heads, block, dim], v_code uint8
-    [n_blocks, heads, dim, block], k_exp and v_exp int8 [n_blocks, heads], mean_code int8
-    [n_blocks, heads, dim], mean_exp int8 [n_blocks, heads], all contiguous; kind E4M3 or INT8."""
+    """Blocks of keys and values, all tensors contiguous and on one device.
+    kind E4M3 or INT8: k_code uint8 [n_blocks, heads, block, dim], v_code uint8 [n_blocks, heads,
+    dim, block], k_exp and v_exp int8 [n_blocks, heads], mean_code int8 [n_blocks, heads, dim],
+    mean_exp int8 [n_blocks, heads].
+    kind E2M1 (4 bits, a scale for each 32 dims of a token): k_code and v_code uint8 [n_blocks,
+    heads, block, dim / 2], k_exp and v_exp uint8 [n_blocks, heads, dim / 32, block], exponents + 127;
+    no means, so nothing is selected of it."""
 
-    def __init__(self, k_code, v_code, k_exp, v_exp, mean_code, mean_exp, *, kind: int = E4M3):
+    def __init__(self, k_code, v_code, k_exp, v_exp, mean_code=None, mean_exp=None, *, kind: int = E4M3):
         _need(k_code, (torch.uint8,), "k_code")
         if k_code.dim() != 4:
-            raise ValueError("k_code must be [n_blocks, heads, block, dim]")
+            raise ValueError("k_code must have 4 dimensions")
+        if kind not in (E4M3, INT8, E2M1):
+            raise ValueError("kind must be E4M3, INT8 or E2M1")
         n, h, t, d = k_code.shape
-        _need(v_code, (torch.uint8,), "v_code", (n, h, d, t))
-        for x, name in ((k_exp, "k_exp"), (v_exp, "v_exp"), (mean_exp, "mean_exp")):
-            _need(x, (torch.int8,), name, (n, h))
-        _need(mean_code, (torch.int8,), "mean_code", (n, h, d))
-        if kind not in (E4M3, INT8):
-            raise ValueError("kind must be E4M3 or INT8")
-        self.tensors = (k_code, v_code, k_exp, v_exp, mean_code, mean_exp)
+        if kind == E2M1:
+            _need(v_code, (torch.uint8,), "v_code", (n, h, t, d))
+            d *= 2
+            for x, name in ((k_exp, "k_exp"), (v_exp, "v_exp")):
+                _need(x, (torch.uint8,), name, (n, h, d // 32, t))
+            if mean_code is not None or mean_exp is not None:
+                raise ValueError("a cache in 4 bits has no means")
+            self.tensors = (k_code, v_code, k_exp, v_exp)
+        else:
+            _need(v_code, (torch.uint8,), "v_code", (n, h, d, t))
+            for x, name in ((k_exp, "k_exp"), (v_exp, "v_exp"), (mean_exp, "mean_exp")):
+                _need(x, (torch.int8,), name, (n, h))
+            _need(mean_code, (torch.int8,), "mean_code", (n, h, d))
+            self.tensors = (k_code, v_code, k_exp, v_exp, mean_code, mean_exp)
         for x in self.tensors:
             if not x.is_contiguous() or x.device != k_code.device:
                 raise ValueError("a cache's tensors must be contiguous and on one device")
-        self.k_code, self.v_code, self.k_exp, self.v_exp, self.mean_code, self.mean_exp = self.tensors
+        self.k_code, self.v_code, self.k_exp, self.v_exp = self.tensors[:4]
+        self.mean_code, self.mean_exp = mean_code, mean_exp
         self.n_blocks, self.heads, self.block, self.dim, self.kind = n, h, t, d, kind
         self.device, self.index = k_code.device, k_code.get_device()
-        self._arg = _CacheArg(*(x.data_ptr() for x in self.tensors), n, h, d, t, kind)
+        at = [x.data_ptr() for x in self.tensors] + [None] * (6 - len(self.tensors))
+        self._arg = _CacheArg(*at, n, h, d, t, kind)
         self._ref = ctypes.addressof(self._arg)
 
     @property
@@ -113,6 +128,10 @@ def new_cache(n_blocks: int, heads: int, dim: int, *, block: int = 64, kind: int
     def z(*shape, dtype=torch.int8):
         return torch.zeros(shape, dtype=dtype, device=device)
 
+    if kind == E2M1:
+        codes, exps = (n_blocks, heads, block, dim // 2), (n_blocks, heads, dim // 32, block)
+        return Cache(*(torch.zeros(codes, dtype=torch.uint8, device=device) for _ in range(2)),
+                     *(torch.full(exps, 127, dtype=torch.uint8, device=device) for _ in range(2)), kind=kind)
     return Cache(z(n_blocks, heads, block, dim, dtype=torch.uint8),
                  z(n_blocks, heads, dim, block, dtype=torch.uint8), z(n_blocks, heads),
                  z(n_blocks, heads), z(n_blocks, heads, dim), z(n_blocks, heads), kind=kind)

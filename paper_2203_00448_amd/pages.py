@@ -1,0 +1,164 @@
+"""Python binding of the blocks given to requests (mp_kv_extend, mp_kv_release of
+libmemoplan.so): argument marshalling only, like kv.py.
+
+A program keeps a `Pool` (block ids, and how many of them are taken), its block table, its
+lengths, a `Step` (what the calls of a step read), a status word and a workspace.  `release` takes
+back the blocks of requests that ended, `extend` gives blocks to the new tokens of the others and
+makes the step's lengths, row bounds, positions and slots; nothing waits for the host, so both
+can be recorded in a graph.  Each runs on `stream` (the current one of the pool's device if not
+given), whichever device is current; tensors that are in use on another stream are the caller's to
+wait for.  Outputs are written in place: `length` and the pool's counter too, if no others are given.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import binding, kv
+from .binding import _finish, new_status  # noqa: F401
+from .kv import _need
+
+_lib = None
+
+
+def load_library():
+    """The library with these entry points declared."""
+    global _lib
+    if _lib is None:
+        L = binding.load_library()
+        p, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+        L.mp_kv_extend.argtypes = [p, i64, p, p, i64, i64, i32, p, p, i64, i64, p, p, p, p, p, p, sz, p, p]
+        L.mp_kv_extend.restype = i32
+        L.mp_kv_release.argtypes = [p, i64, p, p, i64, i64, i32, p, p, i64, p, p, p, sz, p, p]
+        L.mp_kv_release.restype = i32
+        L.mp_kv_pages_workspace_size.argtypes = [i64]
+        L.mp_kv_pages_workspace_size.restype = sz
+        _lib = L
+    return _lib
+
+
+def _vector(t, dtypes, name, n, index):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtypes or t.shape != (n,):
+        _need(t, dtypes, name, (n,))
+    if not t.is_contiguous() or t.get_device() != index:
+        raise ValueError(f"{name} must be contiguous and on the device of the pool")
+    return t.data_ptr() or None
+
+
+class Pool:
+    """Block ids int32 [n] and how many of them are taken, int64 [1]: ids[:used] are, the rest is given
+    out in order.  Two handles may share `ids`."""
+
+    def __init__(self, ids, used):
+        _need(ids, (torch.int32,), "ids")
+        _need(used, (torch.int64,), "used", (1,))
+        if ids.dim() != 1 or not ids.is_contiguous() or used.device != ids.device:
+            raise ValueError("ids must be a contiguous vector, on the device of used")
+        self.ids, self.used = ids, used
+        self.device, self.index = ids.device, ids.get_device()
+
+
+def new_pool(n_blocks: int, *, device="cuda") -> Pool:
+    """Blocks 0 to n_blocks - 1, all free."""
+    return Pool(torch.arange(n_blocks, dtype=torch.int32, device=device),
+                torch.zeros(1, dtype=torch.int64, device=device))
+
+
+class Step:
+    """What the calls of a step read: length int32 [n_seqs], begin int64 [n_seqs + 1], position int32
+    [tokens], slot int64 [tokens]."""
+
+    def __init__(self, length, begin, position, slot):
+        self.length, self.begin, self.position, self.slot = length, begin, position, slot
+
+
+def new_step(n_seqs: int, tokens: int, *, device="cuda") -> Step:
+    """A step of at most `tokens` new tokens."""
+    def z(n, dtype):
+        return torch.zeros(n, dtype=dtype, device=device)
+
+    return Step(z(n_seqs, torch.int32), z(n_seqs + 1, torch.int64), z(tokens, torch.int32), z(tokens, torch.int64))
+
+
+def workspace(n_seqs: int, *, device="cuda"):
+    """A new workspace of mp_kv_pages_workspace_size bytes."""
+    return torch.empty(int(load_library().mp_kv_pages_workspace_size(n_seqs)), dtype=torch.uint8, device=device)
+
+
+def _space(n, workspace, pool):
+    if workspace is None:
+        workspace = globals()["workspace"](n, device=pool.device)
+    elif not workspace.is_cuda:
+        raise TypeError("workspace must be a CUDA (HIP) tensor")
+    elif not workspace.is_contiguous() or workspace.get_device() != pool.index:
+        raise ValueError("workspace must be contiguous and on the device of the pool")
+    return workspace
+
+
+def _table(table, n, index):
+    _need(table, (torch.int32,), "table")
+    if table.dim() != 2 or table.shape[0] != n or table.get_device() != index:
+        raise ValueError("table must be [n_seqs, width], on the device of the pool")
+    width = table.shape[1]
+    if width > 1 and table.stride(1) != 1:
+        raise ValueError("a row of table must be contiguous")
+    if n > 1 and table.stride(0) < width:
+        raise ValueError("rows of table must not share places")
+    return table.data_ptr() or None, max(width, table.stride(0)), width
+
+
+def extend(pool: Pool, table, length, more, *, block: int = 64, step: Step, length_out=None, used_out=None,
+           status=None, workspace=None, check: bool = True, stream=None) -> Step:
+    """Give blocks to more int32 [n_seqs] new tokens of sequences that hold `length` int32 [n_seqs]
+    (mp_kv_extend): entries of table int32 [n_seqs, width] and the pool's counter are written in place, the lengths
+    to length_out (`length` if not given), the rest to `step`, which is returned. """
+    if stream is not None or kv._device() != pool.index:  # a launch would be the current device's
+        with kv._current(pool, stream):
+            return extend(pool, table, length, more, block=block, step=step, length_out=length_out,
+                          used_out=used_out, status=status, workspace=workspace, check=check)
+    L = load_library()
+    n = length.numel()
+    t, t_stride, width = _table(table, n, pool.index)
+    lengths = _vector(length, (torch.int32,), "length", n, pool.index)
+    new = _vector(more, (torch.int32,), "more", n, pool.index)
+    out = lengths if length_out is None else _vector(length_out, (torch.int32,), "length_out", n, pool.index)
+    used = pool.used.data_ptr()
+    used_to = used if used_out is None else _vector(used_out, (torch.int64,), "used_out", 1, pool.index)
+    begin = _vector(step.begin, (torch.int64,), "step.begin", n + 1, pool.index)
+    room = step.slot.numel()
+    position = _vector(step.position, (torch.int32,), "step.position", room, pool.index)
+    slot = _vector(step.slot, (torch.int64,), "step.slot", room, pool.index)
+    space = _space(n, workspace, pool)
+    status = kv._word(status, pool)
+    rc = L.mp_kv_extend(pool.ids.data_ptr() or None, pool.ids.numel(), used, t, t_stride, width, block, lengths,
+                        new, n, room, out, used_to, begin, position, slot, space.data_ptr(), space.nbytes,
+                        status.data_ptr(), kv._stream(pool.index))
+    _finish(rc, status, "pages.extend", check)
+    return step
+
+
+def release(pool: Pool, table, length, done, *, block: int = 64, length_out=None, used_out=None, status=None,
+            workspace=None, check: bool = True, stream=None):
+    """Take back the blocks of the sequences with done bool or uint8 [n_seqs] set (mp_kv_release): the pool's
+    ids and counter are written in place, the lengths (0 for these) to length_out, `length` if not given.
+    Returns length_out."""
+    if stream is not None or kv._device() != pool.index:  # a launch would be the current device's
+        with kv._current(pool, stream):
+            return release(pool, table, length, done, block=block, length_out=length_out, used_out=used_out,
+                           status=status, workspace=workspace, check=check)
+    L = load_library()
+    n = length.numel()
+    t, t_stride, width = _table(table, n, pool.index)
+    lengths = _vector(length, (torch.int32,), "length", n, pool.index)
+    ended = _vector(done, (torch.bool, torch.uint8), "done", n, pool.index)
+    out = lengths if length_out is None else _vector(length_out, (torch.int32,), "length_out", n, pool.index)
+    used = pool.used.data_ptr()
+    used_to = used if used_out is None else _vector(used_out, (torch.int64,), "used_out", 1, pool.index)
+    space = _space(n, workspace, pool)
+    status = kv._word(status, pool)
+    rc = L.mp_kv_release(pool.ids.data_ptr() or None, pool.ids.numel(), used, t, t_stride, width, block, lengths,
+                         ended, n, out, used_to, space.data_ptr(), space.nbytes, status.data_ptr(),
+                         kv._stream(pool.index))
+    _finish(rc, status, "pages.release", check)
+    return length if length_out is None else length_out
