@@ -114,7 +114,7 @@ __device__ __forceinline__ void query_pieces(const KvAttend& k, const float (&x)
 // of quarter g then has the scores of tokens [16 g, + 16), four in a row from the four tiles.  Of the
 // values it reads those tokens' dims [D/16 n, + D/16): row n of the second product's tile t is dim D/16 n + t.
 template <int D, int PIECES, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void kv4_rows_kernel(KvAttend k) {
+__global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : WAVES == 8 || (D == 128 && PIECES == 2) ? 2 : 3) void kv4_rows_kernel(KvAttend k) {
     constexpr int KD = D / 4, KS = KD / 8;  // dims of a lane's keys; steps of the first product
     constexpr int VD = D / 16;              // dims of a lane's values
     constexpr int KE = D == 256 ? 2 : 1;    // scales of a lane's dims of a key
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void
     const int head = (int)(blockIdx.x % heads);
     // chunks slowest: workgroups go to the XCDs in turn, and first chunks, which every row group
     // has, must not all meet one of them
-    const uint32_t rest = blockIdx.x / heads, units = (uint32_t)k.shape.units, chunk = rest / units;
+    const uint32_t rest = blockIdx.x / heads, units = (uint32_t)k.shape.units, chunk = n_chunks - 1 - rest / units;
     RowGroup rg;
     if (!row_group(k, rest % units, &rg)) return;
     const int64_t last_row = min((int64_t)rg.n_rows, rg.row0 + 16) - 1;
@@ -276,32 +276,33 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void
         for (int half = 0; half < 2; ++half) {
             bf8_t hi, lo;
             split8(s + 8 * half, &hi, &lo);
-            // two tokens' dims d and d + 1 as they come, to two dims of two tokens
-            Words8 f[VD];
+            float scale[8];
 #pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-                const int at = 8 * half + j;
-                const float sa = scale_of(e[at / 4], at % 4), sb = scale_of(e[at / 4], at % 4 + 1);
-                const auto turn = [&](auto sel, int word, int d) {
-                    const uint32_t ta = pair_of<decltype(sel)::value>(vw[at][word], sa);
-                    const uint32_t tb = pair_of<decltype(sel)::value>(vw[at + 1][word], sb);
-                    f[d].w[j / 2] = __builtin_amdgcn_perm(tb, ta, 0x05040100u);
-                    f[d + 1].w[j / 2] = __builtin_amdgcn_perm(tb, ta, 0x07060302u);
-                };
+            for (int j = 0; j < 8; ++j) scale[j] = scale_of(e[2 * half + j / 4], j % 4);
+            // two dims at a time: of each token a byte, of two tokens' bytes each dim's pair
+            const auto dims = [&](auto sel, int word, int d) {
+                Words8 f[2];
 #pragma unroll
-                for (int word = 0; word < (VD > 8 ? 2 : 1); ++word) {
-                    turn(std::integral_constant<int, 0>(), word, 8 * word);
-                    turn(std::integral_constant<int, 1>(), word, 8 * word + 2);
-                    if constexpr (VD >= 8) {
-                        turn(std::integral_constant<int, 2>(), word, 8 * word + 4);
-                        turn(std::integral_constant<int, 3>(), word, 8 * word + 6);
-                    }
+                for (int j = 0; j < 8; j += 2) {
+                    const uint32_t ta = pair_of<decltype(sel)::value>(vw[8 * half + j][word], scale[j]);
+                    const uint32_t tb = pair_of<decltype(sel)::value>(vw[8 * half + j + 1][word], scale[j + 1]);
+                    f[0].w[j / 2] = __builtin_amdgcn_perm(tb, ta, 0x05040100u);
+                    f[1].w[j / 2] = __builtin_amdgcn_perm(tb, ta, 0x07060302u);
                 }
-            }
 #pragma unroll
-            for (int t = 0; t < VD; ++t) {
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[t].v, hi, acc[t], 0, 0, 0);
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[t].v, lo, acc[t], 0, 0, 0);
+                for (int i = 0; i < 2; ++i) {
+                    acc[d + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[i].v, hi, acc[d + i], 0, 0, 0);
+                    acc[d + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[i].v, lo, acc[d + i], 0, 0, 0);
+                }
+            };
+#pragma unroll
+            for (int word = 0; word < (VD > 8 ? 2 : 1); ++word) {
+                dims(std::integral_constant<int, 0>(), word, 8 * word);
+                dims(std::integral_constant<int, 1>(), word, 8 * word + 2);
+                if constexpr (VD >= 8) {
+                    dims(std::integral_constant<int, 2>(), word, 8 * word + 4);
+                    dims(std::integral_constant<int, 3>(), word, 8 * word + 6);
+                }
             }
         }
         if (more) {
@@ -609,12 +610,253 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_tiles_kernel(KvAtte
     store_rows<D>(k, row, chunk, acc, m, l, h);
 }
 
+// Many rows, heads of 128: two teams of four waves, 32 rows each wave, over one key head and one chunk
+// of tokens in tiles of 64.  Of a SIMD's two waves one is of each team, and the teams take turns: while one
+// is at its matrix products (the last tile's second one, this tile's first) the other is at its softmax; a
+// barrier ends a turn.
+//
+// A team's half of the conversion and of the loads for the next tiles goes between its matrix
+// instructions: in the turn of the first product of tile i the keys of tile i + 1 and the values of tile i are
+// put into LDS, loaded in the turn before, and keys i + 2 and values i + 1 are loaded.  With team 0 at tile i in
+// turn 2 i and team 1 in turn 2 i + 1, keys i are read in these two turns and values i in the next two: each
+// is whole the turn before, and two tiles' room is enough for both.
+template <int PIECES>
+__global__ __launch_bounds__(512, 2) void kv4_pair_kernel(KvAttend k) {
+    constexpr int D = 128, KS = D / 16, DT = D / 32, GROUPS = D / 32;
+    extern __shared__ __align__(16) char lds_raw[];
+    Tile4<D>* const lds = reinterpret_cast<Tile4<D>*>(lds_raw);
+    const int tid = threadIdx.x & 255, lane = tid & 63, n = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), team = wave >> 2;
+    const KvArgs& a = k.a;
+    if (blockIdx.x == 0) kv_check_begin(a);
+    // key heads fastest: workgroups of one head share an XCD's L2 where 8 and the number of
+    // heads divide
+    const uint32_t heads = a.c.heads, n_chunks = (uint32_t)k.shape.n_chunks;
+    const int head = (int)(blockIdx.x % heads);
+    const uint32_t rest = blockIdx.x / heads, chunk = rest % n_chunks;
+    RowGroup rg;
+    if (!tile_group<256>(k, rest / n_chunks, &rg)) return;
+    const int32_t most = row_of(k, rg, head, min((int64_t)rg.n_rows, rg.row0 + 256) - 1).last;
+    const int64_t start = chunk * k.shape.chunk;
+    if (chunk > 0 && start > most) return;
+    const int32_t x0 = (int32_t)start;
+    const int32_t x1 = (int32_t)min((int64_t)most + 1, start + k.shape.chunk);
+    const int32_t tiles = (x1 - x0 + 63) >> 6;  // 0 where no row sees anything
+
+    // this wave's rows, and the last position that all of them see
+    const int64_t wave_row0 = rg.row0 + 32 * wave;
+    const bool awake = wave_row0 < rg.n_rows;  // has rows
+    const int32_t wave_least = row_of(k, rg, head, wave_row0).last;
+    const Row row = row_of(k, rg, head, wave_row0 + n);
+
+    // a thread moves 16 dims of a token's keys (r 0) and of its values (r 1); table entries are read a
+    // tile ahead of the loads, keys a tile ahead of values
+    const int lb = a.log_block, block = 1 << lb;
+    const uint32_t page_size = heads * (uint32_t)(D / 2) << lb, exp_size = heads * (uint32_t)GROUPS << lb;
+    Pages pages = {a.s.table + rg.q.s * a.s.table_stride, (uint32_t)max(most, 0) >> lb,
+                   (uint32_t)a.c.n_blocks, 0};
+    const int token = team * 32 + tid / 8, piece = tid % 8 * 2;
+    const uint32_t slot = token & (block - 1);
+    const uint32_t code_at = (((uint32_t)head << lb) + slot) * (D / 2) + piece * 4;
+    const uint32_t exp_at = (((uint32_t)head * GROUPS + piece / 4) << lb) + slot;
+    uint2 codes[2] = {};
+    uint32_t exps[2] = {}, entry[2] = {};
+    auto tile_of = [&](int r, int v_tile) { return v_tile + 1 - r; };
+    auto find = [&](int r, int v_tile) {
+        entry[r] = pages.entry((uint32_t)(x0 + tile_of(r, v_tile) * 64 + token) >> lb);
+    };
+    auto load = [&](int r) {
+        const uint64_t page = pages.page(entry[r]);
+        codes[r] = *reinterpret_cast<const uint2*>((r ? a.c.v_code : a.c.k_code) + page * page_size + code_at);
+        exps[r] = (uint8_t)(r ? a.c.v_exp : a.c.k_exp)[page * exp_size + exp_at];
+    };
+    // places past the end may hold anything: a scale of one makes their values finite
+    auto put = [&](int r, int v_tile, int half) {
+        const int tile = tile_of(r, v_tile);
+        const uint32_t e = x0 + tile * 64 + token > most ? 127u : exps[r];
+        uint4* const to = r ? lds[tile & 1].v[token] : lds[tile & 1].k[token];
+        to[(piece + half) ^ (r ? v4_key<D>(token) : k4_key<D>(token))] =
+            __builtin_bit_cast(uint4, codes_to_bf(half ? codes[r].y : codes[r].x, __uint_as_float(e << 23)));
+    };
+    if (tiles > 0) {
+        find(0, -1);  // keys 0
+        load(0);
+        find(0, 0), find(1, 0);  // keys 1, values 0
+    }
+    bf8_t q[PIECES][KS];
+    float c;
+    {
+        uint4 raw[KS];
+#pragma unroll
+        for (int i = 0; i < KS; ++i) raw[i] = load8_16bit(k.q, row.token, row.head, i * 16 + h * 8);
+        float y[KS][8], top = 0.0f;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            to_float8(k.q, raw[i], y[i]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(y[i][j]));
+        }
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        query_pieces<PIECES>(k, y, top, q, &c);
+    }
+    float16_t acc[DT], s[2];
+#pragma unroll
+    for (int t = 0; t < DT; ++t) acc[t] = float16_t{};
+    s[0] = s[1] = float16_t{};
+    bf8_t w[PIECES][4] = {};
+    float m = -INFINITY, l = 0.0f;
+
+    auto turn = [&]() {
+        __builtin_amdgcn_sched_barrier(0);
+        __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // Piece `p` of a team's moving of data in the turn of tile i's first product: four pieces put keys
+    // i + 1 and values i, the others load the ones after.
+    constexpr int kPieces = 8;
+    auto move = [&](int p, int i) {
+        if (p < 4)
+            put(p / 2, i, p % 2);
+        else if (p < 6)
+            load(p - 4);
+        else
+            find(p - 6, i + 2);
+    };
+    // Factors from LDS: keys of instruction step i, product t; values of step i, dims t.
+    const int k_token = (n & 0x13) | (n & 4) << 1 | (n & 8) >> 1, k_mine = h ^ k4_key<D>(k_token);
+    const int v_token = 8 * h + (lane >> 2 & 3), v_dim = (n & 16) + (lane & 3) * 4;
+    auto k_factor = [&](int tile, int i, int t) {
+        return __builtin_bit_cast(bf8_t, lds[tile & 1].k[t * 32 + k_token][k_mine ^ (i * 2)]);
+    };
+    auto v_factor = [&](int tile, int i, int t) {
+        union {
+            short4_t s[2];
+            bf8_t v;
+        } f;
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+            // the low bits of the token that exchange the pieces are a lane's own
+            const uint4* const at = &lds[tile & 1].v[i * 16 + 4 * z + v_token][((t * 32 + v_dim) >> 3) ^ v4_key<D>(v_token)];
+            f.s[z] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) short4_t*)(reinterpret_cast<const short4_t*>(at) + (v_dim >> 2 & 1)));
+        }
+        return f.v;
+    };
+    // The second product of tile i - 1 (SECOND) and the first of tile i (FIRST), factors read kAhead
+    // instructions ahead of their use: left to itself the compiler reads each just before.
+    auto products = [&](auto second, auto first_too, int i) {
+        constexpr int kSecond = second() ? 4 * DT : 0, kAll = kSecond + (first_too() ? 2 * KS : 0);
+        constexpr int kAhead = 6;
+        __builtin_amdgcn_s_setprio(1);  // the other wave's vector instructions fill what these leave
+        bf8_t f[kAhead];
+        auto factor = [&](int j) {
+            return j < kSecond ? v_factor(i - 1, j / DT, j % DT) : k_factor(i, (j - kSecond) / 2, (j - kSecond) % 2);
+        };
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) f[j] = factor(j);
+        __builtin_amdgcn_sched_barrier(0);
+        if (first_too()) s[0] = s[1] = float16_t{};
+#pragma unroll
+        for (int j = 0; j < kAll; ++j) {
+            const bf8_t use = f[j % kAhead];
+#pragma unroll
+            for (int p = 0; p < PIECES; ++p) {
+                if (j < kSecond) {
+                    acc[j % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(use, w[p][j / DT], acc[j % DT], 0, 0, 0);
+                } else {
+                    const int z = j - kSecond;
+                    s[z % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(use, q[p][z / 2], s[z % 2], 0, 0, 0);
+                }
+            }
+            if (j + kAhead < kAll) f[j % kAhead] = factor(j + kAhead);
+            if (first_too() && j % 2 == 1 && j / 2 < kPieces) move(j / 2, i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+        if (first_too())
+#pragma unroll
+            for (int p = kAll / 2; p < kPieces; ++p) move(p, i);
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+
+    // keys 0 put before the first turn; then keys 1 and values 0 on their way
+    if (tiles > 0) {
+        put(0, -1, 0), put(0, -1, 1);
+        load(0), load(1);
+        find(0, 1), find(1, 1);
+    }
+    turn();
+    if (team) turn();
+    if (!awake) {  // only moves data
+        for (int tile = 0; tile < tiles; ++tile) {
+            for (int p = 0; p < kPieces; ++p) move(p, tile);
+            turn();
+            turn();
+        }
+        if (!team) turn();
+        if (pages.bad()) raise_status(a.status, MP_EINVAL);
+        return;
+    }
+    if (tiles > 0) products(No{}, Yes{}, 0);
+    for (int tile = 0; tile < tiles; ++tile) {
+        const int32_t x = x0 + tile * 64;
+        turn();
+        // register r of product t is token 32 t + 16 (r / 8) + 8 h + r % 8
+        if (x + 63 > wave_least) {
+            const int seen = row.last - x - h * 8;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    s[t][r] = t * 32 + (r >> 3) * 16 + (r & 7) > seen ? -INFINITY : s[t][r];
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 32; ++r) top = fmaxf(top, s[r / 16][r % 16]);
+        {
+            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+        }
+        const float new_m = fmaxf(m, top * c + kBelow);
+        if (__any(new_m - m > kSlack)) {
+            const float fall = __builtin_amdgcn_exp2f(m - (new_m == -INFINITY ? 0.0f : new_m));
+#pragma unroll
+            for (int t = 0; t < DT; ++t) acc[t] *= fall;
+            l *= fall;
+            m = new_m;
+        }
+        const float from = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float e[8], sum = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 2][i % 2 * 8 + r], c, -from));
+                sum += e[r];
+            }
+            l += sum;
+            if constexpr (PIECES == 1)
+                w[0][i] = round8(e);
+            else
+                split8(e, &w[0][i], &w[1][i]);
+        }
+        turn();
+        products(Yes{}, Yes{}, tile + 1);  // the last one's scores are of no tile
+    }
+    if (!team) turn();
+    if (pages.bad()) raise_status(a.status, MP_EINVAL);
+    store_rows<D>(k, row, chunk, acc, m, l, h);
+}
+
 template <int D, int PIECES>
 hipError_t launch_d(const KvAttend& k, hipStream_t st) {
     const KvAttendShape& sh = k.shape;
     const dim3 grid((uint32_t)(sh.units * k.a.c.heads * sh.n_chunks));
     constexpr int kLds = 2 * sizeof(Tile4<D>);
-    if (sh.form == KvForm::tiles) {
+    if (sh.form == KvForm::pair) {  // heads of 128
+        kv4_pair_kernel<PIECES><<<grid, 512, 2 * sizeof(Tile4<128>), st>>>(k);
+    } else if (sh.form == KvForm::tiles) {
         if (kLds > 65536)
             if (hipError_t e = hipFuncSetAttribute((const void*)kv4_tiles_kernel<D, PIECES>,
                                                    hipFuncAttributeMaxDynamicSharedMemorySize, kLds);

@@ -1218,7 +1218,7 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     if (keep > 0 || !s.begin || piece <= 16 || (piece <= 64 && s.longest > 512))
         sh.form = KvForm::rows;
     else
-        sh.form = c.dim == 128 && piece >= 4096 && c.kind != MP_KV_E2M1 ? KvForm::pair : KvForm::tiles;
+        sh.form = c.dim == 128 && piece >= 4096 ? KvForm::pair : KvForm::tiles;
     sh.rows = sh.form == KvForm::rows ? 16 : sh.form == KvForm::tiles ? 128 : 256;
     const int64_t per = (group + sh.rows - 1) / sh.rows;
     if (keep > 0)
@@ -1238,6 +1238,11 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     // chunks 290 us (559 in chunks of 2048: the partial results are 32-bit).
     const int64_t wide = sh.units * c.heads;
     int64_t chunk = longest < ((int64_t)2048 * 256) / (wide > 0 ? wide : 1) ? longest * wide / 256 : 2048;
+    // In 4 bits two workgroups a compute unit are one round of a launch: where chunks up to 4096 make that
+    // many, those.  Measured with 1024 / 2048 / 4096: two sequences of 131072 75 / 63 / 59 us; 64 of 1-16384 tokens,
+    // which are more, 104 / 95 / 99.
+    if (c.kind == MP_KV_E2M1 && wide > 0 && chunk == 2048 && longest <= (int64_t)4096 * 512 / wide)
+        chunk = longest * wide / 512;
     if (chunk < 512) chunk = 512;
     if (longest <= 1024) chunk = 1024;
     if (sh.form != KvForm::rows) {
