@@ -38,10 +38,12 @@ def load_library():
     return _lib
 
 
-def _vector(t, dtypes, name, n, index):
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtypes or t.shape != (n,):
-        _need(t, dtypes, name, (n,))
-    if not t.is_contiguous() or t.get_device() != index:
+def _vector(t, dtype, name, n, index):
+    """A vector's address.  These calls are short beside what a launch costs, so their checks look at each
+    property once."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_cuda or t.shape != (n,):
+        _need(t, (dtype,), name, (n,))
+    if t.get_device() != index or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous and on the device of the pool")
     return t.data_ptr() or None
 
@@ -57,6 +59,7 @@ class Pool:
             raise ValueError("ids must be a contiguous vector, on the device of used")
         self.ids, self.used = ids, used
         self.device, self.index = ids.device, ids.get_device()
+        self._at = (ids.data_ptr() or None, ids.numel(), used.data_ptr())
 
 
 def new_pool(n_blocks: int, *, device="cuda") -> Pool:
@@ -91,21 +94,23 @@ def _space(n, workspace, pool):
         workspace = globals()["workspace"](n, device=pool.device)
     elif not workspace.is_cuda:
         raise TypeError("workspace must be a CUDA (HIP) tensor")
-    elif not workspace.is_contiguous() or workspace.get_device() != pool.index:
+    elif workspace.get_device() != pool.index or not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous and on the device of the pool")
     return workspace
 
 
 def _table(table, n, index):
-    _need(table, (torch.int32,), "table")
-    if table.dim() != 2 or table.shape[0] != n or table.get_device() != index:
+    if not isinstance(table, torch.Tensor) or table.dtype is not torch.int32 or not table.is_cuda:
+        _need(table, (torch.int32,), "table")
+    shape = table.shape
+    if len(shape) != 2 or shape[0] != n or table.get_device() != index:
         raise ValueError("table must be [n_seqs, width], on the device of the pool")
-    width = table.shape[1]
-    if width > 1 and table.stride(1) != 1:
+    width, (stride, step) = shape[1], table.stride()
+    if width > 1 and step != 1:
         raise ValueError("a row of table must be contiguous")
-    if n > 1 and table.stride(0) < width:
+    if n > 1 and stride < width:
         raise ValueError("rows of table must not share places")
-    return table.data_ptr() or None, max(width, table.stride(0)), width
+    return table.data_ptr() or None, max(width, stride), width
 
 
 def extend(pool: Pool, table, length, more, *, block: int = 64, step: Step, length_out=None, used_out=None,
@@ -118,22 +123,21 @@ def extend(pool: Pool, table, length, more, *, block: int = 64, step: Step, leng
             return extend(pool, table, length, more, block=block, step=step, length_out=length_out,
                           used_out=used_out, status=status, workspace=workspace, check=check)
     L = load_library()
-    n = length.numel()
-    t, t_stride, width = _table(table, n, pool.index)
-    lengths = _vector(length, (torch.int32,), "length", n, pool.index)
-    new = _vector(more, (torch.int32,), "more", n, pool.index)
-    out = lengths if length_out is None else _vector(length_out, (torch.int32,), "length_out", n, pool.index)
-    used = pool.used.data_ptr()
-    used_to = used if used_out is None else _vector(used_out, (torch.int64,), "used_out", 1, pool.index)
-    begin = _vector(step.begin, (torch.int64,), "step.begin", n + 1, pool.index)
+    n, index = length.numel(), pool.index
+    t, t_stride, width = _table(table, n, index)
+    lengths = _vector(length, torch.int32, "length", n, index)
+    new = _vector(more, torch.int32, "more", n, index)
+    out = lengths if length_out is None else _vector(length_out, torch.int32, "length_out", n, index)
+    ids, n_ids, used = pool._at
+    used_to = used if used_out is None else _vector(used_out, torch.int64, "used_out", 1, index)
+    begin = _vector(step.begin, torch.int64, "step.begin", n + 1, index)
     room = step.slot.numel()
-    position = _vector(step.position, (torch.int32,), "step.position", room, pool.index)
-    slot = _vector(step.slot, (torch.int64,), "step.slot", room, pool.index)
+    position = _vector(step.position, torch.int32, "step.position", room, index)
+    slot = _vector(step.slot, torch.int64, "step.slot", room, index)
     space = _space(n, workspace, pool)
     status = kv._word(status, pool)
-    rc = L.mp_kv_extend(pool.ids.data_ptr() or None, pool.ids.numel(), used, t, t_stride, width, block, lengths,
-                        new, n, room, out, used_to, begin, position, slot, space.data_ptr(), space.nbytes,
-                        status.data_ptr(), kv._stream(pool.index))
+    rc = L.mp_kv_extend(ids, n_ids, used, t, t_stride, width, block, lengths, new, n, room, out, used_to, begin,
+                        position, slot, space.data_ptr(), space.nbytes, status.data_ptr(), kv._stream(index))
     _finish(rc, status, "pages.extend", check)
     return step
 
@@ -148,17 +152,19 @@ def release(pool: Pool, table, length, done, *, block: int = 64, length_out=None
             return release(pool, table, length, done, block=block, length_out=length_out, used_out=used_out,
                            status=status, workspace=workspace, check=check)
     L = load_library()
-    n = length.numel()
-    t, t_stride, width = _table(table, n, pool.index)
-    lengths = _vector(length, (torch.int32,), "length", n, pool.index)
-    ended = _vector(done, (torch.bool, torch.uint8), "done", n, pool.index)
-    out = lengths if length_out is None else _vector(length_out, (torch.int32,), "length_out", n, pool.index)
-    used = pool.used.data_ptr()
-    used_to = used if used_out is None else _vector(used_out, (torch.int64,), "used_out", 1, pool.index)
+    n, index = length.numel(), pool.index
+    t, t_stride, width = _table(table, n, index)
+    lengths = _vector(length, torch.int32, "length", n, index)
+    if done.dtype is torch.uint8:
+        ended = _vector(done, torch.uint8, "done", n, index)
+    else:
+        ended = _vector(done, torch.bool, "done", n, index)
+    out = lengths if length_out is None else _vector(length_out, torch.int32, "length_out", n, index)
+    ids, n_ids, used = pool._at
+    used_to = used if used_out is None else _vector(used_out, torch.int64, "used_out", 1, index)
     space = _space(n, workspace, pool)
     status = kv._word(status, pool)
-    rc = L.mp_kv_release(pool.ids.data_ptr() or None, pool.ids.numel(), used, t, t_stride, width, block, lengths,
-                         ended, n, out, used_to, space.data_ptr(), space.nbytes, status.data_ptr(),
-                         kv._stream(pool.index))
+    rc = L.mp_kv_release(ids, n_ids, used, t, t_stride, width, block, lengths, ended, n, out, used_to,
+                         space.data_ptr(), space.nbytes, status.data_ptr(), kv._stream(index))
     _finish(rc, status, "pages.release", check)
     return length if length_out is None else length_out

@@ -15,7 +15,7 @@ import torch
 
 from . import binding, kv
 from .binding import MP_OK, PlanError
-from .kv import _MOVED, _RowsArg, _need, _rows
+from .kv import _MOVED, _need, _rows
 
 _lib = None
 
@@ -79,6 +79,7 @@ class Rotation:
             magnitude = 0.1 * math.log(factor) + 1.0 if scaling == "blend" else 1.0
         self.freq, self.turned, self.pairs, self.magnitude = freq, turned, bool(pairs), float(magnitude)
         self.device, self.index = freq.device, freq.get_device()
+        self._freq = freq.data_ptr()
 
 
 def rotate(rotation: Rotation, position, q, k=None, *, out=None, k_out=None, inverse: bool = False, stream=None):
@@ -89,29 +90,35 @@ def rotate(rotation: Rotation, position, q, k=None, *, out=None, k_out=None, inv
         with kv._current(rotation, stream):
             return rotate(rotation, position, q, k, out=out, k_out=k_out, inverse=inverse)
     L = load_library()
-    if q.dim() != 3 or (k is not None and k.dim() != 3):
+    shape = q.shape
+    if len(shape) != 3 or (k is not None and k.dim() != 3):
         raise ValueError("q and k must be [tokens, heads, dim]")
     if k is None and k_out is not None:
         raise ValueError("k_out needs k")
     index = rotation.index
-    n, heads, dim = q.shape
-    _need(position, (torch.int32,), "position", (n,))
-    if not position.is_contiguous() or position.get_device() != index:
+    n, heads, dim = shape
+    if not isinstance(position, torch.Tensor) or position.dtype is not torch.int32 or position.shape != (n,):
+        _need(position, (torch.int32,), "position", (n,))
+    if position.get_device() != index or not position.is_contiguous():
         raise ValueError("position must be contiguous and on the device of the rotation")
-    qa = _rows(q, "q", q.shape, _MOVED, index)
+    dtypes = (q.dtype,)
+    qa = _rows(q, "q", shape, _MOVED, index)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    oa = _rows(out, "out", q.shape, (q.dtype,), index)
-    ka, koa, k_heads = _RowsArg(), _RowsArg(), 0
+        out = torch.empty(shape, dtype=q.dtype, device=q.device)
+    oa = _rows(out, "out", shape, dtypes, index)
+    ka = koa = None
+    k_heads = 0
     if k is not None:
         k_heads = k.shape[1]
-        ka = _rows(k, "k", (n, k_heads, dim), (q.dtype,), index)
+        shape = (n, k_heads, dim)
+        ka = _rows(k, "k", shape, dtypes, index)
         if k_out is None:
-            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-        koa = _rows(k_out, "k_out", k.shape, (q.dtype,), index)
-    rc = L.mp_rotate(position.data_ptr() or None, n, rotation.freq.data_ptr(), rotation.turned, int(rotation.pairs),
-                     rotation.magnitude, int(inverse), dim, ctypes.addressof(qa), heads, ctypes.addressof(oa),
-                     ctypes.addressof(ka), k_heads, ctypes.addressof(koa), kv._stream(index))
+            k_out = torch.empty(shape, dtype=k.dtype, device=k.device)
+        koa = _rows(k_out, "k_out", shape, dtypes, index)
+    at = ctypes.addressof
+    rc = L.mp_rotate(position.data_ptr() or None, n, rotation._freq, rotation.turned, rotation.pairs,
+                     rotation.magnitude, inverse, dim, at(qa), heads, at(oa), ka and at(ka), k_heads,
+                     koa and at(koa), kv._stream(index))
     if rc != MP_OK:
         raise PlanError(rc, "rotary.rotate")
     return out if k is None else (out, k_out)
