@@ -1,11 +1,11 @@
-"""A decode step in planned memory: a few attention layers over 8-bit caches, whose
+"""A decode step in planned memory: a few attention layers over caches in 8 or 4 bits, whose
 intermediates are planned once, from the trace of one step, and then live at
 their offsets of one slab for every step.
 
 The trace has what a step makes and drops: the projected rows, the selected
 blocks, the attention's result, the operators' workspaces, the hidden states between
 layers.  What outlives the step is not in it: the caches, which grow by a token a step, are
-held in blocks (kv.py), and the last hidden state, which the caller may keep or pass to
+held in blocks (kv.py), their tables and lengths (pages.py), and the last hidden state, which the caller may keep or pass to
 the next step, has memory of its own.  The operators write into the planned views, so a step
 allocates nothing and can be recorded in a graph.
 
@@ -17,18 +17,24 @@ import sys
 
 import torch
 
-from . import binding, kv
+from . import binding, kv, pages, rotary
 
 
 class DecodeStep:
     """`layers` attention layers with projections, one token of `n_seqs` sequences a step.
 
+    keep: blocks that a query reads, 0 for all (a cache in 4 bits, kind E2M1, always has all).
+    rotation: a rotary.Rotation by which queries and keys are turned, in place, before they are used.
+    paged: blocks are taken from a pool as sequences grow, and `retire` gives back those of sequences that
+    ended; otherwise every sequence has its blocks from the start.
     planned=False gives every intermediate memory of its own: the same step, for comparison."""
 
     def __init__(self, *, layers=4, n_seqs=8, hidden=512, q_heads=8, heads=2, dim=64, block=16, keep=8,
-                 longest=1024, kind=kv.E4M3, planned=True, seed=0):
+                 longest=1024, kind=kv.E4M3, planned=True, seed=0, rotation=None, paged=False):
         self.layers, self.n_seqs, self.hidden = layers, n_seqs, hidden
-        self.q_heads, self.heads, self.dim, self.keep = q_heads, heads, dim, keep
+        self.q_heads, self.heads, self.dim = q_heads, heads, dim
+        self.keep = 0 if kind == kv.E2M1 else keep
+        self.rotation, self.paged = rotation, paged
         gen = torch.Generator(device="cuda").manual_seed(seed)
 
         def weight(*shape):
@@ -41,7 +47,15 @@ class DecodeStep:
         self.caches = [kv.new_cache(n_seqs * width, heads, dim, block=block, kind=kind) for _ in range(layers)]
         order = torch.randperm(n_seqs * width, generator=gen, device="cuda").to(torch.int32)
         self.length = torch.zeros(n_seqs, dtype=torch.int32, device="cuda")
-        self.seqs = kv.Seqs(order.view(n_seqs, width), self.length, longest=longest)
+        self.table = order.view(n_seqs, width)
+        if paged:
+            self.pool = pages.Pool(order, torch.zeros(1, dtype=torch.int64, device="cuda"))
+            self.table = torch.full((n_seqs, width), -1, dtype=torch.int32, device="cuda")
+            self.pages_space = pages.workspace(n_seqs)
+        # what a step is about: a token more of each sequence, at which positions and places
+        self.more = torch.ones(n_seqs, dtype=torch.int32, device="cuda")
+        self.step = pages.new_step(n_seqs, n_seqs)
+        self.seqs = kv.Seqs(self.table, self.length, longest=longest)
         self.status = kv.new_status()
         self._lay_out(planned)
 
@@ -50,12 +64,14 @@ class DecodeStep:
         n, out = self.n_seqs, []
         spaces = [kv.workspace_size(op, self.caches[0], self.seqs, q_heads=self.q_heads, keep=self.keep)
                   for op in (kv.OP_SELECT, kv.OP_ATTEND)]
+        listed = self.keep > 0
         for i in range(self.layers):
             project, _write, select, attend, merge = range(5 * i, 5 * i + 5)
-            out += [("rows", i, torch.bfloat16, (n, self.q_heads + 2 * self.heads, self.dim), project, attend),
-                    ("blocks", i, torch.int32, (n, self.heads, self.keep), select, attend),
-                    ("select_space", i, torch.uint8, (max(16, spaces[0]),), select, select),
-                    ("result", i, torch.bfloat16, (n, self.q_heads, self.dim), attend, merge),
+            out.append(("rows", i, torch.bfloat16, (n, self.q_heads + 2 * self.heads, self.dim), project, attend))
+            if listed:
+                out += [("blocks", i, torch.int32, (n, self.heads, self.keep), select, attend),
+                        ("select_space", i, torch.uint8, (max(16, spaces[0]),), select, select)]
+            out += [("result", i, torch.bfloat16, (n, self.q_heads, self.dim), attend, merge),
                     ("attend_space", i, torch.uint8, (max(16, spaces[1]),), attend, attend),
                     ("added", i, torch.bfloat16, (n, self.hidden), merge, merge)]
             if i < self.layers - 1:
@@ -95,23 +111,39 @@ class DecodeStep:
     def run(self, x):
         """One token of every sequence: x [n_seqs, hidden] in, the last layer's hidden state out.  That
         is one tensor for all steps: the next step's x may be it, and its end writes it again."""
-        self.length.add_(1)
+        if self.paged:
+            pages.extend(self.pool, self.table, self.length, self.more, block=self.caches[0].block, step=self.step,
+                         workspace=self.pages_space, status=self.status, check=False)
+        else:
+            self.length.add_(1)
+            if self.rotation is not None:
+                torch.sub(self.length, 1, out=self.step.position)
         for i, cache in enumerate(self.caches):
-            at = {name: self.at[name, i] for name in ("rows", "blocks", "select_space", "result", "attend_space",
-                                                      "merged", "added")}
+            at = {name: self.at.get((name, i)) for name in ("rows", "blocks", "select_space", "result",
+                                                            "attend_space", "merged", "added")}
             torch.mm(x, self.w_in[i], out=at["rows"].view(self.n_seqs, -1))
             q = at["rows"][:, :self.q_heads]
             k = at["rows"][:, self.q_heads:self.q_heads + self.heads]
             v = at["rows"][:, self.q_heads + self.heads:]
+            if self.rotation is not None:
+                rotary.rotate(self.rotation, self.step.position, q, k, out=q, k_out=k)
             kv.write(cache, self.seqs, k, v, status=self.status, check=False)
-            kv.select(cache, self.seqs, q, keep=self.keep, first=1, recent=2, out=at["blocks"],
-                      workspace=at["select_space"], status=self.status, check=False)
+            if self.keep:
+                kv.select(cache, self.seqs, q, keep=self.keep, first=1, recent=2, out=at["blocks"],
+                          workspace=at["select_space"], status=self.status, check=False)
             kv.attend(cache, self.seqs, q, blocks=at["blocks"], out=at["result"],
                       workspace=at["attend_space"], status=self.status, check=False)
             torch.mm(at["result"].view(self.n_seqs, -1), self.w_out[i], out=at["added"])
             torch.add(x, at["added"], out=at["merged"])
             x = at["merged"]
         return x
+
+    def retire(self, done):
+        """Sequences with done bool [n_seqs] set start anew; their blocks go back to the pool."""
+        if not self.paged:
+            raise ValueError("only blocks of a pool go back")
+        pages.release(self.pool, self.table, self.length, done, block=self.caches[0].block,
+                      workspace=self.pages_space, status=self.status, check=False)
 
     def check(self):
         """Waits for the steps so far and raises what any of their calls met."""
@@ -120,8 +152,9 @@ class DecodeStep:
             raise binding.PlanError(status, "decode step")
 
 
-def main(steps=300):
-    planned, apart = DecodeStep(), DecodeStep(planned=False)
+def compare(steps, what, **options):
+    """Steps in planned memory beside the same ones with memory of their own."""
+    planned, apart = DecodeStep(**options), DecodeStep(planned=False, **options)
     gen = torch.Generator(device="cuda").manual_seed(1)
     same = True
     for _ in range(steps):
@@ -130,10 +163,16 @@ def main(steps=300):
     planned.check()
     apart.check()
     cached = sum(c.nbytes for c in planned.caches)
-    print(f"{steps} steps of {planned.layers} layers: intermediates {planned.bytes} bytes planned, "
+    print(f"{what}: {steps} steps of {planned.layers} layers: intermediates {planned.bytes} bytes planned, "
           f"{planned.unplanned_bytes} apart; caches {cached} bytes; results "
           f"{'the same' if same else 'DIFFER'}")
     return same
+
+
+def main(steps=300):
+    same = compare(steps, "8 bits, selected blocks")
+    return compare(steps, "4 bits, rotary positions, blocks from a pool", kind=kv.E2M1, paged=True,
+                   rotation=rotary.Rotation(64)) and same
 
 
 if __name__ == "__main__":
