@@ -67,7 +67,7 @@ struct KvAttend {
 };
 
 KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t q_heads,
-                              int64_t keep);
+                              int64_t keep, int32_t dtype = MP_BF16);
 hipError_t launch_kv_attend(const KvAttend& a, hipStream_t st);
 
 struct KvSelect {

@@ -10,8 +10,13 @@
 // left to be followed: sizes that differ between tokens, groups or blocks cost nothing.  Queries are
 // brought to [2^-4, 2^-3) by a power of two per row, and weights lie 24 powers below one, so that no product
 // leaves the range of 32-bit floats.  A 16-bit float query is two bfloat16 pieces, which hold it
-// exactly.  Weights are two pieces (16 bits) where few rows share what is read, and where results are 16-bit
-// floats; one (8 bits, as the results have) in the tiles of bfloat16 rows, whose time is the products'.
+// exactly, and a weight two pieces (16 bits), where few rows share what is read and the products are
+// free beside it.  In tiles, whose time is the products', a weight has as many bits as the results: one piece
+// (8 bits) of bfloat16 rows; of rows of 16-bit floats such a float (11 bits), which takes codes and queries
+// as such floats too, as far as these hold them.
+//
+// The instructions that take codes of 4 bits with their scales as they are were not used: beside 8-bit factors
+// of different sizes their sums are off by up to 2^-11 of the largest product.
 //
 // Both products are taken transposed, S^T = K Q^T and O^T = V^T W^T: the weights come out of the first
 // in the lanes that the second one wants them in.
@@ -81,6 +86,30 @@ __device__ __forceinline__ bf8_t round8(const float* x) {
     return o.v;
 }
 
+// Eight codes at their scale as 16-bit floats, eight values as these, and the product of such or of bfloat16.
+__device__ __forceinline__ uint4 codes_to_f16(uint32_t w, float scale) {
+    return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3)));
+}
+__device__ __forceinline__ Words8 half8(const float* x) {
+    Words8 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const half2_t r = __builtin_convertvector((float2_t{x[2 * i], x[2 * i + 1]}), half2_t);
+        o.w[i] = __builtin_bit_cast(uint32_t, r);
+    }
+    return o;
+}
+template <bool F16>
+__device__ __forceinline__ float16_t product(const Words8& a, const Words8& b, float16_t c) {
+    if constexpr (F16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
+}
+
 // Values of a query, a row's largest `top`, as factors of the first product (PIECES of them); *scale what
 // their scores are multiplied by, not negative: the query takes the sign.
 template <int PIECES, int N>
@@ -132,8 +161,8 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : WAVES == 8 || (D == 128 
     RowGroup rg;
     if (!row_group(k, rest % units, &rg)) return;
     const int64_t last_row = min((int64_t)rg.n_rows, rg.row0 + 16) - 1;
-    const int32_t most = row_of(k, rg, head, last_row).last;  // the last position any row sees
-    const int32_t least = row_of(k, rg, head, rg.row0).last;  // all rows see up to here
+    const int32_t most = wave_one(row_of(k, rg, head, last_row).last);  // the last position any row sees
+    const int32_t least = wave_one(row_of(k, rg, head, rg.row0).last);  // all rows see up to here
     const int lb = a.log_block, block = 1 << lb;
     const int64_t start = chunk * k.shape.chunk, end_all = (int64_t)most + 1;
     if (chunk > 0 && start >= end_all) return;
@@ -428,12 +457,19 @@ __device__ __forceinline__ int v4_key(int token) {
     return D == 64 ? (token >> 1 & 1) << 2 : (token & 3) << 2;
 }
 
-template <int D, int PIECES>
+// F16, rows of 16-bit floats: the tile as 16-bit floats, so that one instruction holds a query's and a
+// weight's 11 bits.  A group of codes that these cannot hold exactly (scales outside 2^-23..2^13, codes not all zero)
+// marks its tile, and the workgroup takes a marked tile as bfloat16, with queries and weights in two pieces.
+// Heads of 256 have no registers for both: all their tiles are taken so.
+template <int D, bool F16>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_tiles_kernel(KvAttend k) {
     constexpr int KS = D / 16, DT = D / 32, GROUPS = D / 32;
     constexpr int UNITS = 128 * GROUPS / 256;  // groups of 32 dims that a thread moves in a tile, keys first
+    constexpr bool kPieces = F16 && D == 256;  // every tile
+    constexpr float kShift = F16 ? -10.0f : kBelow, kLag = F16 ? 4.0f : kSlack;  // weights of 16-bit floats reach 2^14
     extern __shared__ __align__(16) char lds_raw[];
     Tile4<D>* const lds = reinterpret_cast<Tile4<D>*>(lds_raw);
+    __shared__ int32_t marked[2];  // the first token of the last marked tile of each room
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const KvArgs& a = k.a;
@@ -445,7 +481,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_tiles_kernel(KvAtte
     const uint32_t rest = blockIdx.x / heads, chunk = rest % n_chunks;
     RowGroup rg;
     if (!tile_group<128>(k, rest / n_chunks, &rg)) return;
-    const int32_t most = row_of(k, rg, head, min((int64_t)rg.n_rows, rg.row0 + 128) - 1).last;
+    const int32_t most = wave_one(row_of(k, rg, head, min((int64_t)rg.n_rows, rg.row0 + 128) - 1).last);
     const int64_t start = chunk * k.shape.chunk;
     if (chunk > 0 && start > most) return;
     const int32_t x0 = (int32_t)start;
@@ -454,12 +490,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_tiles_kernel(KvAtte
     // this wave's rows: the last position that any sees, and the last that all see
     const int64_t wave_row0 = rg.row0 + 32 * wave;
     const bool awake = wave_row0 < rg.n_rows;
-    const int32_t wave_most = awake ? row_of(k, rg, head, min((int64_t)rg.n_rows, wave_row0 + 32) - 1).last : -1;
-    const int32_t wave_least = awake ? row_of(k, rg, head, wave_row0).last : -1;
+    const int32_t wave_most =
+        wave_one(awake ? row_of(k, rg, head, min((int64_t)rg.n_rows, wave_row0 + 32) - 1).last : -1);
+    const int32_t wave_least = wave_one(awake ? row_of(k, rg, head, wave_row0).last : -1);
     const Row row = row_of(k, rg, head, wave_row0 + n);
 
-    bf8_t q[PIECES][KS];
-    float c;
+    Words8 q[KS];    // bfloat16 factors, or the 16-bit floats as they are
+    float c, c_odd;  // what scores are multiplied by, and those of marked tiles
     {
         uint4 raw[KS];
 #pragma unroll
@@ -472,8 +509,33 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_tiles_kernel(KvAtte
             for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(y[i][j]));
         }
         top = fmaxf(top, __shfl_xor(top, 32, kWave));
-        query_pieces<PIECES>(k, y, top, q, &c);
+        if constexpr (F16) {
+            const uint32_t flip = k.scale < 0.0f ? 0x80008000u : 0u;
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                q[i].w[0] = raw[i].x ^ flip, q[i].w[1] = raw[i].y ^ flip;
+                q[i].w[2] = raw[i].z ^ flip, q[i].w[3] = raw[i].w ^ flip;
+            }
+            c = fminf(fmaxf(fabsf(k.scale) * kLog2e, 1.17549435e-38f), 3.4e38f);
+        } else {
+            bf8_t f[1][KS];
+            query_pieces<1>(k, y, top, f, &c);
+#pragma unroll
+            for (int i = 0; i < KS; ++i) q[i].v = f[0][i];
+        }
+        c_odd = c;
     }
+    // 8 values of the query as a marked tile takes them: two pieces, exact
+    const auto odd_query = [&](int i, bf8_t* hi, bf8_t* lo) {
+        float y[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t w = q[i].w[j];
+            asm volatile("" : "+v"(w));  // made here each time: kept through the loop it would take registers
+            pair_to_float(false, w, y + 2 * j);
+        }
+        split8(y, hi, lo);
+    };
     float16_t acc[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[t] = float16_t{};
@@ -507,7 +569,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_tiles_kernel(KvAtte
     };
     // the loaded codes (of the tile at x) in LDS; places past the end may hold anything: a scale of one
     // makes their values finite
-    auto put = [&](int buf, int32_t x) {
+    auto put = [&](int buf, int32_t x, auto as_f16) {
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
             const int token = token_of(u);
@@ -517,100 +579,147 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_tiles_kernel(KvAtte
             const int key = is_v(u) ? v4_key<D>(token) : k4_key<D>(token);
             const uint32_t w[4] = {codes[u].x, codes[u].y, codes[u].z, codes[u].w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                to[(group * 4 + i) ^ key] = __builtin_bit_cast(uint4, codes_to_bf(w[i], scale));
+            for (int i = 0; i < 4; ++i) {
+                uint4 f;
+                if constexpr (decltype(as_f16)::value)
+                    f = codes_to_f16(w[i], scale);
+                else
+                    f = __builtin_bit_cast(uint4, codes_to_bf(w[i], scale));
+                to[(group * 4 + i) ^ key] = f;
+            }
+            if constexpr (decltype(as_f16)::value)
+                if (e - 104u > 36u && ((w[0] | w[1] | w[2] | w[3]) & 0x77777777u) != 0) marked[buf] = x;
         }
     };
+    using No = std::false_type;
+    using AsF16 = std::integral_constant<bool, F16 && !kPieces>;
     const int k_token = (n & 0x13) | (n & 4) << 1 | (n & 8) >> 1;
     const int v_token = 8 * h + (lane >> 2 & 3), v_dim = (n & 16) + (lane & 3) * 4;
 
     int buf = 0;
+    if (AsF16::value) {
+        if (tid < 2) marked[tid] = -1;
+        __syncthreads();
+    }
     if (x0 < x1) {
         find(x0);
         load();
         find(x0 + 64);
-        put(0, x0);
+        put(0, x0, AsF16());
     }
+    // a tile: its scores, weights and products, as 16-bit floats or (ODD) as a marked one
+    const auto tile = [&](int32_t x, auto odd) {
+        constexpr bool ODD = decltype(odd)::value;
+        float16_t s[2] = {float16_t{}, float16_t{}};
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+            bf8_t hi = {}, lo = {};
+            if constexpr (ODD) odd_query(i, &hi, &lo);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int token = t * 32 + k_token;
+                Words8 f;
+                f.v = __builtin_bit_cast(bf8_t, lds[buf].k[token][(i * 2 + h) ^ k4_key<D>(token)]);
+                if constexpr (ODD) {
+                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, hi, s[t], 0, 0, 0);
+                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, lo, s[t], 0, 0, 0);
+                } else {
+                    s[t] = product<F16>(f, q[i], s[t]);
+                }
+            }
+        }
+        // register r of product t is token 32 t + 16 (r / 8) + 8 h + r % 8
+        if (x + 63 > wave_least) {
+            const int seen = row.last - x - h * 8;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    s[t][r] = t * 32 + (r >> 3) * 16 + (r & 7) > seen ? -INFINITY : s[t][r];
+        }
+        const float by = ODD ? c_odd : c;
+        float top = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 32; ++r) top = fmaxf(top, s[r / 16][r % 16]);
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        const float new_m = fmaxf(m, top * by + kShift);
+        if (__any(new_m - m > kLag)) {
+            const float fall = __builtin_amdgcn_exp2f(m - (new_m == -INFINITY ? 0.0f : new_m));
+#pragma unroll
+            for (int t = 0; t < DT; ++t) acc[t] *= fall;
+            l *= fall;
+            m = new_m;
+        }
+        const float from = m == -INFINITY ? 0.0f : m;
+        const auto weights = [&](int i, Words8* w) {
+            float e[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 2][i % 2 * 8 + r], by, -from));
+                l += e[r];
+            }
+            if constexpr (ODD)
+                split8(e, &w[0].v, &w[1].v);
+            else if constexpr (F16)
+                w[0] = half8(e);
+            else
+                w[0].v = round8(e);
+        };
+        Words8 w[4], pieces[2];
+        if constexpr (!ODD)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) weights(i, &w[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (ODD) weights(i, pieces);
+#pragma unroll
+            for (int t = 0; t < DT; ++t) {
+                union {
+                    short4_t s[2];
+                    Words8 f;
+                } f;
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    const int token = i * 16 + 4 * z + v_token, d = t * 32 + v_dim;
+                    auto* const from8 = reinterpret_cast<short4_t*>(&lds[buf].v[token][(d >> 3) ^ v4_key<D>(token)]) + (d >> 2 & 1);
+                    f.s[z] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)from8);
+                }
+                if constexpr (ODD) {
+                    acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.f.v, pieces[0].v, acc[t], 0, 0, 0);
+                    acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.f.v, pieces[1].v, acc[t], 0, 0, 0);
+                } else {
+                    acc[t] = product<F16>(f.f, w[i], acc[t]);
+                }
+            }
+        }
+    };
     for (int32_t x = x0; x < x1; x += 64, buf ^= 1) {
         if (x + 64 < x1) {
             load();
             find(x + 128);
         }
         __syncthreads();  // the tile is whole; the other one is read no more
-        if (x <= wave_most) {
-            float16_t s[2] = {float16_t{}, float16_t{}};
-#pragma unroll
-            for (int i = 0; i < KS; ++i)
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const int token = t * 32 + k_token;
-                    const bf8_t f = __builtin_bit_cast(bf8_t, lds[buf].k[token][(i * 2 + h) ^ k4_key<D>(token)]);
-#pragma unroll
-                    for (int p = 0; p < PIECES; ++p)
-                        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[p][i], s[t], 0, 0, 0);
-                }
-            // register r of product t is token 32 t + 16 (r / 8) + 8 h + r % 8
-            if (x + 63 > wave_least) {
-                const int seen = row.last - x - h * 8;
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        s[t][r] = t * 32 + (r >> 3) * 16 + (r & 7) > seen ? -INFINITY : s[t][r];
-            }
-            float top = -INFINITY;
-#pragma unroll
-            for (int r = 0; r < 32; ++r) top = fmaxf(top, s[r / 16][r % 16]);
-            top = fmaxf(top, __shfl_xor(top, 32, kWave));
-            const float new_m = fmaxf(m, top * c + kBelow);
-            if (__any(new_m - m > kSlack)) {
-                const float fall = __builtin_amdgcn_exp2f(m - (new_m == -INFINITY ? 0.0f : new_m));
-#pragma unroll
-                for (int t = 0; t < DT; ++t) acc[t] *= fall;
-                l *= fall;
-                m = new_m;
-            }
-            const float from = m == -INFINITY ? 0.0f : m;
-            bf8_t w[PIECES][4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float e[8];
-#pragma unroll
-                for (int r = 0; r < 8; ++r) {
-                    e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 2][i % 2 * 8 + r], c, -from));
-                    l += e[r];
-                }
-                if constexpr (PIECES == 1)
-                    w[0][i] = round8(e);
-                else
-                    split8(e, &w[0][i], &w[1][i]);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int t = 0; t < DT; ++t) {
-                    union {
-                        short4_t s[2];
-                        bf8_t v;
-                    } f;
-#pragma unroll
-                    for (int z = 0; z < 2; ++z) {
-                        const int token = i * 16 + 4 * z + v_token, d = t * 32 + v_dim;
-                        auto* const from8 = reinterpret_cast<short4_t*>(&lds[buf].v[token][(d >> 3) ^ v4_key<D>(token)]) + (d >> 2 & 1);
-                        f.s[z] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) short4_t*)from8);
-                    }
-#pragma unroll
-                    for (int p = 0; p < PIECES; ++p)
-                        acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.v, w[p][i], acc[t], 0, 0, 0);
-                }
+        if (kPieces) {
+            if (x <= wave_most) tile(x, std::integral_constant<bool, kPieces>());
+        } else if (F16 && __builtin_expect(wave_one(marked[buf]) == x, 0)) {  // the same for the workgroup: the tile once more, then the next one's codes
+            find(x);
+            load();
+            put(buf, x, No());
+            __syncthreads();
+            if (x <= wave_most) tile(x, AsF16());
+            find(x + 64);
+            load();
+            find(x + 128);
+        } else if (x <= wave_most) {
+            tile(x, No());
         }
-        if (x + 64 < x1) put(buf ^ 1, x + 64);
+        if (x + 64 < x1) put(buf ^ 1, x + 64, AsF16());
     }
     if (pages.bad()) raise_status(a.status, MP_EINVAL);
     store_rows<D>(k, row, chunk, acc, m, l, h);
 }
 
-// Many rows, heads of 128: two teams of four waves, 32 rows each wave, over one key head and one chunk
+// Many bfloat16 rows, heads of 128: two teams of four waves, 32 rows each wave, over one key head and one chunk
 // of tokens in tiles of 64.  Of a SIMD's two waves one is of each team, and the teams take turns: while one
 // is at its matrix products (the last tile's second one, this tile's first) the other is at its softmax; a
 // barrier ends a turn.
@@ -620,7 +729,6 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_tiles_kernel(KvAtte
 // put into LDS, loaded in the turn before, and keys i + 2 and values i + 1 are loaded.  With team 0 at tile i in
 // turn 2 i and team 1 in turn 2 i + 1, keys i are read in these two turns and values i in the next two: each
 // is whole the turn before, and two tiles' room is enough for both.
-template <int PIECES>
 __global__ __launch_bounds__(512, 2) void kv4_pair_kernel(KvAttend k) {
     constexpr int D = 128, KS = D / 16, DT = D / 32, GROUPS = D / 32;
     extern __shared__ __align__(16) char lds_raw[];
@@ -636,7 +744,7 @@ __global__ __launch_bounds__(512, 2) void kv4_pair_kernel(KvAttend k) {
     const uint32_t rest = blockIdx.x / heads, chunk = rest % n_chunks;
     RowGroup rg;
     if (!tile_group<256>(k, rest / n_chunks, &rg)) return;
-    const int32_t most = row_of(k, rg, head, min((int64_t)rg.n_rows, rg.row0 + 256) - 1).last;
+    const int32_t most = wave_one(row_of(k, rg, head, min((int64_t)rg.n_rows, rg.row0 + 256) - 1).last);
     const int64_t start = chunk * k.shape.chunk;
     if (chunk > 0 && start > most) return;
     const int32_t x0 = (int32_t)start;
@@ -646,7 +754,7 @@ __global__ __launch_bounds__(512, 2) void kv4_pair_kernel(KvAttend k) {
     // this wave's rows, and the last position that all of them see
     const int64_t wave_row0 = rg.row0 + 32 * wave;
     const bool awake = wave_row0 < rg.n_rows;  // has rows
-    const int32_t wave_least = row_of(k, rg, head, wave_row0).last;
+    const int32_t wave_least = wave_one(row_of(k, rg, head, wave_row0).last);
     const Row row = row_of(k, rg, head, wave_row0 + n);
 
     // a thread moves 16 dims of a token's keys (r 0) and of its values (r 1); table entries are read a
@@ -683,7 +791,7 @@ __global__ __launch_bounds__(512, 2) void kv4_pair_kernel(KvAttend k) {
         load(0);
         find(0, 0), find(1, 0);  // keys 1, values 0
     }
-    bf8_t q[PIECES][KS];
+    bf8_t q[1][KS];
     float c;
     {
         uint4 raw[KS];
@@ -697,13 +805,13 @@ __global__ __launch_bounds__(512, 2) void kv4_pair_kernel(KvAttend k) {
             for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(y[i][j]));
         }
         top = fmaxf(top, __shfl_xor(top, 32, kWave));
-        query_pieces<PIECES>(k, y, top, q, &c);
+        query_pieces<1>(k, y, top, q, &c);
     }
     float16_t acc[DT], s[2];
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[t] = float16_t{};
     s[0] = s[1] = float16_t{};
-    bf8_t w[PIECES][4] = {};
+    bf8_t w[4] = {};
     float m = -INFINITY, l = 0.0f;
 
     auto turn = [&]() {
@@ -759,14 +867,11 @@ __global__ __launch_bounds__(512, 2) void kv4_pair_kernel(KvAttend k) {
 #pragma unroll
         for (int j = 0; j < kAll; ++j) {
             const bf8_t use = f[j % kAhead];
-#pragma unroll
-            for (int p = 0; p < PIECES; ++p) {
-                if (j < kSecond) {
-                    acc[j % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(use, w[p][j / DT], acc[j % DT], 0, 0, 0);
-                } else {
-                    const int z = j - kSecond;
-                    s[z % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(use, q[p][z / 2], s[z % 2], 0, 0, 0);
-                }
+            if (j < kSecond) {
+                acc[j % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(use, w[j / DT], acc[j % DT], 0, 0, 0);
+            } else {
+                const int z = j - kSecond;
+                s[z % 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(use, q[0][z / 2], s[z % 2], 0, 0, 0);
             }
             if (j + kAhead < kAll) f[j % kAhead] = factor(j + kAhead);
             if (first_too() && j % 2 == 1 && j / 2 < kPieces) move(j / 2, i);
@@ -836,10 +941,7 @@ __global__ __launch_bounds__(512, 2) void kv4_pair_kernel(KvAttend k) {
                 sum += e[r];
             }
             l += sum;
-            if constexpr (PIECES == 1)
-                w[0][i] = round8(e);
-            else
-                split8(e, &w[0][i], &w[1][i]);
+            w[i] = round8(e);
         }
         turn();
         products(Yes{}, Yes{}, tile + 1);  // the last one's scores are of no tile
@@ -854,15 +956,15 @@ hipError_t launch_d(const KvAttend& k, hipStream_t st) {
     const KvAttendShape& sh = k.shape;
     const dim3 grid((uint32_t)(sh.units * k.a.c.heads * sh.n_chunks));
     constexpr int kLds = 2 * sizeof(Tile4<D>);
-    if (sh.form == KvForm::pair) {  // heads of 128
-        kv4_pair_kernel<PIECES><<<grid, 512, 2 * sizeof(Tile4<128>), st>>>(k);
+    if (sh.form == KvForm::pair) {  // bfloat16 rows, heads of 128
+        kv4_pair_kernel<<<grid, 512, 2 * sizeof(Tile4<128>), st>>>(k);
     } else if (sh.form == KvForm::tiles) {
         if (kLds > 65536)
-            if (hipError_t e = hipFuncSetAttribute((const void*)kv4_tiles_kernel<D, PIECES>,
+            if (hipError_t e = hipFuncSetAttribute((const void*)kv4_tiles_kernel<D, PIECES == 2>,
                                                    hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
                 e != hipSuccess)
                 return e;
-        kv4_tiles_kernel<D, PIECES><<<grid, 256, kLds, st>>>(k);
+        kv4_tiles_kernel<D, PIECES == 2><<<grid, 256, kLds, st>>>(k);
     } else if (D < 256 && grid.x <= 256) {  // a compute unit for every workgroup
         if constexpr (D < 256) kv4_rows_kernel<D, PIECES, 8><<<grid, 512, 0, st>>>(k);
     } else {

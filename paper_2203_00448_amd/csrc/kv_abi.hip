@@ -1,4 +1,4 @@
-// C ABI entry points of the 8-bit key/value cache: host-side argument checks, then
+// C ABI entry points of the key/value cache: host-side argument checks, then
 // launches on the caller's stream.  No allocation, no synchronisation.
 #include "kv.hpp"
 
@@ -143,7 +143,7 @@ extern "C" int32_t mp_kv_attend(const mp_kv_cache* cache, const mp_kv_seqs* seqs
         !rows_ok(out, seqs->n_tokens, q_heads, false, &k.out) || q->dtype != out->dtype ||
         !rows_apart(out, seqs->n_tokens, q_heads, cache->dim))
         return MP_EINVAL;
-    k.shape = kv_attend_shape(*cache, *seqs, q_heads, keep);
+    k.shape = kv_attend_shape(*cache, *seqs, q_heads, keep, q->dtype);
     if (!k.shape.ok || workspace_bytes < k.shape.workspace || !aligned(workspace, 16) ||
         (k.shape.workspace > 0 && !workspace))
         return MP_EINVAL;
@@ -192,8 +192,11 @@ extern "C" size_t mp_kv_workspace_size(int32_t op, const mp_kv_cache* cache,
         keep > kMaxCount / 64 || (cache->kind == MP_KV_E2M1 && (op != MP_OP_KV_ATTEND || keep > 0)))
         return 0;
     if (op == MP_OP_KV_ATTEND) {
-        const KvAttendShape sh = kv_attend_shape(*cache, *seqs, q_heads, keep);
-        return sh.ok ? sh.workspace : 0;
+        // rows of either type
+        const KvAttendShape a = kv_attend_shape(*cache, *seqs, q_heads, keep, MP_BF16);
+        const KvAttendShape b = kv_attend_shape(*cache, *seqs, q_heads, keep, MP_F16);
+        const size_t x = a.ok ? a.workspace : 0, y = b.ok ? b.workspace : 0;
+        return x > y ? x : y;
     }
     if (op == MP_OP_KV_SELECT) {
         if (q_heads / cache->heads > kMaxSelectGroup) return 0;

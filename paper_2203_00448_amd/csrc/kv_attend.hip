@@ -1196,7 +1196,7 @@ hipError_t launch_kv_join(const KvAttend& k, hipStream_t st) {
 }
 
 KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t q_heads,
-                              int64_t keep) {
+                              int64_t keep, int32_t dtype) {
     KvAttendShape sh = {};
     const int64_t group = q_heads / c.heads;
     // The form by the rows of the longest piece (new tokens times query heads a key head).  Rows against
@@ -1219,6 +1219,15 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
         sh.form = KvForm::rows;
     else
         sh.form = c.dim == 128 && piece >= 4096 ? KvForm::pair : KvForm::tiles;
+    // In 4 bits pairs are for bfloat16 rows (16-bit floats would want registers for both forms of their tiles) and for
+    // launches of four rounds of workgroups.  Tiles against pairs, us, as above:
+    //             1024 new     2048 new     2048 of 8192
+    //   1 seq.    70 / 71      99 / 134     312 / 297
+    //   4         122 / 212    165 / 167    975 / 860
+    //   16        481 / 463
+    if (c.kind == MP_KV_E2M1 && sh.form == KvForm::pair &&
+        (dtype != MP_BF16 || (s.n_tokens * group / 256 + s.n_seqs) * c.heads < 1024))
+        sh.form = KvForm::tiles;
     sh.rows = sh.form == KvForm::rows ? 16 : sh.form == KvForm::tiles ? 128 : 256;
     const int64_t per = (group + sh.rows - 1) / sh.rows;
     if (keep > 0)

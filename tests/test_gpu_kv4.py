@@ -81,7 +81,13 @@ class Setup:
         return out
 
 
-ONE, TWO = 2.0 ** -8, 2.0 ** -15  # the rounding of a weight: 8 bits; 8 bits and 8 of what these leave
+# The rounding of a weight: 8 bits; 11 bits; 8 bits and 8 of what these leave.
+ONE, HALF, TWO = 2.0 ** -8, 2.0 ** -11, 2.0 ** -15
+
+
+def of_tiles(dtype, dim=128):
+    """The rounding where many rows share what is read."""
+    return ONE if dtype == BF16 else HALF if dim < 256 else TWO
 
 
 def near(out, lse, want, dtype, weights):
@@ -90,11 +96,12 @@ def near(out, lse, want, dtype, weights):
     Weights are rounded (`weights`) and have 2^-20 from the exponential and the sums.  The largest of a row
     is 2^-24 at least, and what is below 2^-126, the least that a float has all its bits at, may be zero: a
     weight, relative to the largest, and its product with a value by 2^-102 each (`floor`: times the sum of 1 + |v|).
-    The result is rounded once, in steps that end."""
+    Weights of 11 bits end in steps of 2^-24 where the largest is 2^10 at least: half a step is 2^-35 of it; values
+    beside them end in these steps too, half of one 2^-25.  The result is rounded once, in steps that end."""
     ref, ref_lse, mass, delta, floor = want
     score = (ref.shape[-1] + 8) * 2.0 ** -24 * delta[..., None]
     bound = HALF_STEP[dtype] * np.abs(ref) + (weights + 2.0 ** -20 + 2.5 * score) * mass * 1.01 + LEAST_STEP[dtype]
-    bound += 2.0 ** -102 * floor
+    bound += (2.0 ** -35 if weights == HALF else 2.0 ** -102) * floor + (2.0 ** -25 if weights == HALF else 0.0)
     off = np.abs(host(out.double()) - ref)
     assert np.all(off <= bound), (off / bound).max()
     if lse is not None:
@@ -229,7 +236,7 @@ def test_attend_prompt(block, dim, heads, group, dtype, new):
     # the bounds that the handle gives where none are named: all rows one sequence's, a whole row of the table
     piece, longest = sum(new) * group, s.table.shape[1] * block
     few = piece <= 16 or (piece <= 64 and longest > 512)
-    s.attend(length, new, q, weights=TWO if few or dtype == F16 else ONE)
+    s.attend(length, new, q, weights=TWO if few else of_tiles(dtype, dim))
 
 
 @pytest.mark.parametrize("dtype,dim,length,new", [(BF16, 128, [5000], None), (F16, 64, [9000, 3000], None),
@@ -241,7 +248,24 @@ def test_attend_chunks(dtype, dim, length, new):
     s.fill()
     n = len(length) if new is None else sum(new)
     few = new is None or sum(new) * 4 <= 64
-    s.attend(length, new, s.rows(n, 4, dtype), weights=TWO if few or dtype == F16 else ONE)
+    s.attend(length, new, s.rows(n, 4, dtype), weights=TWO if few else of_tiles(dtype, dim))
+
+
+@pytest.mark.parametrize("block", [16, 64])
+@pytest.mark.parametrize("length,new,heads", [
+    ([1100] + [1 + i % 70 for i in range(120)], [1100] + [1 + i % 70 for i in range(120)], 8),
+    ([1300], [1100], 64), ([5] * 60 + [1500, 40], [9] * 60 + [1030, 60], 17)])
+def test_attend_many_prompts(length, new, heads, block):
+    """Calls of over a thousand workgroups of 256 rows: teams of waves in turn, sequences in order or by what they
+    see, rows that see nothing, tokens of sizes far apart."""
+    s = Setup(length, heads=heads, block=block)
+    k, v = s.rows(sum(length)), s.rows(sum(length))
+    v[::7] *= 2.0 ** 40
+    v[:, :, 64:96] *= 2.0 ** -60
+    k[::5, :, :32] *= 2.0 ** -20
+    s.store(length, length, k, v)
+    assert (sum(new) * 4 // 256 + len(new)) * heads >= 1024 and max(new) * 4 >= 4096
+    s.attend(length, new, s.rows(sum(new), heads * 4), weights=ONE)
 
 
 def test_rows_that_see_nothing():
@@ -283,7 +307,30 @@ def test_values_of_sizes_far_apart(new, dtype):
         v[150:153] *= 2.0 ** -55
         v[:, :, 32:64] *= 2.0 ** 45
         s.store([200], [200], k, v)
-    s.attend([200], new, q, weights=TWO if new is None or dtype == F16 else ONE)
+    s.attend([200], new, q, weights=TWO if new is None else of_tiles(dtype))
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("odd", [[0], [1], [2, 3], [4], [0, 1, 2, 3, 4]])
+def test_scales_that_16_bit_floats_do_not_hold(odd, dim):
+    """Rows of 16-bit floats: steps of 64 tokens whose keys or values lie outside that type's range, beside others
+    within it; values beyond it with weights that bring them back; groups of zeros, which no scale disturbs."""
+    s = Setup([300], heads=1, dim=dim)
+    k, v = s.rows(300, size=0.25).float(), s.rows(300).float()
+    k[7], v[9] = 0.0, 0.0
+    v[130, :, :32] = 0.0
+    for t in odd:
+        at = slice(64 * t, 64 * t + 60)
+        k[at, :, 32:64] *= 2.0 ** -30
+        v[at] *= 2.0 ** -27
+        v[64 * t + 5] = 400000.0
+        k[64 * t + 5] = -1.0
+    s.store([300], [300], k.to(BF16), v.to(BF16))
+    q = (s.rows(200, 4, F16, size=0.1).float() + 2.0).to(F16)
+    # a score of -2 sqrt(dim) and more below the others: at most e^-16 of the weights, with any of these values
+    s.attend([300], [200], q, weights=of_tiles(F16, dim))
+    s.attend([300], [200], -q, scale=-(dim ** -0.5), weights=of_tiles(F16, dim))
+    s.attend([300], None, q[:1], weights=TWO)
 
 
 @pytest.mark.parametrize("new", [None, [70]])
@@ -333,7 +380,7 @@ def test_repeats_and_views(dtype, new):
     n = 2 if new is None else sum(new)
     wide = torch.randn(n, 2, 8, 136, device="cuda").to(dtype)
     q = wide[:, 1, :, :128]
-    want = s.attend([700, 150], new, q, weights=TWO if new is None or dtype == F16 else ONE)
+    want = s.attend([700, 150], new, q, weights=TWO if new is None else of_tiles(dtype))
     seqs, _ = s.seqs([700, 150], new)
     room = torch.full((n, 9, 130), 5.0, dtype=dtype, device="cuda")
     out = room[:, :8, 1:129]

@@ -6,7 +6,7 @@ import torch
 
 from gpu_util import dev, host, need_gpu
 from kv4_defs import RefCache4
-from test_gpu_kv4 import ONE, TWO, near
+from test_gpu_kv4 import near, of_tiles
 from test_gpu_pages import Ref
 from test_gpu_rotary import reference
 
@@ -146,7 +146,7 @@ def test_requests_come_and_go(dtype, dim, block, group):
         for name in ("k_code", "v_code", "k_exp", "v_exp"):
             assert np.array_equal(host(getattr(cache, name)), getattr(ref, name)), (turn, name)
         want = ref.attend(plan.table, plan.length, begin, host(q.double()), dim ** -0.5)
-        near(got, None, want, dtype, ONE if dtype == torch.bfloat16 else TWO)
+        near(got, None, want, dtype, of_tiles(dtype))
         # the slots say where the rows went
         flat = cache.k_code.transpose(1, 2).reshape(-1, heads, dim // 2)[step.slot]
         assert torch.equal(flat, dev(np.stack([ref.k_code[s // block, :, s % block] for s in slot]), torch.uint8))
