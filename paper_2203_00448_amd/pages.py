@@ -41,10 +41,10 @@ def load_library():
 def _vector(t, dtype, name, n, index):
     """A vector's address.  These calls are short beside what a launch costs, so their checks look at each
     property once."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_cuda or t.shape != (n,):
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.dim() != 1 or t.numel() != n or not t.is_cuda:
         _need(t, (dtype,), name, (n,))
     if t.get_device() != index or not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous and on the device of the pool")
+        raise ValueError(f"{name} must be contiguous and on one device with the others")
     return t.data_ptr() or None
 
 
@@ -74,6 +74,11 @@ class Step:
 
     def __init__(self, length, begin, position, slot):
         self.length, self.begin, self.position, self.slot = length, begin, position, slot
+        n, room, self.index = length.numel(), slot.numel(), begin.get_device()
+        _vector(length, torch.int32, "length", n, self.index)
+        self._at = (_vector(begin, torch.int64, "begin", n + 1, self.index),
+                    _vector(position, torch.int32, "position", room, self.index),
+                    _vector(slot, torch.int64, "slot", room, self.index), room, n)
 
 
 def new_step(n_seqs: int, tokens: int, *, device="cuda") -> Step:
@@ -130,10 +135,9 @@ def extend(pool: Pool, table, length, more, *, block: int = 64, step: Step, leng
     out = lengths if length_out is None else _vector(length_out, torch.int32, "length_out", n, index)
     ids, n_ids, used = pool._at
     used_to = used if used_out is None else _vector(used_out, torch.int64, "used_out", 1, index)
-    begin = _vector(step.begin, torch.int64, "step.begin", n + 1, index)
-    room = step.slot.numel()
-    position = _vector(step.position, torch.int32, "step.position", room, index)
-    slot = _vector(step.slot, torch.int64, "step.slot", room, index)
+    begin, position, slot, room, of = step._at
+    if of != n or step.index != index:
+        raise ValueError("step must be of as many sequences and on the device of the pool")
     space = _space(n, workspace, pool)
     status = kv._word(status, pool)
     rc = L.mp_kv_extend(ids, n_ids, used, t, t_stride, width, block, lengths, new, n, room, out, used_to, begin,
