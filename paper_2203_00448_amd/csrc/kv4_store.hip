@@ -11,6 +11,8 @@ namespace mp {
 
 namespace {
 
+constexpr int kOnce = 2;  // pieces of a lane whose loads are on their way together
+
 // A token of a call: its place in its block, and the block.
 struct KvPlace {
     int64_t page;
@@ -108,21 +110,30 @@ __global__ __launch_bounds__(256) void kv4_write_kernel(KvArgs a, KvRows k, KvRo
     if (!kv_place(a, token, &p)) return;
     bool finite = true;
     // all lanes of a scale's four are in or out: items is a multiple of 8
-    for (int i = lane; i < items; i += kWave) {
-        const int head = i / vecs, d = i % vecs * 8;
-        const Raw8 kr = load_raw8(k, token, head, d), vr = load_raw8(v, token, head, d);
-        const Places at = places(a, p, head, d);
-        float x[8];
-        int exp;
-        bool fine;
-        raw8_to_float(k, kr, x);
-        reinterpret_cast<uint32_t*>(a.c.k_code)[at.word] = encode8(x, &exp, &fine);
-        finite = finite && fine;
-        if (d % 32 == 0) a.c.k_exp[at.exp] = (int8_t)exp;
-        raw8_to_float(v, vr, x);
-        reinterpret_cast<uint32_t*>(a.c.v_code)[at.word] = encode8(x, &exp, &fine);
-        finite = finite && fine;
-        if (d % 32 == 0) a.c.v_exp[at.exp] = (int8_t)exp;
+    for (int i0 = lane; i0 < items; i0 += kOnce * kWave) {
+        Raw8 kr[kOnce], vr[kOnce];
+#pragma unroll
+        for (int j = 0; j < kOnce; ++j) {
+            const int i = i0 + j * kWave, head = i / vecs, d = i % vecs * 8;
+            if (i < items) kr[j] = load_raw8(k, token, head, d), vr[j] = load_raw8(v, token, head, d);
+        }
+#pragma unroll
+        for (int j = 0; j < kOnce; ++j) {
+            const int i = i0 + j * kWave, head = i / vecs, d = i % vecs * 8;
+            if (i >= items) break;
+            const Places at = places(a, p, head, d);
+            float x[8];
+            int exp;
+            bool fine;
+            raw8_to_float(k, kr[j], x);
+            reinterpret_cast<uint32_t*>(a.c.k_code)[at.word] = encode8(x, &exp, &fine);
+            finite = finite && fine;
+            if (d % 32 == 0) a.c.k_exp[at.exp] = (int8_t)exp;
+            raw8_to_float(v, vr[j], x);
+            reinterpret_cast<uint32_t*>(a.c.v_code)[at.word] = encode8(x, &exp, &fine);
+            finite = finite && fine;
+            if (d % 32 == 0) a.c.v_exp[at.exp] = (int8_t)exp;
+        }
     }
     if (!finite) raise_status(a.status, MP_EINVAL);
 }
@@ -134,17 +145,28 @@ __global__ __launch_bounds__(256) void kv4_read_kernel(KvArgs a, KvRows k, KvRow
     const int lane = threadIdx.x & 63, vecs = a.c.dim / 8, items = a.c.heads * vecs;
     KvPlace p;
     if (!kv_place(a, token, &p)) return;
-    for (int i = lane; i < items; i += kWave) {
-        const int head = i / vecs, d = i % vecs * 8;
-        const Places at = places(a, p, head, d);
-        const uint32_t kw = reinterpret_cast<const uint32_t*>(a.c.k_code)[at.word];
-        const uint32_t vw = reinterpret_cast<const uint32_t*>(a.c.v_code)[at.word];
-        const int ke = (uint8_t)a.c.k_exp[at.exp], ve = (uint8_t)a.c.v_exp[at.exp];
-        float x[8];
-        decode8(kw, ke, x);
-        store8(k, token, head, d, x);
-        decode8(vw, ve, x);
-        store8(v, token, head, d, x);
+    for (int i0 = lane; i0 < items; i0 += kOnce * kWave) {
+        uint32_t kw[kOnce], vw[kOnce];
+        int ke[kOnce], ve[kOnce];
+#pragma unroll
+        for (int j = 0; j < kOnce; ++j) {
+            const int i = i0 + j * kWave;
+            if (i >= items) break;
+            const Places at = places(a, p, i / vecs, i % vecs * 8);
+            kw[j] = reinterpret_cast<const uint32_t*>(a.c.k_code)[at.word];
+            vw[j] = reinterpret_cast<const uint32_t*>(a.c.v_code)[at.word];
+            ke[j] = (uint8_t)a.c.k_exp[at.exp], ve[j] = (uint8_t)a.c.v_exp[at.exp];
+        }
+#pragma unroll
+        for (int j = 0; j < kOnce; ++j) {
+            const int i = i0 + j * kWave, head = i / vecs, d = i % vecs * 8;
+            if (i >= items) break;
+            float x[8];
+            decode8(kw[j], ke[j], x);
+            store8(k, token, head, d, x);
+            decode8(vw[j], ve[j], x);
+            store8(v, token, head, d, x);
+        }
     }
 }
 
