@@ -51,6 +51,7 @@ struct KvAttendShape {
     int64_t chunk;     // tokens (of the sequence, or of its listed blocks) of a workgroup
     int64_t n_chunks;
     bool ordered;      // row groups of tiles by what they see
+    uint32_t spread;   // in 4 bits, few rows: the step between the row groups of neighbouring workgroups
     size_t workspace;
 };
 

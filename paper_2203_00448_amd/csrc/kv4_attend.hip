@@ -159,7 +159,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : WAVES == 8 || (D == 128 
     // has, must not all meet one of them
     const uint32_t rest = blockIdx.x / heads, units = (uint32_t)k.shape.units, chunk = n_chunks - 1 - rest / units;
     RowGroup rg;
-    if (!row_group(k, rest % units, &rg)) return;
+    if (!row_group(k, (uint32_t)((uint64_t)(rest % units) * k.shape.spread % units), &rg)) return;
     const int64_t last_row = min((int64_t)rg.n_rows, rg.row0 + 16) - 1;
     const int32_t most = wave_one(row_of(k, rg, head, last_row).last);  // the last position any row sees
     const int32_t least = wave_one(row_of(k, rg, head, rg.row0).last);  // all rows see up to here

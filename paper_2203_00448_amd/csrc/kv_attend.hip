@@ -1236,6 +1236,7 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
         sh.units = s.n_tokens * group / sh.rows + s.n_seqs;
     else
         sh.units = s.n_seqs * per;
+    if (c.kind == MP_KV_E2M1 && sh.form == KvForm::rows && s.begin) sh.units |= 1;  // for `spread`
     const int64_t longest = keep > 0 ? keep * c.block : s.longest;
     // Tokens of a workgroup: a workgroup's start, end and part of the join cost as much as some
     // hundred tokens, few long ones leave compute units idle.  2048, or less where that makes
@@ -1246,12 +1247,19 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     // after 20000 tokens 118 us (two: 149, eight: 114), prompts that fill the device without
     // chunks 290 us (559 in chunks of 2048: the partial results are 32-bit).
     const int64_t wide = sh.units * c.heads;
-    int64_t chunk = longest < ((int64_t)2048 * 256) / (wide > 0 ? wide : 1) ? longest * wide / 256 : 2048;
+    // In 4 bits by the row groups that there are where all sequences have alike: the bound counts one too many of
+    // each.  64 sequences of 4096 tokens, 4 new: 80 us, 93 by the bound, in two chunks.
+    int64_t busy = wide;
+    if (c.kind == MP_KV_E2M1 && sh.form == KvForm::rows && s.begin) {
+        const int64_t least = s.n_tokens * group / sh.rows;
+        busy = (least > s.n_seqs ? least : s.n_seqs) * c.heads;
+    }
+    int64_t chunk = longest < ((int64_t)2048 * 256) / (busy > 0 ? busy : 1) ? longest * busy / 256 : 2048;
     // In 4 bits two workgroups a compute unit are one round of a launch: where chunks up to 4096 make that
     // many, those.  Measured with 1024 / 2048 / 4096: two sequences of 131072 75 / 63 / 59 us; 64 of 1-16384 tokens,
     // which are more, 104 / 95 / 99.
-    if (c.kind == MP_KV_E2M1 && wide > 0 && chunk == 2048 && longest <= (int64_t)4096 * 512 / wide)
-        chunk = longest * wide / 512;
+    if (c.kind == MP_KV_E2M1 && busy > 0 && chunk == 2048 && longest <= (int64_t)4096 * 512 / busy)
+        chunk = longest * busy / 512;
     if (chunk < 512) chunk = 512;
     if (longest <= 1024) chunk = 1024;
     if (sh.form != KvForm::rows) {
@@ -1272,6 +1280,23 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     // a level of a row group (the rows before it over the group's) has 30 bits
     sh.ordered = sh.form != KvForm::rows && s.begin && s.n_seqs <= 64 && sh.n_chunks == 1 &&
                  s.longest < ((int64_t)1 << 30) * sh.rows / group;
+    // The bound on the row groups has an empty one for most sequences, and workgroups go to the compute units in
+    // turn, wherever others have ended: empty ones at even distances leave some units three and others none.  So
+    // neighbours are about 0.618 of the (odd) count apart: 64 sequences of 4096 tokens, 4 new, 4 query heads a key
+    // head, 63 us, 80 in order (every second group is empty); 2 new 60 and 49 (every third).
+    sh.spread = 1;
+    if (s.begin && sh.units > 2 && sh.units < most) {
+        const auto common = [](int64_t a, int64_t b) {
+            while (b) {
+                const int64_t r = a % b;
+                a = b, b = r;
+            }
+            return a;
+        };
+        int64_t step = sh.units * 618 / 1000;
+        while (common(sh.units, step) != 1) ++step;
+        sh.spread = (uint32_t)step;
+    }
     return sh;
 }
 
