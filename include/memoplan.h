@@ -335,7 +335,7 @@ int32_t mp_plan_breadth_batch(const int64_t* begin, int64_t n_traces, const int3
                               int64_t n_tensors, int32_t policy, int64_t* offset_out,
                               int64_t* peak_out, int32_t* status_out, void* stream);
 
-/* ---- A key/value cache in 8 bits ------------------------------------------
+/* ---- A key/value cache in 8 or 4 bits -------------------------------------
  *
  * The memory of a decode loop that no static plan holds, because it grows by a
  * token a step: the keys and values of attention, in blocks of tokens that a
@@ -472,7 +472,12 @@ int32_t mp_kv_read(const mp_kv_cache* cache, const mp_kv_seqs* seqs, const mp_kv
  * largest value.  exp(...) is held to 11 bits before the product with v, and in
  * steps of 2^-28 where it, times the scale of v_j's block, is below 2^-18 of the row's
  * largest such product; sums and maxima are in 32 bits.  The order of every sum
- * is fixed by the arguments, so a call repeats bit for bit. */
+ * is fixed by the arguments, so a call repeats bit for bit.
+ * Kind MP_KV_E2M1: factors are bfloat16 (16-bit float queries in two pieces), which hold queries
+ * down to 2^-126 of their largest and all codes at their scales exactly, so sizes of values that differ
+ * between tokens or dims cost no bits.  exp(...) is held to 16 bits for few rows, to 8 in tiles of bfloat16
+ * rows; in tiles of 16-bit float rows (heads of 64 and 128) to 11 bits, in steps of 2^-34 of the row's
+ * largest, by steps of 64 tokens whose values such floats hold, down to their least step, others to 16. */
 int32_t mp_kv_attend(const mp_kv_cache* cache, const mp_kv_seqs* seqs, const mp_kv_rows* q,
                      int32_t q_heads, float scale, const int32_t* blocks, int64_t keep,
                      const mp_kv_rows* out, float* lse_out, void* workspace,

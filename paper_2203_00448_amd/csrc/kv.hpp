@@ -1,4 +1,4 @@
-// The 8-bit key/value cache: arguments of its kernels and their common device code.
+// The key/value cache: arguments of its kernels and their common device code.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -142,6 +142,15 @@ __device__ __forceinline__ void query_pieces(const KvAttend& k, const float (&x)
 // Tokens: key row n of tile t holds token 4 n + t of the step, lane quarter g a quarter of its dims.  A lane
 // of quarter g then has the scores of tokens [16 g, + 16), four in a row from the four tiles.  Of the
 // values it reads those tokens' dims [D/16 n, + D/16): row n of the second product's tile t is dim D/16 n + t.
+// The instructions that convert take two dims of a token, those that multiply want two tokens of a dim: a byte
+// permute a pair turns them, two dims at a time, which keeps the factors' registers few.
+//
+// What bounds it is memory where there are many workgroups: 64 sequences of 1-16384 tokens 90 us, 4.3 TB/s, of 8192
+// each 116 us, 4.9 TB/s; two of 131072 58 us, 4.9 TB/s (a large copy: 4.9).  A step of 64 tokens has 350 vector and 48
+// matrix instructions a wave, about half of the time that its 8.7 KB take.  It was 112 and 105 us with registers
+// spilled at three waves a SIMD: heads of 128 have three with bfloat16 rows, two with 16-bit floats (whose queries take
+// 16 registers more).  One sequence of 1000 tokens 10 us: dependent loads, two steps a wave, and code met for
+// the first time.
 template <int D, int PIECES, int WAVES>
 __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : WAVES == 8 || (D == 128 && PIECES == 2) ? 2 : 3) void kv4_rows_kernel(KvAttend k) {
     constexpr int KD = D / 4, KS = KD / 8;  // dims of a lane's keys; steps of the first product
@@ -156,10 +165,10 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : WAVES == 8 || (D == 128 
     const uint32_t heads = a.c.heads, n_chunks = (uint32_t)k.shape.n_chunks;
     const int head = (int)(blockIdx.x % heads);
     // chunks slowest: workgroups go to the XCDs in turn, and first chunks, which every row group
-    // has, must not all meet one of them
+    // has, must not all meet one of them; last chunks first, which only long sequences have
     const uint32_t rest = blockIdx.x / heads, units = (uint32_t)k.shape.units, chunk = n_chunks - 1 - rest / units;
     RowGroup rg;
-    if (!row_group(k, (uint32_t)((uint64_t)(rest % units) * k.shape.spread % units), &rg)) return;
+    if (!row_group<16>(k, (uint32_t)((uint64_t)(rest % units) * k.shape.spread % units), &rg)) return;
     const int64_t last_row = min((int64_t)rg.n_rows, rg.row0 + 16) - 1;
     const int32_t most = wave_one(row_of(k, rg, head, last_row).last);  // the last position any row sees
     const int32_t least = wave_one(row_of(k, rg, head, rg.row0).last);  // all rows see up to here
@@ -457,9 +466,15 @@ __device__ __forceinline__ int v4_key(int token) {
     return D == 64 ? (token >> 1 & 1) << 2 : (token & 3) << 2;
 }
 
+// Measured, 333 rows of heads of 64 after 20000 tokens, 16-bit floats: 109 us and the join, 500 TFLOP/s.  Four
+// sequences of 2048 tokens, 700 new, 32 query heads over 8, bfloat16: heads of 64 111 us, of 128 162 us, of 256
+// 441 us; 16-bit floats 122, 188 and 559.  A tile's softmax takes a wave about 900 cycles of vector instructions
+// (512 of them exponentials), its products of heads of 64 512.
+//
 // F16, rows of 16-bit floats: the tile as 16-bit floats, so that one instruction holds a query's and a
 // weight's 11 bits.  A group of codes that these cannot hold exactly (scales outside 2^-23..2^13, codes not all zero)
-// marks its tile, and the workgroup takes a marked tile as bfloat16, with queries and weights in two pieces.
+// marks its tile, and the workgroup takes a marked tile as bfloat16, with queries and weights in two pieces.  (All tiles
+// in two pieces: 143 us instead of 112 for the rows above.)
 // Heads of 256 have no registers for both: all their tiles are taken so.
 template <int D, bool F16>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_tiles_kernel(KvAttend k) {
@@ -729,6 +744,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_tiles_kernel(KvAtte
 // put into LDS, loaded in the turn before, and keys i + 2 and values i + 1 are loaded.  With team 0 at tile i in
 // turn 2 i and team 1 in turn 2 i + 1, keys i are read in these two turns and values i in the next two: each
 // is whole the turn before, and two tiles' room is enough for both.
+//
+// Measured, prompts of 228-4096 tokens, 32 query heads over 8: 257 us, 900 TFLOP/s; four of 4096 tokens 573 us,
+// 960 TFLOP/s (tiles: 267 and 603).  Without the priority of the products 274 us.  Keys left as codes in LDS, read in a
+// quarter of its time and converted by each wave: 285 us, as the conversions meet the other team's softmax.
 __global__ __launch_bounds__(512, 2) void kv4_pair_kernel(KvAttend k) {
     constexpr int D = 128, KS = D / 16, DT = D / 32, GROUPS = D / 32;
     extern __shared__ __align__(16) char lds_raw[];

@@ -159,7 +159,7 @@ __global__ __launch_bounds__(WAVES * 64, WAVES == 8 ? 2 : D == 256 ? 1 : 3) void
     // has, must not all meet one of them
     const uint32_t rest = blockIdx.x / heads, units = (uint32_t)k.shape.units, chunk = rest / units;
     RowGroup rg;
-    if (!row_group(k, rest % units, &rg)) return;
+    if (!row_group<16>(k, rest % units, &rg)) return;
     const int64_t last_row = min((int64_t)rg.n_rows, rg.row0 + 16) - 1;
     const int32_t most = row_of(k, rg, head, last_row).last;  // the last position any row sees
     const int32_t least = row_of(k, rg, head, rg.row0).last;  // all rows see up to here

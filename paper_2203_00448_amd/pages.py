@@ -8,6 +8,8 @@ makes the step's lengths, row bounds, positions and slots; nothing waits for the
 can be recorded in a graph.  Each runs on `stream` (the current one of the pool's device if not
 given), whichever device is current; tensors that are in use on another stream are the caller's to
 wait for.  Outputs are written in place: `length` and the pool's counter too, if no others are given.
+The tensors that a handle was made of stay the caller's: changing their values, not their places, changes
+what the next call sees, and another tensor in an attribute's place does not.
 """
 from __future__ import annotations
 
@@ -59,7 +61,7 @@ class Pool:
             raise ValueError("ids must be a contiguous vector, on the device of used")
         self.ids, self.used = ids, used
         self.device, self.index = ids.device, ids.get_device()
-        self._at = (ids.data_ptr() or None, ids.numel(), used.data_ptr())
+        self._at, self._held = (ids.data_ptr() or None, ids.numel(), used.data_ptr()), (ids, used)
 
 
 def new_pool(n_blocks: int, *, device="cuda") -> Pool:
@@ -79,6 +81,7 @@ class Step:
         self._at = (_vector(begin, torch.int64, "begin", n + 1, self.index),
                     _vector(position, torch.int32, "position", room, self.index),
                     _vector(slot, torch.int64, "slot", room, self.index), room, n)
+        self._held = (begin, position, slot)
 
 
 def new_step(n_seqs: int, tokens: int, *, device="cuda") -> Step:

@@ -79,7 +79,7 @@ class Rotation:
             magnitude = 0.1 * math.log(factor) + 1.0 if scaling == "blend" else 1.0
         self.freq, self.turned, self.pairs, self.magnitude = freq, turned, bool(pairs), float(magnitude)
         self.device, self.index = freq.device, freq.get_device()
-        self._freq = freq.data_ptr()
+        self._freq, self._held = freq.data_ptr(), freq
 
 
 def rotate(rotation: Rotation, position, q, k=None, *, out=None, k_out=None, inverse: bool = False, stream=None):
