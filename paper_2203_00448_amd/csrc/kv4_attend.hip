@@ -708,27 +708,33 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_tiles_kernel(KvAtte
             }
         }
     };
-    for (int32_t x = x0; x < x1; x += 64, buf ^= 1) {
-        if (x + 64 < x1) {
-            load();
-            find(x + 128);
-        }
-        __syncthreads();  // the tile is whole; the other one is read no more
-        if (kPieces) {
+    for (int32_t x = x0;;) {
+        // left at a marked tile, so that what it takes is no part of the loop's registers
+        for (; x < x1; x += 64, buf ^= 1) {
+            if (x + 64 < x1) {
+                load();
+                find(x + 128);
+            }
+            __syncthreads();  // the tile is whole; the other one is read no more
+            if (AsF16::value && wave_one(marked[buf]) == x) break;  // the same for the workgroup
             if (x <= wave_most) tile(x, std::integral_constant<bool, kPieces>());
-        } else if (F16 && __builtin_expect(wave_one(marked[buf]) == x, 0)) {  // the same for the workgroup: the tile once more, then the next one's codes
-            find(x);
-            load();
-            put(buf, x, No());
-            __syncthreads();
-            if (x <= wave_most) tile(x, AsF16());
+            if (x + 64 < x1) put(buf ^ 1, x + 64, AsF16());
+        }
+        if (!AsF16::value || x >= x1) break;
+        // the tile once more, then the next one's codes
+        find(x);
+        load();
+        put(buf, x, No());
+        __syncthreads();
+        if (x <= wave_most) tile(x, AsF16());
+        if (x + 64 < x1) {
             find(x + 64);
             load();
             find(x + 128);
-        } else if (x <= wave_most) {
-            tile(x, No());
+            put(buf ^ 1, x + 64, AsF16());
         }
-        if (x + 64 < x1) put(buf ^ 1, x + 64, AsF16());
+        x += 64;
+        buf ^= 1;
     }
     if (pages.bad()) raise_status(a.status, MP_EINVAL);
     store_rows<D>(k, row, chunk, acc, m, l, h);
