@@ -66,16 +66,16 @@ __device__ __forceinline__ Need need_of(const Pages& p, int32_t length, int32_t 
 
 // What a new token of sequence s writes: `offset` tokens after the `held` ones; `first` its first new block's
 // place in ids.
-__device__ __forceinline__ void place_token(const Pages& p, int64_t s, int64_t row, int64_t held, int64_t offset,
-                                            int64_t first) {
+__device__ __forceinline__ void place_token(const Pages& p, int32_t s, int32_t row, int32_t held, int32_t offset,
+                                            int32_t first) {
     const int lb = p.log_block;
-    const int64_t pos = held + offset, have = (held + ((int64_t)1 << lb) - 1) >> lb;
-    const int64_t block = pos >> lb, at = pos & ((1 << lb) - 1);
+    const int32_t pos = held + offset, have = (int32_t)(((uint32_t)held + (1u << lb) - 1) >> lb);
+    const int32_t block = pos >> lb, at = pos & ((1 << lb) - 1);
     int32_t* const entry = p.table + s * p.table_stride + block;
     const int32_t id = block >= have ? p.ids[first + block - have] : *entry;
     if (id < 0) raise_status(p.status, MP_EINVAL);
     if (block >= have && at == 0) *entry = id;
-    if (p.position_out) p.position_out[row] = (int32_t)pos;
+    if (p.position_out) p.position_out[row] = pos;
     if (p.slot_out) p.slot_out[row] = ((int64_t)id << lb) + at;
 }
 
@@ -213,7 +213,7 @@ __global__ __launch_bounds__(kThreads) void kv_pages_sum_kernel(Pages p) {
                 else
                     hi = mid;
             }
-            place_token(p, lo, row, lengths[lo], row - bounds[lo], firsts[lo]);
+            place_token(p, lo, row, lengths[lo], row - bounds[lo], (int32_t)firsts[lo]);
         }
     } else {
         for (int s = tid >> 6; s < p.n_seqs; s += kThreads / 64)
@@ -222,42 +222,44 @@ __global__ __launch_bounds__(kThreads) void kv_pages_sum_kernel(Pages p) {
 }
 
 // A wave has kRun groups of 64 consecutive tokens.  It finds the sequence of its first one, 64 bounds a turn, and
-// those of the others among the next 64 bounds at a time.  1.4 million tokens of 2048 sequences 14 us, for 17 MB of
-// stores: a chain of loads (bounds, a sequence's numbers, its ids) four times.  One group a wave 18 us, eight 15.
+// those of the others among the next 64 bounds at a time.  1.4 million tokens of 2048 sequences 12 us, for 17 MB of
+// stores: its instructions (14 us with 64-bit places) and a chain of loads, bounds, a sequence's numbers, its ids.
 __global__ __launch_bounds__(256) void kv_pages_fill_kernel(Pages p) {
-    const int64_t total = p.first[p.n_seqs + 1], n_seqs = p.n_seqs;
-    const int64_t* const begin = p.begin_out;
+    // sequences, tokens of the call, positions and places in ids are all below 2^31
+    const int32_t total = (int32_t)p.first[p.n_seqs + 1], n_seqs = (int32_t)p.n_seqs;
+    const auto begin = [&](int32_t s) { return (int32_t)p.begin_out[s]; };
     const int lane = threadIdx.x & 63;
-    int64_t row0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * (64 * kRun);
-    if (row0 >= total) return;  // whole waves
-    int64_t lo = 0, hi = n_seqs;
+    const int64_t row00 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * (64 * kRun);
+    if (row00 >= total) return;  // whole waves
+    int32_t row0 = (int32_t)row00, lo = 0, hi = n_seqs;
     while (hi - lo > 1) {
-        const int64_t step = (hi - lo + kWave - 1) / kWave, at = lo + lane * step;
-        const uint64_t below = __ballot(at < hi && begin[min(at, n_seqs)] <= row0);
+        const int32_t step = (hi - lo + kWave - 1) / kWave;
+        const int64_t at = lo + (int64_t)lane * step;
+        const uint64_t below = __ballot(at < hi && begin((int32_t)min(at, (int64_t)n_seqs)) <= row0);
         const int count = below == ~0ull ? kWave : __ffsll((unsigned long long)~below) - 1;
-        lo += (int64_t)max(0, count - 1) * step;
+        lo += max(0, count - 1) * step;
         hi = min(hi, lo + step);
     }
-    int64_t base = lo + 1, from_lo = begin[lo];  // sequence lo begins at from_lo; the bounds from `base` on
-    int64_t b = base + lane < n_seqs ? begin[base + lane] : INT64_MAX;
+    int32_t base = lo + 1, from_lo = begin(lo);  // sequence lo begins at from_lo; the bounds from `base` on
+    int32_t b = base + lane < n_seqs ? begin(base + lane) : INT32_MAX;
     for (int run = 0; run < kRun && row0 < total; ++run, row0 += 64) {
-        const int64_t row = row0 + lane, last = min(total, row0 + 64) - 1, find = min(row, last);
-        int64_t s = lo, from = from_lo;
+        const int32_t row = row0 + lane, last = min(total, row0 + 64) - 1, find = min(row, last);
+        int32_t s = lo, from = from_lo;
         for (;;) {
             int count = 0;  // of these bounds, how many are at most the lane's row
 #pragma unroll
             for (int bit = 32; bit > 0; bit >>= 1)
                 if (__shfl(b, count + bit - 1, kWave) <= find) count += bit;
-            if (count == 63 && __shfl(b, 63, kWave) <= find) count = 64;
-            const int64_t at = __shfl(b, max(0, count - 1), kWave);
+            const int32_t end = __builtin_amdgcn_readlane(b, 63);
+            if (count == 63 && end <= find) count = 64;
+            const int32_t at = __shfl(b, max(0, count - 1), kWave);
             if (count > 0) s = base + count - 1, from = at;
-            const int64_t end = __shfl(b, 63, kWave);
-            if (end > last) break;  // INT64_MAX past the last sequence
+            if (end > last) break;  // INT32_MAX past the last sequence
             lo = base + 63, from_lo = end, base += kWave;
-            b = base + lane < n_seqs ? begin[base + lane] : INT64_MAX;
+            b = base + lane < n_seqs ? begin(base + lane) : INT32_MAX;
         }
         if (row < total)
-            place_token(p, s, row, (int64_t)p.length_out[s] - p.more[s], row - from, p.first[s]);
+            place_token(p, s, row, p.length_out[s] - p.more[s], row - from, (int32_t)p.first[s]);
     }
 }
 

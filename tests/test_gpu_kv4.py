@@ -393,6 +393,80 @@ def test_repeats_and_views(dtype, new):
     assert bool((room[:, 8] == 5).all()) and bool((room[..., 0] == 5).all()) and bool((room[..., 129:] == 5).all())
 
 
+@pytest.mark.parametrize("dtype,length,new", [(BF16, [3000, 900], None), (F16, [5000, 64], [100, 30]),
+                                              (BF16, [4000, 700], [60, 700])])
+def test_recorded(dtype, length, new):
+    """A write and an attention in chunks in one graph, replayed with other rows, eager work between."""
+    a, b = Setup(length, heads=2), Setup(length, heads=2)
+    a.fill()
+    for x, y in zip(a.cache.tensors, b.cache.tensors):
+        y.copy_(x)
+    n = 2 if new is None else sum(new)
+    seqs = [s.seqs(length, new)[0] for s in (a, b)]
+    q, k, v = a.rows(n, 8, dtype), a.rows(n, 2, dtype), a.rows(n, 2, dtype)
+    ws = [s.kv.workspace(s.kv.OP_ATTEND, s.cache, x, q_heads=8) for s, x in zip((a, b), seqs)]
+    status, outs = a.kv.new_status(), [torch.zeros_like(q) for _ in range(2)]
+
+    def both(s, x, space, out):
+        s.kv.write(s.cache, x, k, v, status=status, check=False)
+        s.kv.attend(s.cache, x, q, out=out, workspace=space, status=status, check=False)
+
+    both(a, seqs[0], ws[0], outs[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both(a, seqs[0], ws[0], outs[0])
+    for i in range(5):
+        for t, rows in ((q, a.rows(n, 8, dtype)), (k, a.rows(n, 2, dtype)), (v, a.rows(n, 2, dtype))):
+            t.copy_(rows)
+        graph.replay()
+        both(b, seqs[1], ws[1], outs[1])
+        assert torch.equal(outs[0], outs[1]), i
+        assert all(torch.equal(x, y) for x, y in zip(a.cache.tensors, b.cache.tensors))
+    assert int(status.item()) == 0
+
+
+def test_places_past_32_bits():
+    """Blocks whose codes lie more than 2^32 bytes into a cache, table rows and query rows as far apart."""
+    need_gpu()
+    from paper_2203_00448_amd import kv
+    n_blocks, dim = (1 << 20) + 5, 128
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("not enough memory")
+    c = [torch.empty(n_blocks, 1, 64, dim // 2, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    c += [torch.empty(n_blocks, 1, dim // 32, 64, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    cache = kv.Cache(*c, kind=kv.E2M1)
+    wide = torch.zeros(2, (1 << 30) + 3, dtype=torch.int32, device="cuda")
+    table = wide[:, :3]
+    table[0] = torch.tensor([n_blocks - 1, 3, n_blocks - 2])
+    table[1] = torch.tensor([n_blocks - 4, n_blocks - 3, 0])
+    s = Setup([150, 100], heads=1, garbage=False)
+    for x, y in zip(s.table, ([n_blocks - 1, 3, n_blocks - 2], [n_blocks - 4, n_blocks - 3])):
+        s.order = getattr(s, "order", {}) | {int(b): int(f) for b, f in zip(x, y)}
+    rows = torch.zeros(2 * (1 << 31) + 4096, dtype=BF16, device="cuda")
+    q = rows.as_strided((250, 1, 128), (1 << 24, 128, 1))
+    q.copy_(s.rows(250))
+    k, v = s.rows(250), s.rows(250)
+    length = torch.tensor([150, 100], dtype=torch.int32, device="cuda")
+    begin = torch.tensor([0, 150, 250], dtype=torch.int64, device="cuda")
+    seqs = kv.Seqs(table, length, begin=begin, tokens=250)
+    kv.write(cache, seqs, k, v)
+    s.ref.write(s.table, [150, 100], [0, 150, 250], host(k.double()), host(v.double()))
+    for small, far in s.order.items():
+        if far != 0:
+            got = host(cache.k_code[far])
+            used = 64 if far not in (n_blocks - 2, n_blocks - 3) else (150 - 128 if far == n_blocks - 2 else 100 - 64)
+            assert np.array_equal(got[:, :used], s.ref.k_code[small][:, :used])
+    near(kv.attend(cache, seqs, q), None, s.ref.attend(s.table, [150, 100], [0, 150, 250], host(q.double()), dim ** -0.5),
+         BF16, ONE)
+    ones = kv.Seqs(table, length)
+    got = kv.attend(cache, ones, q[:2])
+    near(got, None, s.ref.attend(s.table, [150, 100], [0, 1, 2], host(q[:2].double()), dim ** -0.5), BF16, TWO)
+    back = kv.read(cache, seqs, dtype=F32)
+    want = s.ref.read(s.table, [150, 100], [0, 150, 250])
+    assert np.array_equal(host(back[0]), want[0]) and np.array_equal(host(back[1]), want[1])
+
+
 def test_rows_behind_the_last_sequence_are_left():
     """A padded batch: sequences of no rows at the end, rows that are no sequence's."""
     s = Setup([90, 20, 30], heads=1)
