@@ -54,54 +54,76 @@ __device__ __forceinline__ float2_t sin_cos(int32_t position, double freq) {
     return float2_t{quarter & 2 ? -a : a, quarter == 1 || quarter == 2 ? -b : b};
 }
 
-__device__ __forceinline__ float load_one(const KvRows& r, int64_t at) {
-    if (r.dtype == MP_F32) return reinterpret_cast<const float*>(r.data)[at];
-    const uint16_t x = reinterpret_cast<const uint16_t*>(r.data)[at];
-    return r.dtype == MP_BF16 ? __uint_as_float((uint32_t)x << 16) : half_to_float(x);
-}
-__device__ __forceinline__ void store_one(const KvRows& r, int64_t at, float x) {
-    if (r.dtype == MP_F32)
-        reinterpret_cast<float*>(r.data)[at] = x;
+// VB bytes (an element at least) of elements of BYTES each, as words, as floats and back.
+template <int VB>
+struct Piece {
+    uint32_t w[(VB + 3) / 4];
+};
+template <int VB>
+__device__ __forceinline__ Piece<VB> load_piece(const char* p) {
+    Piece<VB> x;
+    if constexpr (VB == 16)
+        *reinterpret_cast<uint4_t*>(x.w) = *reinterpret_cast<const uint4_t*>(p);
+    else if constexpr (VB == 8)
+        *reinterpret_cast<uint2*>(x.w) = *reinterpret_cast<const uint2*>(p);
+    else if constexpr (VB == 4)
+        x.w[0] = *reinterpret_cast<const uint32_t*>(p);
     else
-        reinterpret_cast<uint16_t*>(r.data)[at] =
-            (uint16_t)(r.dtype == MP_BF16 ? float_to_bf16(x) : float_to_half(x));
+        x.w[0] = *reinterpret_cast<const uint16_t*>(p);
+    return x;
 }
-
-template <int BYTES, int N>
-__device__ __forceinline__ void load_vec(const KvRows& r, int64_t at, float (&x)[N]) {
-    if constexpr (BYTES == 4) {
-        const float4_t w = *reinterpret_cast<const float4_t*>(r.data + at * 4);
+template <int VB>
+__device__ __forceinline__ void store_piece(char* p, const Piece<VB>& x) {
+    if constexpr (VB == 16)
+        *reinterpret_cast<uint4_t*>(p) = *reinterpret_cast<const uint4_t*>(x.w);
+    else if constexpr (VB == 8)
+        *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(x.w);
+    else if constexpr (VB == 4)
+        *reinterpret_cast<uint32_t*>(p) = x.w[0];
+    else
+        *reinterpret_cast<uint16_t*>(p) = (uint16_t)x.w[0];
+}
+// As the type DTYPE is known to the compiler: conversions take a third of the instructions otherwise.
+template <int DTYPE, int VB>
+__device__ __forceinline__ void to_floats(const Piece<VB>& p, float* x) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = w[i];
-    } else {
-        const uint4_t w = *reinterpret_cast<const uint4_t*>(r.data + at * 2);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) pair_to_float(r.dtype == MP_BF16, w[i], x + 2 * i);
+    for (int i = 0; i < (VB + 3) / 4; ++i) {
+        if constexpr (DTYPE == MP_F32)
+            x[i] = __uint_as_float(p.w[i]);
+        else if constexpr (VB >= 4)
+            pair_to_float(DTYPE == MP_BF16, p.w[i], x + 2 * i);
+        else
+            x[0] = DTYPE == MP_BF16 ? __uint_as_float(p.w[0] << 16) : half_to_float(p.w[0]);
     }
 }
-template <int BYTES, int N>
-__device__ __forceinline__ void store_vec(const KvRows& r, int64_t at, const float (&x)[N]) {
-    if constexpr (BYTES == 4) {
-        *reinterpret_cast<float4_t*>(r.data + at * 4) = float4_t{x[0], x[1], x[2], x[3]};
-    } else {
-        uint4_t w;
+template <int DTYPE, int VB>
+__device__ __forceinline__ Piece<VB> from_floats(const float* x) {
+    typedef __bf16 bf2_t __attribute__((ext_vector_type(2)));
+    Piece<VB> p;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            w[i] = r.dtype == MP_BF16 ? float_to_bf16(x[2 * i]) | float_to_bf16(x[2 * i + 1]) << 16
-                                      : float_to_half(x[2 * i]) | float_to_half(x[2 * i + 1]) << 16;
-        *reinterpret_cast<uint4_t*>(r.data + at * 2) = w;
+    for (int i = 0; i < (VB + 3) / 4; ++i) {
+        if constexpr (DTYPE == MP_F32)
+            p.w[i] = __float_as_uint(x[i]);
+        else if constexpr (VB < 4)
+            p.w[0] = DTYPE == MP_BF16 ? float_to_bf16(x[0]) : float_to_half(x[0]);
+        else if constexpr (DTYPE == MP_BF16)
+            p.w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((float2_t{x[2 * i], x[2 * i + 1]}), bf2_t));
+        else
+            p.w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((float2_t{x[2 * i], x[2 * i + 1]}), half2_t));
     }
+    return p;
 }
 
-// BYTES of an element; WIDE: 16 bytes at a time, with `turned` and `dim` in whole pieces of them (of
-// `turned / 2` where PAIRS is not set).  A thread keeps its place in a head and goes through the (token, head)
-// pairs of the workgroup.
+// VB bytes at a time, V elements, with `dim` and `turned` in whole pieces of them (`turned / 2`
+// where PAIRS is not set; a single element of a pair has the other one beside it).  A thread keeps its place in a
+// head and goes through the (token, head) pairs of the workgroup.
 //
-// 16384 tokens of 40 heads of 128, 16-bit: 69 us, 4.9 TB/s (a large copy: 4.9).  8191 of 27 heads of 96 in 32 bits
-// 32 us, 5.3 TB/s on inputs that the caches hold, 46 us cold; 64 tokens of 40 heads 4.6 us traced.
-template <int BYTES, bool PAIRS, bool WIDE>
+// 16384 tokens of 40 heads of 128, 16-bit: 69 us, 4.9 TB/s (a large copy: 4.9).  8191 of 27 heads of 96, 64
+// turned, in 32 bits 29 us, 5.9 TB/s on inputs that the caches hold, 39 us cold (32 and 46 with loads of their own for
+// the lanes that turn nothing); 64 tokens of 40 heads 4.6 us traced.
+template <int DTYPE, bool PAIRS, int VB>
 __global__ __launch_bounds__(256) void kv_rotary_kernel(Rotary a) {
-    constexpr int V = WIDE ? 16 / BYTES : 1;
+    constexpr int BYTES = DTYPE == MP_F32 ? 4 : 2, V = VB / BYTES;
     extern __shared__ __align__(16) float lds[];
     const int pairs = a.turned / 2, tid = threadIdx.x;
     const int64_t token0 = (int64_t)blockIdx.x * a.tokens;
@@ -115,64 +137,57 @@ __global__ __launch_bounds__(256) void kv_rotary_kernel(Rotary a) {
         sines[i] = sc[0] * a.magnitude * a.sign;
     }
     __syncthreads();
-    // pieces of a head: turned ones, then the others
-    const int turned_pieces = PAIRS ? (WIDE ? a.turned / V : pairs) : pairs / V;
+    // pieces of a head: turned ones (with PAIRS and single elements, one for two), then the others
+    const int turned_pieces = PAIRS && V > 1 ? a.turned / V : pairs / V;
     const int pieces = turned_pieces + (a.dim - a.turned) / V;
     const int lanes = 1 << a.log_lanes, side = 256 >> a.log_lanes;
     const int all = tokens * a.heads;
     for (int u = tid >> a.log_lanes; u < all; u += side) {
         const int t = (int)(((float)u + 0.5f) * a.by_heads), head = u - t * a.heads;
         const bool is_k = head >= a.q_heads;
-        const KvRows& in = is_k ? a.k : a.q;
-        const KvRows& out = is_k ? a.k_out : a.q_out;
-        const int own = is_k ? head - a.q_heads : head;
-        const int64_t from = (token0 + t) * in.token_stride + own * in.head_stride;
-        const int64_t to = (token0 + t) * out.token_stride + own * out.head_stride;
+        // field by field: of a struct that a lane chooses the fields are loaded again for every head (46 us cold became 59)
+        const int64_t index = is_k ? head - a.q_heads : head, token = token0 + t;
+        const char* const from = (is_k ? a.k.data : a.q.data) + (token * (is_k ? a.k.token_stride : a.q.token_stride) +
+                                                                 index * (is_k ? a.k.head_stride : a.q.head_stride)) * BYTES;
+        char* const to = (is_k ? a.k_out.data : a.q_out.data) +
+                         (token * (is_k ? a.k_out.token_stride : a.q_out.token_stride) +
+                          index * (is_k ? a.k_out.head_stride : a.q_out.head_stride)) * BYTES;
         const float* const cs = cosines + t * pairs;
         const float* const sn = sines + t * pairs;
         for (int piece = tid & (lanes - 1); piece < pieces; piece += lanes) {
-            if (piece >= turned_pieces) {
-                if (!(is_k ? a.k_copy : a.q_copy)) continue;
-                const int d = a.turned + (piece - turned_pieces) * V;
-                if constexpr (WIDE)
-                    *reinterpret_cast<uint4_t*>(out.data + (to + d) * BYTES) =
-                        *reinterpret_cast<const uint4_t*>(in.data + (from + d) * BYTES);
-                else if constexpr (BYTES == 4)
-                    reinterpret_cast<uint32_t*>(out.data)[to + d] = reinterpret_cast<const uint32_t*>(in.data)[from + d];
-                else
-                    reinterpret_cast<uint16_t*>(out.data)[to + d] = reinterpret_cast<const uint16_t*>(in.data)[from + d];
-                continue;
-            }
-            if constexpr (!WIDE) {
-                const int d = PAIRS ? 2 * piece : piece, e = PAIRS ? d + 1 : d + pairs;
-                const float x = load_one(in, from + d), y = load_one(in, from + e);
-                const float c = cs[piece], s = sn[piece];
-                store_one(out, to + d, x * c - y * s);
-                store_one(out, to + e, x * s + y * c);
-            } else if constexpr (PAIRS) {
-                float x[V];
-                load_vec<BYTES>(in, from + piece * V, x);
+            const bool turn = piece < turned_pieces;
+            if (!turn && !(is_k ? a.k_copy : a.q_copy)) continue;
+            if constexpr (PAIRS && V > 1) {  // one load of all lanes, whether they turn it or not
+                const int d = piece * V;
+                Piece<VB> own = load_piece<VB>(from + d * BYTES);
+                if (turn) {
+                    float x[V];
+                    to_floats<DTYPE, VB>(own, x);
 #pragma unroll
-                for (int i = 0; i < V; i += 2) {
-                    const float c = cs[piece * (V / 2) + i / 2], s = sn[piece * (V / 2) + i / 2];
-                    const float p = x[i], q = x[i + 1];
-                    x[i] = p * c - q * s;
-                    x[i + 1] = p * s + q * c;
+                    for (int i = 0; i < V; i += 2) {
+                        const float c = cs[(d + i) / 2], s = sn[(d + i) / 2], p = x[i], q = x[i + 1];
+                        x[i] = p * c - q * s;
+                        x[i + 1] = p * s + q * c;
+                    }
+                    own = from_floats<DTYPE, VB>(x);
                 }
-                store_vec<BYTES>(out, to + piece * V, x);
+                store_piece<VB>(to + d * BYTES, own);
+            } else if (!turn) {
+                const int d = a.turned + (piece - turned_pieces) * V;
+                store_piece<VB>(to + d * BYTES, load_piece<VB>(from + d * BYTES));
             } else {
+                const int d = PAIRS ? 2 * piece : piece * V, e = PAIRS ? d + 1 : d + pairs;
                 float x[V], y[V];
-                load_vec<BYTES>(in, from + piece * V, x);
-                load_vec<BYTES>(in, from + pairs + piece * V, y);
+                to_floats<DTYPE, VB>(load_piece<VB>(from + d * BYTES), x);
+                to_floats<DTYPE, VB>(load_piece<VB>(from + e * BYTES), y);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    const float c = cs[piece * V + i], s = sn[piece * V + i];
-                    const float p = x[i], q = y[i];
+                    const float c = cs[piece * V + i], s = sn[piece * V + i], p = x[i], q = y[i];
                     x[i] = p * c - q * s;
                     y[i] = p * s + q * c;
                 }
-                store_vec<BYTES>(out, to + piece * V, x);
-                store_vec<BYTES>(out, to + pairs + piece * V, y);
+                store_piece<VB>(to + d * BYTES, from_floats<DTYPE, VB>(x));
+                store_piece<VB>(to + e * BYTES, from_floats<DTYPE, VB>(y));
             }
         }
     }
@@ -210,12 +225,28 @@ bool same_rows(const KvRows& a, const KvRows& b) {
     return a.data == b.data && a.token_stride == b.token_stride && a.head_stride == b.head_stride;
 }
 
-template <int BYTES, bool PAIRS>
-void launch(const Rotary& a, bool wide, dim3 grid, size_t room, hipStream_t st) {
-    if (wide)
-        kv_rotary_kernel<BYTES, PAIRS, true><<<grid, 256, room, st>>>(a);
+// The most bytes, a power of two up to 16, that divide a row's place and strides.
+int alignment(const KvRows& r) {
+    const uintptr_t size = r.dtype == MP_F32 ? 4 : 2;
+    const uintptr_t all = reinterpret_cast<uintptr_t>(r.data) | r.token_stride * size | r.head_stride * size | 16;
+    return (int)(all & -all);
+}
+
+template <int DTYPE, bool PAIRS>
+void launch(const Rotary& a, int vb, dim3 grid, size_t room, hipStream_t st) {
+    if (vb == 16)
+        kv_rotary_kernel<DTYPE, PAIRS, 16><<<grid, 256, room, st>>>(a);
+    else if (vb == 8)
+        kv_rotary_kernel<DTYPE, PAIRS, 8><<<grid, 256, room, st>>>(a);
+    else if (vb == 4)
+        kv_rotary_kernel<DTYPE, PAIRS, 4><<<grid, 256, room, st>>>(a);
     else
-        kv_rotary_kernel<BYTES, PAIRS, false><<<grid, 256, room, st>>>(a);
+        kv_rotary_kernel<DTYPE, PAIRS, DTYPE == MP_F32 ? 4 : 2><<<grid, 256, room, st>>>(a);
+}
+
+template <int DTYPE>
+void launch(const Rotary& a, bool pairs, int vb, dim3 grid, size_t room, hipStream_t st) {
+    pairs ? launch<DTYPE, true>(a, vb, grid, room, st) : launch<DTYPE, false>(a, vb, grid, room, st);
 }
 
 }  // namespace
@@ -250,11 +281,14 @@ extern "C" int32_t mp_rotate(const int32_t* position, int64_t n_tokens, const do
     a.q_copy = !same_rows(a.q, a.q_out), a.k_copy = !same_rows(a.k, a.k_out);
     a.magnitude = magnitude, a.sign = inverse ? -1.0f : 1.0f, a.by_heads = 1.0f / a.heads;
     const bool pairs = layout == MP_ROTARY_PAIRS, f32 = a.q.dtype == MP_F32;
-    const int v = f32 ? 4 : 8;
-    const bool wide = a.q.wide && a.q_out.wide && a.k.wide && a.k_out.wide && dim % v == 0 &&
-                      (pairs ? turned : turned / 2) % v == 0;
-    const int per = wide ? v : 1;
-    const int pieces = (pairs ? (wide ? turned / v : turned / 2) : turned / 2 / per) + (dim - turned) / per;
+    // the widest pieces that everything is whole ones of.  16-bit, by these and by elements: 32534 tokens of 9 heads
+    // of 96, 76 turned in pairs (8 bytes) 34 and 78 us; 16384 of 40 heads of 66 in pairs (4 bytes) 95 and 128.
+    const int size = f32 ? 4 : 2, whole = pairs ? turned : turned / 2;
+    int vb = alignment(a.q);
+    for (const KvRows* r : {&a.q_out, &a.k, &a.k_out}) vb = alignment(*r) < vb ? alignment(*r) : vb;
+    while (vb > size && (dim % (vb / size) != 0 || whole % (vb / size) != 0)) vb /= 2;
+    const int v = vb / size;
+    const int pieces = (pairs && v > 1 ? turned / v : turned / 2 / v) + (dim - turned) / v;
     while ((1 << a.log_lanes) < pieces && a.log_lanes < 8) ++a.log_lanes;
     // tokens of a workgroup: a few thousand pieces, but a workgroup for every place of the device first;
     // their angles fit 32 KiB
@@ -267,9 +301,10 @@ extern "C" int32_t mp_rotate(const int32_t* position, int64_t n_tokens, const do
     const dim3 grid((uint32_t)groups);
     const size_t room = (size_t)a.tokens * turned * 4;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (f32)
-        pairs ? launch<4, true>(a, wide, grid, room, st) : launch<4, false>(a, wide, grid, room, st);
-    else
-        pairs ? launch<2, true>(a, wide, grid, room, st) : launch<2, false>(a, wide, grid, room, st);
+    switch (a.q.dtype) {
+        case MP_BF16: launch<MP_BF16>(a, pairs, vb, grid, room, st); break;
+        case MP_F16: launch<MP_F16>(a, pairs, vb, grid, room, st); break;
+        default: launch<MP_F32>(a, pairs, vb, grid, room, st);
+    }
     return hipGetLastError() == hipSuccess ? MP_OK : MP_EDEVICE;
 }

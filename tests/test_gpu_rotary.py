@@ -119,7 +119,7 @@ def test_scaled_frequencies(scaling):
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("pairs", [False, True])
-@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("shift", [0, 1, 2, 4])  # of elements: 2 to 16 bytes at a time
 def test_in_place_and_strided(shift, pairs, dtype):
     """Queries and keys side by side in wider rows, turned where they are; the rest of the rows is left."""
     rotary = module()
