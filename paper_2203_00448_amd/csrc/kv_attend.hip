@@ -1195,6 +1195,38 @@ hipError_t launch_kv_join(const KvAttend& k, hipStream_t st) {
     return hipGetLastError();
 }
 
+// Chunks of a sequence for tiles in 4 bits: as many as nearly fill one to four rounds of workgroups, by the estimated
+// time.  A last round that is not full takes `alone` of a full one and as much of the rest as it is full: its
+// workgroups have a compute unit to themselves.  Every chunk writes its rows' results in 32 bits, which the join
+// reads.  Sequences of different lengths do not have all chunks; one round would not even that out.  us, by
+// four workgroups a compute unit and by this:
+//   333 rows after 20000 tokens, 32 query heads over 8 of 128, 16-bit floats 195, 169 (12 and 5 chunks); bfloat16, of 64
+//   105, 98; 3 such sequences, of 128 442, 416; 200 rows, of 256 427, 365; 64 rows each of 16 sequences of 8000, of
+//   128 195, 177; 128 rows after 131072, 8 over 8 of 256 279, 262; 900 rows of 3000, 28 over 4 of 64 53, 55.
+// Several sequences with heads of 64 keep four a unit: 333 rows of 3 after 20000 tokens, 28 over 4 265, 271 by this.
+static int64_t kv4_tile_chunks(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t q_heads,
+                               int32_t dtype, int64_t units) {
+    const int64_t group = q_heads / c.heads;
+    int64_t groups = (std::min(s.most_new, s.n_tokens) * group + 127) / 128;  // of a sequence, and of all
+    groups = (s.n_seqs > 0 && groups > units / s.n_seqs ? units : std::max<int64_t>(groups * s.n_seqs, 1)) * c.heads;
+    const int64_t places = 256 * (c.dim == 256 ? 1 : c.dim == 128 ? 2 : dtype == MP_F16 ? 3 : 4);
+    const double alone = c.dim == 256 ? 1.0 : c.dim == 128 ? 0.6 : 0.4;
+    const double work = 4.0 * 128 * groups * s.longest * c.dim / (c.dim == 256 ? 5e8 : 8e8);  // us
+    const double join = 8.0 * s.n_tokens * q_heads * (c.dim + 4) / 4.9e6;
+    int64_t best = 1;
+    double least = 0;
+    for (int64_t round = 0; round <= 4; ++round) {
+        if (round == 1 && s.n_seqs > 1) continue;
+        const int64_t chunks = round == 0 ? 1 : round * places / groups;
+        if (chunks < 1) continue;
+        const double full = (double)(groups * chunks) / places, rest = full - floor(full);
+        const double cost = work / full * (floor(full) + (rest > 0 ? alone + (1 - alone) * rest : 0)) +
+                            (chunks > 1 ? 5 + join * chunks : 0);
+        if (round == 0 || cost < least) best = chunks, least = cost;
+    }
+    return best;
+}
+
 KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t q_heads,
                               int64_t keep, int32_t dtype) {
     KvAttendShape sh = {};
@@ -1243,7 +1275,7 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     // fewer workgroups than compute units, 512 at least and all in one up to 1024.  Measured with
     // 512 / 1024 / 2048 / 4096: 64 sequences of 1-16384 tokens 155 / 146 / 149 / 157 us, of 8192
     // each 196 / 186 / 182 / 179, one of 4000 13 / 16 / 21 / 28, 32 of 1-1000 17 / 13 / 13 / 13.
-    // Tiles are split only as far as four workgroups a compute unit need it: a piece of 333 rows
+    // Tiles are split only as far as four workgroups a compute unit need it (in 4 bits: as above): a piece of 333 rows
     // after 20000 tokens 118 us (two: 149, eight: 114), prompts that fill the device without
     // chunks 290 us (559 in chunks of 2048: the partial results are 32-bit).
     const int64_t wide = sh.units * c.heads;
@@ -1263,7 +1295,9 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     if (chunk < 512) chunk = 512;
     if (longest <= 1024) chunk = 1024;
     if (sh.form != KvForm::rows) {
-        const int64_t chunks = wide > 0 ? (4 * 256 + wide - 1) / wide : 1;
+        int64_t chunks = wide > 0 ? (4 * 256 + wide - 1) / wide : 1;
+        if (c.kind == MP_KV_E2M1 && sh.form == KvForm::tiles && (c.dim > 64 || s.n_seqs == 1))
+            chunks = kv4_tile_chunks(c, s, q_heads, dtype, sh.units);
         chunk = (longest + chunks - 1) / chunks;
         if (chunk < 512) chunk = 512;
     }
