@@ -466,15 +466,15 @@ __device__ __forceinline__ int v4_key(int token) {
     return D == 64 ? (token >> 1 & 1) << 2 : (token & 3) << 2;
 }
 
-// Measured, 333 rows of heads of 64 after 20000 tokens, 16-bit floats: 109 us and the join, 500 TFLOP/s.  Four
-// sequences of 2048 tokens, 700 new, 32 query heads over 8, bfloat16: heads of 64 111 us, of 128 162 us, of 256
-// 441 us; 16-bit floats 122, 188 and 559.  A tile's softmax takes a wave about 900 cycles of vector instructions
+// Measured, 333 rows of heads of 64 after 20000 tokens, 16-bit floats: 101 us and the join, 540 TFLOP/s.  Four
+// sequences of 2048 tokens, 700 new, 32 query heads over 8, bfloat16: heads of 64 62 us, of 128 110 us, of 256
+// 312 us; 16-bit floats 65, 115 and 418.  A tile's softmax takes a wave about 900 cycles of vector instructions
 // (512 of them exponentials), its products of heads of 64 512.
 //
 // F16, rows of 16-bit floats: the tile as 16-bit floats, so that one instruction holds a query's and a
 // weight's 11 bits.  A group of codes that these cannot hold exactly (scales outside 2^-23..2^13, codes not all zero)
 // marks its tile, and the workgroup takes a marked tile as bfloat16, with queries and weights in two pieces.  (All tiles
-// in two pieces: 143 us instead of 112 for the rows above.)
+// in two pieces: 143 us, with the join, instead of 112 for the rows above.)
 // Heads of 256 have no registers for both: all their tiles are taken so.
 template <int D, bool F16>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_tiles_kernel(KvAttend k) {

@@ -1195,15 +1195,16 @@ hipError_t launch_kv_join(const KvAttend& k, hipStream_t st) {
     return hipGetLastError();
 }
 
-// Chunks of a sequence for tiles in 4 bits: as many as nearly fill one to four rounds of workgroups, by the estimated
-// time.  A last round that is not full takes `alone` of a full one and as much of the rest as it is full: its
+// Chunks of a sequence for tiles in 4 bits: one, or as many as nearly fill up to four rounds of workgroups, by the
+// estimated time.  A last round that is not full takes `alone` of a full one and as much of the rest as it is full: its
 // workgroups have a compute unit to themselves.  Every chunk writes its rows' results in 32 bits, which the join
-// reads.  Sequences of different lengths do not have all chunks; one round would not even that out.  us, by
-// four workgroups a compute unit and by this:
-//   333 rows after 20000 tokens, 32 query heads over 8 of 128, 16-bit floats 195, 169 (12 and 5 chunks); bfloat16, of 64
-//   105, 98; 3 such sequences, of 128 442, 416; 200 rows, of 256 427, 365; 64 rows each of 16 sequences of 8000, of
-//   128 195, 177; 128 rows after 131072, 8 over 8 of 256 279, 262; 900 rows of 3000, 28 over 4 of 64 53, 55.
-// Several sequences with heads of 64 keep four a unit: 333 rows of 3 after 20000 tokens, 28 over 4 265, 271 by this.
+// reads.  Sequences of different lengths do not have all chunks: one round of them would not be even; with heads of
+// 64, rounds are not even either, and four workgroups a compute unit it is.  us, by four a unit always and by this, 32
+// query heads over 8:
+//   333 rows after 20000 tokens, heads of 64 105, 98; of 128, 16-bit floats 195, 169 (12 and 5 chunks); 3 such
+//   sequences, bfloat16 442, 416; 200 rows, heads of 256 427, 365; 64 rows each of 16 sequences of 8000 195, 177;
+//   4 sequences of 2048 tokens, 700 new, heads of 64 111, 62 (one chunk), of 128 172, 113, of 256 437, 312; one of
+//   2048, all new, 105, 64.
 static int64_t kv4_tile_chunks(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t q_heads,
                                int32_t dtype, int64_t units) {
     const int64_t group = q_heads / c.heads;
@@ -1216,8 +1217,11 @@ static int64_t kv4_tile_chunks(const mp_kv_cache& c, const mp_kv_seqs& s, int32_
     int64_t best = 1;
     double least = 0;
     for (int64_t round = 0; round <= 4; ++round) {
-        if (round == 1 && s.n_seqs > 1) continue;
-        const int64_t chunks = round == 0 ? 1 : round * places / groups;
+        int64_t chunks = round == 0 ? 1 : round * places / groups;
+        if (round > 0 && s.n_seqs > 1) {
+            if (c.dim > 64 ? round == 1 : round > 1) continue;
+            if (c.dim == 64) chunks = (4 * 256 + units * c.heads - 1) / (units * c.heads);
+        }
         if (chunks < 1) continue;
         const double full = (double)(groups * chunks) / places, rest = full - floor(full);
         const double cost = work / full * (floor(full) + (rest > 0 ? alone + (1 - alone) * rest : 0)) +
@@ -1254,9 +1258,9 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     // In 4 bits pairs are for bfloat16 rows (16-bit floats would want registers for both forms of their tiles) and for
     // launches of four rounds of workgroups.  Tiles against pairs, us, as above:
     //             1024 new     2048 new     2048 of 8192
-    //   1 seq.    70 / 71      99 / 134     312 / 297
-    //   4         122 / 212    165 / 167    975 / 860
-    //   16        481 / 463
+    //   1 seq.    69 / 76      64 / 132     277 / 310
+    //   4         122 / 213    169 / 168    970 / 860
+    //   16        485 / 465    680 / 672
     if (c.kind == MP_KV_E2M1 && sh.form == KvForm::pair &&
         (dtype != MP_BF16 || (s.n_tokens * group / 256 + s.n_seqs) * c.heads < 1024))
         sh.form = KvForm::tiles;
@@ -1296,8 +1300,7 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     if (longest <= 1024) chunk = 1024;
     if (sh.form != KvForm::rows) {
         int64_t chunks = wide > 0 ? (4 * 256 + wide - 1) / wide : 1;
-        if (c.kind == MP_KV_E2M1 && sh.form == KvForm::tiles && (c.dim > 64 || s.n_seqs == 1))
-            chunks = kv4_tile_chunks(c, s, q_heads, dtype, sh.units);
+        if (c.kind == MP_KV_E2M1 && sh.form == KvForm::tiles) chunks = kv4_tile_chunks(c, s, q_heads, dtype, sh.units);
         chunk = (longest + chunks - 1) / chunks;
         if (chunk < 512) chunk = 512;
     }
