@@ -241,7 +241,9 @@ def test_attend_prompt(block, dim, heads, group, dtype, new):
 
 @pytest.mark.parametrize("dtype,dim,length,new", [(BF16, 128, [5000], None), (F16, 64, [9000, 3000], None),
                                                   (BF16, 128, [20000, 100], [40, 40]), (F16, 256, [6000], [3]),
-                                                  (BF16, 64, [7000], [100])])
+                                                  (BF16, 64, [7000], [100]), (BF16, 128, [9001], [33]),
+                                                  (F16, 128, [9001], [40]), (F16, 64, [10000], [65]),
+                                                  (F16, 256, [5000, 2000], [30, 70]), (BF16, 256, [8999], [25])])
 def test_attend_chunks(dtype, dim, length, new):
     """Long sequences in chunks that are joined; the last chunks of the shorter ones see nothing."""
     s = Setup(length, heads=1, dim=dim)
