@@ -22,6 +22,8 @@ struct Rotary {
     int32_t dim, turned, tokens;  // tokens of a workgroup
     int32_t q_copy, k_copy;  // whether the elements that are not turned have to be copied
     int32_t log_lanes;       // threads of a head
+    // Pieces of a head: those that are turned, all of 16 bytes, with the single pairs, with the single others.
+    int32_t turned_pieces, wide, pairs_to, pieces;
     float magnitude, sign;
     float by_heads;          // 1 / heads
 };
@@ -54,34 +56,40 @@ __device__ __forceinline__ float2_t sin_cos(int32_t position, double freq) {
     return float2_t{quarter & 2 ? -a : a, quarter == 1 || quarter == 2 ? -b : b};
 }
 
-// VB bytes (an element at least) of elements of BYTES each, as words, as floats and back.
+// VB bytes of elements, 16 or one element's, as words; a piece of 16 bytes lies anywhere where WHOLE is not set (its
+// elements are aligned, the load and the store need no more).
 template <int VB>
 struct Piece {
     uint32_t w[(VB + 3) / 4];
 };
-template <int VB>
+typedef uint32_t any4_t __attribute__((ext_vector_type(4), aligned(2)));
+template <int VB, bool WHOLE>
 __device__ __forceinline__ Piece<VB> load_piece(const char* p) {
     Piece<VB> x;
-    if constexpr (VB == 16)
-        *reinterpret_cast<uint4_t*>(x.w) = *reinterpret_cast<const uint4_t*>(p);
-    else if constexpr (VB == 8)
-        *reinterpret_cast<uint2*>(x.w) = *reinterpret_cast<const uint2*>(p);
-    else if constexpr (VB == 4)
+    if constexpr (VB == 16) {
+        const uint4_t w = WHOLE ? *reinterpret_cast<const uint4_t*>(p) : (uint4_t)*reinterpret_cast<const any4_t*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x.w[i] = w[i];
+    } else if constexpr (VB == 4) {
         x.w[0] = *reinterpret_cast<const uint32_t*>(p);
-    else
+    } else {
         x.w[0] = *reinterpret_cast<const uint16_t*>(p);
+    }
     return x;
 }
-template <int VB>
+template <int VB, bool WHOLE>
 __device__ __forceinline__ void store_piece(char* p, const Piece<VB>& x) {
-    if constexpr (VB == 16)
-        *reinterpret_cast<uint4_t*>(p) = *reinterpret_cast<const uint4_t*>(x.w);
-    else if constexpr (VB == 8)
-        *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(x.w);
-    else if constexpr (VB == 4)
+    if constexpr (VB == 16) {
+        const uint4_t w = {x.w[0], x.w[1], x.w[2], x.w[3]};
+        if constexpr (WHOLE)
+            *reinterpret_cast<uint4_t*>(p) = w;
+        else
+            *reinterpret_cast<any4_t*>(p) = w;
+    } else if constexpr (VB == 4) {
         *reinterpret_cast<uint32_t*>(p) = x.w[0];
-    else
+    } else {
         *reinterpret_cast<uint16_t*>(p) = (uint16_t)x.w[0];
+    }
 }
 // As the type DTYPE is known to the compiler: conversions take a third of the instructions otherwise.
 template <int DTYPE, int VB>
@@ -114,16 +122,28 @@ __device__ __forceinline__ Piece<VB> from_floats(const float* x) {
     return p;
 }
 
-// VB bytes at a time, V elements, with `dim` and `turned` in whole pieces of them (`turned / 2`
-// where PAIRS is not set; a single element of a pair has the other one beside it).  A thread keeps its place in a
-// head and goes through the (token, head) pairs of the workgroup.
+// With roundings that do not depend on the place in a piece: to 32 bits, and from there.  (The empty statements keep the
+// compiler from one instruction for a sum and its rounding to 16 bits, which it takes here and not there.)
+__device__ __forceinline__ void turned_pair(float p, float q, float c, float s, float* x, float* y) {
+    float a = __builtin_fmaf(p, c, -(q * s)), b = __builtin_fmaf(p, s, q * c);
+    asm("" : "+v"(a));
+    asm("" : "+v"(b));
+    *x = a, *y = b;
+}
+
+// 16 bytes at a time, V elements.  WHOLE: rows lie at multiples of 16 bytes, `dim` and `turned` are whole pieces of them
+// (`turned / 2` where PAIRS is not set).  Otherwise pieces lie anywhere, and the last one of the turned elements and of
+// the others begins earlier, in the one before, where outputs are not their inputs: both write the same.  Of rows turned
+// in place, whose elements may be written before the other piece reads them, and of fewer than V elements, what is left
+// goes one by one.  A thread keeps its place in a head and goes through the (token, head) pairs of the workgroup.
 //
 // 16384 tokens of 40 heads of 128, 16-bit: 69 us, 4.9 TB/s (a large copy: 4.9).  8191 of 27 heads of 96, 64
 // turned, in 32 bits 29 us, 5.9 TB/s on inputs that the caches hold, 39 us cold (32 and 46 with loads of their own for
-// the lanes that turn nothing); 64 tokens of 40 heads 4.6 us traced.
-template <int DTYPE, bool PAIRS, int VB>
+// the lanes that turn nothing); 64 tokens of 40 heads 4 us traced.  Not whole, 16-bit, 16384 tokens of 40 heads, halves:
+// of 66 31 us (100 by single elements, 35 with what is left of a head by them), 50 turned of 128 88 (228, 144).
+template <int DTYPE, bool PAIRS, bool WHOLE>
 __global__ __launch_bounds__(256) void kv_rotary_kernel(Rotary a) {
-    constexpr int BYTES = DTYPE == MP_F32 ? 4 : 2, V = VB / BYTES;
+    constexpr int BYTES = DTYPE == MP_F32 ? 4 : 2, V = 16 / BYTES;
     extern __shared__ __align__(16) float lds[];
     const int pairs = a.turned / 2, tid = threadIdx.x;
     const int64_t token0 = (int64_t)blockIdx.x * a.tokens;
@@ -137,9 +157,8 @@ __global__ __launch_bounds__(256) void kv_rotary_kernel(Rotary a) {
         sines[i] = sc[0] * a.magnitude * a.sign;
     }
     __syncthreads();
-    // pieces of a head: turned ones (with PAIRS and single elements, one for two), then the others
-    const int turned_pieces = PAIRS && V > 1 ? a.turned / V : pairs / V;
-    const int pieces = turned_pieces + (a.dim - a.turned) / V;
+    const int turned_pieces = a.turned_pieces, wide = a.wide, pieces = WHOLE ? wide : a.pieces;
+    const int each = PAIRS ? a.turned : pairs, rest = a.dim - a.turned;
     const int lanes = 1 << a.log_lanes, side = 256 >> a.log_lanes;
     const int all = tokens * a.heads;
     for (int u = tid >> a.log_lanes; u < all; u += side) {
@@ -155,39 +174,55 @@ __global__ __launch_bounds__(256) void kv_rotary_kernel(Rotary a) {
         const float* const cs = cosines + t * pairs;
         const float* const sn = sines + t * pairs;
         for (int piece = tid & (lanes - 1); piece < pieces; piece += lanes) {
+            if (!WHOLE && piece >= wide) {
+                const bool turn = piece < a.pairs_to;
+                if (!turn && !(is_k ? a.k_copy : a.q_copy)) continue;
+                const int pair = turned_pieces * (PAIRS ? V / 2 : V) + piece - wide;
+                const int d = !turn ? a.dim - (pieces - piece) : PAIRS ? 2 * pair : pair;
+                Piece<BYTES> first = load_piece<BYTES, true>(from + d * BYTES);
+                if (turn) {
+                    const int e = PAIRS ? d + 1 : d + pairs;
+                    const float c = cs[pair], s = sn[pair];
+                    float p, q;
+                    to_floats<DTYPE, BYTES>(load_piece<BYTES, true>(from + e * BYTES), &q);
+                    to_floats<DTYPE, BYTES>(first, &p);
+                    float x, y;
+                    turned_pair(p, q, c, s, &x, &y);
+                    store_piece<BYTES, true>(to + e * BYTES, from_floats<DTYPE, BYTES>(&y));
+                    first = from_floats<DTYPE, BYTES>(&x);
+                }
+                store_piece<BYTES, true>(to + d * BYTES, first);
+                continue;
+            }
             const bool turn = piece < turned_pieces;
             if (!turn && !(is_k ? a.k_copy : a.q_copy)) continue;
-            if constexpr (PAIRS && V > 1) {  // one load of all lanes, whether they turn it or not
-                const int d = piece * V;
-                Piece<VB> own = load_piece<VB>(from + d * BYTES);
+            if constexpr (PAIRS) {  // one load of all lanes, whether they turn it or not
+                const int at = (turn ? piece : piece - turned_pieces) * V, end = (turn ? each : rest) - V;
+                const int d = (turn ? 0 : a.turned) + (WHOLE ? at : min(at, end));
+                Piece<16> own = load_piece<16, WHOLE>(from + d * BYTES);
                 if (turn) {
                     float x[V];
-                    to_floats<DTYPE, VB>(own, x);
+                    to_floats<DTYPE, 16>(own, x);
 #pragma unroll
                     for (int i = 0; i < V; i += 2) {
-                        const float c = cs[(d + i) / 2], s = sn[(d + i) / 2], p = x[i], q = x[i + 1];
-                        x[i] = p * c - q * s;
-                        x[i + 1] = p * s + q * c;
+                        const float c = cs[(d + i) / 2], s = sn[(d + i) / 2];
+                        turned_pair(x[i], x[i + 1], c, s, &x[i], &x[i + 1]);
                     }
-                    own = from_floats<DTYPE, VB>(x);
+                    own = from_floats<DTYPE, 16>(x);
                 }
-                store_piece<VB>(to + d * BYTES, own);
+                store_piece<16, WHOLE>(to + d * BYTES, own);
             } else if (!turn) {
-                const int d = a.turned + (piece - turned_pieces) * V;
-                store_piece<VB>(to + d * BYTES, load_piece<VB>(from + d * BYTES));
+                const int at = (piece - turned_pieces) * V, d = a.turned + (WHOLE ? at : min(at, rest - V));
+                store_piece<16, WHOLE>(to + d * BYTES, load_piece<16, WHOLE>(from + d * BYTES));
             } else {
-                const int d = PAIRS ? 2 * piece : piece * V, e = PAIRS ? d + 1 : d + pairs;
+                const int d = WHOLE ? piece * V : min(piece * V, each - V), e = d + pairs;
                 float x[V], y[V];
-                to_floats<DTYPE, VB>(load_piece<VB>(from + d * BYTES), x);
-                to_floats<DTYPE, VB>(load_piece<VB>(from + e * BYTES), y);
+                to_floats<DTYPE, 16>(load_piece<16, WHOLE>(from + d * BYTES), x);
+                to_floats<DTYPE, 16>(load_piece<16, WHOLE>(from + e * BYTES), y);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float c = cs[piece * V + i], s = sn[piece * V + i], p = x[i], q = y[i];
-                    x[i] = p * c - q * s;
-                    y[i] = p * s + q * c;
-                }
-                store_piece<VB>(to + d * BYTES, from_floats<DTYPE, VB>(x));
-                store_piece<VB>(to + e * BYTES, from_floats<DTYPE, VB>(y));
+                for (int i = 0; i < V; ++i) turned_pair(x[i], y[i], cs[d + i], sn[d + i], &x[i], &y[i]);
+                store_piece<16, WHOLE>(to + d * BYTES, from_floats<DTYPE, 16>(x));
+                store_piece<16, WHOLE>(to + e * BYTES, from_floats<DTYPE, 16>(y));
             }
         }
     }
@@ -225,28 +260,14 @@ bool same_rows(const KvRows& a, const KvRows& b) {
     return a.data == b.data && a.token_stride == b.token_stride && a.head_stride == b.head_stride;
 }
 
-// The most bytes, a power of two up to 16, that divide a row's place and strides.
-int alignment(const KvRows& r) {
-    const uintptr_t size = r.dtype == MP_F32 ? 4 : 2;
-    const uintptr_t all = reinterpret_cast<uintptr_t>(r.data) | r.token_stride * size | r.head_stride * size | 16;
-    return (int)(all & -all);
-}
-
-template <int DTYPE, bool PAIRS>
-void launch(const Rotary& a, int vb, dim3 grid, size_t room, hipStream_t st) {
-    if (vb == 16)
-        kv_rotary_kernel<DTYPE, PAIRS, 16><<<grid, 256, room, st>>>(a);
-    else if (vb == 8)
-        kv_rotary_kernel<DTYPE, PAIRS, 8><<<grid, 256, room, st>>>(a);
-    else if (vb == 4)
-        kv_rotary_kernel<DTYPE, PAIRS, 4><<<grid, 256, room, st>>>(a);
-    else
-        kv_rotary_kernel<DTYPE, PAIRS, DTYPE == MP_F32 ? 4 : 2><<<grid, 256, room, st>>>(a);
-}
-
 template <int DTYPE>
-void launch(const Rotary& a, bool pairs, int vb, dim3 grid, size_t room, hipStream_t st) {
-    pairs ? launch<DTYPE, true>(a, vb, grid, room, st) : launch<DTYPE, false>(a, vb, grid, room, st);
+void launch(const Rotary& a, bool pairs, bool whole, dim3 grid, size_t room, hipStream_t st) {
+    if (pairs)
+        whole ? kv_rotary_kernel<DTYPE, true, true><<<grid, 256, room, st>>>(a)
+              : kv_rotary_kernel<DTYPE, true, false><<<grid, 256, room, st>>>(a);
+    else
+        whole ? kv_rotary_kernel<DTYPE, false, true><<<grid, 256, room, st>>>(a)
+              : kv_rotary_kernel<DTYPE, false, false><<<grid, 256, room, st>>>(a);
 }
 
 }  // namespace
@@ -281,15 +302,15 @@ extern "C" int32_t mp_rotate(const int32_t* position, int64_t n_tokens, const do
     a.q_copy = !same_rows(a.q, a.q_out), a.k_copy = !same_rows(a.k, a.k_out);
     a.magnitude = magnitude, a.sign = inverse ? -1.0f : 1.0f, a.by_heads = 1.0f / a.heads;
     const bool pairs = layout == MP_ROTARY_PAIRS, f32 = a.q.dtype == MP_F32;
-    // the widest pieces that everything is whole ones of.  16-bit, by these and by elements: 32534 tokens of 9 heads
-    // of 96, 76 turned in pairs (8 bytes) 34 and 78 us; 16384 of 40 heads of 66 in pairs (4 bytes) 95 and 128.
-    const int size = f32 ? 4 : 2, whole = pairs ? turned : turned / 2;
-    int vb = alignment(a.q);
-    for (const KvRows* r : {&a.q_out, &a.k, &a.k_out}) vb = alignment(*r) < vb ? alignment(*r) : vb;
-    while (vb > size && (dim % (vb / size) != 0 || whole % (vb / size) != 0)) vb /= 2;
-    const int v = vb / size;
-    const int pieces = (pairs && v > 1 ? turned / v : turned / 2 / v) + (dim - turned) / v;
-    while ((1 << a.log_lanes) < pieces && a.log_lanes < 8) ++a.log_lanes;
+    const int v = f32 ? 4 : 8, each = pairs ? turned : turned / 2;
+    const int rest = a.q_copy || a.k_copy ? dim - turned : 0;
+    const bool whole = a.q.wide && a.q_out.wide && a.k.wide && a.k_out.wide && dim % v == 0 && each % v == 0;
+    const bool twice = a.q_copy && a.k_copy;  // a last piece may begin in the one before
+    a.turned_pieces = twice && each >= v ? (each + v - 1) / v : each / v;
+    a.wide = a.turned_pieces + (twice && rest >= v ? (rest + v - 1) / v : rest / v);
+    a.pairs_to = a.wide + (twice && each >= v ? 0 : each % v / (pairs ? 2 : 1));
+    a.pieces = a.pairs_to + (twice && rest >= v ? 0 : rest % v);
+    while ((1 << a.log_lanes) < a.pieces && a.log_lanes < 8) ++a.log_lanes;
     // tokens of a workgroup: a few thousand pieces, but a workgroup for every place of the device first;
     // their angles fit 32 KiB
     int64_t tokens = 4096 / ((int64_t)a.heads << a.log_lanes);
@@ -302,9 +323,9 @@ extern "C" int32_t mp_rotate(const int32_t* position, int64_t n_tokens, const do
     const size_t room = (size_t)a.tokens * turned * 4;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     switch (a.q.dtype) {
-        case MP_BF16: launch<MP_BF16>(a, pairs, vb, grid, room, st); break;
-        case MP_F16: launch<MP_F16>(a, pairs, vb, grid, room, st); break;
-        default: launch<MP_F32>(a, pairs, vb, grid, room, st);
+        case MP_BF16: launch<MP_BF16>(a, pairs, whole, grid, room, st); break;
+        case MP_F16: launch<MP_F16>(a, pairs, whole, grid, room, st); break;
+        default: launch<MP_F32>(a, pairs, whole, grid, room, st);
     }
     return hipGetLastError() == hipSuccess ? MP_OK : MP_EDEVICE;
 }

@@ -144,6 +144,35 @@ def test_in_place_and_strided(shift, pairs, dtype):
     near(rotary.rotate(r, dev(p, torch.int32), same), same, p, r)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("pairs", [False, True])
+@pytest.mark.parametrize("dim,turned", [(66, 66), (66, 6), (96, 76), (70, 62), (128, 50), (41, 34), (16, 2), (192, 134),
+                                        (256, 74), (25, 18)])
+def test_no_whole_pieces(dim, turned, pairs, dtype):
+    """Heads and turned elements that are no multiples of 16 bytes: out of place, in place, and one of the two; what
+    lies between the heads is left."""
+    rotary = module()
+    r = rotary.Rotation(turned, pairs=pairs)
+    rows = torch.randn(37, 9, dim + 3, device="cuda").to(dtype)
+    q, k = rows[:, :5, 1:dim + 1], rows[:, 6:9, 1:dim + 1]
+    p = positions(37, 5000)
+    at, q0, k0, before = dev(p, torch.int32), q.clone(), k.clone(), rows.clone()
+    wide = torch.full((37, 9, dim + 3), 7.0, device="cuda").to(dtype)
+    apart = rotary.rotate(r, at, q, k, out=wide[:, :5, 2:dim + 2], k_out=wide[:, 6:9, 2:dim + 2])
+    assert torch.equal(rows, before) and bool((wide[:, 5] == 7).all())
+    assert bool((wide[:, :, :2] == 7).all()) and bool((wide[:, :, dim + 2:] == 7).all())
+    near(apart[0], q0, p, r)
+    near(apart[1], k0, p, r)
+    k_out = torch.empty_like(k0)
+    rotary.rotate(r, at, q, k, out=q, k_out=k_out)
+    assert torch.equal(q, apart[0]) and torch.equal(k_out, apart[1]) and torch.equal(k, k0)
+    q.copy_(q0)
+    rotary.rotate(r, at, q, k, out=q, k_out=k)
+    assert torch.equal(q, apart[0]) and torch.equal(k, apart[1])
+    q.copy_(q0), k.copy_(k0)
+    assert torch.equal(rows, before)
+
+
 @pytest.mark.parametrize("pairs", [False, True])
 def test_gradient(pairs):
     """The inverse turn is the gradient: against differences of the definition, and <turn x, y> = <x, inverse y>."""
