@@ -1205,6 +1205,8 @@ hipError_t launch_kv_join(const KvAttend& k, hipStream_t st) {
 //   sequences, bfloat16 442, 416; 200 rows, heads of 256 427, 365; 64 rows each of 16 sequences of 8000 195, 177;
 //   4 sequences of 2048 tokens, 700 new, heads of 64 111, 62 (one chunk), of 128 172, 113, of 256 437, 312; one of
 //   2048, all new, 105, 64.
+// Chunks of 128 tokens at least: 100 rows after 412 tokens 20 us in one chunk, 16 by this; 33 rows of 4 sequences of
+// 4000 tokens, 8 query heads over 2 of 256, 56 in chunks of 512 and 42.
 static int64_t kv4_tile_chunks(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t q_heads,
                                int32_t dtype, int64_t units) {
     const int64_t group = q_heads / c.heads;
@@ -1223,9 +1225,10 @@ static int64_t kv4_tile_chunks(const mp_kv_cache& c, const mp_kv_seqs& s, int32_
             if (c.dim == 64) chunks = (4 * 256 + units * c.heads - 1) / (units * c.heads);
         }
         if (chunks < 1) continue;
+        chunks = std::min(chunks, std::max<int64_t>(s.longest / 128, 1));
         const double full = (double)(groups * chunks) / places, rest = full - floor(full);
         const double cost = work / full * (floor(full) + (rest > 0 ? alone + (1 - alone) * rest : 0)) +
-                            (chunks > 1 ? 5 + join * chunks : 0);
+                            (chunks > 1 ? 5 + join * chunks : 0) + 3 * std::max(full, 1.0);
         if (round == 0 || cost < least) best = chunks, least = cost;
     }
     return best;
@@ -1302,10 +1305,11 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
         int64_t chunks = wide > 0 ? (4 * 256 + wide - 1) / wide : 1;
         if (c.kind == MP_KV_E2M1 && sh.form == KvForm::tiles) chunks = kv4_tile_chunks(c, s, q_heads, dtype, sh.units);
         chunk = (longest + chunks - 1) / chunks;
-        if (chunk < 512) chunk = 512;
+        if (c.kind != MP_KV_E2M1 && chunk < 512) chunk = 512;
     }
     // a multiple of what the waves of a workgroup take together
-    sh.chunk = (chunk + 255) / 256 * 256;
+    const int64_t together = c.kind == MP_KV_E2M1 && sh.form != KvForm::rows ? 128 : 256;
+    sh.chunk = (std::max<int64_t>(chunk, together) + together - 1) / together * together;
     sh.n_chunks = longest > 0 ? (longest + sh.chunk - 1) / sh.chunk : 1;
     const int64_t rows = s.n_tokens * q_heads, most = INT32_MAX;
     // the product of workgroups and chunks may be past 64 bits
