@@ -1254,7 +1254,14 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     // over 1000 workgroups of long sequences (16 of 8192 tokens, 100 new: 387 / 352), and lose otherwise
     // (64 of 2048, 32 new: 98 / 167; of 512, all new: 310 / 361).
     const int64_t piece = (s.most_new < s.n_tokens ? s.most_new : s.n_tokens) * group;
-    if (keep > 0 || !s.begin || piece <= 16 || (piece <= 64 && s.longest > 512))
+    // In 4 bits tiles take little chunks too.  Rows against tiles, us, 32 query heads over 8, heads of 64, 128 and 256,
+    // bfloat16 (16-bit floats of 256: 137 / 174 and 156 / 207):
+    //                                 32 rows                       48 rows                     64 rows
+    //   16 sequences of 4096 tokens   35 / 29, 38 / 47, 85 / 127    41 / 36, 52 / 55, 115 / 131  44 / 40, 58 / 58, 133 / 135
+    //   64 of 4096                    81 / 75, 120 / 111, 286 / 447 114 / 100, 166 / 137, 393 / 448 136 / 103, 208 / 135, 505 / 451
+    //   two of 40000                                                46 / 34, 62 / 61, 129 / 152  49 / 38, 67 / 63, 154 / 157
+    const int64_t most_by_rows = c.kind != MP_KV_E2M1 || (c.dim == 256 && dtype == MP_F16) ? 64 : 48;
+    if (keep > 0 || !s.begin || piece <= 16 || (piece <= most_by_rows && s.longest > 512))
         sh.form = KvForm::rows;
     else
         sh.form = c.dim == 128 && piece >= 4096 ? KvForm::pair : KvForm::tiles;

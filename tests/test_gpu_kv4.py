@@ -85,6 +85,11 @@ class Setup:
 ONE, HALF, TWO = 2.0 ** -8, 2.0 ** -11, 2.0 ** -15
 
 
+def most_by_rows(dtype, dim):
+    """Rows of a longest piece that go by 16, with weights in two pieces."""
+    return 64 if dtype == F16 and dim == 256 else 48
+
+
 def of_tiles(dtype, dim=128):
     """The rounding where many rows share what is read."""
     return ONE if dtype == BF16 else HALF if dim < 256 else TWO
@@ -235,8 +240,20 @@ def test_attend_prompt(block, dim, heads, group, dtype, new):
     q = s.rows(sum(new), heads * group, dtype)
     # the bounds that the handle gives where none are named: all rows one sequence's, a whole row of the table
     piece, longest = sum(new) * group, s.table.shape[1] * block
-    few = piece <= 16 or (piece <= 64 and longest > 512)
+    few = piece <= 16 or (piece <= most_by_rows(dtype, dim) and longest > 512)
     s.attend(length, new, q, weights=TWO if few else of_tiles(dtype, dim))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("new", [[9, 1, 2], [10, 1, 2], [1, 0, 15], [12, 2, 3]])
+def test_attend_pieces_of_either_form(new, dim, dtype):
+    """48, 52, 64 and 68 rows after up to 700 tokens."""
+    length = [700, 30, 657]
+    s = Setup(length, heads=2, dim=dim)
+    s.fill()
+    few = sum(new) * 4 <= most_by_rows(dtype, dim)
+    s.attend(length, new, s.rows(sum(new), 8, dtype), weights=TWO if few else of_tiles(dtype, dim))
 
 
 @pytest.mark.parametrize("dtype,dim,length,new", [(BF16, 128, [5000], None), (F16, 64, [9000, 3000], None),
@@ -249,7 +266,7 @@ def test_attend_chunks(dtype, dim, length, new):
     s = Setup(length, heads=1, dim=dim)
     s.fill()
     n = len(length) if new is None else sum(new)
-    few = new is None or sum(new) * 4 <= 64
+    few = new is None or sum(new) * 4 <= most_by_rows(dtype, dim)
     s.attend(length, new, s.rows(n, 4, dtype), weights=TWO if few else of_tiles(dtype, dim))
 
 
