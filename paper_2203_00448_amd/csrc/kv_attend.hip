@@ -1204,7 +1204,7 @@ hipError_t launch_kv_join(const KvAttend& k, hipStream_t st) {
 //   333 rows after 20000 tokens, heads of 64 105, 98; of 128, 16-bit floats 195, 169 (12 and 5 chunks); 3 such
 //   sequences, bfloat16 442, 416; 200 rows, heads of 256 427, 365; 64 rows each of 16 sequences of 8000 195, 177;
 //   4 sequences of 2048 tokens, 700 new, heads of 64 111, 62 (one chunk), of 128 172, 113, of 256 437, 312; one of
-//   2048, all new, 105, 64.
+//   2048, all new, 105, 64; 16 new rows of each of 32 sequences of 1000 tokens, heads of 64, 24 in one chunk, 32 in three.
 // Chunks of 128 tokens at least: 100 rows after 412 tokens 20 us in one chunk, 16 by this; 33 rows of 4 sequences of
 // 4000 tokens, 8 query heads over 2 of 256, 56 in chunks of 512 and 42.
 static int64_t kv4_tile_chunks(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t q_heads,
@@ -1213,7 +1213,7 @@ static int64_t kv4_tile_chunks(const mp_kv_cache& c, const mp_kv_seqs& s, int32_
     int64_t groups = (std::min(s.most_new, s.n_tokens) * group + 127) / 128;  // of a sequence, and of all
     groups = (s.n_seqs > 0 && groups > units / s.n_seqs ? units : std::max<int64_t>(groups * s.n_seqs, 1)) * c.heads;
     const int64_t places = 256 * (c.dim == 256 ? 1 : c.dim == 128 ? 2 : dtype == MP_F16 ? 3 : 4);
-    const double alone = c.dim == 256 ? 1.0 : c.dim == 128 ? 0.6 : 0.4;
+    const double alone = c.dim == 256 ? 1.0 : c.dim == 128 ? 0.6 : dtype == MP_F16 ? 0.4 : 0.3;
     const double work = 4.0 * 128 * groups * s.longest * c.dim / (c.dim == 256 ? 5e8 : 8e8);  // us
     const double join = 8.0 * s.n_tokens * q_heads * (c.dim + 4) / 4.9e6;
     int64_t best = 1;
