@@ -52,6 +52,7 @@ struct KvAttendShape {
     int64_t n_chunks;
     bool ordered;      // row groups of tiles by what they see
     uint32_t spread;   // in 4 bits, few rows: the step between the row groups of neighbouring workgroups
+    uint32_t each;     // as above, where all sequences have alike: rows of a sequence; 0: not known
     size_t workspace;
 };
 

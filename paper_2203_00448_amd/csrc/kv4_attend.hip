@@ -166,9 +166,25 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : WAVES == 8 || (D == 128 
     const int head = (int)(blockIdx.x % heads);
     // chunks slowest: workgroups go to the XCDs in turn, and first chunks, which every row group
     // has, must not all meet one of them; last chunks first, which only long sequences have
-    const uint32_t rest = blockIdx.x / heads, units = (uint32_t)k.shape.units, chunk = n_chunks - 1 - rest / units;
+    const uint32_t rest = blockIdx.x / heads;
+    uint32_t chunk, unit;
+    if (const uint32_t each = k.shape.each) {
+        // row groups that sequences of `each` rows have, then, of all chunks, those that are empty if they do
+        const uint32_t per = (each + 15) / 16, n_seqs = (uint32_t)a.s.n_seqs, all = n_seqs * per;
+        const bool had = rest < all * n_chunks;
+        const uint32_t r = had ? rest : rest - all * n_chunks, of = had ? all : n_seqs, u = r % of;
+        const uint32_t s = had ? u / per : u;
+        chunk = n_chunks - 1 - r / of;
+        const auto first = [&](uint32_t i) { return (uint32_t)((uint64_t)i * each / 16) + i; };
+        unit = first(s) + (had ? u - s * per : per);
+        if (!had && unit >= first(s + 1)) return;
+    } else {
+        const uint32_t units = (uint32_t)k.shape.units;
+        chunk = n_chunks - 1 - rest / units;
+        unit = (uint32_t)((uint64_t)(rest % units) * k.shape.spread % units);
+    }
     RowGroup rg;
-    if (!row_group<16>(k, (uint32_t)((uint64_t)(rest % units) * k.shape.spread % units), &rg)) return;
+    if (!row_group<16>(k, unit, &rg)) return;
     const int64_t last_row = min((int64_t)rg.n_rows, rg.row0 + 16) - 1;
     const int32_t most = wave_one(row_of(k, rg, head, last_row).last);  // the last position any row sees
     const int32_t least = wave_one(row_of(k, rg, head, rg.row0).last);  // all rows see up to here

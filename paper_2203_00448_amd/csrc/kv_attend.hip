@@ -1282,7 +1282,13 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
         sh.units = s.n_tokens * group / sh.rows + s.n_seqs;
     else
         sh.units = s.n_seqs * per;
-    if (c.kind == MP_KV_E2M1 && sh.form == KvForm::rows && s.begin) sh.units |= 1;  // for `spread`
+    if (c.kind == MP_KV_E2M1 && sh.form == KvForm::rows && s.begin) {
+        if (s.n_seqs > 1 && s.most_new > 0 && s.n_tokens == s.n_seqs * s.most_new) {
+            sh.each = (uint32_t)piece;
+            sh.units = s.n_seqs * ((piece + 15) / 16 + 1);
+        }
+        sh.units |= sh.each ? 0 : 1;  // for `spread`
+    }
     const int64_t longest = keep > 0 ? keep * c.block : s.longest;
     // Tokens of a workgroup: a workgroup's start, end and part of the join cost as much as some
     // hundred tokens, few long ones leave compute units idle.  2048, or less where that makes
@@ -1299,6 +1305,7 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     if (c.kind == MP_KV_E2M1 && sh.form == KvForm::rows && s.begin) {
         const int64_t least = s.n_tokens * group / sh.rows;
         busy = (least > s.n_seqs ? least : s.n_seqs) * c.heads;
+        if (sh.each) busy = s.n_seqs * ((piece + 15) / 16) * c.heads;
     }
     int64_t chunk = longest < ((int64_t)2048 * 256) / (busy > 0 ? busy : 1) ? longest * busy / 256 : 2048;
     // In 4 bits two workgroups a compute unit are one round of a launch: where chunks up to 4096 make that
@@ -1329,9 +1336,10 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     sh.ordered = sh.form != KvForm::rows && s.begin && s.n_seqs <= 64 && sh.n_chunks == 1 &&
                  s.longest < ((int64_t)1 << 30) * sh.rows / group;
     // The bound on the row groups has an empty one for most sequences, and workgroups go to the compute units in
-    // turn, wherever others have ended: empty ones at even distances leave some units three and others none.  So
-    // neighbours are about 0.618 of the (odd) count apart: 64 sequences of 4096 tokens, 4 new, 4 query heads a key
-    // head, 63 us, 80 in order (every second group is empty); 2 new 60 and 49 (every third).
+    // turn, wherever others have ended: empty ones at even distances leave some units three and others none.  Where
+    // all sequences have as many rows (`each`), the empty ones go last: 64 sequences of 4096 tokens, 4 new, 4 query heads
+    // a key head, 51 us, 80 in order; 2 new 52 and 49; 16 sequences, 8 new, 31.  Else neighbours are about 0.618 of the
+    // (odd) count apart: these three 63, 60 and 39.
     sh.spread = 1;
     if (s.begin && sh.units > 2 && sh.units < most) {
         const auto common = [](int64_t a, int64_t b) {

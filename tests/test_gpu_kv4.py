@@ -256,6 +256,31 @@ def test_attend_pieces_of_either_form(new, dim, dtype):
     s.attend(length, new, s.rows(sum(new), 8, dtype), weights=TWO if few else of_tiles(dtype, dim))
 
 
+@pytest.mark.parametrize("dtype,dim", [(BF16, 128), (F16, 64), (BF16, 256)])
+@pytest.mark.parametrize("group,each", [(4, 1), (4, 2), (4, 4), (4, 3), (7, 3), (7, 2), (16, 3), (8, 5)])
+def test_attend_alike(group, each, dim, dtype):
+    """As many new tokens of every sequence: row groups in their order."""
+    from paper_2203_00448_amd import binding
+
+    length = [700, 30, 657, 64, 5200, 5, 16]
+    s = Setup(length, heads=2, dim=dim)
+    s.fill()
+    n = len(length) * each
+    bounds = {"most_new": each, "longest": 5200}
+    s.attend(length, [each] * 7, s.rows(n, 2 * group, dtype), weights=TWO, **bounds)
+    for new in ([0, 0, 0, 1, 0, 0, 0], [each, each, each, each, each, each, 0], [0] * 7):
+        # bounds that end before the rows do: the call says so; no row but theirs is written
+        begin = np.concatenate([[0], np.cumsum(new)])
+        q = s.rows(n, 2 * group, dtype)
+        seqs = s.kv.Seqs(s.d_table, torch.tensor(length, dtype=torch.int32, device="cuda"),
+                         begin=torch.from_numpy(begin.astype(np.int64)).cuda(), tokens=n, **bounds)
+        out, lse = torch.full_like(q, 3.0), torch.full(q.shape[:2], 7.0, dtype=F32, device="cuda")
+        with pytest.raises(binding.PlanError):
+            s.kv.attend(s.cache, seqs, q, scale=dim ** -0.5, out=out, lse=lse)
+        end = int(begin[-1])
+        assert bool((out[end:] == 3.0).all()) and bool((lse[end:] == 7.0).all())
+
+
 @pytest.mark.parametrize("dtype,dim,length,new", [(BF16, 128, [5000], None), (F16, 64, [9000, 3000], None),
                                                   (BF16, 128, [20000, 100], [40, 40]), (F16, 256, [6000], [3]),
                                                   (BF16, 64, [7000], [100]), (BF16, 128, [9001], [33]),
