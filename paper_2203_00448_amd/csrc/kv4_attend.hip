@@ -490,17 +490,22 @@ __device__ __forceinline__ int v4_key(int token) {
 // F16, rows of 16-bit floats: the tile as 16-bit floats, so that one instruction holds a query's and a
 // weight's 11 bits.  A group of codes that these cannot hold exactly (scales outside 2^-23..2^13, codes not all zero)
 // marks its tile, and the workgroup takes a marked tile as bfloat16, with queries and weights in two pieces.  (All tiles
-// in two pieces: 143 us, with the join, instead of 112 for the rows above.)
+// in two pieces: 143 us, with the join, instead of 112 for the rows above.)  Weights of 16-bit floats lie around 2^10,
+// where those have most bits; beside values of scales past 2^13 they would leave the range of the sums, so a workgroup
+// that meets such values takes that tile and all after it as bfloat16, weights 24 powers below one.
 // Heads of 256 have no registers for both: all their tiles are taken so.
+// Heads of 64 have three waves a SIMD (168 registers, none spilled); left to itself the compiler takes 180.
 template <int D, bool F16>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_tiles_kernel(KvAttend k) {
+__global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 && F16 ? 3 : 2) void kv4_tiles_kernel(KvAttend k) {
     constexpr int KS = D / 16, DT = D / 32, GROUPS = D / 32;
     constexpr int UNITS = 128 * GROUPS / 256;  // groups of 32 dims that a thread moves in a tile, keys first
     constexpr bool kPieces = F16 && D == 256;  // every tile
-    constexpr float kShift = F16 ? -10.0f : kBelow, kLag = F16 ? 4.0f : kSlack;  // weights of 16-bit floats reach 2^14
+    constexpr bool kHalves = F16 && !kPieces;  // tiles as 16-bit floats, whose weights reach 2^14, but for marked ones
+    constexpr float kShift = kHalves ? -10.0f : kBelow, kLag = kHalves ? 4.0f : kSlack;
     extern __shared__ __align__(16) char lds_raw[];
     Tile4<D>* const lds = reinterpret_cast<Tile4<D>*>(lds_raw);
     __shared__ int32_t marked[2];  // the first token of the last marked tile of each room
+    __shared__ int32_t met_large;  // values of a marked tile had a scale past 2^13
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const KvArgs& a = k.a;
@@ -620,16 +625,19 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_tiles_kernel(KvAtte
             }
             if constexpr (decltype(as_f16)::value)
                 if (e - 104u > 36u && ((w[0] | w[1] | w[2] | w[3]) & 0x77777777u) != 0) marked[buf] = x;
+            if constexpr (kHalves && !decltype(as_f16)::value)
+                if (is_v(u) && e > 140u && ((w[0] | w[1] | w[2] | w[3]) & 0x77777777u) != 0) met_large = 1;
         }
     };
     using No = std::false_type;
-    using AsF16 = std::integral_constant<bool, F16 && !kPieces>;
+    using AsF16 = std::integral_constant<bool, kHalves>;
     const int k_token = (n & 0x13) | (n & 4) << 1 | (n & 8) >> 1;
     const int v_token = 8 * h + (lane >> 2 & 3), v_dim = (n & 16) + (lane & 3) * 4;
 
     int buf = 0;
     if (AsF16::value) {
         if (tid < 2) marked[tid] = -1;
+        if (tid == 0) met_large = 0;
         __syncthreads();
     }
     if (x0 < x1) {
@@ -638,9 +646,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_tiles_kernel(KvAtte
         find(x0 + 64);
         put(0, x0, AsF16());
     }
+    bool large = false;  // the same for the workgroup
     // a tile: its scores, weights and products, as 16-bit floats or (ODD) as a marked one
     const auto tile = [&](int32_t x, auto odd) {
         constexpr bool ODD = decltype(odd)::value;
+        const float shift = ODD && large ? kBelow : kShift, lag = ODD && large ? kSlack : kLag;
         float16_t s[2] = {float16_t{}, float16_t{}};
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
@@ -673,8 +683,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_tiles_kernel(KvAtte
 #pragma unroll
         for (int r = 0; r < 32; ++r) top = fmaxf(top, s[r / 16][r % 16]);
         top = fmaxf(top, __shfl_xor(top, 32, kWave));
-        const float new_m = fmaxf(m, top * by + kShift);
-        if (__any(new_m - m > kLag)) {
+        const float new_m = fmaxf(m, top * by + shift);
+        if (__any(new_m - m > lag)) {
             const float fall = __builtin_amdgcn_exp2f(m - (new_m == -INFINITY ? 0.0f : new_m));
 #pragma unroll
             for (int t = 0; t < DT; ++t) acc[t] *= fall;
@@ -732,7 +742,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_tiles_kernel(KvAtte
                 find(x + 128);
             }
             __syncthreads();  // the tile is whole; the other one is read no more
-            if (AsF16::value && wave_one(marked[buf]) == x) break;  // the same for the workgroup
+            if (AsF16::value && (large || wave_one(marked[buf]) == x)) break;  // the same for the workgroup
             if (x <= wave_most) tile(x, std::integral_constant<bool, kPieces>());
             if (x + 64 < x1) put(buf ^ 1, x + 64, AsF16());
         }
@@ -742,6 +752,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_tiles_kernel(KvAtte
         load();
         put(buf, x, No());
         __syncthreads();
+        large = wave_one(met_large) != 0;  // not written again before the next tile's barrier
         if (x <= wave_most) tile(x, AsF16());
         if (x + 64 < x1) {
             find(x + 64);

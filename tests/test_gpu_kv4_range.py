@@ -1,0 +1,77 @@
+"""The ends of the ranges that the 4-bit cache's attention takes: values, keys, queries and scales whose products or
+sums in 32 bits could leave the range of such floats although the result does not, in each form of the kernel."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import host
+from test_gpu_kv4 import BF16, F16, HALF, LEAST_STEP, HALF_STEP, TWO, Setup, of_tiles
+
+pytestmark = pytest.mark.gpu
+
+
+def attend(s, length, new, q, scale):
+    seqs, begin = s.seqs(length, new)
+    out = s.kv.attend(s.cache, seqs, q, scale=scale)
+    return host(out.double()), s.ref.attend(s.table, length, begin, host(q.double()), scale)
+
+
+def within(out, want, dtype, weights, dims=slice(None), more=0.0):
+    """The bound of test_gpu_kv4.near for some of the dims, and `more`."""
+    ref, _, mass, delta, floor = want
+    score = (ref.shape[-1] + 8) * 2.0 ** -24 * delta[..., None]
+    ref, mass, floor = ref[..., dims], mass[..., dims], floor[..., dims]
+    bound = HALF_STEP[dtype] * np.abs(ref) + (weights + 2.0 ** -20 + 2.5 * score) * mass * 1.01 + LEAST_STEP[dtype]
+    bound += (2.0 ** -35 if weights == HALF else 2.0 ** -102) * floor + (2.0 ** -25 if weights == HALF else 0.0) + more
+    off = np.abs(out[..., dims] - ref)
+    assert np.all(off <= bound), (off / bound).max()  # also where it is no number
+
+
+def filled(dim, far, size, key, largest):
+    """300 tokens of a head; the key of token 70 far above the others'; one token of each of the steps `far` with values
+    of `size` in dims 32 to 63 and with the keys `key`."""
+    s = Setup([300], heads=1, dim=dim)
+    k, v = s.rows(300, size=0.25).float(), s.rows(300).float()
+    tokens = [64 * t + 3 for t in far]
+    k[70] = largest
+    for t in tokens:
+        k[t] = key
+        v[t, :, 32:64] = size
+    s.store([300], [300], k.to(BF16), v.to(BF16))
+    return s, tokens
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("size", [2.0 ** 120, -6.0 * 2.0 ** 120, 2.0 ** 100])
+@pytest.mark.parametrize("far", [[0], [1], [2], [4], [0, 2], [0, 1, 2, 3, 4]])
+def test_large_values_that_others_outweigh(far, size, dim):
+    """Rows of 16-bit floats over values that these do not hold, the most weight of their steps (keys of 1) and none
+    beside a key of 16 that comes later or came before: exp(-15 * 2 sqrt(dim)) < 2^-340 of the sum, below 2^-200
+    with any of these values.  So the result is that without them, to 2^-60."""
+    s, tokens = filled(dim, far, size, 1.0, 16.0)
+    q = (s.rows(200, 4, F16, size=0.01).float() + 2.0).to(F16)
+    length, begin = [300], [0, 200]
+    for t in tokens:  # the definition without them
+        s.ref.v_code[s.table[0][t // 64], :, t % 64] = 0
+    for sign in (1.0, -1.0):
+        out, want = attend(s, length, [200], sign * q, sign * dim ** -0.5)
+        within(out, want, F16, of_tiles(F16, dim), more=2.0 ** -60)
+    out, want = attend(s, length, None, q[-1:], dim ** -0.5)
+    within(out, want, F16, TWO, more=2.0 ** -60)
+
+
+@pytest.mark.parametrize("dim,key,size", [(64, [4.0, 4.0], 2.0 ** 100), (128, [6.0, 4.0], 2.0 ** 104),
+                                          (256, [6.0, 6.0], 2.0 ** 100)])
+@pytest.mark.parametrize("far", [[0], [2], [1, 3]])
+def test_large_values_of_small_weight(far, dim, key, size):
+    """Shares of 2^-90 to 2^-98 that the values bring back into range, in the steps that hold them and in those
+    after."""
+    s, _ = filled(dim, far, size, torch.tensor(key, device="cuda").repeat(dim // 2), 8.0)
+    q = (2.0 + 2.0 ** -8 * torch.randint(-1, 2, (200, 4, dim), device="cuda").float()).to(F16)
+    out, want = attend(s, [300], [200], q, dim ** -0.5)
+    assert 1.0 < np.abs(want[0][-1, :, 32:64]).max() < 60000.0
+    # weights of 8 and 8 bits bring these dims' mass; what is beside them is less than 2^-4 of it at 11 bits
+    within(out, want, F16, TWO, slice(32, 64))
+    within(out, want, F16, of_tiles(F16, dim), slice(0, 32))
+    if dim > 64:
+        within(out, want, F16, of_tiles(F16, dim), slice(64, None))
