@@ -33,6 +33,7 @@ typedef short short4_t __attribute__((ext_vector_type(4)));
 constexpr int kStep = 64;           // tokens a wave takes at a time
 constexpr float kBelow = 24.0f;     // of a row's largest weight below one, in powers of two
 constexpr int kQueryExp = -4;       // of a row's largest query value
+constexpr int kKeyDown = 19;        // as 16-bit floats these are at 2^15, and keys this many powers smaller
 // How far the largest weight may grow above that before the running maximum follows: bfloat16 weights
 // lose no bits by it.
 constexpr float kSlack = 6.0f;
@@ -110,15 +111,27 @@ __device__ __forceinline__ float16_t product(const Words8& a, const Words8& b, f
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
 }
 
-// Values of a query, a row's largest `top`, as factors of the first product (PIECES of them); *scale what
-// their scores are multiplied by, not negative: the query takes the sign.
+// What brings a row's query, `top` its largest value, to the size that it has as a factor of the first product (in
+// two steps: 2^-131 is no float's least power), and what the scores are multiplied by then, not negative: the
+// query takes the sign.
+struct QueryScale {
+    float f, f2, c;
+};
+__device__ __forceinline__ QueryScale query_scale(const KvAttend& k, float top) {
+    uint32_t frac;
+    const int e = min(127, max(-90, exponent_of(top, &frac) - 1));  // 2^e <= top < 2^(e + 1)
+    const int up = kQueryExp - e;
+    // not infinite, and not zero beside a masked score's infinity
+    const float c = fabsf(k.scale) * kLog2e * pow2f(-up / 2) * pow2f(up / 2 - up);
+    return {pow2f(up / 2), k.scale < 0.0f ? -pow2f(up - up / 2) : pow2f(up - up / 2),
+            fminf(fmaxf(c, 1.17549435e-38f), 3.4e38f)};
+}
+// Values of a query as factors of the first product (PIECES of them); *scale as above.
 template <int PIECES, int N>
 __device__ __forceinline__ void query_pieces(const KvAttend& k, const float (&x)[N][8], float top,
                                              bf8_t (&q)[PIECES][N], float* scale) {
-    uint32_t frac;
-    const int e = min(127, max(-90, exponent_of(top, &frac) - 1));  // 2^e <= top < 2^(e + 1)
-    const int up = kQueryExp - e;  // in two steps: -131 is no exponent of a float
-    const float f = pow2f(up / 2), f2 = k.scale < 0.0f ? -pow2f(up - up / 2) : pow2f(up - up / 2);
+    const QueryScale by = query_scale(k, top);
+    const float f = by.f, f2 = by.f2;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         float y[8];
@@ -129,9 +142,7 @@ __device__ __forceinline__ void query_pieces(const KvAttend& k, const float (&x)
         else
             split8(y, &q[0][i], &q[1][i]);
     }
-    // not infinite, and not zero beside a masked score's infinity
-    const float c = fabsf(k.scale) * kLog2e * pow2f(-up / 2) * pow2f(up / 2 - up);
-    *scale = fminf(fmaxf(c, 1.17549435e-38f), 3.4e38f);
+    *scale = by.c;
 }
 
 // Few rows: 16 columns of rows, one key head, one chunk of tokens.  Each of four or eight waves takes
@@ -531,35 +542,53 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 && F16 ? 3 : 2) void kv
     const int32_t wave_least = wave_one(awake ? row_of(k, rg, head, wave_row0).last : -1);
     const Row row = row_of(k, rg, head, wave_row0 + n);
 
-    Words8 q[KS];    // bfloat16 factors, or the 16-bit floats as they are
+    Words8 q[KS];    // bfloat16 factors, or 16-bit floats, the row's largest from 2^15 on (so these lose no bits)
     float c, c_odd;  // what scores are multiplied by, and those of marked tiles
     {
         uint4 raw[KS];
 #pragma unroll
         for (int i = 0; i < KS; ++i) raw[i] = load8_16bit(k.q, row.token, row.head, i * 16 + h * 8);
-        float y[KS][8], top = 0.0f;
-#pragma unroll
-        for (int i = 0; i < KS; ++i) {
-            to_float8(k.q, raw[i], y[i]);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(y[i][j]));
-        }
-        top = fmaxf(top, __shfl_xor(top, 32, kWave));
         if constexpr (F16) {
-            const uint32_t flip = k.scale < 0.0f ? 0x80008000u : 0u;
+            half2_t peak = {};
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
-                q[i].w[0] = raw[i].x ^ flip, q[i].w[1] = raw[i].y ^ flip;
-                q[i].w[2] = raw[i].z ^ flip, q[i].w[3] = raw[i].w ^ flip;
+                q[i].w[0] = raw[i].x, q[i].w[1] = raw[i].y, q[i].w[2] = raw[i].z, q[i].w[3] = raw[i].w;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    peak = __builtin_elementwise_max(peak, __builtin_bit_cast(half2_t, q[i].w[j] & 0x7fff7fffu));
             }
-            c = fminf(fmaxf(fabsf(k.scale) * kLog2e, 1.17549435e-38f), 3.4e38f);
+            float top = fmaxf((float)peak[0], (float)peak[1]);
+            top = fmaxf(top, __shfl_xor(top, 32, kWave));
+            // a row of less than 2^-15 stays below 2^15: two factors of such floats are enough
+            const QueryScale by = query_scale(k, fminf(fmaxf(top, 0x1p-15f), 65504.0f));
+            uint32_t frac;
+            const int up = exponent_of(fabsf(by.f * by.f2), &frac) - 1 + kKeyDown, most_up = min(up, 15);
+            const _Float16 f = (_Float16)pow2f(most_up), f2 = (_Float16)copysignf(pow2f(up - most_up), by.f2);
+#pragma unroll
+            for (int i = 0; i < KS; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    half2_t x = __builtin_bit_cast(half2_t, q[i].w[j]);
+                    x = x * half2_t{f, f} * half2_t{f2, f2};
+                    q[i].w[j] = __builtin_bit_cast(uint32_t, x);
+                }
+            c_odd = by.c;
+            c = fmaxf(c_odd * pow2f(-kKeyDown), 1.17549435e-38f);
         } else {
+            float y[KS][8], top = 0.0f;
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                to_float8(k.q, raw[i], y[i]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(y[i][j]));
+            }
+            top = fmaxf(top, __shfl_xor(top, 32, kWave));
             bf8_t f[1][KS];
             query_pieces<1>(k, y, top, f, &c);
 #pragma unroll
             for (int i = 0; i < KS; ++i) q[i].v = f[0][i];
+            c_odd = c;
         }
-        c_odd = c;
     }
     // 8 values of the query as a marked tile takes them: two pieces, exact
     const auto odd_query = [&](int i, bf8_t* hi, bf8_t* lo) {
@@ -610,7 +639,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 && F16 ? 3 : 2) void kv
         for (int u = 0; u < UNITS; ++u) {
             const int token = token_of(u);
             const uint32_t e = x + token > most ? 127u : exps[u];
-            const float scale = __uint_as_float(e << 23);
+            // keys as bfloat16 beside queries of 16-bit floats: these are 2^19 times what bfloat16 ones are
+            const uint32_t down = F16 && !decltype(as_f16)::value && !is_v(u) ? kKeyDown : 0;
+            const float scale = __uint_as_float((max(e, down) - down) << 23);
             uint4* const to = is_v(u) ? lds[buf].v[token] : lds[buf].k[token];
             const int key = is_v(u) ? v4_key<D>(token) : k4_key<D>(token);
             const uint32_t w[4] = {codes[u].x, codes[u].y, codes[u].z, codes[u].w};

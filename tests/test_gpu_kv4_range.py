@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from gpu_util import host
-from test_gpu_kv4 import BF16, F16, HALF, LEAST_STEP, HALF_STEP, TWO, Setup, of_tiles
+from test_gpu_kv4 import BF16, F16, HALF, HALF_STEP, LEAST_STEP, ONE, TWO, Setup, of_tiles
 
 pytestmark = pytest.mark.gpu
 
@@ -75,3 +75,20 @@ def test_large_values_of_small_weight(far, dim, key, size):
     within(out, want, F16, of_tiles(F16, dim), slice(0, 32))
     if dim > 64:
         within(out, want, F16, of_tiles(F16, dim), slice(64, None))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("new", [None, [130]])
+def test_large_queries_and_keys_of_a_tiny_scale(new, dim, dtype):
+    """Products of queries and keys past 2^128, which the scale brings back to some units; and a head whose scores all
+    but vanish.  (All keys' scales are past what 16-bit floats hold, so their rows' weights have 16 bits in tiles.)"""
+    s = Setup([200], heads=2, dim=dim)
+    k, v = s.rows(200).float(), s.rows(200)
+    k[:, 0] *= 2.0 ** 116
+    k[:, 1] *= 2.0 ** -90
+    s.store([200], [200], k.to(BF16), v)
+    q = s.rows(1 if new is None else 130, 8, dtype, size=2.0 ** 9)
+    for scale in (2.0 ** -126, -(2.0 ** -126)):
+        out, want = attend(s, [200], new, q, scale)
+        within(out, want, dtype, TWO if new is None or dtype == F16 else ONE)
