@@ -111,27 +111,29 @@ __device__ __forceinline__ float16_t product(const Words8& a, const Words8& b, f
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, b.v, c, 0, 0, 0);
 }
 
-// What brings a row's query, `top` its largest value, to the size that it has as a factor of the first product (in
-// two steps: 2^-131 is no float's least power), and what the scores are multiplied by then, not negative: the
-// query takes the sign.
+// What brings a row's query, `top` its largest value, to the size that it has as a factor of the first product:
+// 2^up and the scale's sign (zero for one of zero); and what the scores are multiplied by then, not negative.
 struct QueryScale {
-    float f, f2, c;
+    int up;
+    float sign, c;
 };
 __device__ __forceinline__ QueryScale query_scale(const KvAttend& k, float top) {
     uint32_t frac;
     const int e = min(127, max(-90, exponent_of(top, &frac) - 1));  // 2^e <= top < 2^(e + 1)
-    const int up = kQueryExp - e;
-    // not infinite, and not zero beside a masked score's infinity
-    const float c = fabsf(k.scale) * kLog2e * pow2f(-up / 2) * pow2f(up / 2 - up);
-    return {pow2f(up / 2), k.scale < 0.0f ? -pow2f(up - up / 2) : pow2f(up - up / 2),
-            fminf(fmaxf(c, 1.17549435e-38f), 3.4e38f)};
+    const float size = fabsf(k.scale);  // its fraction and exponent are those of the smallest floats too
+    const int ec = __builtin_amdgcn_frexp_expf(size);
+    // c is no less than 2^-126, so that it is not zero beside a masked score's infinity: for a scale so small beside
+    // large keys the query gives way, and all of it for a scale of zero
+    const int up = min(kQueryExp - e, ec + 125);
+    const float c = __builtin_ldexpf(__builtin_amdgcn_frexp_mantf(size) * kLog2e, ec - up);
+    return {up, size == 0.0f ? 0.0f : k.scale < 0.0f ? -1.0f : 1.0f, fminf(fmaxf(c, 1.17549435e-38f), 3.4e38f)};
 }
 // Values of a query as factors of the first product (PIECES of them); *scale as above.
 template <int PIECES, int N>
 __device__ __forceinline__ void query_pieces(const KvAttend& k, const float (&x)[N][8], float top,
                                              bf8_t (&q)[PIECES][N], float* scale) {
     const QueryScale by = query_scale(k, top);
-    const float f = by.f, f2 = by.f2;
+    const float f = pow2f(by.up / 2), f2 = by.sign * pow2f(by.up - by.up / 2);  // 2^-131 is no float's least power
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         float y[8];
@@ -561,9 +563,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 && F16 ? 3 : 2) void kv
             top = fmaxf(top, __shfl_xor(top, 32, kWave));
             // a row of less than 2^-15 stays below 2^15: two factors of such floats are enough
             const QueryScale by = query_scale(k, fminf(fmaxf(top, 0x1p-15f), 65504.0f));
-            uint32_t frac;
-            const int up = exponent_of(fabsf(by.f * by.f2), &frac) - 1 + kKeyDown, most_up = min(up, 15);
-            const _Float16 f = (_Float16)pow2f(most_up), f2 = (_Float16)copysignf(pow2f(up - most_up), by.f2);
+            const int up = by.up + kKeyDown, most_up = min(up, 15);
+            const _Float16 f = (_Float16)pow2f(most_up), f2 = (_Float16)(by.sign * pow2f(up - most_up));
 #pragma unroll
             for (int i = 0; i < KS; ++i)
 #pragma unroll

@@ -92,3 +92,21 @@ def test_large_queries_and_keys_of_a_tiny_scale(new, dim, dtype):
     for scale in (2.0 ** -126, -(2.0 ** -126)):
         out, want = attend(s, [200], new, q, scale)
         within(out, want, dtype, TWO if new is None or dtype == F16 else ONE)
+
+
+@pytest.mark.parametrize("scale", [0.0, 2.0 ** -149, -(2.0 ** -149), 2.0 ** -137, 2.0 ** -128, 2.0 ** -126])
+@pytest.mark.parametrize("dtype,dim,new,heads", [
+    (t, d, n, 1) for t in (BF16, F16) for d in (64, 128, 256) for n in (None, 130)] + [(BF16, 128, 1030, 60)])
+def test_the_largest_keys_beside_no_scale(dtype, dim, new, heads, scale):
+    """Keys of the largest size, of either sign, whose products with the queries are near 2^128: a scale of zero makes
+    their scores zero, and the least ones less than 2^-10.  (1030 rows of 60 heads: teams of waves in turn.)"""
+    n = new or 200
+    s = Setup([n], heads=heads, dim=dim)
+    k, v = s.rows(n).float(), s.rows(n)
+    k[:] = 6.0 * 2.0 ** 120
+    k[::3] *= -1.0
+    s.store([n], [n], k.to(BF16), v)
+    rows = 1 if new is None else n
+    q = (2.0 + 2.0 ** -4 * torch.randint(-8, 9, (rows, 4 * heads, dim), device="cuda").float()).to(dtype)
+    out, want = attend(s, [n], None if new is None else [n], q, scale)
+    within(out, want, dtype, TWO if new is None or dtype == F16 else ONE)
