@@ -1283,7 +1283,8 @@ KvAttendShape kv_attend_shape(const mp_kv_cache& c, const mp_kv_seqs& s, int32_t
     else
         sh.units = s.n_seqs * per;
     if (c.kind == MP_KV_E2M1 && sh.form == KvForm::rows && s.begin) {
-        if (s.n_seqs > 1 && s.most_new > 0 && s.n_tokens == s.n_seqs * s.most_new) {
+        // (most_new may be anything: no product of it)
+        if (s.n_seqs > 1 && s.most_new > 0 && s.n_tokens % s.n_seqs == 0 && s.n_tokens / s.n_seqs == s.most_new) {
             sh.each = (uint32_t)piece;
             sh.units = s.n_seqs * ((piece + 15) / 16 + 1);
         }
