@@ -26,7 +26,9 @@ class DecodeStep:
     keep: blocks that a query reads, 0 for all (a cache in 4 bits, kind E2M1, always has all).
     rotation: a rotary.Rotation by which queries and keys are turned, in place, before they are used.
     paged: blocks are taken from a pool as sequences grow, and `retire` gives back those of sequences that
-    ended; otherwise every sequence has its blocks from the start.
+    ended; otherwise every sequence has its blocks from the start.  Where blocks or a table's room do not suffice for a
+    token of every sequence, the step is refused for all: lengths, tables and caches stay as they are, its result
+    means nothing, and `check` says so.
     planned=False gives every intermediate memory of its own: the same step, for comparison."""
 
     def __init__(self, *, layers=4, n_seqs=8, hidden=512, q_heads=8, heads=2, dim=64, block=16, keep=8,
@@ -55,7 +57,9 @@ class DecodeStep:
         # what a step is about: a token more of each sequence, at which positions and places
         self.more = torch.ones(n_seqs, dtype=torch.int32, device="cuda")
         self.step = pages.new_step(n_seqs, n_seqs)
-        self.seqs = kv.Seqs(self.table, self.length, longest=longest)
+        # a step that the pool refuses has bounds of zero: no row is any sequence's, so nothing is written
+        bounds = dict(begin=self.step.begin, tokens=n_seqs, most_new=1) if paged else {}
+        self.seqs = kv.Seqs(self.table, self.length, longest=longest, **bounds)
         self.status = kv.new_status()
         self._lay_out(planned)
 
