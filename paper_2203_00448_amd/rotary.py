@@ -4,7 +4,8 @@ like kv.py, and the frequencies that a program makes once.
 `rotate` turns pairs of elements of queries and keys by position * frequency, before they are written
 to the cache and attended to.  It runs on `stream` (the current one of the queries' device if not given),
 whichever device is current; tensors that are in use on another stream are the caller's to wait for.  It
-builds no graph: the gradient of a turn is the inverse one, `rotate(..., inverse=True)`.
+builds no graph (tensors that require a gradient are refused where one is recorded): the gradient of a turn is the
+inverse one, `rotate(..., inverse=True)`.
 """
 from __future__ import annotations
 
@@ -90,6 +91,9 @@ def rotate(rotation: Rotation, position, q, k=None, *, out=None, k_out=None, inv
         with kv._current(rotation, stream):
             return rotate(rotation, position, q, k, out=out, k_out=k_out, inverse=inverse)
     L = load_library()
+    if (q.requires_grad or (k is not None and k.requires_grad) or (out is not None and out.requires_grad)
+            or (k_out is not None and k_out.requires_grad)) and torch.is_grad_enabled():
+        raise ValueError("rotate builds no graph: call it under torch.no_grad(), and with inverse=True for the gradient")
     shape = q.shape
     if len(shape) != 3 or (k is not None and k.dim() != 3):
         raise ValueError("q and k must be [tokens, heads, dim]")
