@@ -571,8 +571,8 @@ size_t mp_kv_pages_workspace_size(int64_t n_seqs);
  *   position[n_tokens] int32; freq[turned / 2] double, device memory
  *   q, k: rows of q_heads and k_heads heads of `dim` elements (k_heads 0: no k,
  *              which may then be NULL); q_out, k_out of the same types.  An output
- *              is its input (the same data and strides) or shares no memory with
- *              an input or the other output. */
+ *              is its input (the same data and strides, whatever those of an axis of
+ *              one are) or shares no memory with an input or the other output. */
 #define MP_ROTARY_HALVES 0
 #define MP_ROTARY_PAIRS 1
 int32_t mp_rotate(const int32_t* position, int64_t n_tokens, const double* freq, int32_t turned,

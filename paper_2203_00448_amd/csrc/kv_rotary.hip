@@ -256,8 +256,10 @@ bool rows_apart(const KvRows& r, int64_t tokens, int64_t heads, int64_t dim) {
     return n_outer <= 1 || outer >= extent;
 }
 
-bool same_rows(const KvRows& a, const KvRows& b) {
-    return a.data == b.data && a.token_stride == b.token_stride && a.head_stride == b.head_stride;
+// Whether rows are the same places.  An axis of one has no stride.
+bool same_rows(const KvRows& a, const KvRows& b, int64_t tokens, int64_t heads) {
+    return a.data == b.data && (tokens <= 1 || a.token_stride == b.token_stride) &&
+           (heads <= 1 || a.head_stride == b.head_stride);
 }
 
 template <int DTYPE>
@@ -299,7 +301,8 @@ extern "C" int32_t mp_rotate(const int32_t* position, int64_t n_tokens, const do
     if (n_tokens == 0) return MP_OK;
     a.position = position, a.freq = freq, a.n_tokens = n_tokens;
     a.q_heads = q_heads, a.heads = q_heads + k_heads, a.dim = dim, a.turned = turned;
-    a.q_copy = !same_rows(a.q, a.q_out), a.k_copy = !same_rows(a.k, a.k_out);
+    a.q_copy = !same_rows(a.q, a.q_out, n_tokens, q_heads);
+    a.k_copy = k_heads > 0 ? !same_rows(a.k, a.k_out, n_tokens, k_heads) : a.q_copy;
     a.magnitude = magnitude, a.sign = inverse ? -1.0f : 1.0f, a.by_heads = 1.0f / a.heads;
     const bool pairs = layout == MP_ROTARY_PAIRS, f32 = a.q.dtype == MP_F32;
     const int v = f32 ? 4 : 8, each = pairs ? turned : turned / 2;
