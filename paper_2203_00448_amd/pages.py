@@ -72,7 +72,8 @@ def new_pool(n_blocks: int, *, device="cuda") -> Pool:
 
 class Step:
     """What the calls of a step read: length int32 [n_seqs], begin int64 [n_seqs + 1], position int32
-    [tokens], slot int64 [tokens]."""
+    [tokens], slot int64 [tokens].  `length` is where the last `extend` with this handle put the lengths: in place
+    where no length_out was given, so the first tensor is filled only as a call's length_out."""
 
     def __init__(self, length, begin, position, slot):
         self.length, self.begin, self.position, self.slot = length, begin, position, slot
@@ -125,7 +126,8 @@ def extend(pool: Pool, table, length, more, *, block: int = 64, step: Step, leng
            status=None, workspace=None, check: bool = True, stream=None) -> Step:
     """Give blocks to more int32 [n_seqs] new tokens of sequences that hold `length` int32 [n_seqs]
     (mp_kv_extend): entries of table int32 [n_seqs, width] and the pool's counter are written in place, the lengths
-    to length_out (`length` if not given), the rest to `step`, which is returned. """
+    to length_out (`length` if not given), which is step.length from then on, the rest to `step`, which is
+    returned."""
     if stream is not None or kv._device() != pool.index:  # a launch would be the current device's
         with kv._current(pool, stream):
             return extend(pool, table, length, more, block=block, step=step, length_out=length_out,
@@ -145,6 +147,7 @@ def extend(pool: Pool, table, length, more, *, block: int = 64, step: Step, leng
     status = kv._word(status, pool)
     rc = L.mp_kv_extend(ids, n_ids, used, t, t_stride, width, block, lengths, new, n, room, out, used_to, begin,
                         position, slot, space.data_ptr(), space.nbytes, status.data_ptr(), kv._stream(index))
+    step.length = length if length_out is None else length_out
     _finish(rc, status, "pages.extend", check)
     return step
 
