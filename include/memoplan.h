@@ -514,8 +514,9 @@ size_t mp_kv_workspace_size(int32_t op, const mp_kv_cache* cache, const mp_kv_se
  * The tables, lengths, row bounds and positions of the cache's calls, kept on the
  * device: nothing of a step waits for the host.
  *
- * A pool of blocks: ids[n_ids] int32, of which ids[0 .. *used) are taken (their
- * order there means nothing) and the others free, given out in order.  `used_out`
+ * A pool of blocks: ids[n_ids] int32, of which ids[*used ..) are free, given out in
+ * order.  As many blocks as *used are taken; which ones, tables and lengths say: the
+ * entries before *used mean nothing once blocks came back.  `used_out`
  * may be `used`, `length_out` may be `length`; other outputs share no memory with
  * any argument.  `block` is 16, 32 or 64; table_stride, table_width and table as
  * in mp_kv_seqs.

@@ -51,8 +51,8 @@ def _vector(t, dtype, name, n, index):
 
 
 class Pool:
-    """Block ids int32 [n] and how many of them are taken, int64 [1]: ids[:used] are, the rest is given
-    out in order.  Two handles may share `ids`."""
+    """Block ids int32 [n] and how many blocks are taken, int64 [1]: ids[used:] are free and given out in order,
+    what lies before them means nothing once a block came back.  Two handles may share `ids`."""
 
     def __init__(self, ids, used):
         _need(ids, (torch.int32,), "ids")
