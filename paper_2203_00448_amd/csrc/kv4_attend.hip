@@ -1,7 +1,7 @@
 // Attention over the 4-bit key/value cache.
 //
 // For a row (a query and one of its heads) with scores s_j = scale * q.k_j,
-//   out = sum_j 2^(c s_j - M) v_j / sum_j 2^(c s_j - M),   c = log2 e, M = max_j c s_j + 24,
+//   out = sum_j 2^(c s_j - M - 24) v_j / sum_j 2^(c s_j - M - 24),   c = log2 e, M = max_j c s_j,
 // in one pass over the cache with a running M: when it grows, what was summed so far is multiplied
 // by 2^(M_old - M_new).
 //
@@ -37,6 +37,50 @@ constexpr int kKeyDown = 19;        // as 16-bit floats these are at 2^15, and k
 // How far the largest weight may grow above that before the running maximum follows: bfloat16 weights
 // lose no bits by it.
 constexpr float kSlack = 6.0f;
+// The exponent of a weight is one multiply-add, c s - (M + 24), which is off a rounded M by half of its last place.
+// Scores beyond this are rounded first, so that none is above its maximum by more than that may lag.
+constexpr float kLargeScore = 0x1p16f;
+
+// c s, and c s - m with the product rounded by itself.
+__device__ __forceinline__ float score_of(float s, float c) {
+#pragma clang fp contract(off)
+    return s * c;
+}
+__device__ __forceinline__ float below_maximum(float s, float c, float m) {
+#pragma clang fp contract(off)
+    return s * c - m;
+}
+
+// A row's running maximum of c s: with the shift, M + 24, which weights are 2^(c s - m) below; or, once some
+// maximum of the wave is large (`far`), M itself.
+struct Maximum {
+    float m = -INFINITY;
+    bool far = false;
+};
+// It follows `top`, the largest of these scores, where it is more than `lag` behind.  Then `fall(f)` has to multiply
+// what was summed by f.  Weights are 2^(*c s - *from) afterwards, `shift` powers below one at the maximum; where it is
+// far `lower(c, m)` has to replace scores s by c s - m, and *c is one.
+template <typename Fall, typename Lower>
+__device__ __forceinline__ void follow(float top, float shift, float lag, Maximum* at, float* c, float* from, Fall fall,
+                                       Lower lower) {
+    const float new_m = fmaxf(at->m, top * *c + (at->far ? 0.0f : shift));
+    if (__any(new_m - at->m > lag)) {
+        fall(__builtin_amdgcn_exp2f(at->m - (new_m == -INFINITY ? 0.0f : new_m)));
+        const bool large = __any(fabsf(new_m) > kLargeScore && new_m != -INFINITY);
+        at->m = large && !at->far ? new_m - shift : new_m;
+        at->far = at->far || large;
+    }
+    *from = at->m == -INFINITY ? 0.0f : at->m;
+    if (at->far) {
+        const float m = fmaxf(at->m, score_of(top, *c)), base = m == -INFINITY ? 0.0f : m;
+        fall(__builtin_amdgcn_exp2f(at->m - base));
+        at->m = m;
+        lower(*c, base);
+        *c = 1.0f, *from = shift;
+    }
+}
+// For results that are joined: the maximum's part in the sums, and the power of two that is left to them.
+__device__ __forceinline__ float left_of(const Maximum& at, float shift) { return at.far ? shift : 0.0f; }
 
 union Words8 {
     uint32_t w[4];
@@ -284,7 +328,8 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : WAVES == 8 || (D == 128 
         query_pieces<PIECES>(k, y, top, q, &c);
     }
     float4_t acc[VD];
-    float m = -INFINITY, l = 0.0f;
+    Maximum at;
+    float l = 0.0f;
 #pragma unroll
     for (int t = 0; t < VD; ++t) acc[t] = float4_t{0, 0, 0, 0};
 
@@ -324,18 +369,20 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : WAVES == 8 || (D == 128 
         for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
         top = fmaxf(top, __shfl_xor(top, 16, kWave));
         top = fmaxf(top, __shfl_xor(top, 32, kWave));
-        const float new_m = fmaxf(m, top * c + kBelow);
-        if (__any(new_m - m > kSlack)) {
-            const float fall = __builtin_amdgcn_exp2f(m - (new_m == -INFINITY ? 0.0f : new_m));
+        float by = c, from;
+        follow(top, kBelow, kSlack, &at, &by, &from,
+               [&](float fall) {
 #pragma unroll
-            for (int t = 0; t < VD; ++t) acc[t] *= fall;
-            l *= fall;
-            m = new_m;
-        }
-        const float from = m == -INFINITY ? 0.0f : m;
+                   for (int t = 0; t < VD; ++t) acc[t] *= fall;
+                   l *= fall;
+               },
+               [&](float scale, float base) {
+#pragma unroll
+                   for (int i = 0; i < 16; ++i) s[i] = below_maximum(s[i], scale, base);
+               });
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -from));
+            s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], by, -from));
             l += s[i];
         }
         const uint32_t e[4] = {ve.x, ve.y, ve.z, ve.w};
@@ -383,7 +430,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : WAVES == 8 || (D == 128 
     l += __shfl_xor(l, 16, kWave);
     l += __shfl_xor(l, 32, kWave);
     if (g == 0) {
-        sm[wave][n] = m;
+        sm[wave][n] = at.far ? at.m : at.m - kBelow;
         sl[wave][n] = l;
     }
 #pragma unroll
@@ -422,7 +469,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : WAVES == 8 || (D == 128 
 #pragma unroll
         for (int i = 0; i < D / 16; i += 4)
             *reinterpret_cast<float4_t*>(to + i) = float4_t{o[i], o[i + 1], o[i + 2], o[i + 3]};
-        if (d0 == 0) part_out.sums[index * n_chunks + chunk] = float4_t{top, total, 0, 0};
+        if (d0 == 0) part_out.sums[index * n_chunks + chunk] = float4_t{top, total * pow2f((int)kBelow), kBelow, 0};
     } else {
         // a row that sees nothing: weights and sums are zero
         const float norm = total > 0.0f ? 1.0f / total : total == 0.0f ? 0.0f : total;
@@ -432,14 +479,16 @@ __global__ __launch_bounds__(WAVES * 64, D == 256 ? 1 : WAVES == 8 || (D == 128 
 #pragma unroll
         for (int i = 0; i < D / 16; i += kOnce) store_16bit<kOnce>(k.out, r.token, r.head, d0 + i, o + i);
         if (k.lse && d0 == 0)
-            k.lse[index] = total > 0.0f ? (base + log2f(total)) * kLn2 : total == 0.0f ? -INFINITY : total;
+            k.lse[index] = total > 0.0f ? (base + log2f(total * pow2f((int)kBelow))) * kLn2
+                                        : total == 0.0f ? -INFINITY : total;
     }
 }
 
-// The result of a wave of 32 rows, a column each: lane half h has dims 4 h + [0, 4) of every eight.
+// The result of a wave of 32 rows, a column each: lane half h has dims 4 h + [0, 4) of every eight.  Weights
+// lie `shift` powers below 2^m.
 template <int D>
 __device__ __forceinline__ void store_rows(const KvAttend& k, const Row& row, uint32_t chunk,
-                                           const float16_t (&acc)[D / 32], float m, float l, int h) {
+                                           const float16_t (&acc)[D / 32], float m, float l, float shift, int h) {
     const float total = l + __shfl_xor(l, 32, kWave);
     if (!row.live) return;
     const uint32_t n_chunks = (uint32_t)k.shape.n_chunks;
@@ -464,10 +513,11 @@ __device__ __forceinline__ void store_rows(const KvAttend& k, const Row& row, ui
                 *reinterpret_cast<float4_t*>(to + d) = float4_t{o[0], o[1], o[2], o[3]};
         }
     if (h == 0) {
+        const float sum = total * pow2f((int)shift);
         if (!whole)
-            part_out.sums[index * n_chunks + chunk] = float4_t{m, total, 0, 0};
+            part_out.sums[index * n_chunks + chunk] = float4_t{m, sum, shift, 0};
         else if (k.lse)
-            k.lse[index] = total > 0.0f ? (m + log2f(total)) * kLn2 : total == 0.0f ? -INFINITY : total;
+            k.lse[index] = sum > 0.0f ? (m + log2f(sum)) * kLn2 : sum == 0.0f ? -INFINITY : sum;
     }
 }
 
@@ -605,7 +655,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 && F16 ? 3 : 2) void kv
     float16_t acc[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t) acc[t] = float16_t{};
-    float m = -INFINITY, l = 0.0f;
+    Maximum at;
+    float l = 0.0f;
 
     // unit u of a thread: 32 dims of a token's keys or values; table entries are read a tile ahead
     const int lb = a.log_block, block = 1 << lb;
@@ -678,11 +729,12 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 && F16 ? 3 : 2) void kv
         find(x0 + 64);
         put(0, x0, AsF16());
     }
-    bool large = false;  // the same for the workgroup
+    bool large = false;    // the same for the workgroup
+    float shift = kShift;  // of its weights below one
     // a tile: its scores, weights and products, as 16-bit floats or (ODD) as a marked one
     const auto tile = [&](int32_t x, auto odd) {
         constexpr bool ODD = decltype(odd)::value;
-        const float shift = ODD && large ? kBelow : kShift, lag = ODD && large ? kSlack : kLag;
+        const float below = ODD ? shift : kShift, lag = ODD && large ? kSlack : kLag;
         float16_t s[2] = {float16_t{}, float16_t{}};
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
@@ -710,20 +762,22 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 && F16 ? 3 : 2) void kv
                 for (int r = 0; r < 16; ++r)
                     s[t][r] = t * 32 + (r >> 3) * 16 + (r & 7) > seen ? -INFINITY : s[t][r];
         }
-        const float by = ODD ? c_odd : c;
+        float by = ODD ? c_odd : c;
         float top = -INFINITY;
 #pragma unroll
         for (int r = 0; r < 32; ++r) top = fmaxf(top, s[r / 16][r % 16]);
         top = fmaxf(top, __shfl_xor(top, 32, kWave));
-        const float new_m = fmaxf(m, top * by + shift);
-        if (__any(new_m - m > lag)) {
-            const float fall = __builtin_amdgcn_exp2f(m - (new_m == -INFINITY ? 0.0f : new_m));
+        float from;
+        follow(top, below, lag, &at, &by, &from,
+               [&](float fall) {
 #pragma unroll
-            for (int t = 0; t < DT; ++t) acc[t] *= fall;
-            l *= fall;
-            m = new_m;
-        }
-        const float from = m == -INFINITY ? 0.0f : m;
+                   for (int t = 0; t < DT; ++t) acc[t] *= fall;
+                   l *= fall;
+               },
+               [&](float scale, float base) {
+#pragma unroll
+                   for (int r = 0; r < 32; ++r) s[r / 16][r % 16] = below_maximum(s[r / 16][r % 16], scale, base);
+               });
         const auto weights = [&](int i, Words8* w) {
             float e[8];
 #pragma unroll
@@ -784,7 +838,17 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 && F16 ? 3 : 2) void kv
         load();
         put(buf, x, No());
         __syncthreads();
-        large = wave_one(met_large) != 0;  // not written again before the next tile's barrier
+        if (!large && wave_one(met_large) != 0) {  // not written again before the next tile's barrier
+            constexpr float kFall = 0x1p-34f;
+            static_assert(!kHalves || kBelow - kShift == 34.0f);
+            large = true;
+            shift = kBelow;
+            if (at.far) {  // sums go with the shift
+#pragma unroll
+                for (int t = 0; t < DT; ++t) acc[t] *= kFall;
+                l *= kFall;
+            }
+        }
         if (x <= wave_most) tile(x, AsF16());
         if (x + 64 < x1) {
             find(x + 64);
@@ -796,7 +860,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 && F16 ? 3 : 2) void kv
         buf ^= 1;
     }
     if (pages.bad()) raise_status(a.status, MP_EINVAL);
-    store_rows<D>(k, row, chunk, acc, m, l, h);
+    store_rows<D>(k, row, chunk, acc, at.m, l, left_of(at, shift), h);
 }
 
 // Many bfloat16 rows, heads of 128: two teams of four waves, 32 rows each wave, over one key head and one chunk
@@ -896,7 +960,8 @@ __global__ __launch_bounds__(512, 2) void kv4_pair_kernel(KvAttend k) {
     for (int t = 0; t < DT; ++t) acc[t] = float16_t{};
     s[0] = s[1] = float16_t{};
     bf8_t w[4] = {};
-    float m = -INFINITY, l = 0.0f;
+    Maximum at;
+    float l = 0.0f;
 
     auto turn = [&]() {
         __builtin_amdgcn_sched_barrier(0);
@@ -1007,21 +1072,23 @@ __global__ __launch_bounds__(512, 2) void kv4_pair_kernel(KvAttend k) {
             const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
             top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
         }
-        const float new_m = fmaxf(m, top * c + kBelow);
-        if (__any(new_m - m > kSlack)) {
-            const float fall = __builtin_amdgcn_exp2f(m - (new_m == -INFINITY ? 0.0f : new_m));
+        float by = c, from;
+        follow(top, kBelow, kSlack, &at, &by, &from,
+               [&](float fall) {
 #pragma unroll
-            for (int t = 0; t < DT; ++t) acc[t] *= fall;
-            l *= fall;
-            m = new_m;
-        }
-        const float from = m == -INFINITY ? 0.0f : m;
+                   for (int t = 0; t < DT; ++t) acc[t] *= fall;
+                   l *= fall;
+               },
+               [&](float scale, float base) {
+#pragma unroll
+                   for (int r = 0; r < 32; ++r) s[r / 16][r % 16] = below_maximum(s[r / 16][r % 16], scale, base);
+               });
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float e[8], sum = 0.0f;
 #pragma unroll
             for (int r = 0; r < 8; ++r) {
-                e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 2][i % 2 * 8 + r], c, -from));
+                e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 2][i % 2 * 8 + r], by, -from));
                 sum += e[r];
             }
             l += sum;
@@ -1032,7 +1099,7 @@ __global__ __launch_bounds__(512, 2) void kv4_pair_kernel(KvAttend k) {
     }
     if (!team) turn();
     if (pages.bad()) raise_status(a.status, MP_EINVAL);
-    store_rows<D>(k, row, chunk, acc, m, l, h);
+    store_rows<D>(k, row, chunk, acc, at.m, l, left_of(at, kBelow), h);
 }
 
 template <int D, int PIECES>

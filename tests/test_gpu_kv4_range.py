@@ -110,3 +110,87 @@ def test_the_largest_keys_beside_no_scale(dtype, dim, new, heads, scale):
     q = (2.0 + 2.0 ** -4 * torch.randint(-8, 9, (rows, 4 * heads, dim), device="cuda").float()).to(dtype)
     out, want = attend(s, [n], None if new is None else [n], q, scale)
     within(out, want, dtype, TWO if new is None or dtype == F16 else ONE)
+
+
+LENGTHS = [(t, d, 300, n, 4, 1) for t in (BF16, F16) for d in (64, 128, 256) for n in (None, 130)]
+LONG = [(BF16, 128, 5000, None, 4, 1), (F16, 64, 9000, 65, 4, 1), (BF16, 256, 6000, 40, 4, 1), (F16, 128, 7000, 9, 2, 2)]
+
+
+@pytest.mark.parametrize("dtype,dim,length,new,group,heads,power", [
+    (*x, p) for p in (10, 15, 17, 20, 24, 26, 27, 28, 29, 30, 31, 33, 48, 90, 115) for x in LENGTHS] + [
+    (*x, p) for p in (20, 28, 31, 90) for x in LONG] + [(BF16, 128, 1030, 1030, 4, 60, p) for p in (20, 31)])
+def test_scores_of_any_size(dtype, dim, length, new, group, heads, power):
+    """Scores up to 2^(power + 1) beside ones of about one, in the same steps and in others, and a few tokens whose scores are
+    the same largest one: those share all the weight, whatever their last places are rounded to.
+
+    The largest keys are all ones (exact: codes of 1); the others of that size have two dims or more of another value,
+    so their scores are 2^(power - 8) lower at least (dim is 256 at most), where the arithmetic of a score is off by
+    (dim + 8) 2^-24 of it: less than a sixteenth of that.  Equal keys have the same error."""
+    s = Setup([length], heads=heads, dim=dim)
+    rng = np.random.default_rng(power)
+    ones = np.ones((length, heads, dim))
+    ones[:, :, 3] = ones[:, :, dim - 2] = 0.5
+    most = np.flatnonzero(rng.random(length) < 0.03)
+    first = length - (new or 1)
+    most = np.concatenate([most, [first // 2]])  # every row sees one
+    ones[most] = 1.0
+    small = rng.random(length) < 0.3
+    small[most] = False
+    small[:64] = True
+    k = np.where(small[:, None, None], ones * 2.0 ** -power * rng.choice([1.0, -1.0], (length, 1, 1)), ones)
+    if first // 2 < 64:
+        k[first // 2] = 1.0
+    v = s.rows(length)
+    s.store([length], [length], torch.from_numpy(k).to(BF16).cuda(), v)
+    q = torch.ones(new or 1, heads * group, dim, device="cuda").to(dtype)
+    scale = float(np.float32((1.0 + rng.random()) * 2.0 ** power / dim))
+    for sign in (1.0, -1.0):
+        seqs, begin = s.seqs([length], None if new is None else [new])
+        lse = torch.zeros(q.shape[:2], device="cuda")
+        out = host(s.kv.attend(s.cache, seqs, sign * q, scale=sign * scale, lse=lse).double())
+        ref, ref_lse, mass, _, _ = s.ref.attend(s.table, [length], begin, host(sign * q.double()), sign * scale)
+        piece, longest = q.shape[0] * group, s.table.shape[1] * s.block
+        few = piece <= 16 or (piece <= (64 if dtype == F16 and dim == 256 else 48) and longest > 512)
+        weights = TWO if new is None or few else of_tiles(dtype, dim)
+        # a score's own error where the next ones still have weight: below 2^15 (e^-64 and 2^-92 of the rest from there)
+        score = 2.5 * (dim + 8) * 2.0 ** -24 * (2.0 ** (power + 1) if power < 14 else 0.0)
+        bound = HALF_STEP[dtype] * np.abs(ref) + (weights + 2.0 ** -19 + score) * mass * 1.01 + 2.0 ** -25
+        off = np.abs(out - ref)
+        assert np.all(off <= bound), (off / bound).max()
+        got = host(lse.double())
+        room = (dim + 8) * 2.0 ** -24 * 2.0 ** (power + 1) + 2.0 ** -20 * (1 + np.abs(ref_lse))
+        assert np.all(np.abs(got - ref_lse) <= room)
+
+
+@pytest.mark.parametrize("power", [10, 20, 28, 29, 31, 60])
+@pytest.mark.parametrize("dim,new", [(64, None), (128, None), (256, None), (64, 130), (128, 130), (256, 130)])
+def test_large_values_of_large_scores(dim, new, power):
+    """Two hundred tokens of the same score with values near the end of the range: their sum is past it."""
+    s = Setup([300], heads=1, dim=dim)
+    k, v = torch.ones(300, 1, dim, device="cuda"), torch.full((300, 1, dim), 6.0 * 2.0 ** 120, device="cuda")
+    k[::3, :, 5] = 0.5
+    v[::3] = -1.0
+    s.store([300], [300], k.to(BF16), v.to(BF16))
+    q = torch.ones(new or 1, 4, dim, device="cuda").to(BF16)
+    out, want = attend(s, [300], None if new is None else [new], q, 2.0 ** power / dim)
+    ref = want[0]
+    # the others have e^-(2^power / (2 dim)) of the weight, less than 2^-2; a score is off by (dim + 8) 2^-24 of it
+    weights = (TWO if new is None else ONE) + 2.0 ** -19 + 2.5 * (dim + 8) * 2.0 ** -14 * (power == 10)
+    assert np.all(np.abs(out - ref) <= (2.0 ** -8 + weights * 1.01) * np.abs(want[2]))
+
+
+@pytest.mark.parametrize("power", [8, 14, 20, 28, 31, 90])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("far", [[0], [2], [0, 2, 4]])
+def test_large_values_that_large_scores_outweigh(far, dim, power):
+    """Both at once, rows of 16-bit floats: token 70, whose key is 16 where the others' are one or less, has all the
+    weight, so the result is its values; rows from 100 on."""
+    s, _ = filled(dim, far, 6.0 * 2.0 ** 120, 1.0, 16.0)
+    q = torch.full((200, 4, dim), 2.0, dtype=F16, device="cuda")
+    q[::7] = 1.0
+    v = s.ref.values([s.table[0][1]], 0)[1][70 - 64]
+    for sign in (1.0, -1.0):
+        seqs, _ = s.seqs([300], [200])
+        out = host(s.kv.attend(s.cache, seqs, sign * q, scale=sign * 2.0 ** power / dim).double())
+        # the other scores are 15 * 2^power lower or more: e^-3840; what is left is the roundings of a weight and the result
+        assert np.all(np.abs(out - v) <= (2.0 ** -11 + of_tiles(F16, dim) + 2.0 ** -19) * np.abs(v))
