@@ -66,7 +66,7 @@ __device__ __forceinline__ void follow(float top, float shift, float lag, Maximu
     const float new_m = fmaxf(at->m, top * *c + (at->far ? 0.0f : shift));
     if (__any(new_m - at->m > lag)) {
         fall(__builtin_amdgcn_exp2f(at->m - (new_m == -INFINITY ? 0.0f : new_m)));
-        const bool large = __any(fabsf(new_m) > kLargeScore && new_m != -INFINITY);
+        const bool large = __any(fabsf(new_m) > kLargeScore && fabsf(new_m) < INFINITY);
         at->m = large && !at->far ? new_m - shift : new_m;
         at->far = at->far || large;
     }

@@ -197,3 +197,39 @@ def test_large_values_that_large_scores_outweigh(far, dim, power):
         out = host(s.kv.attend(s.cache, seqs, sign * q, scale=sign * 2.0 ** power / dim).double())
         # the other scores are 15 * 2^power lower or more: e^-3840; what is left is the roundings of a weight and the result
         assert np.all(np.abs(out - v) <= (2.0 ** -11 + of_tiles(F16, dim) + 2.0 ** -19) * np.abs(v))
+
+
+@pytest.mark.parametrize("dtype,dim,length,new,heads", [
+    (t, d, 300, n, 1) for t in (BF16, F16) for d in (64, 128, 256) for n in (None, 10, 200)] + [(BF16, 128, 1100, 1030, 60)])
+def test_queries_that_are_no_numbers(dtype, dim, length, new, heads):
+    """Infinities and NaN in some queries make those rows NaN and cost the others nothing."""
+    s = Setup([length], heads=heads, dim=dim)
+    s.fill()
+    n = new or 1
+    q = s.rows(n, 4 * heads, dtype)
+    odd = [(0, 1), (3, 2), (n - 1, 0), (n // 2, 3)] if n > 1 else [(0, 1)]
+    bad = q.clone()
+    for i, (token, head) in enumerate(odd):
+        bad[token, head, i] = (float("nan"), float("inf"), float("-inf"), float("nan"))[i]
+    seqs, begin = s.seqs([length], None if new is None else [new])
+    got = host(s.kv.attend(s.cache, seqs, bad).double())
+    want = s.ref.attend(s.table, [length], begin, host(q.double()), dim ** -0.5)
+    for token, head in odd:
+        assert np.isnan(got[token, head]).all()
+        got[token, head] = want[0][token, head]
+    within(got, want, dtype, TWO if new is None else of_tiles(dtype, dim))
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("new", [None, 130])
+def test_the_smallest_16_bit_queries(new, dim):
+    """Multiples of the least such float, and rows of zeros."""
+    s = Setup([300], heads=1, dim=dim)
+    s.fill()
+    n = new or 1
+    q = torch.randint(-9, 10, (n, 4, dim), device="cuda").float()
+    q[:, 1] *= 100.0
+    q[0, 0] = 0.0
+    q = (q * 2.0 ** -24).to(F16)
+    out, want = attend(s, [300], None if new is None else [new], q, 2.0 ** 17)
+    within(out, want, F16, TWO if new is None else of_tiles(F16, dim))
