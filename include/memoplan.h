@@ -478,7 +478,7 @@ int32_t mp_kv_read(const mp_kv_cache* cache, const mp_kv_seqs* seqs, const mp_kv
  * between tokens or dims cost no bits.  exp(...) is held to 16 bits for few rows, to 8 in tiles of bfloat16
  * rows; in tiles of 16-bit float rows (heads of 64 and 128) to 11 bits, in steps of 2^-34 of the row's
  * largest, by steps of 64 tokens whose values such floats hold, down to their least step; others, and those
- * after one with values of scales past 2^13, to 16. */
+ * after one with values of scales past 2^13, to 16.  Scores times log2 e have to be below 2^127. */
 int32_t mp_kv_attend(const mp_kv_cache* cache, const mp_kv_seqs* seqs, const mp_kv_rows* q,
                      int32_t q_heads, float scale, const int32_t* blocks, int64_t keep,
                      const mp_kv_rows* out, float* lse_out, void* workspace,

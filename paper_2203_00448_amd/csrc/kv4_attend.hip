@@ -545,10 +545,12 @@ __device__ __forceinline__ int v4_key(int token) {
     return D == 64 ? (token >> 1 & 1) << 2 : (token & 3) << 2;
 }
 
-// Measured, 333 rows of heads of 64 after 20000 tokens, 16-bit floats: 101 us and the join, 540 TFLOP/s.  Four
-// sequences of 2048 tokens, 700 new, 32 query heads over 8, bfloat16: heads of 64 62 us, of 128 110 us, of 256
-// 312 us; 16-bit floats 65, 115 and 418.  A tile's softmax takes a wave about 900 cycles of vector instructions
-// (512 of them exponentials), its products of heads of 64 512.
+// Measured, 333, 127 and 18 rows after 19678, 7516 and 1097 tokens, 4 heads of 64, 7 query heads each, 16-bit floats:
+// 98-105 us and the join, 520-560 TFLOP/s.  A tile's softmax takes a wave about 900 cycles of vector instructions (512 of
+// them exponentials), its products of heads of 64 512; counted, vector instructions take 64% of the time of the SIMDs
+// that work, matrix ones 29%, and compute units stand idle for a quarter of the launch: 800 workgroups of unlike
+// lengths for 768 places.  Four sequences of 2048 tokens, 700 new, 32 query heads over 8, bfloat16: heads of 64
+// 61 us, of 128 104 us, of 256 312 us; 16-bit floats 66, 113 and 418.
 //
 // F16, rows of 16-bit floats: the tile as 16-bit floats, so that one instruction holds a query's and a
 // weight's 11 bits.  A group of codes that these cannot hold exactly (scales outside 2^-23..2^13, codes not all zero)
@@ -557,7 +559,7 @@ __device__ __forceinline__ int v4_key(int token) {
 // where those have most bits; beside values of scales past 2^13 they would leave the range of the sums, so a workgroup
 // that meets such values takes that tile and all after it as bfloat16, weights 24 powers below one.
 // Heads of 256 have no registers for both: all their tiles are taken so.
-// Heads of 64 have three waves a SIMD (168 registers, none spilled); left to itself the compiler takes 180.
+// Heads of 64 have three waves a SIMD (168 registers, three spilled beside the loop); unasked the compiler takes more.
 template <int D, bool F16>
 __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 && F16 ? 3 : 2) void kv4_tiles_kernel(KvAttend k) {
     constexpr int KS = D / 16, DT = D / 32, GROUPS = D / 32;
@@ -874,9 +876,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : D == 64 && F16 ? 3 : 2) void kv
 // turn 2 i and team 1 in turn 2 i + 1, keys i are read in these two turns and values i in the next two: each
 // is whole the turn before, and two tiles' room is enough for both.
 //
-// Measured, prompts of 228-4096 tokens, 32 query heads over 8: 257 us, 900 TFLOP/s; four of 4096 tokens 573 us,
-// 960 TFLOP/s (tiles: 267 and 603).  Without the priority of the products 274 us.  Keys left as codes in LDS, read in a
-// quarter of its time and converted by each wave: 285 us, as the conversions meet the other team's softmax.
+// Measured, prompts of 228-4096 tokens, 32 query heads over 8: 257-268 us, 860-900 TFLOP/s; four of 4096 tokens 567-608 us,
+// 900-970 TFLOP/s (tiles, beside 257 and 573: 267 and 603).  Counted, matrix instructions take 45% of a SIMD's time,
+// vector ones 59%, the LDS is active for 35%: the turns overlap little of the two.  Without the priority of the products
+// 274 us.  Keys left as codes in LDS, read in a quarter of its time and converted by each wave: 285 us, as the
+// conversions meet the other team's softmax.
 __global__ __launch_bounds__(512, 2) void kv4_pair_kernel(KvAttend k) {
     constexpr int D = 128, KS = D / 16, DT = D / 32, GROUPS = D / 32;
     extern __shared__ __align__(16) char lds_raw[];
