@@ -18,7 +18,7 @@ import ctypes
 import torch
 
 from . import binding, kv
-from .binding import _finish, new_status  # noqa: F401
+from .binding import MP_OK, _finish, new_status  # noqa: F401
 from .kv import _need
 
 _lib = None
@@ -147,7 +147,8 @@ def extend(pool: Pool, table, length, more, *, block: int = 64, step: Step, leng
     status = kv._word(status, pool)
     rc = L.mp_kv_extend(ids, n_ids, used, t, t_stride, width, block, lengths, new, n, room, out, used_to, begin,
                         position, slot, space.data_ptr(), space.nbytes, status.data_ptr(), kv._stream(index))
-    step.length = length if length_out is None else length_out
+    if rc == MP_OK:
+        step.length = length if length_out is None else length_out
     _finish(rc, status, "pages.extend", check)
     return step
 
